@@ -490,6 +490,50 @@ int sq_scale_rollback(int fmt, int64_t n, uint8_t* scales, const float* applied,
  */
 int sq_byte_diff(int64_t n, const uint8_t* a, const uint8_t* b, uint64_t* counts, void* stream);
 
+/*
+ * Tokens to experts and back: what feeds the grouped products and takes their
+ * outputs to the tokens.  Each of T tokens names K experts (pair p = t*K + k).
+ *
+ * sq_moe_sort orders the N = T*K pairs by expert, pairs of one expert in pair
+ * order:
+ *   slot[p]     place of pair p, a permutation of 0 .. N-1; pairs whose id is
+ *               outside 0 .. E-1 (say -1) are dropped and take the last places
+ *   token[s]    the token at place s
+ *   offsets[e]  first place of expert e, e = 0 .. E; offsets[E] is the number
+ *               of routed pairs, so pair p is routed iff slot[p] < offsets[E]
+ * ids: int32 or int64 [T, K] (id_bytes 4 or 8); offsets int32 [E+1]; token
+ * int32 [N]; slot int32 [T, K]; all naturally aligned.  T >= 0 (offsets are
+ * written as zeros when T = 0), K >= 1, 1 <= E <= 2048, T*K < 2^31.  workspace:
+ * at least sq_moe_sort_workspace(T, K, E) bytes (0 for few pairs), 4-byte
+ * aligned, contents irrelevant.
+ *
+ * sq_moe_gather: Xs[slot[p]] = X[p / K] for routed pairs, zeros for dropped
+ *   ones: all N rows of Xs are written, expert e's being [offsets[e],
+ *   offsets[e+1]).
+ * sq_moe_combine: out[t] = sum over the routed pairs k = 0 .. K-1 of
+ *   weights[t,k] Ys[slot[t,k]], fp32 in that order; weights NULL: 1 each, which
+ *   is the gradient of sq_moe_gather (out = dX for Ys = dXs).
+ * sq_moe_combine_bwd: the gradients of sq_moe_combine for dOut [T, H],
+ *   dYs[slot[t,k]] = weights[t,k] dOut[t]   (zeros for dropped pairs; all N rows)
+ *   dweights[t,k]  = dOut[t] . Ys[slot[t,k]]   (0 for dropped pairs), fp32 sums
+ *   in a fixed order.
+ * X, Xs, Ys, dYs, dOut, out: rows of H elements, fp32 or bf16 by the dtype
+ * given (sq_out_dtype), 16-byte aligned, H % 8 == 0; Ys and dYs must not
+ * overlap.  weights, dweights: fp32 [T, K].  Rows of dropped pairs are not
+ * read into any result, whatever they hold.  Row addresses are 64-bit: N*H may
+ * exceed 2^31.  A slot outside 0 .. N-1 counts as dropped.
+ */
+size_t sq_moe_sort_workspace(int64_t T, int64_t K, int64_t E);
+int sq_moe_sort(int64_t T, int64_t K, int64_t E, const void* ids, int id_bytes, int32_t* offsets, int32_t* token,
+                int32_t* slot, void* workspace, size_t workspace_bytes, void* stream);
+int sq_moe_gather(int64_t T, int64_t K, int64_t E, int64_t H, const void* X, int dtype, const int32_t* slot,
+                  const int32_t* offsets, void* Xs, void* stream);
+int sq_moe_combine(int64_t T, int64_t K, int64_t E, int64_t H, const void* Ys, int y_dtype, const int32_t* slot,
+                   const int32_t* offsets, const float* weights, void* out, int out_dtype, void* stream);
+int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, const void* dOut, int d_dtype, const void* Ys,
+                       int y_dtype, const int32_t* slot, const int32_t* offsets, const float* weights, void* dYs,
+                       int dy_dtype, float* dweights, void* stream);
+
 /* Human-readable name of a status code (static storage). */
 const char* sq_status_str(int status);
 

@@ -2,42 +2,19 @@
 // argument validation, then one or a few launches on the caller's stream.
 // Nothing here allocates device memory or synchronises.
 #include <hip/hip_runtime.h>
-#include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
 #include <vector>
 
-#include "../../include/scaleqlora.h"
+#include "sq_checks.h"
 #include "sq_launch.h"
-
-#define SQ_EXPORT extern "C" __attribute__((visibility("default")))
 
 static_assert(SQ_DSCALE_SCRATCH_BYTES == sq::kDscaleScratchBytes, "header and library agree on the scratch size");
 
 namespace {
 
-constexpr int64_t kDimMax = (int64_t(1) << 31) - 1;
-
-int block_of(int fmt) { return fmt == SQ_MXFP4 ? 32 : 16; }
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-// The GEMM kernels address each operand through one buffer resource with a
-// 32-bit byte range (offsets from 2^31 up read as zeros), so every operand
-// must stay below 2 GiB.
-constexpr int64_t kOperandBytesMax = (int64_t(1) << 31) - 16;
-
-int check_layer(int fmt, int64_t T, int64_t O, int64_t I) {
-  if (fmt != SQ_MXFP4 && fmt != SQ_NVFP4) return SQ_ERR_FORMAT;
-  if (T < 0 || O < 1 || I < 1 || T > kDimMax || O > kDimMax || I > kDimMax) return SQ_ERR_SHAPE;
-  if (O % 8 != 0 || I % block_of(fmt) != 0) return SQ_ERR_SHAPE;
-  if (T * I * 2 > kOperandBytesMax || T * O * 2 > kOperandBytesMax || O * I / 2 > kOperandBytesMax)
-    return SQ_ERR_SHAPE;
-  return SQ_OK;
-}
-
-bool ws2_ok(float ws2) { return isfinite(ws2) && ws2 > 0.0f; }
+using namespace sq;
 
 int check_gemm(int fmt, int64_t T, int64_t O, int64_t I, const void* act, const uint8_t* codes,
                const uint8_t* scales, float ws2, const void* out, int out_dtype) {
@@ -50,8 +27,6 @@ int check_gemm(int fmt, int64_t T, int64_t O, int64_t I, const void* act, const 
   if (!aligned(act, 16) || !aligned(out, 16) || !aligned(codes, 4)) return SQ_ERR_ALIGN;
   return SQ_OK;
 }
-
-int hip_status(int rc) { return rc == 0 ? SQ_OK : SQ_ERR_HIP; }
 
 int check_merge_plane(int fmt, int64_t n, const uint8_t* scales, const float* delta, const uint8_t* src,
                       float ws2, int mode) {

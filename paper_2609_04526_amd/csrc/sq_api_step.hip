@@ -1,0 +1,90 @@
+// C ABI of what a training step runs around the frozen-code products (declared
+// in include/scaleqlora.h): host-side argument validation, then launches on the
+// caller's stream.  Nothing here allocates device memory or synchronises.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "sq_checks.h"
+#include "sq_launch.h"
+
+namespace {
+
+using namespace sq;
+
+bool dtype_ok(int d) { return d == SQ_OUT_F32 || d == SQ_OUT_BF16; }
+
+// ---------------------------------------------------------------- experts
+constexpr int64_t kMoeExpertsMax = 2048;   // the sort's counters of one key each in LDS
+
+int check_pairs(int64_t T, int64_t K, int64_t E) {
+  if (T < 0 || K < 1 || E < 1 || T > kDimMax || K > kDimMax || E > kMoeExpertsMax) return SQ_ERR_SHAPE;
+  return T * K > kDimMax ? SQ_ERR_SHAPE : SQ_OK;
+}
+
+int check_rows(int64_t T, int64_t K, int64_t E, int64_t H, const int32_t* slot, const int32_t* offsets) {
+  const int st = check_pairs(T, K, E);
+  if (st != SQ_OK) return st;
+  if (H < 1 || H % 8 != 0 || H > kDimMax) return SQ_ERR_SHAPE;
+  if (!offsets || (T > 0 && !slot)) return SQ_ERR_ARG;
+  return aligned(slot, 4) && aligned(offsets, 4) ? SQ_OK : SQ_ERR_ALIGN;
+}
+
+}  // namespace
+
+SQ_EXPORT size_t sq_moe_sort_workspace(int64_t T, int64_t K, int64_t E) {
+  if (check_pairs(T, K, E) != SQ_OK || moe_sort_one(T * K)) return 0;
+  return (size_t)((T * K + kMoeChunk - 1) / kMoeChunk + 1) * (size_t)(E + 1) * 4;
+}
+
+SQ_EXPORT int sq_moe_sort(int64_t T, int64_t K, int64_t E, const void* ids, int id_bytes, int32_t* offsets,
+                          int32_t* token, int32_t* slot, void* workspace, size_t workspace_bytes, void* stream) {
+  const int st = check_pairs(T, K, E);
+  if (st != SQ_OK) return st;
+  if (id_bytes != 4 && id_bytes != 8) return SQ_ERR_ARG;
+  if (!offsets || (T > 0 && (!ids || !token || !slot))) return SQ_ERR_ARG;
+  if (!aligned(ids, (uintptr_t)id_bytes) || !aligned(offsets, 4) || !aligned(token, 4) || !aligned(slot, 4))
+    return SQ_ERR_ALIGN;
+  const size_t need = sq_moe_sort_workspace(T, K, E);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 4)) return SQ_ERR_ALIGN;
+  return hip_status(moe_sort_launch(T, (int)K, (int)E, ids, id_bytes, offsets, token, slot, workspace,
+                                    static_cast<hipStream_t>(stream)));
+}
+
+SQ_EXPORT int sq_moe_gather(int64_t T, int64_t K, int64_t E, int64_t H, const void* X, int dtype, const int32_t* slot,
+                            const int32_t* offsets, void* Xs, void* stream) {
+  const int st = check_rows(T, K, E, H, slot, offsets);
+  if (st != SQ_OK) return st;
+  if (!dtype_ok(dtype) || (T > 0 && (!X || !Xs))) return SQ_ERR_ARG;
+  if (!aligned(X, 16) || !aligned(Xs, 16)) return SQ_ERR_ALIGN;
+  if (T == 0) return SQ_OK;
+  return hip_status(moe_gather_launch(T, (int)K, (int)H, dtype == SQ_OUT_BF16, X, slot, offsets + E, Xs,
+                                      static_cast<hipStream_t>(stream)));
+}
+
+SQ_EXPORT int sq_moe_combine(int64_t T, int64_t K, int64_t E, int64_t H, const void* Ys, int y_dtype,
+                             const int32_t* slot, const int32_t* offsets, const float* weights, void* out,
+                             int out_dtype, void* stream) {
+  const int st = check_rows(T, K, E, H, slot, offsets);
+  if (st != SQ_OK) return st;
+  if (!dtype_ok(y_dtype) || !dtype_ok(out_dtype) || (T > 0 && (!Ys || !out))) return SQ_ERR_ARG;
+  if (!aligned(Ys, 16) || !aligned(out, 16) || !aligned(weights, 4)) return SQ_ERR_ALIGN;
+  if (T == 0) return SQ_OK;
+  return hip_status(moe_combine_launch(T, (int)K, (int)H, Ys, y_dtype == SQ_OUT_BF16, slot, offsets + E, weights, out,
+                                       out_dtype == SQ_OUT_BF16, static_cast<hipStream_t>(stream)));
+}
+
+SQ_EXPORT int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, const void* dOut, int d_dtype,
+                                 const void* Ys, int y_dtype, const int32_t* slot, const int32_t* offsets,
+                                 const float* weights, void* dYs, int dy_dtype, float* dweights, void* stream) {
+  const int st = check_rows(T, K, E, H, slot, offsets);
+  if (st != SQ_OK) return st;
+  if (!dtype_ok(d_dtype) || !dtype_ok(y_dtype) || !dtype_ok(dy_dtype)) return SQ_ERR_ARG;
+  if (T > 0 && (!dOut || !Ys || !weights || !dYs || !dweights)) return SQ_ERR_ARG;
+  if (!aligned(dOut, 16) || !aligned(Ys, 16) || !aligned(dYs, 16) || !aligned(weights, 4) || !aligned(dweights, 4))
+    return SQ_ERR_ALIGN;
+  if (T == 0) return SQ_OK;
+  return hip_status(moe_combine_bwd_launch(T, (int)K, (int)H, dOut, d_dtype == SQ_OUT_BF16, Ys, y_dtype == SQ_OUT_BF16,
+                                           slot, offsets + E, weights, dYs, dy_dtype == SQ_OUT_BF16, dweights,
+                                           static_cast<hipStream_t>(stream)));
+}

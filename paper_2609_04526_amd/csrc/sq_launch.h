@@ -160,4 +160,20 @@ int applied_launch(int fmt, int64_t n, const uint8_t* before, const uint8_t* aft
 int rollback_launch(int fmt, int64_t n, uint8_t* scales, const float* applied, hipStream_t s);
 int byte_diff_launch(int64_t n, const uint8_t* a, const uint8_t* b, uint64_t* counts, hipStream_t s);
 
+// Tokens to experts and back (sq_moe.hip).  routed: device pointer to the
+// number of routed pairs (the sort's offsets[E]).
+constexpr int kMoeChunk = 4096;           // pairs per workgroup of the sort over many pairs
+constexpr int kMoeWaveTokens = 2048;      // tokens from which the combine's gradients take a wave per token
+// One launch sorts up to this many pairs.
+constexpr bool moe_sort_one(int64_t N) { return N <= 65536; }
+int moe_sort_launch(int64_t T, int K, int E, const void* ids, int id_bytes, int32_t* offsets, int32_t* token,
+                    int32_t* slot, void* workspace, hipStream_t s);
+int moe_gather_launch(int64_t T, int K, int H, int bf16, const void* X, const int32_t* slot, const int32_t* routed,
+                      void* Xs, hipStream_t s);
+int moe_combine_launch(int64_t T, int K, int H, const void* Ys, int y_bf16, const int32_t* slot, const int32_t* routed,
+                       const float* weights, void* out, int out_bf16, hipStream_t s);
+int moe_combine_bwd_launch(int64_t T, int K, int H, const void* dOut, int d_bf16, const void* Ys, int y_bf16,
+                           const int32_t* slot, const int32_t* routed, const float* weights, void* dYs, int g_bf16,
+                           float* dw, hipStream_t s);
+
 }  // namespace sq

@@ -143,6 +143,14 @@ def _load():
         "sq_scale_applied_delta": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_p, _c_p, _c_p, _c_p]),
         "sq_scale_rollback": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_p, _c_p, _c_p]),
         "sq_byte_diff": (ctypes.c_int, [_c_i64, _c_p, _c_p, _c_p, _c_p]),
+        "sq_moe_sort_workspace": (ctypes.c_size_t, [_c_i64, _c_i64, _c_i64]),
+        "sq_moe_sort": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_p, _c_p, _c_p, _c_p,
+                                       ctypes.c_size_t, _c_p]),
+        "sq_moe_gather": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_p, _c_p, _c_p, _c_p]),
+        "sq_moe_combine": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_p, _c_p, _c_p, _c_p,
+                                          ctypes.c_int, _c_p]),
+        "sq_moe_combine_bwd": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_p, ctypes.c_int,
+                                              _c_p, _c_p, _c_p, _c_p, ctypes.c_int, _c_p, _c_p]),
         "sq_status_str": (ctypes.c_char_p, [ctypes.c_int]),
         "sq_abi_version": (ctypes.c_int, []),
     }
@@ -824,6 +832,104 @@ def sq_byte_diff(a, b, counts=None):
     _dev(a, b, counts)
     _check("sq_byte_diff", load().sq_byte_diff(a.numel(), _ptr(a), _ptr(b), _ptr(counts), _stream()))
     return counts
+
+
+# ---------------------------------------------------------------- tokens to experts and back
+_I32 = torch.int32
+_IDS = (torch.int64, torch.int32)
+
+
+def _dtype_of(t):
+    return OUT_BF16 if t.dtype is _BF16 else OUT_F32
+
+
+def _slots(slot, offsets):
+    """T, K and the number of experts of a sort's outputs."""
+    T, K = _dims2(slot, "slot")
+    _need(slot, "slot", _I32)
+    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError("offsets must be a 1-D tensor of n_experts + 1 elements")
+    _need(offsets, "offsets", _I32)
+    return T, K, offsets.numel() - 1
+
+
+def sq_moe_sort(ids, n_experts, offsets=None, token=None, slot=None, workspace=None):
+    """(offsets int32 [E+1], token int32 [T*K], slot int32 [T, K]) of the pairs of ids [T, K] by expert."""
+    T, K = _dims2(ids, "ids")
+    _need(ids, "ids", _IDS)
+    if offsets is None:
+        offsets = torch.empty(n_experts + 1, dtype=_I32, device=ids.device)
+    if token is None:
+        token = torch.empty(T * K, dtype=_I32, device=ids.device)
+    if slot is None:
+        slot = torch.empty((T, K), dtype=_I32, device=ids.device)
+    _need(offsets, "offsets", _I32, (n_experts + 1,))
+    _need(token, "token", _I32, (T * K,))
+    _need(slot, "slot", _I32, (T, K))
+    ws_bytes = int(load().sq_moe_sort_workspace(T, K, n_experts))
+    if ws_bytes and workspace is None:
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=ids.device)
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8)
+    _dev(ids, offsets, token, slot, workspace)
+    _check("sq_moe_sort", load().sq_moe_sort(T, K, n_experts, _ptr(ids), ids.element_size(), _ptr(offsets), _ptr(token),
+                                             _ptr(slot), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                             _stream()))
+    return offsets, token, slot
+
+
+def sq_moe_sort_workspace(T, K, n_experts):
+    return int(load().sq_moe_sort_workspace(T, K, n_experts))
+
+
+def sq_moe_gather(X, slot, offsets, Xs=None):
+    """Xs[slot[t, k]] = X[t] (zeros for dropped pairs), [T*K, H] of X's dtype."""
+    T, K, E = _slots(slot, offsets)
+    H = _dims2(X, "X")[1]
+    _need(X, "X", _OUT, (T, H))
+    if Xs is None:
+        Xs = torch.empty((T * K, H), dtype=X.dtype, device=X.device)
+    _need(Xs, "Xs", X.dtype, (T * K, H))
+    _dev(X, slot, offsets, Xs)
+    _check("sq_moe_gather", load().sq_moe_gather(T, K, E, H, _ptr(X), _dtype_of(X), _ptr(slot), _ptr(offsets), _ptr(Xs),
+                                                 _stream()))
+    return Xs
+
+
+def sq_moe_combine(Ys, slot, offsets, weights=None, out_dtype=torch.float32, out=None):
+    """out[t] = sum_k weights[t, k] Ys[slot[t, k]] over routed pairs; weights None: 1 (the gradient of sq_moe_gather)."""
+    T, K, E = _slots(slot, offsets)
+    H = _dims2(Ys, "Ys")[1]
+    _need(Ys, "Ys", _OUT, (T * K, H))
+    if weights is not None:
+        _need(weights, "weights", _F32, (T, K))
+    if out is None:
+        out = torch.empty((T, H), dtype=out_dtype, device=Ys.device)
+    _need(out, "out", _OUT, (T, H))
+    _dev(Ys, slot, offsets, weights, out)
+    _check("sq_moe_combine", load().sq_moe_combine(T, K, E, H, _ptr(Ys), _dtype_of(Ys), _ptr(slot), _ptr(offsets),
+                                                   _ptr(weights), _ptr(out), _dtype_of(out), _stream()))
+    return out
+
+
+def sq_moe_combine_bwd(dOut, Ys, slot, offsets, weights, out_dtype=None, dYs=None, dweights=None):
+    """(dYs [T*K, H], dweights fp32 [T, K]) of sq_moe_combine; dYs in out_dtype (Ys's by default)."""
+    T, K, E = _slots(slot, offsets)
+    H = _dims2(Ys, "Ys")[1]
+    _need(Ys, "Ys", _OUT, (T * K, H))
+    _need(dOut, "dOut", _OUT, (T, H))
+    _need(weights, "weights", _F32, (T, K))
+    if dYs is None:
+        dYs = torch.empty((T * K, H), dtype=Ys.dtype if out_dtype is None else out_dtype, device=Ys.device)
+    if dweights is None:
+        dweights = torch.empty((T, K), dtype=_F32, device=Ys.device)
+    _need(dYs, "dYs", _OUT, (T * K, H))
+    _need(dweights, "dweights", _F32, (T, K))
+    _dev(dOut, Ys, slot, offsets, weights, dYs, dweights)
+    _check("sq_moe_combine_bwd", load().sq_moe_combine_bwd(T, K, E, H, _ptr(dOut), _dtype_of(dOut), _ptr(Ys),
+                                                           _dtype_of(Ys), _ptr(slot), _ptr(offsets), _ptr(weights),
+                                                           _ptr(dYs), _dtype_of(dYs), _ptr(dweights), _stream()))
+    return dYs, dweights
 
 
 def abi_version():
