@@ -83,6 +83,7 @@ typedef enum {
   SQ_RULE_STOCHASTIC = 3,    /* codes by stochastic rounding, per-block scales */
   SQ_RULE_WHOLE_TENSOR = 4   /* one scale from the tensor amax, nearest-even codes */
 } sq_rule;
+typedef enum { SQ_ACT_INT8 = 0, SQ_ACT_E4M3 = 1 } sq_act_format;
 
 /*
  * Forward, Y = X W^T (paper Section 2 storage equation; Section 3,
@@ -533,6 +534,51 @@ int sq_moe_combine(int64_t T, int64_t K, int64_t E, int64_t H, const void* Ys, i
 int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, const void* dOut, int d_dtype, const void* Ys,
                        int y_dtype, const int32_t* slot, const int32_t* offsets, const float* weights, void* dYs,
                        int dy_dtype, float* dweights, void* stream);
+
+/*
+ * Activations kept in 8 bits between the forward and the backward pass.  The
+ * scale gradient is the only backward product that needs a layer's input X, so
+ * X can be kept as 8-bit values with one E8M0 byte per block of 32 columns
+ * (33/64 of its bf16 bytes) and read as such:
+ *
+ *   SQ_ACT_INT8: k = floor(log2 amax) - 6; q = x 2^-k to the nearest whole
+ *          number, ties to even, held to +-127 (two's complement byte)
+ *   SQ_ACT_E4M3: k = ceil(log2(amax / 448)); q = x 2^-k to the nearest E4M3,
+ *          ties to even
+ *   x^ = q 2^k, byte k + 127 with k held to [-126, 127] (an all-zero block: byte
+ *   1).  A block holding an Inf or NaN gets byte 255 and zero codes, and reads
+ *   as NaN.
+ *
+ * sq_act_pack: X bf16 [T, I] -> codes_out uint8 [T, I], scales_out uint8
+ *   [T, I/32].  sq_act_unpack: the values x^ as bf16 [T, I] (q 2^k is exact in
+ *   bf16; values below its range are rounded to nearest even).  I % 32 == 0; X
+ *   and codes 16-byte aligned; T*I <= 2^40.
+ *
+ * sq_bwd_dscale_act8: sq_bwd_dscale with x^ in the place of X, bit for bit what
+ *   that call computes for the unpacked x^.  I % 32 == 0 for either weight
+ *   format; x_codes 16-byte aligned; workspace as sq_bwd_dscale's, of
+ *   sq_bwd_dscale_act8_workspace bytes; the rest as sq_bwd_dscale.
+ *
+ * sq_bwd_dscale_act8_batched: the scale gradients of E stacked experts, whose
+ *   rows of dY bf16 [N, O] stand one expert after another: expert e has rows
+ *   [offsets[e], offsets[e+1]), offsets int32 [E+1] on the DEVICE (as
+ *   sq_moe_sort writes them: nothing waits for the host).  Row s of dY meets
+ *   row rows[s] of x^ [T, I] (rows int32 [N]: sq_moe_sort's token, so that
+ *   experts read one copy of the layer's tokens), or row s when rows is NULL
+ *   (then N == T).  codes uint8 [E, O, I/2]; dS fp32 [E, O, G], every plane
+ *   written (zeros for an expert without rows).  A row number outside 0 .. T-1
+ *   reads as a row of zeros, and offsets are held to 0 .. N.  1 <= E <= 65535; T*I and
+ *   N*O*2 below 2 GiB.  Deterministic.
+ */
+int sq_act_pack(int act, int64_t T, int64_t I, const void* X, uint8_t* codes_out, uint8_t* scales_out, void* stream);
+int sq_act_unpack(int act, int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, void* X, void* stream);
+size_t sq_bwd_dscale_act8_workspace(int fmt, int64_t T, int64_t O, int64_t I);
+int sq_bwd_dscale_act8(int fmt, int act, int64_t T, int64_t O, int64_t I, const uint8_t* x_codes,
+                       const uint8_t* x_scales, const void* dY, const uint8_t* codes, float* dS, void* workspace,
+                       size_t workspace_bytes, void* stream);
+int sq_bwd_dscale_act8_batched(int fmt, int act, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I,
+                               const uint8_t* x_codes, const uint8_t* x_scales, const int32_t* rows,
+                               const int32_t* offsets, const void* dY, const uint8_t* codes, float* dS, void* stream);
 
 /* Human-readable name of a status code (static storage). */
 const char* sq_status_str(int status);

@@ -88,3 +88,75 @@ SQ_EXPORT int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, con
                                            slot, offsets + E, weights, dYs, dy_dtype == SQ_OUT_BF16, dweights,
                                            static_cast<hipStream_t>(stream)));
 }
+
+// ---------------------------------------------------------------- 8-bit activations
+namespace {
+
+bool act_ok(int act) { return act == SQ_ACT_INT8 || act == SQ_ACT_E4M3; }
+
+int check_act(int act, int64_t T, int64_t I, const void* X, const uint8_t* codes, const uint8_t* scales) {
+  if (!act_ok(act)) return SQ_ERR_ARG;
+  if (T < 0 || I < 1 || T > kDimMax || I > kDimMax || I % 32 != 0 || T > (int64_t(1) << 40) / I) return SQ_ERR_SHAPE;
+  if (T > 0 && (!X || !codes || !scales)) return SQ_ERR_ARG;
+  return aligned(X, 16) && aligned(codes, 16) ? SQ_OK : SQ_ERR_ALIGN;
+}
+
+// The kept activation [Tx, I] and the scale gradient's other operands; N rows of dY.
+int check_dscale8(int fmt, int act, int64_t Tx, int64_t N, int64_t O, int64_t I, const uint8_t* x, const uint8_t* xs,
+                  const void* dY, const uint8_t* codes, const float* dS) {
+  const int st = check_layer(fmt, 0, O, I);
+  if (st != SQ_OK) return st;
+  if (!act_ok(act)) return SQ_ERR_ARG;
+  if (I % 32 != 0 || Tx < 0 || N < 0 || Tx > kDimMax || N > kDimMax / 4) return SQ_ERR_SHAPE;
+  if (Tx * I > kOperandBytesMax || N * O * 2 > kOperandBytesMax) return SQ_ERR_SHAPE;
+  if (!codes || !dS || (N > 0 && !dY) || (Tx > 0 && (!x || !xs))) return SQ_ERR_ARG;
+  return aligned(x, 16) && aligned(dY, 16) && aligned(codes, 4) && aligned(dS, 4) ? SQ_OK : SQ_ERR_ALIGN;
+}
+
+}  // namespace
+
+SQ_EXPORT int sq_act_pack(int act, int64_t T, int64_t I, const void* X, uint8_t* codes_out, uint8_t* scales_out,
+                          void* stream) {
+  const int st = check_act(act, T, I, X, codes_out, scales_out);
+  if (st != SQ_OK || T == 0) return st;
+  return hip_status(act_pack_launch(act, T, I, X, codes_out, scales_out, static_cast<hipStream_t>(stream)));
+}
+
+SQ_EXPORT int sq_act_unpack(int act, int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, void* X,
+                            void* stream) {
+  const int st = check_act(act, T, I, X, codes, scales);
+  if (st != SQ_OK || T == 0) return st;
+  return hip_status(act_unpack_launch(act, T, I, codes, scales, X, static_cast<hipStream_t>(stream)));
+}
+
+SQ_EXPORT size_t sq_bwd_dscale_act8_workspace(int fmt, int64_t T, int64_t O, int64_t I) {
+  if (check_layer(fmt, T, O, I) != SQ_OK || I % 32 != 0) return 0;
+  return dscale_act8_workspace(fmt, (int)T, (int)O, (int)I);
+}
+
+SQ_EXPORT int sq_bwd_dscale_act8(int fmt, int act, int64_t T, int64_t O, int64_t I, const uint8_t* x_codes,
+                                 const uint8_t* x_scales, const void* dY, const uint8_t* codes, float* dS,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  int st = check_layer(fmt, T, O, I);
+  if (st == SQ_OK) st = check_dscale8(fmt, act, T, T, O, I, x_codes, x_scales, dY, codes, dS);
+  if (st != SQ_OK) return st;
+  const size_t need = sq_bwd_dscale_act8_workspace(fmt, T, O, I);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 16)) return SQ_ERR_ALIGN;
+  return hip_status(dscale_act8(fmt, act, (int)T, (int)O, (int)I, x_codes, x_scales, dY, codes, dS, workspace,
+                                static_cast<hipStream_t>(stream)));
+}
+
+SQ_EXPORT int sq_bwd_dscale_act8_batched(int fmt, int act, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I,
+                                         const uint8_t* x_codes, const uint8_t* x_scales, const int32_t* rows,
+                                         const int32_t* offsets, const void* dY, const uint8_t* codes, float* dS,
+                                         void* stream) {
+  const int st = check_dscale8(fmt, act, T, N, O, I, x_codes, x_scales, dY, codes, dS);
+  if (st != SQ_OK) return st;
+  // the tiles of all experts are numbered in 32 bits
+  if (E < 1 || E > 65535 || E * ((O + 127) / 128) * ((I + 127) / 128) > kDimMax) return SQ_ERR_SHAPE;
+  if (!offsets || (N > 0 && !rows && N != T)) return SQ_ERR_ARG;
+  if (!aligned(rows, 4) || !aligned(offsets, 4)) return SQ_ERR_ALIGN;
+  return hip_status(dscale_act8_batched(fmt, act, (int)E, (int)T, (int)N, (int)O, (int)I, x_codes, x_scales, rows,
+                                        offsets, dY, codes, dS, static_cast<hipStream_t>(stream)));
+}

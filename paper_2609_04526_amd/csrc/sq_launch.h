@@ -176,4 +176,15 @@ int moe_combine_bwd_launch(int64_t T, int K, int H, const void* dOut, int d_bf16
                            const int32_t* slot, const int32_t* routed, const float* weights, void* dYs, int g_bf16,
                            float* dw, hipStream_t s);
 
+// Activations kept in 8 bits (sq_act8.hip).  act: 0 int8, 1 E4M3.
+int act_pack_launch(int act, int64_t T, int64_t I, const void* X, uint8_t* codes, uint8_t* scales, hipStream_t s);
+int act_unpack_launch(int act, int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, void* X,
+                      hipStream_t s);
+size_t dscale_act8_workspace(int fmt, int T, int O, int I);
+int dscale_act8(int fmt, int act, int T, int O, int I, const uint8_t* x, const uint8_t* xs, const void* dY,
+                const uint8_t* codes, float* dS, void* workspace, hipStream_t s);
+int dscale_act8_batched(int fmt, int act, int E, int Tx, int N, int O, int I, const uint8_t* x, const uint8_t* xs,
+                        const int32_t* rows, const int32_t* offsets, const void* dY, const uint8_t* codes, float* dS,
+                        hipStream_t s);
+
 }  // namespace sq

@@ -25,6 +25,9 @@ RULE_NEAREST_EVEN, RULE_NEAREST_AWAY, RULE_RTZ, RULE_STOCHASTIC, RULE_WHOLE_TENS
 RULES = {"even": RULE_NEAREST_EVEN, "away": RULE_NEAREST_AWAY, "rtz": RULE_RTZ,
          "stochastic": RULE_STOCHASTIC, "whole_tensor": RULE_WHOLE_TENSOR}
 BLOCK = {MXFP4: 32, NVFP4: 16}
+ACT_INT8, ACT_E4M3 = 0, 1
+ACTS = {"int8": ACT_INT8, "e4m3": ACT_E4M3}
+ACT_BLOCK = 32
 
 _c_i64 = ctypes.c_int64
 _c_p = ctypes.c_void_p
@@ -151,6 +154,13 @@ def _load():
                                           ctypes.c_int, _c_p]),
         "sq_moe_combine_bwd": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_p, ctypes.c_int,
                                               _c_p, _c_p, _c_p, _c_p, ctypes.c_int, _c_p, _c_p]),
+        "sq_act_pack": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_p, _c_p, _c_p, _c_p]),
+        "sq_act_unpack": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_p, _c_p, _c_p, _c_p]),
+        "sq_bwd_dscale_act8_workspace": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64]),
+        "sq_bwd_dscale_act8": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
+                                              _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]),
+        "sq_bwd_dscale_act8_batched": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i64,
+                                                      _c_i64, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p]),
         "sq_status_str": (ctypes.c_char_p, [ctypes.c_int]),
         "sq_abi_version": (ctypes.c_int, []),
     }
@@ -930,6 +940,99 @@ def sq_moe_combine_bwd(dOut, Ys, slot, offsets, weights, out_dtype=None, dYs=Non
                                                            _dtype_of(Ys), _ptr(slot), _ptr(offsets), _ptr(weights),
                                                            _ptr(dYs), _dtype_of(dYs), _ptr(dweights), _stream()))
     return dYs, dweights
+
+
+# ---------------------------------------------------------------- 8-bit activations
+_U8 = torch.uint8
+
+
+def _kept(codes, scales, names=("codes", "scales")):
+    """T, I of a kept activation: codes uint8 [T, I], scales uint8 [T, I/32]."""
+    T, I = _dims2(codes, names[0])
+    if I % ACT_BLOCK:
+        raise ValueError(f"the width {I} is not a multiple of the block {ACT_BLOCK}")
+    _need(codes, names[0], _U8)
+    _need(scales, names[1], _U8, (T, I // ACT_BLOCK))
+    return T, I
+
+
+def sq_act_pack(act, X, codes=None, scales=None):
+    """(codes uint8 [T, I], scales uint8 [T, I/32]) of X bf16 [T, I]; act "int8" or "e4m3"."""
+    act = ACTS.get(act, act)
+    T, I = _dims2(X, "X")
+    _need(X, "X", _BF16)
+    if codes is None:
+        codes = torch.empty((T, I), dtype=_U8, device=X.device)
+    if scales is None:
+        scales = torch.empty((T, I // ACT_BLOCK), dtype=_U8, device=X.device)
+    if _kept(codes, scales) != (T, I):
+        raise ValueError(f"codes has shape {tuple(codes.shape)}, expected {(T, I)}")
+    _dev(X, codes, scales)
+    _check("sq_act_pack", load().sq_act_pack(act, T, I, _ptr(X), _ptr(codes), _ptr(scales), _stream()))
+    return codes, scales
+
+
+def sq_act_unpack(act, codes, scales, X=None):
+    """The kept values as bf16 [T, I]."""
+    act = ACTS.get(act, act)
+    T, I = _kept(codes, scales)
+    if X is None:
+        X = torch.empty((T, I), dtype=_BF16, device=codes.device)
+    _need(X, "X", _BF16, (T, I))
+    _dev(codes, scales, X)
+    _check("sq_act_unpack", load().sq_act_unpack(act, T, I, _ptr(codes), _ptr(scales), _ptr(X), _stream()))
+    return X
+
+
+def sq_bwd_dscale_act8_workspace(fmt, T, O, I):
+    return int(load().sq_bwd_dscale_act8_workspace(_fmt(fmt), T, O, I))
+
+
+def sq_bwd_dscale_act8(fmt, act, x_codes, x_scales, dY, codes, dS=None, workspace=None):
+    """sq_bwd_dscale of a kept X: x_codes uint8 [T, I], x_scales uint8 [T, I/32], dY bf16 [T, O]."""
+    fmt, act = _fmt(fmt), ACTS.get(act, act)
+    T, I = _kept(x_codes, x_scales, ("x_codes", "x_scales"))
+    O = _dims2(dY, "dY")[1]
+    _need(dY, "dY", _BF16, (T, O))
+    G = _layer(fmt, O, I, codes)
+    if dS is None:
+        dS = torch.empty((O, G), dtype=_F32, device=dY.device)
+    _need(dS, "dS", _F32, (O, G))
+    ws_bytes = int(load().sq_bwd_dscale_act8_workspace(fmt, T, O, I))
+    if ws_bytes and workspace is None:
+        workspace = torch.empty(ws_bytes, dtype=_U8, device=dY.device)
+    if workspace is not None:
+        _need(workspace, "workspace", _U8)
+    _dev(x_codes, x_scales, dY, codes, dS, workspace)
+    _check("sq_bwd_dscale_act8", load().sq_bwd_dscale_act8(
+        fmt, act, T, O, I, _ptr(x_codes), _ptr(x_scales), _ptr(dY), _ptr(codes), _ptr(dS), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream()))
+    return dS
+
+
+def sq_bwd_dscale_act8_batched(fmt, act, x_codes, x_scales, rows, offsets, dY, codes, dS=None):
+    """dS fp32 [E, O, G] of E stacked experts (codes uint8 [E, O, I/2]); expert e's rows of dY bf16 [N, O] are
+    [offsets[e], offsets[e+1]) and meet rows rows[s] of the kept X (None: row s)."""
+    fmt, act = _fmt(fmt), ACTS.get(act, act)
+    T, I = _kept(x_codes, x_scales, ("x_codes", "x_scales"))
+    N, O = _dims2(dY, "dY")
+    G = _block(fmt, I)
+    if not isinstance(codes, torch.Tensor) or codes.dim() != 3:
+        raise ValueError("codes must be a 3-D tensor")
+    E = codes.shape[0]
+    _need(codes, "codes", _U8, (E, O, I // 2))
+    _need(dY, "dY", _BF16)
+    _need(offsets, "offsets", _I32, (E + 1,))
+    if rows is not None:
+        _need(rows, "rows", _I32, (N,))
+    if dS is None:
+        dS = torch.empty((E, O, G), dtype=_F32, device=dY.device)
+    _need(dS, "dS", _F32, (E, O, G))
+    _dev(x_codes, x_scales, rows, offsets, dY, codes, dS)
+    _check("sq_bwd_dscale_act8_batched", load().sq_bwd_dscale_act8_batched(
+        fmt, act, E, T, N, O, I, _ptr(x_codes), _ptr(x_scales), _ptr(rows), _ptr(offsets), _ptr(dY), _ptr(codes),
+        _ptr(dS), _stream()))
+    return dS
 
 
 def abi_version():

@@ -1,0 +1,205 @@
+"""8-bit activation checkpoints against the oracle: every bf16 value through
+both packings, and the scale gradient from the kept values, single, split over
+the tokens and batched over experts, bit for bit the bf16 product's on the same
+values and within the fp32 bound of the exact sums."""
+
+import numpy as np
+import pytest
+import torch
+
+from conftest import ensure_library, gpu_ready
+from oracle import linear, step
+from paper_2609_04526_amd import inputs
+from parity_check import assert_elements
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_ready(), reason="needs a GPU")]
+
+BF16 = torch.bfloat16
+BLOCK = {"mx": 32, "nv": 16}
+
+
+@pytest.fixture(scope="module")
+def sq():
+    ensure_library()
+    from paper_2609_04526_amd import sq as _sq
+    return _sq
+
+
+def _all_bf16():
+    return torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(BF16)
+
+
+def _check_pack(sq, act, X):
+    q, s = sq.sq_act_pack(act, X.cuda())
+    rq, rs = step.act_pack(act, X.double().numpy())
+    assert np.array_equal(s.cpu().numpy(), rs)
+    # -0 and 0 are one value to the oracle's whole numbers, and E4M3 keeps the sign
+    assert np.array_equal(q.cpu().numpy(), rq)
+    v = sq.sq_act_unpack(act, q, s)
+    assert v.dtype == BF16
+    want = torch.from_numpy(step.act_unpack(act, rq, rs)).to(torch.float32).to(BF16)
+    assert torch.equal(torch.nan_to_num(v.cpu().float(), nan=777.0), torch.nan_to_num(want.float(), nan=777.0))
+
+
+@pytest.mark.parametrize("act", ["int8", "e4m3"])
+def test_every_bf16_as_a_block_of_its_own(sq, act):
+    """Each value alone with 31 zeros (its own scale), NaN and infinities among them."""
+    X = torch.zeros((2048, 1024), dtype=BF16)
+    X.view(-1, 32)[:, 5] = _all_bf16()
+    _check_pack(sq, act, X)
+
+
+@pytest.mark.parametrize("act", ["int8", "e4m3"])
+@pytest.mark.parametrize("top", [1.0, 1.4921875, 1.75, 1.7578125, 1.9921875, 2.0 ** -120, 2.0 ** -126, 2.0 ** 127])
+def test_every_smaller_bf16_under_one_scale(sq, act, top):
+    """Values of all magnitudes below the block's largest, ties and subnormal steps among them."""
+    v = _all_bf16()
+    v = v[v.float().abs() <= top]                      # finite ones only: NaN compares false
+    v = torch.cat((v, v.new_zeros((-len(v)) % 31)))
+    X = torch.cat((v.view(-1, 31), torch.full((len(v) // 31, 1), top, dtype=BF16)), 1)
+    X = torch.cat((X, X.new_zeros(((-len(X)) % 32, 32)))).view(-1, 1024)
+    _check_pack(sq, act, X.contiguous())
+
+
+@pytest.mark.parametrize("act", ["int8", "e4m3"])
+@pytest.mark.parametrize("T,I", [(1, 32), (3, 96), (129, 480), (1000, 4128)])
+def test_pack_shapes(sq, act, T, I):
+    g = inputs.rng(T + I)
+    X = torch.from_numpy((g.standard_normal((T, I)) * np.exp(2 * g.standard_normal((1, I)))).astype(np.float32)).to(BF16)
+    if T > 1:
+        X[1, 3], X[2, 40] = float("nan"), float("-inf")
+        X[2, :32] = 0
+    _check_pack(sq, act, X)
+
+
+@pytest.mark.parametrize("act", ["int8", "e4m3"])
+def test_unpack_every_code_under_every_scale(sq, act):
+    """All bytes, int8's -128 and E4M3's NaN among them, under all 256 scale bytes."""
+    codes = torch.arange(256, dtype=torch.uint8).repeat(256, 1)
+    scales = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 8)
+    v = sq.sq_act_unpack(act, codes.cuda(), scales.cuda()).cpu().float()
+    ref = step.act_unpack(act, codes.numpy(), scales.numpy())
+    want = torch.from_numpy(ref).to(torch.float32).to(BF16).float()
+    # fp32 holds every product but those below 2^-149; bf16 rounds once more below 2^-133
+    assert torch.equal(torch.nan_to_num(v, nan=777.0), torch.nan_to_num(want, nan=777.0))
+
+
+def _layer(seed, T, O, I, act):
+    X = inputs.bf16_normal(seed, (T, I)) * torch.exp(inputs.bf16_normal(seed + 3, (I,)).float())
+    q, s = step.act_pack(act, X.to(BF16).double().numpy())
+    dY = inputs.bf16_normal(seed + 1, (T, O))
+    return torch.from_numpy(q).cuda(), torch.from_numpy(s).cuda(), dY
+
+
+# few and many stages, ragged tokens, tiles cut at both edges, a split token sum, and one of whole large tiles
+SHAPES = [(0, 64, 128), (1, 8, 32), (63, 264, 96), (64, 256, 512), (65, 520, 288), (700, 264, 256), (1000, 520, 544),
+          (513, 1032, 1056)]
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("act", ["int8", "e4m3"])
+@pytest.mark.parametrize("T,O,I", SHAPES)
+def test_dscale(sq, fmt, act, T, O, I):
+    q, s, dY = _layer(T + O, T, O, I, act)
+    codes = inputs.codes_uniform(T + 9, O, I)
+    cd, dYd = torch.from_numpy(codes).cuda(), dY.cuda()
+    dS = torch.full((O, I // BLOCK[fmt]), float("nan"), device="cuda")
+    sq.sq_bwd_dscale_act8(fmt, act, q, s, dYd, cd, dS=dS)
+    x = step.act_unpack(act, q.cpu().numpy(), s.cpu().numpy())
+    assert torch.equal(dS, sq.sq_bwd_dscale(fmt, torch.from_numpy(x).to(BF16).cuda(), dYd, cd))
+    ref = linear.backward_dscale(fmt, x, dY.double().numpy(), codes)
+    mag = np.abs(linear.code_values(codes)) * (np.abs(dY.double().numpy()).T @ np.abs(x))
+    mag = mag.reshape(O, I // BLOCK[fmt], BLOCK[fmt]).sum(2)
+    assert_elements(dS.cpu().numpy(), ref, mag, T + BLOCK[fmt] + 10, (fmt, act, T, O, I))
+
+
+@pytest.mark.parametrize("T,O,I", [(4096, 4096, 4096), (1999, 1024, 4096), (4096, 4104, 4128)])
+@pytest.mark.parametrize("fmt,act", [("mx", "int8"), ("nv", "e4m3"), ("mx", "e4m3"), ("nv", "int8")])
+def test_dscale_of_large_layers_equals_the_bf16_product(sq, fmt, act, T, O, I):
+    X = inputs.device_bf16_normal(3, (T, I))
+    q, s = sq.sq_act_pack(act, X)
+    x = sq.sq_act_unpack(act, q, s)
+    dY, codes = inputs.device_bf16_normal(4, (T, O)), inputs.device_codes_uniform(5, O, I)
+    dS = torch.full((O, I // BLOCK[fmt]), float("nan"), device="cuda")
+    sq.sq_bwd_dscale_act8(fmt, act, q, s, dY, codes, dS=dS)
+    assert torch.equal(dS, sq.sq_bwd_dscale(fmt, x, dY, codes))
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("act", ["int8", "e4m3"])
+def test_dscale_carries_nan_blocks(sq, fmt, act):
+    T, O, I = 70, 72, 128
+    q, s, dY = _layer(1, T, O, I, act)
+    s[66, 2] = 255
+    codes = torch.from_numpy(inputs.codes_uniform(2, O, I)).cuda()
+    dS = sq.sq_bwd_dscale_act8(fmt, act, q, s, dY.cuda(), codes).cpu()
+    b = BLOCK[fmt]
+    bad = torch.isnan(dS).any(0)
+    assert [i for i in range(I // b) if bad[i]] == list(range(64 // b, 96 // b))
+
+
+def _expert_rows(seed, E, counts, T):
+    g = inputs.rng(seed)
+    offsets = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    return offsets, g.integers(0, T, int(offsets[-1])).astype(np.int32)
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("act", ["int8", "e4m3"])
+@pytest.mark.parametrize("O,I,T,counts", [
+    (72, 96, 50, [0, 1, 63, 64, 65, 0, 130]),
+    (264, 288, 300, [200, 0, 0, 5]),
+    (8, 32, 9, [0, 0, 0]),
+    (256, 256, 2000, [513, 700, 1025]),
+    (520, 256, 40, [7] * 40),
+])
+@pytest.mark.parametrize("indirect", [True, False])
+def test_dscale_batched(sq, fmt, act, O, I, T, counts, indirect):
+    """Each expert's plane is its single product's, bit for bit, from rows picked anywhere in the kept activation."""
+    E, N = len(counts), sum(counts)
+    offsets, rows = _expert_rows(O + I, E, counts, T)
+    if not indirect:
+        T = N
+    q, s, _ = _layer(O + 5, T, O, I, act)
+    dY = inputs.bf16_normal(O + 6, (N, O))
+    codes = torch.from_numpy(np.stack([inputs.codes_uniform(O + 7 + e, O, I) for e in range(E)])).cuda()
+    dS = torch.full((E, O, I // BLOCK[fmt]), float("nan"), device="cuda")
+    rows_d = torch.from_numpy(rows).cuda() if indirect else None
+    sq.sq_bwd_dscale_act8_batched(fmt, act, q, s, rows_d, torch.from_numpy(offsets).cuda(), dY.cuda(), codes, dS=dS)
+    x = step.act_unpack(act, q.cpu().numpy(), s.cpu().numpy())
+    for e, (a, b) in enumerate(zip(offsets[:-1], offsets[1:])):
+        xe = x[rows[a:b]] if indirect else x[a:b]
+        ref = linear.backward_dscale(fmt, xe, dY[a:b].double().numpy(), codes[e].cpu().numpy())
+        mag = np.abs(linear.code_values(codes[e].cpu().numpy())) * (np.abs(dY[a:b].double().numpy()).T @ np.abs(xe))
+        mag = mag.reshape(O, -1, BLOCK[fmt]).sum(2)
+        assert_elements(dS[e].cpu().numpy(), ref, mag, int(b - a) + BLOCK[fmt] + 10, (fmt, act, e))
+
+
+def test_dscale_batched_bounds_its_indexes(sq):
+    """Row numbers outside the kept activation read as zeros; offsets outside the rows are held to them."""
+    T, O, I, N = 20, 16, 64, 30
+    q, s, _ = _layer(3, T, O, I, "int8")
+    dY = inputs.bf16_normal(4, (N, O)).cuda()
+    codes = torch.from_numpy(np.stack([inputs.codes_uniform(5, O, I), inputs.codes_uniform(6, O, I)])).cuda()
+    rows = torch.arange(N, dtype=torch.int32, device="cuda") % T
+    rows[3], rows[4], rows[29] = -1, T, 2 ** 31 - 1
+    offsets = torch.tensor([-5, 10, 1 << 30], dtype=torch.int32, device="cuda")
+    got = sq.sq_bwd_dscale_act8_batched("mx", "int8", q, s, rows, offsets, dY, codes)
+    dY2 = dY.clone()
+    dY2[[3, 4, 29]] = 0
+    rows2 = rows.clamp(0, T - 1)
+    want = sq.sq_bwd_dscale_act8_batched("mx", "int8", q, s, rows2, torch.tensor([0, 10, N], dtype=torch.int32, device="cuda"),
+                                         dY2, codes)
+    assert torch.equal(got, want)
+
+
+def test_streams_and_runs_agree(sq):
+    q, s, dY = _layer(8, 700, 264, 256, "e4m3")
+    dY, codes = dY.cuda(), inputs.device_codes_uniform(9, 264, 256)
+    want = sq.sq_bwd_dscale_act8("nv", "e4m3", q, s, dY, codes)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        got = sq.sq_bwd_dscale_act8("nv", "e4m3", q, s, dY, codes)
+    st.synchronize()
+    assert torch.equal(want, got)

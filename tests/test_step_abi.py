@@ -95,3 +95,49 @@ def test_binding_refuses_what_the_library_cannot_see():
         sq.sq_moe_combine(X, slot, offsets)                  # 4 rows for 8 pairs
     with pytest.raises(ValueError, match="weights"):
         sq.sq_moe_combine(torch.zeros((8, 64)), slot, offsets, torch.zeros((4, 2), dtype=torch.float64))
+
+
+# ---------------------------------------------------------------- 8-bit activations
+@pytest.mark.parametrize("name", ["sq_act_pack", "sq_act_unpack"])
+@pytest.mark.parametrize("kw,status", [
+    (dict(act=2), ARG), (dict(T=-1), SHAPE), (dict(I=0), SHAPE), (dict(I=48), SHAPE), (dict(T=1 << 30, I=1 << 20), SHAPE),
+    (dict(a=None), ARG), (dict(b=None), ARG), (dict(c=None), ARG), (dict(a=OFF), ALIGN),
+])
+def test_act_refusals(lib, name, kw, status):
+    args = dict(act=0, T=16, I=64, a=FAKE, b=FAKE, c=FAKE, stream=None)
+    assert _call(getattr(lib, name), args, kw) == status
+    assert _call(getattr(lib, name), args, dict(T=0, a=None, b=None, c=None)) == 0
+
+
+def test_act_alignment_of_the_second_plane(lib):
+    assert lib.sq_act_pack(0, 16, 64, FAKE, OFF, FAKE, None) == ALIGN
+    assert lib.sq_act_unpack(0, 16, 64, FAKE, FAKE, OFF, None) == ALIGN
+
+
+DS8 = [(dict(fmt=2), FORMAT), (dict(act=-1), ARG), (dict(O=12), SHAPE), (dict(I=48), SHAPE), (dict(fmt=1, I=48), SHAPE),
+       (dict(T=-1), SHAPE), (dict(x=None), ARG), (dict(xs=None), ARG), (dict(dY=None), ARG), (dict(codes=None), ARG),
+       (dict(dS=None), ARG), (dict(x=OFF), ALIGN), (dict(dY=OFF), ALIGN), (dict(codes=FAKE + 2), ALIGN),
+       (dict(dS=FAKE + 2), ALIGN)]
+
+
+@pytest.mark.parametrize("kw,status", DS8 + [
+    (dict(T=1 << 17, I=1 << 13), SHAPE), (dict(T=4096, O=1024, I=4096), WORKSPACE),
+    (dict(T=4096, O=1024, I=4096, ws=FAKE, size=100), WORKSPACE), (dict(T=4096, O=1024, I=4096, ws=OFF, size=1 << 22), ALIGN)])
+def test_dscale_act8_refusals(lib, kw, status):
+    args = dict(fmt=0, act=0, T=64, O=256, I=512, x=FAKE, xs=FAKE, dY=FAKE, codes=FAKE, dS=FAKE, ws=None, size=0, stream=None)
+    assert _call(lib.sq_bwd_dscale_act8, args, kw) == status
+
+
+def test_dscale_act8_workspace(lib):
+    assert lib.sq_bwd_dscale_act8_workspace(0, 4096, 4096, 4096) == 0
+    assert lib.sq_bwd_dscale_act8_workspace(0, 4096, 1024, 4096) == lib.sq_bwd_dscale_workspace(0, 4096, 1024, 4096) > 0
+    assert lib.sq_bwd_dscale_act8_workspace(1, 4096, 1024, 4112) == 0          # not whole blocks of 32
+
+
+@pytest.mark.parametrize("kw,status", DS8 + [
+    (dict(E=0), SHAPE), (dict(E=65536), SHAPE), (dict(N=-1), SHAPE), (dict(N=1 << 30), SHAPE), (dict(rows=None), ARG),
+    (dict(offsets=None), ARG), (dict(rows=FAKE + 2), ALIGN), (dict(offsets=FAKE + 1), ALIGN), (dict(T=1 << 26), SHAPE)])
+def test_dscale_act8_batched_refusals(lib, kw, status):
+    args = dict(fmt=0, act=0, E=4, T=64, N=128, O=256, I=512, x=FAKE, xs=FAKE, rows=FAKE, offsets=FAKE, dY=FAKE, codes=FAKE,
+                dS=FAKE, stream=None)
+    assert _call(lib.sq_bwd_dscale_act8_batched, args, kw) == status
