@@ -83,6 +83,7 @@ typedef enum {
   SQ_RULE_STOCHASTIC = 3,    /* codes by stochastic rounding, per-block scales */
   SQ_RULE_WHOLE_TENSOR = 4   /* one scale from the tensor amax, nearest-even codes */
 } sq_rule;
+typedef enum { SQ_HEAD_MXFP4 = 0, SQ_HEAD_NVFP4 = 1, SQ_HEAD_BF16 = 2 } sq_head_format;
 typedef enum { SQ_ACT_INT8 = 0, SQ_ACT_E4M3 = 1 } sq_act_format;
 
 /*
@@ -579,6 +580,48 @@ int sq_bwd_dscale_act8(int fmt, int act, int64_t T, int64_t O, int64_t I, const 
 int sq_bwd_dscale_act8_batched(int fmt, int act, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I,
                                const uint8_t* x_codes, const uint8_t* x_scales, const int32_t* rows,
                                const int32_t* offsets, const void* dY, const uint8_t* codes, float* dS, void* stream);
+
+/*
+ * Softmax cross entropy of a language-model head over its whole vocabulary and
+ * the gradient of the head's input; the logits are never kept.  The head is
+ * frozen (it has no gradient of its own): W bf16 [V, I] (SQ_HEAD_BF16), or codes
+ * uint8 [V, I/2] with scales uint8 [V, G] and ws2 as the layer stores them
+ * (SQ_HEAD_MXFP4, SQ_HEAD_NVFP4; scales and ws2 are ignored for SQ_HEAD_BF16).
+ *
+ *   l[t,v]  = X[t] . W[v]           fp32 sums of exact products of bf16 values
+ *   lse[t]  = log sum_v exp l[t,v]
+ *   loss[t] = lse[t] - l[t, targets[t]]
+ *   dX[t]   = dloss[t] sum_v (exp(l[t,v] - lse[t]) - [v = targets[t]]) W[v]
+ *
+ * A token whose target lies outside 0 .. V-1 (say -100) is ignored: loss, lse
+ * and its row of dX are 0.  From 257 tokens on ignored tokens take no part in the
+ * products, so a batch of masked prompts costs what its other tokens cost.
+ * Infinities and NaN among a token's logits give NaN (but logits of -inf
+ * beside finite ones count as probability 0).
+ *
+ * sq_ce_fwd: X bf16 [T, I] (16-byte aligned), targets int32 or int64 [T]
+ *   (target_bytes 4 or 8) -> loss, lse fp32 [T].
+ * sq_ce_bwd: the same and lse (as sq_ce_fwd wrote it), dloss fp32 [T] (the
+ *   gradient that reaches each token's loss) -> dX [T, I] in dx_dtype.  The
+ *   logits are formed again in pieces of the vocabulary; their gradients are
+ *   rounded to bf16 for the product with W, as the layers' dY is, and summed in
+ *   fp32 over all pieces.
+ * I % 8 == 0 (SQ_HEAD_BF16) or I % B == 0; V >= 1; T*I*2 below 2 GiB.  codes
+ * 4-byte, W and dX 16-byte aligned.  workspace: 256-byte aligned, of at least
+ * sq_ce_fwd_workspace / sq_ce_bwd_workspace bytes (0 when T = 0), contents
+ * irrelevant: the row statistics (8 bytes per token and 256 entries of the
+ * vocabulary), or one piece's logit gradients (about 256 MiB at most; one of 256
+ * entries at least) and fp32 sums; and for a 4-bit head one piece of it as bf16 (256
+ * MiB at most).  Deterministic.
+ */
+size_t sq_ce_fwd_workspace(int head, int64_t T, int64_t V, int64_t I);
+size_t sq_ce_bwd_workspace(int head, int64_t T, int64_t V, int64_t I);
+int sq_ce_fwd(int head, int64_t T, int64_t V, int64_t I, const void* X, const void* W, const uint8_t* scales, float ws2,
+              const void* targets, int target_bytes, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+              void* stream);
+int sq_ce_bwd(int head, int64_t T, int64_t V, int64_t I, const void* X, const void* W, const uint8_t* scales, float ws2,
+              const void* targets, int target_bytes, const float* lse, const float* dloss, void* dX, int dx_dtype,
+              void* workspace, size_t workspace_bytes, void* stream);
 
 /* Human-readable name of a status code (static storage). */
 const char* sq_status_str(int status);

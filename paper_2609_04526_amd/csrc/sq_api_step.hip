@@ -160,3 +160,73 @@ SQ_EXPORT int sq_bwd_dscale_act8_batched(int fmt, int act, int64_t E, int64_t T,
   return hip_status(dscale_act8_batched(fmt, act, (int)E, (int)T, (int)N, (int)O, (int)I, x_codes, x_scales, rows,
                                         offsets, dY, codes, dS, static_cast<hipStream_t>(stream)));
 }
+
+// ---------------------------------------------------------------- cross entropy
+namespace {
+
+static_assert(SQ_HEAD_MXFP4 == SQ_MXFP4 && SQ_HEAD_NVFP4 == SQ_NVFP4 && SQ_HEAD_BF16 == kCeBf16,
+              "header and library agree on the head formats");
+
+int check_head(int head, int64_t T, int64_t V, int64_t I) {
+  if (head != SQ_HEAD_MXFP4 && head != SQ_HEAD_NVFP4 && head != SQ_HEAD_BF16) return SQ_ERR_FORMAT;
+  if (T < 0 || V < 1 || I < 1 || T > kDimMax || V > kDimMax - 256 || I > kDimMax) return SQ_ERR_SHAPE;
+  if (I % (head == SQ_HEAD_BF16 ? 8 : block_of(head)) != 0) return SQ_ERR_SHAPE;
+  // X and a 256-row tile of the head go through 32-bit offsets
+  if (T * I * 2 > kOperandBytesMax || I * 512 > kOperandBytesMax) return SQ_ERR_SHAPE;
+  return ((V + 255) / 256) * ((T + 63) / 64) > kDimMax ? SQ_ERR_SHAPE : SQ_OK;
+}
+
+int check_ce(int head, int64_t T, int64_t V, int64_t I, const void* X, const void* W, const uint8_t* scales, float ws2,
+             const void* targets, int target_bytes) {
+  const int st = check_head(head, T, V, I);
+  if (st != SQ_OK) return st;
+  if (target_bytes != 4 && target_bytes != 8) return SQ_ERR_ARG;
+  if (!W || (head != SQ_HEAD_BF16 && !scales) || (T > 0 && (!X || !targets))) return SQ_ERR_ARG;
+  if (head == SQ_HEAD_NVFP4 && !ws2_ok(ws2)) return SQ_ERR_ARG;
+  return aligned(X, 16) && aligned(W, head == SQ_HEAD_BF16 ? 16 : 4) && aligned(targets, (uintptr_t)target_bytes)
+             ? SQ_OK : SQ_ERR_ALIGN;
+}
+
+int check_ce_workspace(int bwd, int head, int64_t T, int64_t V, int64_t I, const void* workspace, size_t bytes) {
+  if (!workspace || bytes < ce_workspace(bwd, head, T, V, I)) return SQ_ERR_WORKSPACE;
+  return aligned(workspace, 256) ? SQ_OK : SQ_ERR_ALIGN;
+}
+
+}  // namespace
+
+SQ_EXPORT size_t sq_ce_fwd_workspace(int head, int64_t T, int64_t V, int64_t I) {
+  return check_head(head, T, V, I) != SQ_OK || T == 0 ? 0 : ce_workspace(0, head, T, V, I);
+}
+
+SQ_EXPORT size_t sq_ce_bwd_workspace(int head, int64_t T, int64_t V, int64_t I) {
+  return check_head(head, T, V, I) != SQ_OK || T == 0 ? 0 : ce_workspace(1, head, T, V, I);
+}
+
+SQ_EXPORT int sq_ce_fwd(int head, int64_t T, int64_t V, int64_t I, const void* X, const void* W, const uint8_t* scales,
+                        float ws2, const void* targets, int target_bytes, float* loss, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  int st = check_ce(head, T, V, I, X, W, scales, ws2, targets, target_bytes);
+  if (st != SQ_OK) return st;
+  if (T > 0 && (!loss || !lse)) return SQ_ERR_ARG;
+  if (!aligned(loss, 4) || !aligned(lse, 4)) return SQ_ERR_ALIGN;
+  if (T == 0) return SQ_OK;
+  st = check_ce_workspace(0, head, T, V, I, workspace, workspace_bytes);
+  if (st != SQ_OK) return st;
+  return hip_status(ce_fwd_launch(head, (int)T, V, (int)I, X, W, scales, head == SQ_HEAD_NVFP4 ? ws2 : 1.0f, targets,
+                                  target_bytes, loss, lse, workspace, static_cast<hipStream_t>(stream)));
+}
+
+SQ_EXPORT int sq_ce_bwd(int head, int64_t T, int64_t V, int64_t I, const void* X, const void* W, const uint8_t* scales,
+                        float ws2, const void* targets, int target_bytes, const float* lse, const float* dloss, void* dX,
+                        int dx_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  int st = check_ce(head, T, V, I, X, W, scales, ws2, targets, target_bytes);
+  if (st != SQ_OK) return st;
+  if (!dtype_ok(dx_dtype) || (T > 0 && (!lse || !dloss || !dX))) return SQ_ERR_ARG;
+  if (!aligned(lse, 4) || !aligned(dloss, 4) || !aligned(dX, 16)) return SQ_ERR_ALIGN;
+  if (T == 0) return SQ_OK;
+  st = check_ce_workspace(1, head, T, V, I, workspace, workspace_bytes);
+  if (st != SQ_OK) return st;
+  return hip_status(ce_bwd_launch(head, (int)T, V, (int)I, X, W, scales, head == SQ_HEAD_NVFP4 ? ws2 : 1.0f, targets,
+                                  target_bytes, lse, dloss, dX, dx_dtype == SQ_OUT_BF16, workspace,
+                                  static_cast<hipStream_t>(stream)));
+}

@@ -1,0 +1,671 @@
+// Softmax cross entropy of a language-model head over its whole vocabulary and
+// the gradient of the head's input, without the logits in memory.
+//
+//   l[t,v]  = X[t] . W[v]                       W bf16, or codes x scales
+//   lse[t]  = log sum_v exp l[t,v]              loss[t] = lse[t] - l[t,y_t]
+//   dX[t]   = dloss[t] sum_v (exp(l[t,v] - lse[t]) - [v = y_t]) W[v]
+//
+// Forward: tiles of the logits (256 rows of W by the tokens) leave only each
+// token's maximum and sum of exponentials over the tile; a second kernel joins
+// them.  Backward: pieces of the vocabulary; a piece's logits are formed again
+// and leave as bf16 gradients of the logits, [tokens, piece], which the next
+// product contracts with the same rows of W into fp32 sums.  A 4-bit head's
+// piece is written out as bf16 before it is used (code x scale is exact in
+// bf16; NVFP4's ws2 goes to the fp32 sums).
+//
+// Rows without a target in the vocabulary cost nothing beyond 256 tokens: the
+// rows that have one are numbered first, and tiles past the last of them end at
+// once.  The number stays on the device.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "sq_device.h"
+#include "sq_gemm_args.h"
+#include "sq_launch.h"
+#include "sq_tiles.h"
+
+namespace sq {
+
+namespace {
+
+constexpr int kCeGroup = 4;             // tile rows per group of the tile order
+
+__device__ __forceinline__ int64_t target_at(const void* y, int bytes, int64_t t) {
+  return bytes == 8 ? static_cast<const int64_t*>(y)[t] : (int64_t)static_cast<const int32_t*>(y)[t];
+}
+
+// ------------------------------------------------------------------ rows
+// rows[0 .. n) = the tokens whose target is in the vocabulary, in order; *count
+// = n.  One workgroup: 1024 tokens per step.
+__global__ __launch_bounds__(1024) void ce_rows_kernel(const void* __restrict__ y, int y_bytes, int T, int64_t V,
+                                                       int* __restrict__ count, int* __restrict__ rows) {
+  __shared__ int s_n[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int base = 0;
+  for (int t0 = 0; t0 < T; t0 += 1024) {
+    const int t = t0 + (int)threadIdx.x;
+    bool in = false;
+    if (t < T) {
+      const int64_t v = target_at(y, y_bytes, t);
+      in = v >= 0 && v < V;
+    }
+    const uint64_t b = __ballot(in);
+    if (lane == 0) s_n[wave] = __popcll(b);
+    __syncthreads();
+    int at = base, all = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      at += w < wave ? s_n[w] : 0;
+      all += s_n[w];
+    }
+    if (in) rows[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0))] = t;
+    base += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *count = base;
+}
+
+// ------------------------------------------------------------------ 4-bit heads
+// Rows [v0, v0 + n) of the head as bf16, 8 codes per lane.
+template <int FMT>
+__global__ __launch_bounds__(256) void ce_dequant_kernel(const uint8_t* __restrict__ codes,
+                                                         const uint8_t* __restrict__ scales, int64_t first, int64_t items,
+                                                         uint16_t* __restrict__ out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= items) return;
+  const uint32_t w = reinterpret_cast<const uint32_t*>(codes)[first + i];
+  const uint32_t b = scales[(first + i) / (ScaleOperand<FMT>::kBlock / 8)];
+  reinterpret_cast<uint4*>(out)[i] = ScaleOperand<FMT>::dequant8(w, ScaleOperand<FMT>::of(b));
+}
+
+// ------------------------------------------------------------------ products
+struct CeArgs {
+  const uint16_t* x;        // X [T, H]
+  const uint16_t* w;        // rows [v0, v0 + Vn) of W as bf16, [Vn, H]
+  uint16_t* d;              // gradients of the logits [T, ld], piece columns
+  float* part;              // forward: (max, sum) [tile of all of W][T]
+  float* tlogit;            // forward: the target's logit [T]
+  float* sums;              // backward: fp32 sums of dX, planes of [live rows in whole tiles, H]
+  const int* rows;          // compact row -> token, or null (row = token)
+  const int* count;         // live rows, or null (T)
+  const void* y;
+  const float* lse;
+  const float* dloss;
+  int64_t v0;               // first row of W of this piece
+  int64_t V;
+  int T, H, Vn, ld;
+  int y_bytes;
+  int part_tile0;           // forward: tile of all of W that this piece starts at
+  int split_stages;         // backward: 64-row stages of a whole piece
+  int add;                  // backward: the sums hold earlier pieces
+  float ws2;
+};
+
+// K-contiguous rows picked by number: as DmaKC, with row r0 + r of the tile at
+// row rows[r0 + r] of the matrix.
+template <int R, int NT>
+struct DmaRows {
+  static constexpr int kInst = R / 8 / (NT / 64);
+  static_assert(kInst * (NT / 64) * 8 == R, "tile rows must split over the waves");
+  uint32_t off[kInst];
+  int klim[kInst];
+  __device__ __forceinline__ void init(int ld, int live, int kdim, int r0, int tid, const int* rows) {
+    const int wave = tid >> 6, lane = tid & 63;
+#pragma unroll
+    for (int q = 0; q < kInst; ++q) {
+      const int r = (q * (NT / 64) + wave) * 8 + (lane >> 3);
+      const int c = (lane & 7) ^ swz_kc(r);
+      const int gr = r0 + r;
+      off[q] = kOOB;
+      if (gr < live) off[q] = ((uint32_t)(rows ? rows[gr] : gr) * (uint32_t)ld + (uint32_t)c * 8u) * 2u;
+      klim[q] = kdim - c * 8;
+    }
+  }
+  template <int Q0, int Q1>
+  __device__ __forceinline__ void issue_part(DmaRsrc rs, SQ_LDS uint16_t* s, int k0, int wave) const {
+#pragma unroll
+    for (int q = Q0; q < Q1; ++q) {
+      const uint32_t o = off[q] == kOOB || k0 >= klim[q] ? kOOB : off[q] + (uint32_t)k0 * 2u;
+      dma16(rs, s + (q * (NT / 64) + wave) * 8 * kBK, o);
+    }
+  }
+};
+
+// Split of the vocabulary rows of dX's contraction over workgroups, where the
+// live rows' tiles leave compute units idle (at least 4 stages each).
+__device__ __forceinline__ int ce_splits(int tiles, int stages) {
+  return max(1, min(min(kCUs / max(tiles, 1), stages / 4), 64));
+}
+
+enum CeMode { kCeStats = 0, kCeGrad = 1, kCeDx = 2 };
+
+// The tile product of all three, 256 x BN (logits: W's rows by tokens, so that
+// a lane holds one token's logits and sums them without its neighbours) or BM x
+// 256 (dX: tokens by columns of W).  64-deep stages copied global -> LDS, the
+// operands of a 16-deep slice read while the slice before it multiplies, and
+// the barrier that publishes the next stage before the last slice's products:
+// the schedule of the layer's own products (sq_gemm.hip).
+template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES>
+__global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
+  constexpr int NT = 64 * WGM * WGN;
+  constexpr int WM = BM / WGM, WN = BN / WGN;
+  constexpr int TM = WM / 32, TN = WN / 32;
+  constexpr int kA = BM * kBK * 2, kB = BN * kBK * 2, kStage = kA + kB;
+  constexpr bool kDxMode = MODE == kCeDx;
+  using DA = DmaKC<BM, NT>;
+  using DB = std::conditional_t<kDxMode, DmaNat<BN, NT, kBK>, DmaRows<BN, NT>>;
+  constexpr int kDma = DA::kInst + DB::kInst;
+  constexpr int kAhead = (STAGES - 2) * kDma;
+  static_assert(STAGES >= 2 && STAGES <= 3 && kAhead < 63, "stages");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[STAGES * kStage];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, wave = tid >> 6;
+  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+  const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
+  const int live = g.count ? min(*g.count, g.T) : g.T;
+
+  // tile, and the stages [s_first, s_first + nk) of its contraction
+  const int M = kDxMode ? live : g.Vn, N = kDxMode ? g.H : live, K = kDxMode ? g.Vn : g.H;
+  const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN, tiles = tiles_m * tiles_n;
+  const int splits = kDxMode ? ce_splits(tiles, g.split_stages) : 1;
+  if ((int)blockIdx.x >= tiles * splits) return;
+  const int pos = xcd_stretch((int)blockIdx.x, tiles * splits);
+  const int split = kDxMode ? pos / tiles : 0;
+  int tm, tn;
+  tile_at<kCeGroup>(pos - split * tiles, tiles_m, tiles_n, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  const int nk_all = (K + kBK - 1) / kBK;
+  const int per = (nk_all + splits - 1) / splits;
+  const int s_first = min(split * per, nk_all), nk = min(per, nk_all - s_first);
+
+  DmaRsrc ra, rb;
+  DA dA;
+  DB dB;
+  if constexpr (kDxMode) {
+    ra = make_dma_rsrc(g.d + (size_t)m0 * g.ld, (uint32_t)((size_t)min(BM, M - m0) * g.ld * 2));
+    rb = make_dma_rsrc(g.w + (size_t)s_first * kBK * g.H, (uint32_t)((size_t)(K - min(s_first * kBK, K)) * g.H * 2));
+    dA.init(g.ld, min(BM, M - m0), g.ld, 0, tid);
+    dB.init(g.H, g.H, n0, tid);
+  } else {
+    ra = make_dma_rsrc(g.w + (size_t)m0 * g.H, (uint32_t)((size_t)min(BM, M - m0) * g.H * 2));
+    rb = make_dma_rsrc(g.x, (uint32_t)((size_t)g.T * g.H * 2));
+    dA.init(g.H, min(BM, M - m0), g.H, 0, tid);
+    dB.init(g.H, live, g.H, n0, tid, g.rows);
+  }
+
+  f32x16 acc[TM][TN];
+  float* sums = nullptr;
+  if constexpr (kDxMode) {
+    // this split's plane of the live rows; earlier pieces' sums are carried on
+    sums = g.sums + (size_t)split * tiles_m * BM * g.H;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int col = n0 + wn0 + j * 32 + (lane & 31);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = m0 + wm0 + i * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+          acc[i][j][r] = g.add && col < g.H ? sums[(size_t)row * g.H + col] : 0.0f;
+        }
+      }
+  } else {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+  }
+
+  auto stage_at = [&](auto S) { return (SQ_LDS uint8_t*)lds + decltype(S)::value * kStage; };
+  // halves of the copy of stage kt into buffer S
+  auto dma_half = [&](auto S, int kt, auto HALF) {
+    constexpr int h = decltype(HALF)::value;
+    SQ_LDS uint16_t* a = (SQ_LDS uint16_t*)stage_at(S);
+    SQ_LDS uint16_t* b = (SQ_LDS uint16_t*)(stage_at(S) + kA);
+    const int ka = (s_first + kt) * kBK;
+    dA.template issue_part<h * DA::kInst / 2, (h + 1) * DA::kInst / 2>(ra, a, ka, false, wave_u);
+    if constexpr (kDxMode)
+      dB.template issue_part<h * DB::kInst / 2, (h + 1) * DB::kInst / 2>(rb, b, (uint32_t)(kt * kBK) * (uint32_t)g.H * 2u, wave_u);
+    else
+      dB.template issue_part<h * DB::kInst / 2, (h + 1) * DB::kInst / 2>(rb, b, ka, wave_u);
+  };
+
+  struct Frag {
+    bf16x8 a[TM];
+    bf16x8 b[TN];
+  };
+  Frag F0, F1;
+  auto read = [&](auto S, auto KK, Frag& f) {
+    constexpr int kk = decltype(KK)::value;
+    const SQ_LDS uint16_t* a = (const SQ_LDS uint16_t*)stage_at(S);
+    const SQ_LDS uint16_t* b = (const SQ_LDS uint16_t*)(stage_at(S) + kA);
+    const int chunk = 2 * kk + (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) f.a[i] = *(const SQ_LDS bf16x8*)(a + kc_off(wm0 + i * 32 + (lane & 31), chunk));
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      if constexpr (kDxMode) f.b[j] = nat_frag<BN>(b, kk, wn0 + j * 32, lane);
+      else f.b[j] = *(const SQ_LDS bf16x8*)(b + kc_off(wn0 + j * 32 + (lane & 31), chunk));
+    }
+  };
+  auto mma = [&](Frag& f) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+  using I2 = std::integral_constant<int, 2>;
+  using I3 = std::integral_constant<int, 3>;
+
+  auto step = [&](auto S, int kt) {
+    constexpr int s = decltype(S)::value;
+    using SN = std::integral_constant<int, (s + 1) % STAGES>;            // stage kt + 1
+    using SP = std::integral_constant<int, (s + STAGES - 1) % STAGES>;   // stage kt + STAGES - 1
+    read(S, I1{}, F1);
+    if (kt + STAGES - 1 < nk) dma_half(SP{}, kt + STAGES - 1, I1{});
+    mma(F0);
+    read(S, I2{}, F0);
+    mma(F1);
+    read(S, I3{}, F1);
+    mma(F0);
+    // stage kt + 1 has landed once only the copies of the stages after it are
+    // outstanding; in the last stages everything is waited for
+    if (kt + STAGES - 1 < nk) wait_vm_lgkm0<kAhead>();
+    else wait_vm_lgkm0<0>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (kt + 1 < nk) read(SN{}, I0{}, F0);
+    if (kt + STAGES < nk) dma_half(S, kt + STAGES, I0{});
+    mma(F1);
+  };
+  // prologue: stage 0 whole and its first operands, then stages 1 .. STAGES - 2
+  // and the first half of stage STAGES - 1
+  if (nk > 0) {
+    dma_half(I0{}, 0, I0{});
+    dma_half(I0{}, 0, I1{});
+    wait_vm_lgkm0<0>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    read(I0{}, I0{}, F0);
+    if constexpr (STAGES > 2) {
+      if (1 < nk) {
+        dma_half(I1{}, 1, I0{});
+        dma_half(I1{}, 1, I1{});
+      }
+    }
+    if (STAGES - 1 < nk) dma_half(std::integral_constant<int, STAGES - 1>{}, STAGES - 1, I0{});
+  }
+  for (int kt0 = 0; kt0 < nk; kt0 += STAGES) {
+    step(I0{}, kt0);
+    if (kt0 + 1 < nk) step(I1{}, kt0 + 1);
+    if constexpr (STAGES > 2) {
+      if (kt0 + 2 < nk) step(I2{}, kt0 + 2);
+    }
+  }
+  wait_vm_lgkm0<0>();
+
+  // ---------------------------------------------------------------- epilogue
+  // 32x32 output tile: lane l, register r holds row 8*(r/4) + 4*(l/32) + r%4,
+  // column l%32.
+  if constexpr (kDxMode) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int col = n0 + wn0 + j * 32 + (lane & 31);
+        if (col >= g.H) continue;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = m0 + wm0 + i * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+          sums[(size_t)row * g.H + col] = acc[i][j][r];
+        }
+      }
+  } else {
+    __syncthreads();                     // the operand tiles are done with
+    const int vrow = m0 + wm0 + 4 * (lane >> 5);             // first row of W of this lane's registers
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int row = n0 + wn0 + j * 32 + (lane & 31);       // compact token row
+      const bool in = row < live;
+      const int t = in ? (g.rows ? g.rows[row] : row) : 0;
+      const int64_t y = in ? target_at(g.y, g.y_bytes, t) : -1;
+      const bool valid = y >= 0 && y < g.V;
+      // the target's row counted from this lane's first, or one that no register holds
+      const int64_t off = y - g.v0 - vrow;
+      const int at = valid && off >= 0 && off < WM ? (int)off : -1, end = g.Vn - vrow;
+      if constexpr (MODE == kCeStats) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int v = i * 32 + 8 * (r >> 2) + (r & 3);
+            float l = acc[i][j][r] * g.ws2;
+            if (v == at) g.tlogit[row] = l;
+            l = v < end ? l : -INFINITY;
+            acc[i][j][r] = l;
+            top = fmaxf(top, l);
+          }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float ref = top == -INFINITY ? 0.0f : top;     // nothing to sum: exp(-inf) = 0
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum += __expf(acc[i][j][r] - ref);
+        sum += __shfl_xor(sum, 32);
+        SQ_LDS float* s = (SQ_LDS float*)lds + 2 * ((wave / WGN) * BN + wn0 + j * 32 + (lane & 31));
+        if (lane < 32) {
+          s[0] = top;
+          s[1] = sum;
+        }
+      } else {
+        const float c = valid ? g.dloss[t] : 0.0f, z = valid ? g.lse[t] : 0.0f;
+        // rounded to bf16 for the product with W, as the layers' dY is
+        SQ_LDS uint16_t* s = (SQ_LDS uint16_t*)lds + wave * WM * WN;
+        const int cj = j * 32 + (lane & 31);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float e[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int v = i * 32 + 8 * q + r;
+              const float p = __expf(acc[i][j][4 * q + r] * g.ws2 - z) - (v == at ? 1.0f : 0.0f);
+              e[r] = valid && v < end ? c * p : 0.0f;
+            }
+            u32x2 pair;
+            pair[0] = bits_of(__builtin_convertvector((f32x2{e[0], e[1]}), bf16x2));
+            pair[1] = bits_of(__builtin_convertvector((f32x2{e[2], e[3]}), bf16x2));
+            // 16-byte unit u of token cj at unit u ^ cj
+            const int u = i * 4 + q;
+            *(SQ_LDS u32x2*)(s + cj * WM + ((u ^ cj) & (WM / 8 - 1)) * 8 + 4 * (lane >> 5)) = pair;
+          }
+      }
+    }
+    if constexpr (MODE == kCeStats) {
+      __syncthreads();
+      if (tid < BN && n0 + tid < live) {
+        const SQ_LDS float* s = (const SQ_LDS float*)lds + 2 * tid;
+        float top = s[0], sum = s[1];
+#pragma unroll
+        for (int w = 1; w < WGM; ++w) {
+          const float b = s[2 * w * BN], bs = s[2 * w * BN + 1], m = fmaxf(top, b);
+          const float ref = m == -INFINITY ? 0.0f : m;
+          sum = sum * __expf(top - ref) + bs * __expf(b - ref);
+          top = m;
+        }
+        float2* out = reinterpret_cast<float2*>(g.part) + (size_t)(g.part_tile0 + tm) * g.T + n0 + tid;
+        *out = make_float2(top, sum);
+      }
+    } else {
+      // a wave's own block: WM / 8 lanes take a token's row
+      const SQ_LDS uint16_t* s = (const SQ_LDS uint16_t*)lds + wave * WM * WN;
+      constexpr int kLanes = WM / 8, kTok = 64 / kLanes;
+#pragma unroll
+      for (int it = 0; it < WN / kTok; ++it) {
+        const int cj = it * kTok + lane / kLanes, u = lane % kLanes;
+        const u32x4 v = *(const SQ_LDS u32x4*)(s + cj * WM + ((u ^ cj) & (kLanes - 1)) * 8);
+        const int row = n0 + wn0 + cj, col = m0 + wm0 + u * 8;
+        if (row < live && col < g.ld) *reinterpret_cast<u32x4*>(g.d + (size_t)row * g.ld + col) = v;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ joins
+// loss and lse of 64 tokens per workgroup: 16 waves share the tiles' pairs.
+__global__ __launch_bounds__(1024) void ce_loss_kernel(const float2* __restrict__ part, const float* __restrict__ tlogit,
+                                                       const int* __restrict__ rows, const int* __restrict__ count,
+                                                       const void* __restrict__ y, int y_bytes, int T, int64_t V,
+                                                       int tiles, float* __restrict__ loss, float* __restrict__ lse) {
+  __shared__ float s_top[16][64], s_sum[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int live = count ? min(*count, T) : T;
+  const int row = (int)blockIdx.x * 64 + lane;
+  float top = -INFINITY, sum = 0.0f;
+  if (row < live) {
+#pragma unroll 4
+    for (int i = wave; i < tiles; i += 16) {
+      const float2 p = part[(size_t)i * T + row];
+      const float m = fmaxf(top, p.x), ref = m == -INFINITY ? 0.0f : m;
+      sum = sum * __expf(top - ref) + p.y * __expf(p.x - ref);
+      top = m;
+    }
+  }
+  s_top[wave][lane] = top;
+  s_sum[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && row < live) {
+    for (int w = 1; w < 16; ++w) {
+      const float b = s_top[w][lane], m = fmaxf(top, b), ref = m == -INFINITY ? 0.0f : m;
+      sum = sum * __expf(top - ref) + s_sum[w][lane] * __expf(b - ref);
+      top = m;
+    }
+    const int t = rows ? rows[row] : row;
+    const int64_t v = target_at(y, y_bytes, t);
+    if (v >= 0 && v < V) {
+      const float z = top + __logf(sum);
+      lse[t] = z;
+      loss[t] = z - tlogit[row];
+    }
+  }
+  // tokens without a target (this workgroup's share of all tokens)
+  const int t = (int)blockIdx.x * 64 + lane;
+  if (wave == 1 && t < T) {
+    const int64_t v = target_at(y, y_bytes, t);
+    if (v < 0 || v >= V) lse[t] = loss[t] = 0.0f;
+  }
+}
+
+// dX of one token per workgroup: the splits' planes added in order, times ws2;
+// zeros where there is no target (their rows come after the live ones).
+template <bool BF16>
+__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ sums, const int* __restrict__ rows,
+                                                    const int* __restrict__ count, const void* __restrict__ y,
+                                                    int y_bytes, int T, int64_t V, int H, int bm, int tiles_n, int stages,
+                                                    float ws2, void* __restrict__ dX) {
+  const int live = count ? min(*count, T) : T;
+  const int b = (int)blockIdx.x;
+  auto put = [&](int t, int h, float4 v) {
+    if constexpr (BF16) {
+      u32x2 w;
+      w[0] = bits_of(__builtin_convertvector((f32x2{v.x, v.y}), bf16x2));
+      w[1] = bits_of(__builtin_convertvector((f32x2{v.z, v.w}), bf16x2));
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(dX) + (size_t)t * H + h) = w;
+    } else {
+      *reinterpret_cast<float4*>(static_cast<float*>(dX) + (size_t)t * H + h) = v;
+    }
+  };
+  if (b < live) {
+    const int tiles_m = (live + bm - 1) / bm, splits = ce_splits(tiles_m * tiles_n, stages);
+    const size_t plane = (size_t)tiles_m * bm * H;
+    const int t = rows ? rows[b] : b;
+    for (int h = threadIdx.x * 4; h < H; h += 1024) {
+      float4 v = *reinterpret_cast<const float4*>(sums + (size_t)b * H + h);
+      for (int s = 1; s < splits; ++s) {
+        const float4 u = *reinterpret_cast<const float4*>(sums + s * plane + (size_t)b * H + h);
+        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+      }
+      v.x *= ws2; v.y *= ws2; v.z *= ws2; v.w *= ws2;
+      put(t, h, v);
+    }
+  }
+  const int64_t v = target_at(y, y_bytes, b);
+  if (v < 0 || v >= V)
+    for (int h = threadIdx.x * 4; h < H; h += 1024) put(b, h, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+}
+
+inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
+
+// ------------------------------------------------------------------ plan
+constexpr int64_t kCePieceBytes = int64_t(256) << 20;        // a piece's logit gradients, and a 4-bit head's bf16 rows
+
+struct CePlan {
+  int bt;                   // token extent of the tiles
+  bool compact;             // rows without a target are left out
+  int64_t piece;            // rows of W per piece (a multiple of 256)
+  int pieces;
+  int ld;                   // backward: columns of the logit gradients
+  size_t rows, tlogit, part, wbuf, d, sums, total;           // offsets in the workspace
+};
+
+inline int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
+CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
+  CePlan p{};
+  p.bt = T <= 64 ? 64 : T <= 128 ? 128 : 256;
+  p.compact = T > 256;
+  int64_t most = V;
+  if (bwd) most = kCePieceBytes / (2 * T);
+  if (four_bit || bwd) {                                     // also 32-bit offsets into a piece of W
+    const int64_t by_w = (four_bit ? kCePieceBytes : int64_t(1) << 30) / (2 * H);
+    most = most < by_w ? most : by_w;
+  }
+  most = most / 256 * 256 > 256 ? most / 256 * 256 : 256;
+  p.pieces = (int)((V + most - 1) / most);
+  p.piece = up((V + p.pieces - 1) / p.pieces, 256);
+  p.pieces = (int)((V + p.piece - 1) / p.piece);
+  size_t at = 256;                                           // the count of live rows
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return o;
+  };
+  p.rows = take(p.compact ? (size_t)T * 4 : 0);
+  if (four_bit) p.wbuf = take((size_t)p.piece * H * 2);
+  if (!bwd) {
+    p.tlogit = take((size_t)T * 4);
+    p.part = take((size_t)((V + 255) / 256) * T * 8);
+  } else {
+    p.ld = (int)(p.piece < V ? p.piece : up(V, 64));
+    p.d = take((size_t)T * p.ld * 2);
+    // planes of whole tiles: splits x tiles <= max(CUs, tiles), or one tile row's
+    const int64_t tiles = up(T, p.bt) / p.bt * (up(H, 256) / 256);
+    p.sums = take((size_t)(tiles > kCUs ? tiles : kCUs) * p.bt * 256 * 4);
+  }
+  p.total = at;
+  return p;
+}
+
+template <int MODE>
+int ce_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
+  if (blocks == 0) return 0;
+  const dim3 grid((unsigned)blocks), block(512);
+  if constexpr (MODE == kCeDx) {
+    if (bt == 64) hipLaunchKernelGGL((ce_kernel<MODE, 64, 256, 1, 8, 3>), grid, block, 0, s, g);
+    else if (bt == 128) hipLaunchKernelGGL((ce_kernel<MODE, 128, 256, 2, 4, 3>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((ce_kernel<MODE, 256, 256, 2, 4, 2>), grid, block, 0, s, g);
+  } else {
+    if (bt == 64) hipLaunchKernelGGL((ce_kernel<MODE, 256, 64, 8, 1, 3>), grid, block, 0, s, g);
+    else if (bt == 128) hipLaunchKernelGGL((ce_kernel<MODE, 256, 128, 4, 2, 3>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((ce_kernel<MODE, 256, 256, 2, 4, 2>), grid, block, 0, s, g);
+  }
+  return ok();
+}
+
+// The bf16 rows [v0, v0 + n) of the head: its own, or a 4-bit piece written out.
+int ce_weight(int head, const void* W, const uint8_t* scales, int64_t v0, int64_t n, int64_t H, void* buf,
+              const uint16_t** out, hipStream_t s) {
+  if (head == kCeBf16) {
+    *out = static_cast<const uint16_t*>(W) + v0 * H;
+    return 0;
+  }
+  uint16_t* b = static_cast<uint16_t*>(buf);
+  *out = b;
+  const int64_t first = v0 * H / 8, items = n * H / 8;
+  const dim3 grid((unsigned)((items + 255) / 256)), block(256);
+  const uint8_t* codes = static_cast<const uint8_t*>(W);
+  if (head == kMX) hipLaunchKernelGGL((ce_dequant_kernel<kMX>), grid, block, 0, s, codes, scales, first, items, b);
+  else hipLaunchKernelGGL((ce_dequant_kernel<kNV>), grid, block, 0, s, codes, scales, first, items, b);
+  return ok();
+}
+
+}  // namespace
+
+size_t ce_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H) {
+  return ce_plan(bwd != 0, head != kCeBf16, T, V, H).total;
+}
+
+int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                  const void* y, int y_bytes, float* loss, float* lse, void* workspace, hipStream_t s) {
+  const CePlan p = ce_plan(false, head != kCeBf16, T, V, H);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  CeArgs g{};
+  g.x = static_cast<const uint16_t*>(X);
+  g.y = y; g.y_bytes = y_bytes; g.T = T; g.H = H; g.V = V; g.ws2 = ws2;
+  g.part = reinterpret_cast<float*>(ws + p.part);
+  g.tlogit = reinterpret_cast<float*>(ws + p.tlogit);
+  if (p.compact) {
+    int* count = reinterpret_cast<int*>(ws);
+    int* rows = reinterpret_cast<int*>(ws + p.rows);
+    g.count = count;
+    g.rows = rows;
+    hipLaunchKernelGGL(ce_rows_kernel, dim3(1), dim3(1024), 0, s, y, y_bytes, T, V, count, rows);
+    if (ok() != 0) return -1;
+  }
+  const int64_t tt = (T + p.bt - 1) / p.bt;
+  for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
+    const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
+    if (ce_weight(head, W, scales, v0, n, H, ws + p.wbuf, &g.w, s) != 0) return -1;
+    g.v0 = v0;
+    g.Vn = (int)n;
+    g.part_tile0 = (int)(v0 / 256);
+    if (ce_go<kCeStats>(g, p.bt, (n + 255) / 256 * tt, s) != 0) return -1;
+  }
+  hipLaunchKernelGGL(ce_loss_kernel, dim3((unsigned)((T + 63) / 64)), dim3(1024), 0, s,
+                     reinterpret_cast<const float2*>(g.part), g.tlogit, g.rows, g.count, y, y_bytes, T, V,
+                     (int)((V + 255) / 256), loss, lse);
+  return ok();
+}
+
+int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                  const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16,
+                  void* workspace, hipStream_t s) {
+  const CePlan p = ce_plan(true, head != kCeBf16, T, V, H);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  CeArgs g{};
+  g.x = static_cast<const uint16_t*>(X);
+  g.y = y; g.y_bytes = y_bytes; g.T = T; g.H = H; g.V = V; g.ws2 = ws2;
+  g.lse = lse; g.dloss = dloss;
+  g.d = reinterpret_cast<uint16_t*>(ws + p.d);
+  g.sums = reinterpret_cast<float*>(ws + p.sums);
+  g.ld = p.ld;
+  g.split_stages = (int)((p.piece < V ? p.piece : V) + kBK - 1) / kBK;
+  if (p.compact) {
+    int* count = reinterpret_cast<int*>(ws);
+    int* rows = reinterpret_cast<int*>(ws + p.rows);
+    g.count = count;
+    g.rows = rows;
+    hipLaunchKernelGGL(ce_rows_kernel, dim3(1), dim3(1024), 0, s, y, y_bytes, T, V, count, rows);
+    if (ok() != 0) return -1;
+  }
+  const int64_t tt = (T + p.bt - 1) / p.bt, tn = (H + 255) / 256;
+  const int64_t dx_blocks = tt * tn > kCUs ? tt * tn : kCUs;
+  for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
+    const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
+    if (ce_weight(head, W, scales, v0, n, H, ws + p.wbuf, &g.w, s) != 0) return -1;
+    g.v0 = v0;
+    g.Vn = (int)n;
+    g.add = v0 > 0;
+    if (ce_go<kCeGrad>(g, p.bt, (n + 255) / 256 * tt, s) != 0) return -1;
+    if (ce_go<kCeDx>(g, p.bt, dx_blocks, s) != 0) return -1;
+  }
+  auto finish = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(256), 0, s, g.sums, g.rows, g.count, y, y_bytes, T, V, H, p.bt,
+                       (int)tn, g.split_stages, ws2, dX);
+    return ok();
+  };
+  return dx_bf16 ? finish(ce_dx_kernel<true>) : finish(ce_dx_kernel<false>);
+}
+
+}  // namespace sq

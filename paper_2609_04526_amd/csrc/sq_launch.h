@@ -187,4 +187,13 @@ int dscale_act8_batched(int fmt, int act, int E, int Tx, int N, int O, int I, co
                         const int32_t* rows, const int32_t* offsets, const void* dY, const uint8_t* codes, float* dS,
                         hipStream_t s);
 
+// Cross entropy of a head (sq_ce.hip).  head: 0 MXFP4, 1 NVFP4, 2 bf16 rows.
+constexpr int kCeBf16 = 2;
+size_t ce_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H);
+int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                  const void* y, int y_bytes, float* loss, float* lse, void* workspace, hipStream_t s);
+int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                  const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16,
+                  void* workspace, hipStream_t s);
+
 }  // namespace sq

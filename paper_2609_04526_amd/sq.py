@@ -26,6 +26,8 @@ RULES = {"even": RULE_NEAREST_EVEN, "away": RULE_NEAREST_AWAY, "rtz": RULE_RTZ,
          "stochastic": RULE_STOCHASTIC, "whole_tensor": RULE_WHOLE_TENSOR}
 BLOCK = {MXFP4: 32, NVFP4: 16}
 ACT_INT8, ACT_E4M3 = 0, 1
+HEAD_MXFP4, HEAD_NVFP4, HEAD_BF16 = 0, 1, 2
+HEADS = {"mx": HEAD_MXFP4, "nv": HEAD_NVFP4, "bf16": HEAD_BF16}
 ACTS = {"int8": ACT_INT8, "e4m3": ACT_E4M3}
 ACT_BLOCK = 32
 
@@ -161,6 +163,12 @@ def _load():
                                               _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]),
         "sq_bwd_dscale_act8_batched": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i64,
                                                       _c_i64, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p]),
+        "sq_ce_fwd_workspace": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64]),
+        "sq_ce_bwd_workspace": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64]),
+        "sq_ce_fwd": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p, ctypes.c_float, _c_p,
+                                     ctypes.c_int, _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]),
+        "sq_ce_bwd": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p, ctypes.c_float, _c_p,
+                                     ctypes.c_int, _c_p, _c_p, _c_p, ctypes.c_int, _c_p, ctypes.c_size_t, _c_p]),
         "sq_status_str": (ctypes.c_char_p, [ctypes.c_int]),
         "sq_abi_version": (ctypes.c_int, []),
     }
@@ -1033,6 +1041,72 @@ def sq_bwd_dscale_act8_batched(fmt, act, x_codes, x_scales, rows, offsets, dY, c
         fmt, act, E, T, N, O, I, _ptr(x_codes), _ptr(x_scales), _ptr(rows), _ptr(offsets), _ptr(dY), _ptr(codes),
         _ptr(dS), _stream()))
     return dS
+
+
+# ---------------------------------------------------------------- cross entropy
+def sq_ce_fwd_workspace(head, T, V, I):
+    return int(load().sq_ce_fwd_workspace(HEADS.get(head, head), T, V, I))
+
+
+def sq_ce_bwd_workspace(head, T, V, I):
+    return int(load().sq_ce_bwd_workspace(HEADS.get(head, head), T, V, I))
+
+
+def _head(head, X, W, targets, scales):
+    """T, V, I of a head's operands."""
+    T, I = _dims2(X, "X")
+    V = _dims2(W, "W")[0]
+    _need(X, "X", _BF16)
+    if head == HEAD_BF16:
+        _need(W, "W", _BF16, (V, I))
+    else:
+        G = _block(head, I)
+        _need(W, "W", _U8, (V, I // 2))
+        _need(scales, "scales", _U8, (V, G))
+    _need(targets, "targets", _IDS, (T,))
+    return T, V, I
+
+
+def _scratch(workspace, need, device):
+    if workspace is None:
+        return torch.empty(need, dtype=_U8, device=device) if need else None
+    return _need(workspace, "workspace", _U8)
+
+
+def sq_ce_fwd(head, X, W, targets, scales=None, ws2=1.0, loss=None, lse=None, workspace=None):
+    """(loss, lse) fp32 [T] of X bf16 [T, I] through the head "bf16" (W bf16 [V, I]), "mx" or "nv" (W the codes
+    uint8 [V, I/2], with scales and ws2); targets outside 0 .. V-1 are ignored."""
+    head = HEADS.get(head, head)
+    T, V, I = _head(head, X, W, targets, scales)
+    if loss is None:
+        loss = torch.empty(T, dtype=_F32, device=X.device)
+    if lse is None:
+        lse = torch.empty(T, dtype=_F32, device=X.device)
+    _need(loss, "loss", _F32, (T,))
+    _need(lse, "lse", _F32, (T,))
+    workspace = _scratch(workspace, int(load().sq_ce_fwd_workspace(head, T, V, I)), X.device)
+    _dev(X, W, targets, scales, loss, lse, workspace)
+    _check("sq_ce_fwd", load().sq_ce_fwd(head, T, V, I, _ptr(X), _ptr(W), _ptr(scales), float(ws2), _ptr(targets),
+                                         targets.element_size(), _ptr(loss), _ptr(lse), _ptr(workspace),
+                                         0 if workspace is None else workspace.numel(), _stream()))
+    return loss, lse
+
+
+def sq_ce_bwd(head, X, W, targets, lse, dloss, scales=None, ws2=1.0, out_dtype=torch.float32, dX=None, workspace=None):
+    """dX [T, I] of sq_ce_fwd for dloss fp32 [T]; lse as sq_ce_fwd returned it."""
+    head = HEADS.get(head, head)
+    T, V, I = _head(head, X, W, targets, scales)
+    _need(lse, "lse", _F32, (T,))
+    _need(dloss, "dloss", _F32, (T,))
+    if dX is None:
+        dX = torch.empty((T, I), dtype=out_dtype, device=X.device)
+    _need(dX, "dX", _OUT, (T, I))
+    workspace = _scratch(workspace, int(load().sq_ce_bwd_workspace(head, T, V, I)), X.device)
+    _dev(X, W, targets, scales, lse, dloss, dX, workspace)
+    _check("sq_ce_bwd", load().sq_ce_bwd(head, T, V, I, _ptr(X), _ptr(W), _ptr(scales), float(ws2), _ptr(targets),
+                                         targets.element_size(), _ptr(lse), _ptr(dloss), _ptr(dX), _dtype_of(dX),
+                                         _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+    return dX
 
 
 def abi_version():

@@ -141,3 +141,56 @@ def test_dscale_act8_batched_refusals(lib, kw, status):
     args = dict(fmt=0, act=0, E=4, T=64, N=128, O=256, I=512, x=FAKE, xs=FAKE, rows=FAKE, offsets=FAKE, dY=FAKE, codes=FAKE,
                 dS=FAKE, stream=None)
     assert _call(lib.sq_bwd_dscale_act8_batched, args, kw) == status
+
+
+# ---------------------------------------------------------------- cross entropy
+CE = [(dict(head=3), FORMAT), (dict(head=-1), FORMAT), (dict(T=-1), SHAPE), (dict(V=0), SHAPE), (dict(I=12), SHAPE),
+      (dict(head=0, I=48), SHAPE), (dict(head=1, I=40), SHAPE), (dict(T=1 << 20, I=2048), SHAPE), (dict(V=1 << 31), SHAPE),
+      (dict(X=None), ARG), (dict(W=None), ARG), (dict(y=None), ARG), (dict(yb=2), ARG), (dict(head=0, scales=None), ARG),
+      (dict(head=1, ws2=0.0), ARG), (dict(head=1, ws2=float("inf")), ARG), (dict(X=OFF), ALIGN), (dict(W=OFF), ALIGN),
+      (dict(head=0, W=FAKE + 2), ALIGN), (dict(y=FAKE + 4), ALIGN), (dict(ws=None), WORKSPACE), (dict(size=100), WORKSPACE),
+      (dict(ws=FAKE + 16), ALIGN)]
+
+
+@pytest.mark.parametrize("kw,status", CE + [(dict(loss=None), ARG), (dict(lse=None), ARG), (dict(loss=FAKE + 2), ALIGN),
+                                            (dict(lse=FAKE + 1), ALIGN)])
+def test_ce_fwd_refusals(lib, kw, status):
+    args = dict(head=2, T=64, V=1000, I=512, X=FAKE, W=FAKE, scales=FAKE, ws2=1.0, y=FAKE, yb=8, loss=FAKE, lse=FAKE, ws=FAKE,
+                size=1 << 40, stream=None)
+    assert _call(lib.sq_ce_fwd, args, kw) == status
+
+
+@pytest.mark.parametrize("kw,status", CE + [(dict(lse=None), ARG), (dict(dl=None), ARG), (dict(dX=None), ARG), (dict(dt=2), ARG),
+                                            (dict(lse=FAKE + 2), ALIGN), (dict(dl=FAKE + 2), ALIGN), (dict(dX=OFF), ALIGN)])
+def test_ce_bwd_refusals(lib, kw, status):
+    args = dict(head=2, T=64, V=1000, I=512, X=FAKE, W=FAKE, scales=FAKE, ws2=1.0, y=FAKE, yb=8, lse=FAKE, dl=FAKE, dX=FAKE,
+                dt=1, ws=FAKE, size=1 << 40, stream=None)
+    assert _call(lib.sq_ce_bwd, args, kw) == status
+
+
+def test_ce_without_tokens(lib):
+    assert lib.sq_ce_fwd(2, 0, 1000, 512, None, FAKE, None, 1.0, None, 8, None, None, None, 0, None) == 0
+    assert lib.sq_ce_bwd(2, 0, 1000, 512, None, FAKE, None, 1.0, None, 8, None, None, None, 0, None, 0, None) == 0
+    assert lib.sq_ce_fwd_workspace(2, 0, 1000, 512) == 0
+
+
+@pytest.mark.parametrize("head", [0, 1, 2])
+def test_ce_workspace_stays_bounded(lib, head):
+    """No workspace holds the logits: a large batch over a large vocabulary stays under a gigabyte and a half."""
+    T, V, I = 8192, 160000, 8192
+    assert 0 < lib.sq_ce_fwd_workspace(head, T, V, I) < 3 << 29
+    assert 0 < lib.sq_ce_bwd_workspace(head, T, V, I) < 3 << 29
+    assert lib.sq_ce_fwd_workspace(head, T, V, 12) == 0
+
+
+def test_binding_refuses_a_head_it_cannot_read():
+    from paper_2609_04526_amd import sq
+    X, y = torch.zeros((4, 64), dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int64)
+    with pytest.raises(ValueError, match="W"):
+        sq.sq_ce_fwd("bf16", X, torch.zeros((10, 32), dtype=torch.bfloat16), y)
+    with pytest.raises(ValueError, match="scales"):
+        sq.sq_ce_fwd("mx", X, torch.zeros((10, 32), dtype=torch.uint8), y)
+    with pytest.raises(ValueError, match="targets"):
+        sq.sq_ce_fwd("bf16", X, torch.zeros((10, 64), dtype=torch.bfloat16), y.float())
+    with pytest.raises(ValueError, match="device tensors"):
+        sq.sq_ce_fwd("bf16", X, torch.zeros((10, 64), dtype=torch.bfloat16), y)
