@@ -396,6 +396,196 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ds8_kernel(Ds8Args g) {
   wait_vm_lgkm0<0>();
 }
 
+// One tile per workgroup, for long token sums.  Between two barriers a step reads
+// and multiplies one 64-row stage; x^'s items of the stage two ahead are loaded
+// at its start and written to the freed buffer after its barrier, dY's copy of
+// that stage goes out half there and half in the next step's first slice.
+template <int FMT, int ACT, int BM, int BN, int WGM, int WGN, bool ROWS>
+__global__ __launch_bounds__(64 * WGM * WGN) void ds8_tile_kernel(Ds8Args g) {
+  constexpr int NT = 64 * WGM * WGN;
+  constexpr int WM = BM / WGM, WN = BN / WGN;
+  constexpr int TM = WM / 32, TN = WN / 32;
+  constexpr int kA = BM * kBK * 2, kB = BN * kBK * 2;
+  constexpr int kPer = kBK * (BM / 8) / NT;                   // 8-column items per thread and stage
+  constexpr int kRowStep = NT / (BM / 8);
+  static_assert(kPer * NT == kBK * (BM / 8) && kPer * kRowStep == kBK, "items split over the threads");
+  using DB = DmaNat<BN, NT, kBK>;
+  __shared__ __attribute__((aligned(16))) uint8_t lds0[kA + kB];
+  __shared__ __attribute__((aligned(16))) uint8_t lds1[kA + kB];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, wave = tid >> 6;
+  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+  const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
+  const int O = g.O, I = g.I, G = g.G;
+  const int tiles_m = (I + BM - 1) / BM, tiles_n = (O + BN - 1) / BN, per = tiles_m * tiles_n;
+  const int pos = xcd_stretch((int)blockIdx.x, (int)gridDim.x);
+  const int e = pos / per;
+  int tm, tn;
+  tile_at<8>(pos - e * per, tiles_m, tiles_n, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  int r0, n;
+  if (g.offsets) {                                            // device data: held to the rows there are
+    r0 = __builtin_amdgcn_readfirstlane(min(max(g.offsets[e], 0), g.N));
+    n = __builtin_amdgcn_readfirstlane(min(max(g.offsets[e + 1], r0), g.N)) - r0;
+  } else {
+    r0 = min(e * g.rows_per, g.N);
+    n = min(r0 + g.rows_per, g.N) - r0;
+  }
+  const int nk = (n + kBK - 1) / kBK;
+
+  const int irow = tid / (BM / 8), icol = (tid % (BM / 8)) * 8;
+  const bool icol_in = m0 + icol < I;
+  // x^ by row number, or the group's rows from a base that moves with the stage
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(g.x, (uint32_t)((size_t)g.Tx * I));
+  const __amdgpu_buffer_rsrc_t rxs = make_rsrc(g.xs, (uint32_t)((size_t)g.Tx * (I / 32)));
+  const __amdgpu_buffer_rsrc_t rrow = make_rsrc(g.rows, ROWS ? (uint32_t)g.N * 4u : 0u);
+  uint32_t qoff[ROWS ? 1 : kPer], soff[ROWS ? 1 : kPer];
+  if constexpr (!ROWS) {
+#pragma unroll
+    for (int p = 0; p < kPer; ++p) {
+      const uint32_t r = (uint32_t)(irow + p * kRowStep);
+      qoff[p] = icol_in ? r * (uint32_t)I + (uint32_t)(m0 + icol) : kOOB;
+      soff[p] = icol_in ? r * (uint32_t)(I / 32) + (uint32_t)((m0 + icol) / 32) : kOOB;
+    }
+  }
+  int idx[ROWS ? kPer : 1];
+  auto load_rows = [&](int kt) {
+    if constexpr (ROWS) {
+#pragma unroll
+      for (int p = 0; p < kPer; ++p) {
+        const int k = kt * kBK + irow + p * kRowStep;
+        idx[p] = __builtin_amdgcn_raw_buffer_load_b32(rrow, (int)(k < n ? (uint32_t)(r0 + k) * 4u : kOOB), 0, 0);
+      }
+    }
+  };
+  u32x2 q[kPer];
+  uint32_t sb[kPer];
+  auto load_items = [&](int kt) {
+    if constexpr (ROWS) {
+#pragma unroll
+      for (int p = 0; p < kPer; ++p) {
+        const uint32_t r = (uint32_t)idx[p];
+        const bool in = kt * kBK + irow + p * kRowStep < n && icol_in && r < (uint32_t)g.Tx;
+        const uint32_t oc = in ? r * (uint32_t)I + (uint32_t)(m0 + icol) : kOOB;
+        const uint32_t os = in ? r * (uint32_t)(I / 32) + (uint32_t)((m0 + icol) / 32) : kOOB;
+        q[p] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, (int)oc, 0, 0));
+        sb[p] = __builtin_amdgcn_raw_buffer_load_b8(rxs, (int)os, 0, 0);
+      }
+    } else {
+      const int first = r0 + kt * kBK, left = n - kt * kBK;   // rows of the group from this stage on
+      const __amdgpu_buffer_rsrc_t bx = make_rsrc(g.x + (size_t)first * I, (uint32_t)left * (uint32_t)I);
+      const __amdgpu_buffer_rsrc_t bs = make_rsrc(g.xs + (size_t)first * (I / 32), (uint32_t)left * (uint32_t)(I / 32));
+#pragma unroll
+      for (int p = 0; p < kPer; ++p) {
+        q[p] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(bx, (int)qoff[p], 0, 0));
+        sb[p] = __builtin_amdgcn_raw_buffer_load_b8(bs, (int)soff[p], 0, 0);
+      }
+    }
+  };
+  auto stage = [&](auto S) { return decltype(S)::value == 0 ? (SQ_LDS uint8_t*)lds0 : (SQ_LDS uint8_t*)lds1; };
+  auto commit_items = [&](auto S) {
+    SQ_LDS uint16_t* s = (SQ_LDS uint16_t*)stage(S);
+#pragma unroll
+    for (int p = 0; p < kPer; ++p)
+      *(SQ_LDS u32x4*)(s + nat_off<BM>(irow + p * kRowStep, icol)) = kept8<ACT>(q[p], sb[p]);
+  };
+  const DmaRsrc rb = make_dma_rsrc(g.dy + (size_t)r0 * O, (uint32_t)((size_t)n * O * 2));
+  DB dB;
+  dB.init(O, O, n0, tid);
+  auto dma_half = [&](auto S, int kt, auto HALF) {
+    constexpr int h = decltype(HALF)::value;
+    dB.template issue_part<h * DB::kInst / 2, (h + 1) * DB::kInst / 2>(rb, (SQ_LDS uint16_t*)(stage(S) + kA),
+                                                                      (uint32_t)kt * kBK * (uint32_t)O * 2u, wave_u);
+  };
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+  struct Frag {
+    bf16x8 a[TM];
+    bf16x8 b[TN];
+  };
+  Frag F0, F1;
+  auto read = [&](auto S, auto KK, Frag& f) {
+    constexpr int kk = decltype(KK)::value;
+    const SQ_LDS uint16_t* a = (const SQ_LDS uint16_t*)stage(S);
+    const SQ_LDS uint16_t* b = (const SQ_LDS uint16_t*)(stage(S) + kA);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) f.a[i] = nat_frag<BM>(a, kk, wm0 + i * 32, lane);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) f.b[j] = nat_frag<BN>(b, kk, wn0 + j * 32, lane);
+  };
+  auto mma = [&](Frag& f) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+  using I2 = std::integral_constant<int, 2>;
+  using I3 = std::integral_constant<int, 3>;
+  auto step = [&](auto S, int kt) {
+    using SN = std::integral_constant<int, 1 - decltype(S)::value>;
+    if (kt + 2 < nk) {
+      load_items(kt + 2);
+      load_rows(kt + 3);
+    }
+    read(S, I1{}, F1);
+    if (kt + 1 < nk) dma_half(SN{}, kt + 1, I1{});
+    mma(F0);
+    read(S, I2{}, F0);
+    mma(F1);
+    read(S, I3{}, F1);
+    mma(F0);
+    wait_vm_lgkm0<0>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (kt + 1 < nk) read(SN{}, I0{}, F0);
+    if (kt + 2 < nk) dma_half(S, kt + 2, I0{});
+    mma(F1);
+    if (kt + 2 < nk) commit_items(S);
+  };
+  // prologue: stage 0 whole, stage 1's items and the first half of its copy
+  if (nk > 0) {
+    load_rows(0);
+    load_items(0);
+    load_rows(1);
+    dma_half(I0{}, 0, I0{});
+    dma_half(I0{}, 0, I1{});
+    commit_items(I0{});
+    if (1 < nk) {
+      load_items(1);
+      load_rows(2);
+      commit_items(I1{});
+    }
+    wait_vm_lgkm0<0>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    read(I0{}, I0{}, F0);
+    if (1 < nk) dma_half(I1{}, 1, I0{});
+  }
+  for (int kt0 = 0; kt0 < nk; kt0 += 2) {
+    step(I0{}, kt0);
+    if (kt0 + 1 < nk) step(I1{}, kt0 + 1);
+  }
+  wait_vm_lgkm0<0>();
+
+  float* const dS = g.out + (size_t)e * O * G;
+  u32x4 cw[TM * TN];
+  ds_codes<FMT, TM, TN>(cw, g.codes + (size_t)e * g.code_step, O, I, m0 + wm0, n0 + wn0, lane);
+  if (m0 + BM <= I && n0 + BN <= O)
+    ds_store<FMT, TM, TN, true>(acc, cw, dS, O, I, G, m0 + wm0, n0 + wn0, lane);
+  else
+    ds_store<FMT, TM, TN, false>(acc, cw, dS, O, I, G, m0 + wm0, n0 + wn0, lane);
+}
+
 // dS[i] = sum over s of part[s][i], s in increasing order; n is a multiple of 4.
 __global__ __launch_bounds__(256) void ds8_reduce_kernel(const float* __restrict__ part, float* __restrict__ dS,
                                                          int64_t n, int splits) {
@@ -411,21 +601,26 @@ __global__ __launch_bounds__(256) void ds8_reduce_kernel(const float* __restrict
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
 
-template <int FMT, int ACT, int BM, int BN, int WGM, int WGN>
-int ds8_go(const Ds8Args& g, int per_cu, hipStream_t s) {
-  const int64_t total = (int64_t)((g.I + BM - 1) / BM) * ((g.O + BN - 1) / BN) * g.groups;
-  const int blocks = (int)(total < (int64_t)per_cu * kCUs ? total : (int64_t)per_cu * kCUs);
-  if (g.rows)
-    hipLaunchKernelGGL((ds8_kernel<FMT, ACT, BM, BN, WGM, WGN, true>), dim3((unsigned)blocks), dim3(64 * WGM * WGN), 0, s, g);
-  else
-    hipLaunchKernelGGL((ds8_kernel<FMT, ACT, BM, BN, WGM, WGN, false>), dim3((unsigned)blocks), dim3(64 * WGM * WGN), 0, s, g);
+template <int FMT, int ACT>
+int ds8_go(const Ds8Args& g, bool large, hipStream_t s) {
+  if (large) {
+    const int64_t total = (int64_t)((g.I + 255) / 256) * ((g.O + 255) / 256) * g.groups;
+    const dim3 grid((unsigned)total), block(512);
+    if (g.rows) hipLaunchKernelGGL((ds8_tile_kernel<FMT, ACT, 256, 256, 2, 4, true>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((ds8_tile_kernel<FMT, ACT, 256, 256, 2, 4, false>), grid, block, 0, s, g);
+    return ok();
+  }
+  const int64_t total = (int64_t)((g.I + 127) / 128) * ((g.O + 127) / 128) * g.groups;
+  const dim3 grid((unsigned)(total < 2 * kCUs ? total : 2 * kCUs)), block(512);
+  if (g.rows) hipLaunchKernelGGL((ds8_kernel<FMT, ACT, 128, 128, 2, 4, true>), grid, block, 0, s, g);
+  else hipLaunchKernelGGL((ds8_kernel<FMT, ACT, 128, 128, 2, 4, false>), grid, block, 0, s, g);
   return ok();
 }
 
 int ds8_launch(int fmt, int act, bool large, const Ds8Args& g, hipStream_t s) {
   auto go = [&](auto F, auto A) {
     constexpr int f = decltype(F)::value, a = decltype(A)::value;
-    return large ? ds8_go<f, a, 256, 256, 2, 4>(g, 1, s) : ds8_go<f, a, 128, 128, 2, 4>(g, 2, s);
+    return ds8_go<f, a>(g, large, s);
   };
   using MX = std::integral_constant<int, kMX>;
   using NV = std::integral_constant<int, kNV>;
