@@ -557,7 +557,7 @@ int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, const void* d
  *
  * sq_bwd_dscale_act8: sq_bwd_dscale with x^ in the place of X, bit for bit what
  *   that call computes for the unpacked x^.  I % 32 == 0 for either weight
- *   format; x_codes 16-byte aligned; workspace as sq_bwd_dscale's, of
+ *   format, O and I at most 2^23; x_codes 16-byte aligned; workspace as sq_bwd_dscale's, of
  *   sq_bwd_dscale_act8_workspace bytes; the rest as sq_bwd_dscale.
  *
  * sq_bwd_dscale_act8_batched: the scale gradients of E stacked experts, whose
@@ -568,8 +568,10 @@ int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, const void* d
  *   experts read one copy of the layer's tokens), or row s when rows is NULL
  *   (then N == T).  codes uint8 [E, O, I/2]; dS fp32 [E, O, G], every plane
  *   written (zeros for an expert without rows).  A row number outside 0 .. T-1
- *   reads as a row of zeros, and offsets are held to 0 .. N.  1 <= E <= 65535; T*I and
- *   N*O*2 below 2 GiB.  Deterministic.
+ *   reads as a row of zeros, and offsets are held to 0 .. N.  1 <= E <= 8192; T*I*2
+ *   and N*O*2 below 2 GiB.  workspace: at least
+ *   sq_bwd_dscale_act8_batched_workspace(E, T, I) bytes (mostly the tokens' x^ in
+ *   bf16, for the time of the call), 16-byte aligned, contents irrelevant.  Deterministic.
  */
 int sq_act_pack(int act, int64_t T, int64_t I, const void* X, uint8_t* codes_out, uint8_t* scales_out, void* stream);
 int sq_act_unpack(int act, int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, void* X, void* stream);
@@ -579,7 +581,9 @@ int sq_bwd_dscale_act8(int fmt, int act, int64_t T, int64_t O, int64_t I, const 
                        size_t workspace_bytes, void* stream);
 int sq_bwd_dscale_act8_batched(int fmt, int act, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I,
                                const uint8_t* x_codes, const uint8_t* x_scales, const int32_t* rows,
-                               const int32_t* offsets, const void* dY, const uint8_t* codes, float* dS, void* stream);
+                               const int32_t* offsets, const void* dY, const uint8_t* codes, float* dS,
+                               void* workspace, size_t workspace_bytes, void* stream);
+size_t sq_bwd_dscale_act8_batched_workspace(int64_t E, int64_t T, int64_t I);
 
 /*
  * Softmax cross entropy of a language-model head over its whole vocabulary and

@@ -92,6 +92,8 @@ SQ_EXPORT int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, con
 // ---------------------------------------------------------------- 8-bit activations
 namespace {
 
+constexpr int64_t kExpertsMax = 8192;      // the batched scale gradient's lists in LDS
+
 bool act_ok(int act) { return act == SQ_ACT_INT8 || act == SQ_ACT_E4M3; }
 
 int check_act(int act, int64_t T, int64_t I, const void* X, const uint8_t* codes, const uint8_t* scales) {
@@ -109,6 +111,7 @@ int check_dscale8(int fmt, int act, int64_t Tx, int64_t N, int64_t O, int64_t I,
   if (!act_ok(act)) return SQ_ERR_ARG;
   if (I % 32 != 0 || Tx < 0 || N < 0 || Tx > kDimMax || N > kDimMax / 4) return SQ_ERR_SHAPE;
   if (Tx * I > kOperandBytesMax || N * O * 2 > kOperandBytesMax) return SQ_ERR_SHAPE;
+  if (O > (1 << 23) || I > (1 << 23)) return SQ_ERR_SHAPE;      // a 64-row stage within 32-bit offsets
   if (!codes || !dS || (N > 0 && !dY) || (Tx > 0 && (!x || !xs))) return SQ_ERR_ARG;
   return aligned(x, 16) && aligned(dY, 16) && aligned(codes, 4) && aligned(dS, 4) ? SQ_OK : SQ_ERR_ALIGN;
 }
@@ -147,18 +150,27 @@ SQ_EXPORT int sq_bwd_dscale_act8(int fmt, int act, int64_t T, int64_t O, int64_t
                                 static_cast<hipStream_t>(stream)));
 }
 
+SQ_EXPORT size_t sq_bwd_dscale_act8_batched_workspace(int64_t E, int64_t T, int64_t I) {
+  if (E < 1 || E > kExpertsMax || T < 0 || I < 1 || T > kDimMax || I > kDimMax || I % 32 != 0 || T * I * 2 > kOperandBytesMax) return 0;
+  return dscale_act8_batched_workspace((int)E, (int)T, (int)I);
+}
+
 SQ_EXPORT int sq_bwd_dscale_act8_batched(int fmt, int act, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I,
                                          const uint8_t* x_codes, const uint8_t* x_scales, const int32_t* rows,
                                          const int32_t* offsets, const void* dY, const uint8_t* codes, float* dS,
-                                         void* stream) {
+                                         void* workspace, size_t workspace_bytes, void* stream) {
   const int st = check_dscale8(fmt, act, T, N, O, I, x_codes, x_scales, dY, codes, dS);
   if (st != SQ_OK) return st;
+  if (T * I * 2 > kOperandBytesMax) return SQ_ERR_SHAPE;
   // the tiles of all experts are numbered in 32 bits
-  if (E < 1 || E > 65535 || E * ((O + 127) / 128) * ((I + 127) / 128) > kDimMax) return SQ_ERR_SHAPE;
+  if (E < 1 || E > kExpertsMax || E * ((O + 255) / 256) * ((I + 255) / 256) > kDimMax) return SQ_ERR_SHAPE;
   if (!offsets || (N > 0 && !rows && N != T)) return SQ_ERR_ARG;
   if (!aligned(rows, 4) || !aligned(offsets, 4)) return SQ_ERR_ALIGN;
+  const size_t need = sq_bwd_dscale_act8_batched_workspace(E, T, I);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return SQ_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 16)) return SQ_ERR_ALIGN;
   return hip_status(dscale_act8_batched(fmt, act, (int)E, (int)T, (int)N, (int)O, (int)I, x_codes, x_scales, rows,
-                                        offsets, dY, codes, dS, static_cast<hipStream_t>(stream)));
+                                        offsets, dY, codes, dS, workspace, static_cast<hipStream_t>(stream)));
 }
 
 // ---------------------------------------------------------------- cross entropy

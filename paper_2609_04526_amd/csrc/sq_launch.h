@@ -185,7 +185,8 @@ int dscale_act8(int fmt, int act, int T, int O, int I, const uint8_t* x, const u
                 const uint8_t* codes, float* dS, void* workspace, hipStream_t s);
 int dscale_act8_batched(int fmt, int act, int E, int Tx, int N, int O, int I, const uint8_t* x, const uint8_t* xs,
                         const int32_t* rows, const int32_t* offsets, const void* dY, const uint8_t* codes, float* dS,
-                        hipStream_t s);
+                        void* workspace, hipStream_t s);
+size_t dscale_act8_batched_workspace(int E, int T, int I);
 
 // Cross entropy of a head (sq_ce.hip).  head: 0 MXFP4, 1 NVFP4, 2 bf16 rows.
 constexpr int kCeBf16 = 2;

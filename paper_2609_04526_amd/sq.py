@@ -162,7 +162,9 @@ def _load():
         "sq_bwd_dscale_act8": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
                                               _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]),
         "sq_bwd_dscale_act8_batched": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i64,
-                                                      _c_i64, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p]),
+                                                      _c_i64, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p,
+                                                      ctypes.c_size_t, _c_p]),
+        "sq_bwd_dscale_act8_batched_workspace": (ctypes.c_size_t, [_c_i64, _c_i64, _c_i64]),
         "sq_ce_fwd_workspace": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64]),
         "sq_ce_bwd_workspace": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64]),
         "sq_ce_fwd": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p, ctypes.c_float, _c_p,
@@ -852,6 +854,13 @@ def sq_byte_diff(a, b, counts=None):
     return counts
 
 
+def _scratch(workspace, need, device):
+    """The caller's workspace, or a fresh one of `need` bytes."""
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    return _need(workspace, "workspace", torch.uint8)
+
+
 # ---------------------------------------------------------------- tokens to experts and back
 _I32 = torch.int32
 _IDS = (torch.int64, torch.int32)
@@ -884,11 +893,7 @@ def sq_moe_sort(ids, n_experts, offsets=None, token=None, slot=None, workspace=N
     _need(offsets, "offsets", _I32, (n_experts + 1,))
     _need(token, "token", _I32, (T * K,))
     _need(slot, "slot", _I32, (T, K))
-    ws_bytes = int(load().sq_moe_sort_workspace(T, K, n_experts))
-    if ws_bytes and workspace is None:
-        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=ids.device)
-    if workspace is not None:
-        _need(workspace, "workspace", torch.uint8)
+    workspace = _scratch(workspace, int(load().sq_moe_sort_workspace(T, K, n_experts)), ids.device)
     _dev(ids, offsets, token, slot, workspace)
     _check("sq_moe_sort", load().sq_moe_sort(T, K, n_experts, _ptr(ids), ids.element_size(), _ptr(offsets), _ptr(token),
                                              _ptr(slot), _ptr(workspace), 0 if workspace is None else workspace.numel(),
@@ -1006,11 +1011,7 @@ def sq_bwd_dscale_act8(fmt, act, x_codes, x_scales, dY, codes, dS=None, workspac
     if dS is None:
         dS = torch.empty((O, G), dtype=_F32, device=dY.device)
     _need(dS, "dS", _F32, (O, G))
-    ws_bytes = int(load().sq_bwd_dscale_act8_workspace(fmt, T, O, I))
-    if ws_bytes and workspace is None:
-        workspace = torch.empty(ws_bytes, dtype=_U8, device=dY.device)
-    if workspace is not None:
-        _need(workspace, "workspace", _U8)
+    workspace = _scratch(workspace, int(load().sq_bwd_dscale_act8_workspace(fmt, T, O, I)), dY.device)
     _dev(x_codes, x_scales, dY, codes, dS, workspace)
     _check("sq_bwd_dscale_act8", load().sq_bwd_dscale_act8(
         fmt, act, T, O, I, _ptr(x_codes), _ptr(x_scales), _ptr(dY), _ptr(codes), _ptr(dS), _ptr(workspace),
@@ -1018,7 +1019,11 @@ def sq_bwd_dscale_act8(fmt, act, x_codes, x_scales, dY, codes, dS=None, workspac
     return dS
 
 
-def sq_bwd_dscale_act8_batched(fmt, act, x_codes, x_scales, rows, offsets, dY, codes, dS=None):
+def sq_bwd_dscale_act8_batched_workspace(E, T, I):
+    return int(load().sq_bwd_dscale_act8_batched_workspace(E, T, I))
+
+
+def sq_bwd_dscale_act8_batched(fmt, act, x_codes, x_scales, rows, offsets, dY, codes, dS=None, workspace=None):
     """dS fp32 [E, O, G] of E stacked experts (codes uint8 [E, O, I/2]); expert e's rows of dY bf16 [N, O] are
     [offsets[e], offsets[e+1]) and meet rows rows[s] of the kept X (None: row s)."""
     fmt, act = _fmt(fmt), ACTS.get(act, act)
@@ -1036,10 +1041,11 @@ def sq_bwd_dscale_act8_batched(fmt, act, x_codes, x_scales, rows, offsets, dY, c
     if dS is None:
         dS = torch.empty((E, O, G), dtype=_F32, device=dY.device)
     _need(dS, "dS", _F32, (E, O, G))
-    _dev(x_codes, x_scales, rows, offsets, dY, codes, dS)
+    workspace = _scratch(workspace, int(load().sq_bwd_dscale_act8_batched_workspace(E, T, I)), dY.device)
+    _dev(x_codes, x_scales, rows, offsets, dY, codes, dS, workspace)
     _check("sq_bwd_dscale_act8_batched", load().sq_bwd_dscale_act8_batched(
         fmt, act, E, T, N, O, I, _ptr(x_codes), _ptr(x_scales), _ptr(rows), _ptr(offsets), _ptr(dY), _ptr(codes),
-        _ptr(dS), _stream()))
+        _ptr(dS), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
     return dS
 
 
@@ -1065,12 +1071,6 @@ def _head(head, X, W, targets, scales):
         _need(scales, "scales", _U8, (V, G))
     _need(targets, "targets", _IDS, (T,))
     return T, V, I
-
-
-def _scratch(workspace, need, device):
-    if workspace is None:
-        return torch.empty(need, dtype=_U8, device=device) if need else None
-    return _need(workspace, "workspace", _U8)
 
 
 def sq_ce_fwd(head, X, W, targets, scales=None, ws2=1.0, loss=None, lse=None, workspace=None):

@@ -135,11 +135,12 @@ def test_dscale_act8_workspace(lib):
 
 
 @pytest.mark.parametrize("kw,status", DS8 + [
-    (dict(E=0), SHAPE), (dict(E=65536), SHAPE), (dict(N=-1), SHAPE), (dict(N=1 << 30), SHAPE), (dict(rows=None), ARG),
-    (dict(offsets=None), ARG), (dict(rows=FAKE + 2), ALIGN), (dict(offsets=FAKE + 1), ALIGN), (dict(T=1 << 26), SHAPE)])
+    (dict(E=0), SHAPE), (dict(E=8193), SHAPE), (dict(N=-1), SHAPE), (dict(N=1 << 30), SHAPE), (dict(rows=None), ARG),
+    (dict(offsets=None), ARG), (dict(rows=FAKE + 2), ALIGN), (dict(offsets=FAKE + 1), ALIGN), (dict(T=1 << 26), SHAPE),
+    (dict(T=1 << 21), SHAPE), (dict(ws=None), WORKSPACE), (dict(size=64 * 512 * 2 - 1), WORKSPACE), (dict(ws=OFF), ALIGN)])
 def test_dscale_act8_batched_refusals(lib, kw, status):
     args = dict(fmt=0, act=0, E=4, T=64, N=128, O=256, I=512, x=FAKE, xs=FAKE, rows=FAKE, offsets=FAKE, dY=FAKE, codes=FAKE,
-                dS=FAKE, stream=None)
+                dS=FAKE, ws=FAKE, size=64 * 512 * 2 + 16 + 8 * 256, stream=None)
     assert _call(lib.sq_bwd_dscale_act8_batched, args, kw) == status
 
 
