@@ -467,13 +467,32 @@ __global__ __launch_bounds__(1024) void ce_loss_kernel(const float2* __restrict_
   }
 }
 
-// dX of one token per workgroup: the splits' planes added in order, times ws2;
-// zeros where there is no target (their rows come after the live ones).
+// What the last kernel of the gradient adds up: planes of fp32 sums, and the rows
+// of a 4-bit head past a multiple of 8, which the layer's products do not take.
+struct CeTail {
+  const uint8_t* codes;     // of the first such row
+  const uint8_t* scales;
+  const float* d;           // [T, 8] their logits' gradients
+  int rows;
+  int fmt;
+};
+
+template <int FMT>
+__device__ __forceinline__ float code_at(const uint8_t* codes, const uint8_t* scales, int64_t i) {
+  const float c = e2m1_to_f32((uint32_t)(codes[i >> 1] >> (4 * (i & 1))) & 15u);
+  const uint32_t b = scales[i / ScaleOperand<FMT>::kBlock];
+  return c * (FMT == kMX ? e8m0_to_f32(b) : e4m3_to_f32(b));
+}
+
+// dX of one token per workgroup: the planes added in order, times f (and the
+// tail's rows times ws2); zeros where there is no target (their rows come after
+// the live ones).  planes = 0: as many as the product split the vocabulary into.
 template <bool BF16>
-__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ sums, const int* __restrict__ rows,
-                                                    const int* __restrict__ count, const void* __restrict__ y,
-                                                    int y_bytes, int T, int64_t V, int H, int bm, int tiles_n, int stages,
-                                                    float ws2, void* __restrict__ dX) {
+__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ sums, int planes, int64_t plane_rows,
+                                                    const int* __restrict__ rows, const int* __restrict__ count,
+                                                    const void* __restrict__ y, int y_bytes, int T, int64_t V, int H,
+                                                    int bm, int tiles_n, int stages, float f, float ws2, CeTail tail,
+                                                    void* __restrict__ dX) {
   const int live = count ? min(*count, T) : T;
   const int b = (int)blockIdx.x;
   auto put = [&](int t, int h, float4 v) {
@@ -486,23 +505,143 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ su
       *reinterpret_cast<float4*>(static_cast<float*>(dX) + (size_t)t * H + h) = v;
     }
   };
-  if (b < live) {
-    const int tiles_m = (live + bm - 1) / bm, splits = ce_splits(tiles_m * tiles_n, stages);
-    const size_t plane = (size_t)tiles_m * bm * H;
+  const int64_t target = target_at(y, y_bytes, b);
+  const bool ignored = target < 0 || target >= V;
+  if (b < live && (rows || !ignored)) {
+    if (planes == 0) {
+      const int tiles_m = (live + bm - 1) / bm;
+      planes = ce_splits(tiles_m * tiles_n, stages);
+      plane_rows = (int64_t)tiles_m * bm;
+    }
+    const size_t plane = (size_t)plane_rows * H;
     const int t = rows ? rows[b] : b;
     for (int h = threadIdx.x * 4; h < H; h += 1024) {
       float4 v = *reinterpret_cast<const float4*>(sums + (size_t)b * H + h);
-      for (int s = 1; s < splits; ++s) {
+#pragma unroll 8
+      for (int s = 1; s < planes; ++s) {
         const float4 u = *reinterpret_cast<const float4*>(sums + s * plane + (size_t)b * H + h);
         v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
       }
-      v.x *= ws2; v.y *= ws2; v.z *= ws2; v.w *= ws2;
+      v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+      for (int r = 0; r < tail.rows; ++r) {
+        const float d = tail.d[b * 8 + r] * ws2;
+        const int64_t at = (int64_t)r * H + h;
+        auto w = [&](int i) {
+          return tail.fmt == kMX ? code_at<kMX>(tail.codes, tail.scales, at + i) : code_at<kNV>(tail.codes, tail.scales, at + i);
+        };
+        v.x = __builtin_fmaf(d, w(0), v.x);
+        v.y = __builtin_fmaf(d, w(1), v.y);
+        v.z = __builtin_fmaf(d, w(2), v.z);
+        v.w = __builtin_fmaf(d, w(3), v.w);
+      }
       put(t, h, v);
     }
   }
-  const int64_t v = target_at(y, y_bytes, b);
-  if (v < 0 || v >= V)
+  if (ignored)
     for (int h = threadIdx.x * 4; h < H; h += 1024) put(b, h, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+}
+
+// ------------------------------------------------------------------ 4-bit heads, few tokens
+// With few tokens the time is the head's bytes, and a 4-bit head written out in
+// bf16 first is five times its own.  There the layer's own products read the
+// codes (their few-token strips and narrow tiles), a piece of fp32 logits passes
+// through the workspace, and these kernels do the rest.
+
+// (max, sum) of 256 logits of one token per wave, and the target's logit.
+__global__ __launch_bounds__(256) void ce_part_kernel(const float* __restrict__ logits, int n, int64_t v0, int T,
+                                                      int64_t V, const void* __restrict__ y, int y_bytes,
+                                                      float2* __restrict__ part, float* __restrict__ tlogit) {
+  const int lane = threadIdx.x & 63, t = (int)blockIdx.y * 4 + (threadIdx.x >> 6);
+  if (t >= T) return;
+  const int c0 = (int)blockIdx.x * 256 + lane * 4;
+  float l[4], top = -INFINITY;
+  const int64_t at = target_at(y, y_bytes, t) - v0 - c0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    l[i] = c0 + i < n ? logits[(int64_t)t * n + c0 + i] : -INFINITY;
+    if (at == i && c0 + i < n) tlogit[t] = l[i];
+    top = fmaxf(top, l[i]);
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum += __expf(l[i] - ref);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  if (lane == 0) part[(size_t)blockIdx.x * T + t] = make_float2(top, sum);
+}
+
+// The logits' gradients in bf16, 8 of one token per lane, each group of `width`
+// columns of the vocabulary a [T, its width] matrix of its own.  n, width and
+// v0 are multiples of 8.
+__global__ __launch_bounds__(256) void ce_grad_kernel(const float* __restrict__ logits, int n, int64_t v0, int T,
+                                                      int64_t V, const void* __restrict__ y, int y_bytes,
+                                                      const float* __restrict__ lse, const float* __restrict__ dloss,
+                                                      int width, uint16_t* __restrict__ d) {
+  const int t = (int)blockIdx.y, c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8;
+  if (c >= n) return;
+  const int64_t target = target_at(y, y_bytes, t);
+  const bool valid = target >= 0 && target < V;
+  const float s = valid ? dloss[t] : 0.0f, z = valid ? lse[t] : 0.0f;
+  const float4* l = reinterpret_cast<const float4*>(logits + (int64_t)t * n + c);
+  const float4 a = l[0], b = l[1];
+  const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  const int64_t at = target - v0 - c;
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f32x2 e;
+    e.x = valid ? s * (__expf(x[2 * i] - z) - (at == 2 * i ? 1.0f : 0.0f)) : 0.0f;
+    e.y = valid ? s * (__expf(x[2 * i + 1] - z) - (at == 2 * i + 1 ? 1.0f : 0.0f)) : 0.0f;
+    w[i] = bits_of(__builtin_convertvector(e, bf16x2));
+  }
+  const int group = c / width, first = group * width, own = min(width, n - first);
+  *reinterpret_cast<u32x4*>(d + (size_t)first * T + (size_t)t * own + (c - first)) = w;
+}
+
+// The tail's logits of one token per wave: their part and target's logit (GRAD
+// false), or their gradients in fp32.
+template <int FMT, bool GRAD>
+__global__ __launch_bounds__(64) void ce_tail_kernel(const uint16_t* __restrict__ X, const uint8_t* __restrict__ codes,
+                                                     const uint8_t* __restrict__ scales, int rows, int H, float ws2,
+                                                     int64_t v0, int T, int64_t V, const void* __restrict__ y,
+                                                     int y_bytes, const float* __restrict__ lse,
+                                                     const float* __restrict__ dloss, float2* __restrict__ part,
+                                                     float* __restrict__ tlogit, float* __restrict__ d) {
+  const int t = (int)blockIdx.x, lane = threadIdx.x;
+  float l[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    float sum = 0.0f;
+    if (r < rows) {
+      for (int h = lane; h < H; h += 64)
+        sum = __builtin_fmaf(__uint_as_float((uint32_t)X[(size_t)t * H + h] << 16), code_at<FMT>(codes, scales, (int64_t)r * H + h), sum);
+#pragma unroll
+      for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
+    }
+    l[r] = r < rows ? sum * ws2 : -INFINITY;
+  }
+  if (lane != 0) return;
+  const int64_t target = target_at(y, y_bytes, t), at = target - v0;
+  if constexpr (GRAD) {
+    const bool valid = target >= 0 && target < V;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      if (r < rows) d[t * 8 + r] = valid ? dloss[t] * (__expf(l[r] - lse[t]) - (at == r ? 1.0f : 0.0f)) : 0.0f;
+  } else {
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      top = fmaxf(top, l[r]);
+      if (at == r && r < rows) tlogit[t] = l[r];
+    }
+    const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) sum += __expf(l[r] - ref);
+    part[t] = make_float2(top, sum);
+  }
 }
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
@@ -590,16 +729,148 @@ int ce_weight(int head, const void* W, const uint8_t* scales, int64_t v0, int64_
   return ok();
 }
 
+// ------------------------------------------------------------------ 4-bit heads, few tokens: plan
+constexpr int64_t kCeLogitBytes = int64_t(64) << 20;         // a piece's fp32 logits
+
+struct CeFew {
+  int64_t main;             // rows of the head that the layer's products take (a multiple of 8)
+  int tail;                 // the others, fewer than 8
+  int64_t piece;            // rows per piece of logits
+  int width, groups;        // backward: rows per group of dX's contraction, groups of the whole head
+  size_t tlogit, part, logits, d, sums, dtail, total;
+};
+
+CeFew ce_few_plan(bool bwd, int64_t T, int64_t V, int64_t H) {
+  CeFew p{};
+  p.main = V / 8 * 8;
+  p.tail = (int)(V - p.main);
+  // groups of whole stages, so many that their 256-column tiles fill the CUs
+  const int64_t cols = (H + 255) / 256;
+  int64_t groups = (2 * kCUs + cols - 1) / cols;
+  groups = groups < 64 ? groups : 64;
+  p.width = (int)up((p.main + groups - 1) / groups, 256);
+  if (p.width < 256) p.width = 256;
+  p.groups = (int)((p.main + p.width - 1) / p.width);
+  int64_t rows = kCeLogitBytes / (4 * T);
+  const int64_t by_codes = (int64_t(1) << 31) / H;           // operands below 1 GiB
+  rows = rows < by_codes ? rows : by_codes;
+  p.piece = rows / p.width * p.width > p.width ? rows / p.width * p.width : p.width;
+  const int64_t most = p.piece < p.main ? p.piece : p.main;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return o;
+  };
+  p.logits = take((size_t)most * T * 4);
+  if (!bwd) {
+    p.tlogit = take((size_t)T * 4);
+    p.part = take((size_t)((p.main + 255) / 256 + p.main / p.piece + 2) * T * 8);
+  } else {
+    p.d = take((size_t)p.main * T * 2);
+    p.sums = take((size_t)p.groups * T * H * 4);
+    p.dtail = take((size_t)T * 32);
+  }
+  p.total = at;
+  return p;
+}
+
+// Whether the layer's products take the head (their operands within 32 bits).
+bool ce_few(int head, int64_t T, int64_t V, int64_t H) {
+  if (head == kCeBf16 || T > kCeFewTokens || V < 8) return false;
+  const int64_t width = ce_few_plan(true, T, V, H).width;
+  return width * H <= int64_t(1) << 31 && width * T * 4 <= int64_t(1) << 30;
+}
+
+int ce_few_fwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* codes, const uint8_t* scales, float ws2,
+               const void* y, int y_bytes, float* loss, float* lse, uint8_t* ws, hipStream_t s) {
+  const CeFew p = ce_few_plan(false, T, V, H);
+  const int64_t G = H / (head == kMX ? 32 : 16);
+  float* logits = reinterpret_cast<float*>(ws + p.logits);
+  float2* part = reinterpret_cast<float2*>(ws + p.part);
+  float* tlogit = reinterpret_cast<float*>(ws + p.tlogit);
+  int tiles = 0;
+  for (int64_t v0 = 0; v0 < p.main; v0 += p.piece) {
+    const int n = (int)(p.main - v0 < p.piece ? p.main - v0 : p.piece);
+    if (gemm_fwd(head, T, n, H, X, codes + v0 * H / 2, scales + v0 * G, ws2, logits, 0, s) != 0) return -1;
+    const int nt = (n + 255) / 256;
+    hipLaunchKernelGGL(ce_part_kernel, dim3((unsigned)nt, (unsigned)((T + 3) / 4)), dim3(256), 0, s, logits, n, v0, T, V, y,
+                       y_bytes, part + (size_t)tiles * T, tlogit);
+    if (ok() != 0) return -1;
+    tiles += nt;
+  }
+  if (p.tail > 0) {
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(64), 0, s, static_cast<const uint16_t*>(X), codes + p.main * H / 2,
+                         scales + p.main * G, p.tail, H, ws2, p.main, T, V, y, y_bytes, nullptr, nullptr,
+                         part + (size_t)tiles * T, tlogit, nullptr);
+      return ok();
+    };
+    if ((head == kMX ? go(ce_tail_kernel<kMX, false>) : go(ce_tail_kernel<kNV, false>)) != 0) return -1;
+    ++tiles;
+  }
+  hipLaunchKernelGGL(ce_loss_kernel, dim3((unsigned)((T + 63) / 64)), dim3(1024), 0, s, part, tlogit, nullptr, nullptr, y,
+                     y_bytes, T, V, tiles, loss, lse);
+  return ok();
+}
+
+int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* codes, const uint8_t* scales, float ws2,
+               const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16, uint8_t* ws,
+               hipStream_t s) {
+  const CeFew p = ce_few_plan(true, T, V, H);
+  const int64_t G = H / (head == kMX ? 32 : 16);
+  float* logits = reinterpret_cast<float*>(ws + p.logits);
+  uint16_t* d = reinterpret_cast<uint16_t*>(ws + p.d);
+  float* sums = reinterpret_cast<float*>(ws + p.sums);
+  float* dtail = reinterpret_cast<float*>(ws + p.dtail);
+  for (int64_t v0 = 0; v0 < p.main; v0 += p.piece) {
+    const int n = (int)(p.main - v0 < p.piece ? p.main - v0 : p.piece);
+    if (gemm_fwd(head, T, n, H, X, codes + v0 * H / 2, scales + v0 * G, ws2, logits, 0, s) != 0) return -1;
+    hipLaunchKernelGGL(ce_grad_kernel, dim3((unsigned)((n / 8 + 255) / 256), (unsigned)T), dim3(256), 0, s, logits, n, v0, T,
+                       V, y, y_bytes, lse, dloss, p.width, d + (size_t)v0 * T);
+    if (ok() != 0) return -1;
+  }
+  if (p.tail > 0) {
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(64), 0, s, static_cast<const uint16_t*>(X), codes + p.main * H / 2,
+                         scales + p.main * G, p.tail, H, ws2, p.main, T, V, y, y_bytes, lse, dloss, nullptr, nullptr, dtail);
+      return ok();
+    };
+    if ((head == kMX ? go(ce_tail_kernel<kMX, true>) : go(ce_tail_kernel<kNV, true>)) != 0) return -1;
+  }
+  // dX of every group of rows, as the layer's grouped product: groups of one width
+  // in one call, the last, narrower one in its own
+  ExpertProblem e[64];
+  for (int k = 0; k < p.groups; ++k) {
+    const int64_t v0 = (int64_t)k * p.width;
+    e[k] = ExpertProblem{d + (size_t)v0 * T, nullptr, codes + v0 * H / 2, scales + v0 * G, sums + (size_t)k * T * H, T, ws2};
+  }
+  const int last = (int)(p.main - (int64_t)(p.groups - 1) * p.width), whole = last == p.width ? p.groups : p.groups - 1;
+  if (whole > 0 && gemm_dx_grouped(head, p.width, H, whole, e, 0, s) != 0) return -1;
+  if (whole < p.groups && gemm_dx(head, T, last, H, e[whole].a, e[whole].codes, e[whole].scales, ws2, e[whole].out, 0, s) != 0)
+    return -1;
+  const CeTail tail{codes + p.main * H / 2, scales + p.main * G, dtail, p.tail, head};
+  auto finish = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(256), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, y, y_bytes,
+                       T, V, H, 0, 0, 0, 1.0f, ws2, tail, dX);
+    return ok();
+  };
+  return dx_bf16 ? finish(ce_dx_kernel<true>) : finish(ce_dx_kernel<false>);
+}
+
 }  // namespace
 
 size_t ce_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H) {
+  if (ce_few(head, T, V, H)) return ce_few_plan(bwd != 0, T, V, H).total;
   return ce_plan(bwd != 0, head != kCeBf16, T, V, H).total;
 }
 
 int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
                   const void* y, int y_bytes, float* loss, float* lse, void* workspace, hipStream_t s) {
-  const CePlan p = ce_plan(false, head != kCeBf16, T, V, H);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
+  if (ce_few(head, T, V, H))
+    return ce_few_fwd(head, T, V, H, X, static_cast<const uint8_t*>(W), scales, ws2, y, y_bytes, loss, lse, ws, s);
+  const CePlan p = ce_plan(false, head != kCeBf16, T, V, H);
   CeArgs g{};
   g.x = static_cast<const uint16_t*>(X);
   g.y = y; g.y_bytes = y_bytes; g.T = T; g.H = H; g.V = V; g.ws2 = ws2;
@@ -631,8 +902,11 @@ int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
 int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
                   const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16,
                   void* workspace, hipStream_t s) {
-  const CePlan p = ce_plan(true, head != kCeBf16, T, V, H);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
+  if (ce_few(head, T, V, H))
+    return ce_few_bwd(head, T, V, H, X, static_cast<const uint8_t*>(W), scales, ws2, y, y_bytes, lse, dloss, dX, dx_bf16,
+                      ws, s);
+  const CePlan p = ce_plan(true, head != kCeBf16, T, V, H);
   CeArgs g{};
   g.x = static_cast<const uint16_t*>(X);
   g.y = y; g.y_bytes = y_bytes; g.T = T; g.H = H; g.V = V; g.ws2 = ws2;
@@ -661,8 +935,8 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     if (ce_go<kCeDx>(g, p.bt, dx_blocks, s) != 0) return -1;
   }
   auto finish = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(256), 0, s, g.sums, g.rows, g.count, y, y_bytes, T, V, H, p.bt,
-                       (int)tn, g.split_stages, ws2, dX);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(256), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, y, y_bytes, T, V,
+                       H, p.bt, (int)tn, g.split_stages, ws2, ws2, CeTail{}, dX);
     return ok();
   };
   return dx_bf16 ? finish(ce_dx_kernel<true>) : finish(ce_dx_kernel<false>);

@@ -190,6 +190,7 @@ size_t dscale_act8_batched_workspace(int E, int T, int I);
 
 // Cross entropy of a head (sq_ce.hip).  head: 0 MXFP4, 1 NVFP4, 2 bf16 rows.
 constexpr int kCeBf16 = 2;
+constexpr int kCeFewTokens = 256;         // up to these a 4-bit head is read by the layer's own products
 size_t ce_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H);
 int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
                   const void* y, int y_bytes, float* loss, float* lse, void* workspace, hipStream_t s);
