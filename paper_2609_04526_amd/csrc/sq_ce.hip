@@ -547,8 +547,11 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ su
 // codes (their few-token strips and narrow tiles), a piece of fp32 logits passes
 // through the workspace, and these kernels do the rest.
 
+// A piece's n logits lie in groups of `width` columns, each a [T, its width]
+// matrix of its own (width and n are multiples of 8, width of 256 or n itself).
+
 // (max, sum) of 256 logits of one token per wave, and the target's logit.
-__global__ __launch_bounds__(256) void ce_part_kernel(const float* __restrict__ logits, int n, int64_t v0, int T,
+__global__ __launch_bounds__(256) void ce_part_kernel(const float* __restrict__ logits, int n, int width, int64_t v0, int T,
                                                       int64_t V, const void* __restrict__ y, int y_bytes,
                                                       float2* __restrict__ part, float* __restrict__ tlogit) {
   const int lane = threadIdx.x & 63, t = (int)blockIdx.y * 4 + (threadIdx.x >> 6);
@@ -556,9 +559,11 @@ __global__ __launch_bounds__(256) void ce_part_kernel(const float* __restrict__ 
   const int c0 = (int)blockIdx.x * 256 + lane * 4;
   float l[4], top = -INFINITY;
   const int64_t at = target_at(y, y_bytes, t) - v0 - c0;
+  const int first = c0 / width * width, own = min(width, n - first);
+  const float* row = logits + (int64_t)first * T + (int64_t)t * own - first;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    l[i] = c0 + i < n ? logits[(int64_t)t * n + c0 + i] : -INFINITY;
+    l[i] = c0 + i < n ? row[c0 + i] : -INFINITY;
     if (at == i && c0 + i < n) tlogit[t] = l[i];
     top = fmaxf(top, l[i]);
   }
@@ -573,19 +578,18 @@ __global__ __launch_bounds__(256) void ce_part_kernel(const float* __restrict__ 
   if (lane == 0) part[(size_t)blockIdx.x * T + t] = make_float2(top, sum);
 }
 
-// The logits' gradients in bf16, 8 of one token per lane, each group of `width`
-// columns of the vocabulary a [T, its width] matrix of its own.  n, width and
-// v0 are multiples of 8.
-__global__ __launch_bounds__(256) void ce_grad_kernel(const float* __restrict__ logits, int n, int64_t v0, int T,
+// The logits' gradients in bf16, 8 of one token per lane, in groups of d_width.
+__global__ __launch_bounds__(256) void ce_grad_kernel(const float* __restrict__ logits, int n, int width, int64_t v0, int T,
                                                       int64_t V, const void* __restrict__ y, int y_bytes,
                                                       const float* __restrict__ lse, const float* __restrict__ dloss,
-                                                      int width, uint16_t* __restrict__ d) {
+                                                      int d_width, uint16_t* __restrict__ d) {
   const int t = (int)blockIdx.y, c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8;
   if (c >= n) return;
   const int64_t target = target_at(y, y_bytes, t);
   const bool valid = target >= 0 && target < V;
   const float s = valid ? dloss[t] : 0.0f, z = valid ? lse[t] : 0.0f;
-  const float4* l = reinterpret_cast<const float4*>(logits + (int64_t)t * n + c);
+  const int from = c / width * width;
+  const float4* l = reinterpret_cast<const float4*>(logits + (int64_t)from * T + (int64_t)t * min(width, n - from) + (c - from));
   const float4 a = l[0], b = l[1];
   const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
   const int64_t at = target - v0 - c;
@@ -597,7 +601,7 @@ __global__ __launch_bounds__(256) void ce_grad_kernel(const float* __restrict__ 
     e.y = valid ? s * (__expf(x[2 * i + 1] - z) - (at == 2 * i + 1 ? 1.0f : 0.0f)) : 0.0f;
     w[i] = bits_of(__builtin_convertvector(e, bf16x2));
   }
-  const int group = c / width, first = group * width, own = min(width, n - first);
+  const int first = c / d_width * d_width, own = min(d_width, n - first);
   *reinterpret_cast<u32x4*>(d + (size_t)first * T + (size_t)t * own + (c - first)) = w;
 }
 
@@ -731,6 +735,7 @@ int ce_weight(int head, const void* W, const uint8_t* scales, int64_t v0, int64_
 
 // ------------------------------------------------------------------ 4-bit heads, few tokens: plan
 constexpr int64_t kCeLogitBytes = int64_t(64) << 20;         // a piece's fp32 logits
+constexpr int kCeGroupTokens = 128;
 
 struct CeFew {
   int64_t main;             // rows of the head that the layer's products take (a multiple of 8)
@@ -782,6 +787,36 @@ bool ce_few(int head, int64_t T, int64_t V, int64_t H) {
   return width * H <= int64_t(1) << 31 && width * T * 4 <= int64_t(1) << 30;
 }
 
+// Logits of rows [v0, v0 + n) of the head; the width of their groups goes to
+// *width.  One product over this many rows would take strips or tiles made for a
+// layer's few; as a grouped one over groups of rows it takes the grouped
+// products' tiles (131072 x 4096 MXFP4, us of loss and gradient, one product
+// against groups: 1 token 318, 261; 64 tokens 503, 328; 128 tokens 694, 575; 256
+// tokens 939, 1063; NVFP4 64 tokens 493, 439; 128 tokens 821, 663).
+int ce_few_logits(int head, int T, int64_t v0, int n, int H, const void* X, const uint8_t* codes, const uint8_t* scales,
+                  float ws2, int group, float* logits, int* width, hipStream_t s) {
+  const int64_t G = H / (head == kMX ? 32 : 16);
+  const uint8_t* c = codes + v0 * H / 2;
+  const uint8_t* sc = scales + v0 * G;
+  if (T > kCeGroupTokens || n <= group) {
+    *width = n;
+    return gemm_fwd(head, T, n, H, X, c, sc, ws2, logits, 0, s);
+  }
+  *width = group;
+  ExpertProblem e[kGroupMax];
+  const int whole = n / group, last = n - whole * group;
+  for (int k0 = 0; k0 < whole; k0 += kGroupMax) {
+    const int m = whole - k0 < kGroupMax ? whole - k0 : kGroupMax;
+    for (int k = 0; k < m; ++k) {
+      const int64_t r = (int64_t)(k0 + k) * group;
+      e[k] = ExpertProblem{X, nullptr, c + r * H / 2, sc + r * G, logits + r * T, T, ws2};
+    }
+    if (gemm_fwd_grouped(head, group, H, m, e, 0, s) != 0) return -1;
+  }
+  const int64_t r = (int64_t)whole * group;
+  return last == 0 ? 0 : gemm_fwd(head, T, last, H, X, c + r * H / 2, sc + r * G, ws2, logits + r * T, 0, s);
+}
+
 int ce_few_fwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* codes, const uint8_t* scales, float ws2,
                const void* y, int y_bytes, float* loss, float* lse, uint8_t* ws, hipStream_t s) {
   const CeFew p = ce_few_plan(false, T, V, H);
@@ -792,9 +827,10 @@ int ce_few_fwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   int tiles = 0;
   for (int64_t v0 = 0; v0 < p.main; v0 += p.piece) {
     const int n = (int)(p.main - v0 < p.piece ? p.main - v0 : p.piece);
-    if (gemm_fwd(head, T, n, H, X, codes + v0 * H / 2, scales + v0 * G, ws2, logits, 0, s) != 0) return -1;
+    int width;
+    if (ce_few_logits(head, T, v0, n, H, X, codes, scales, ws2, p.width, logits, &width, s) != 0) return -1;
     const int nt = (n + 255) / 256;
-    hipLaunchKernelGGL(ce_part_kernel, dim3((unsigned)nt, (unsigned)((T + 3) / 4)), dim3(256), 0, s, logits, n, v0, T, V, y,
+    hipLaunchKernelGGL(ce_part_kernel, dim3((unsigned)nt, (unsigned)((T + 3) / 4)), dim3(256), 0, s, logits, n, width, v0, T, V, y,
                        y_bytes, part + (size_t)tiles * T, tlogit);
     if (ok() != 0) return -1;
     tiles += nt;
@@ -825,8 +861,9 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   float* dtail = reinterpret_cast<float*>(ws + p.dtail);
   for (int64_t v0 = 0; v0 < p.main; v0 += p.piece) {
     const int n = (int)(p.main - v0 < p.piece ? p.main - v0 : p.piece);
-    if (gemm_fwd(head, T, n, H, X, codes + v0 * H / 2, scales + v0 * G, ws2, logits, 0, s) != 0) return -1;
-    hipLaunchKernelGGL(ce_grad_kernel, dim3((unsigned)((n / 8 + 255) / 256), (unsigned)T), dim3(256), 0, s, logits, n, v0, T,
+    int width;
+    if (ce_few_logits(head, T, v0, n, H, X, codes, scales, ws2, p.width, logits, &width, s) != 0) return -1;
+    hipLaunchKernelGGL(ce_grad_kernel, dim3((unsigned)((n / 8 + 255) / 256), (unsigned)T), dim3(256), 0, s, logits, n, width, v0, T,
                        V, y, y_bytes, lse, dloss, p.width, d + (size_t)v0 * T);
     if (ok() != 0) return -1;
   }
