@@ -36,6 +36,11 @@ __device__ __forceinline__ int64_t target_at(const void* y, int bytes, int64_t t
   return bytes == 8 ? static_cast<const int64_t*>(y)[t] : (int64_t)static_cast<const int32_t*>(y)[t];
 }
 
+// fp32 of the low or high half of a pair of bf16.
+__device__ __forceinline__ float bf16_half(uint32_t pair, int high) {
+  return __uint_as_float(high ? pair & 0xFFFF0000u : pair << 16);
+}
+
 // ------------------------------------------------------------------ rows
 // rows[0 .. n) = the tokens whose target is in the vocabulary, in order; *count
 // = n.  One workgroup: 1024 tokens per step.
@@ -86,7 +91,7 @@ struct CeArgs {
   const uint16_t* w;        // rows [v0, v0 + Vn) of W as bf16, [Vn, H]
   uint16_t* d;              // gradients of the logits [T, ld], piece columns
   float* part;              // forward: (max, sum) [tile of all of W][T]
-  float* tlogit;            // forward: the target's logit [T]
+  float* tlogit;            // forward: the target's logit [T]; backward: what rounding took from its gradient
   float* sums;              // backward: fp32 sums of dX, planes of [live rows in whole tiles, H]
   const int* rows;          // compact row -> token, or null (row = token)
   const int* count;         // live rows, or null (T)
@@ -331,6 +336,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   } else {
     __syncthreads();                     // the operand tiles are done with
     const int vrow = m0 + wm0 + 4 * (lane >> 5);             // first row of W of this lane's registers
+    const int end = g.Vn - vrow;                              // rows of W from it on
+    const bool whole = m0 + BM <= g.Vn;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const int row = n0 + wn0 + j * 32 + (lane & 31);       // compact token row
@@ -340,27 +347,32 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
       const bool valid = y >= 0 && y < g.V;
       // the target's row counted from this lane's first, or one that no register holds
       const int64_t off = y - g.v0 - vrow;
-      const int at = valid && off >= 0 && off < WM ? (int)off : -1, end = g.Vn - vrow;
+      const int at = valid && off >= 0 && off < WM ? (int)off : -1;
+      // most waves hold whole tiles and no token's target: their registers need
+      // no comparison
+      const bool plain = whole && __ballot(at >= 0) == 0;
       if constexpr (MODE == kCeStats) {
-        float top = -INFINITY;
+        float top = -INFINITY, sum = 0.0f;
+        auto stats = [&](auto PLAIN) {
+          constexpr bool kPlain = decltype(PLAIN)::value;
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+          for (int i = 0; i < TM; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int v = i * 32 + 8 * (r >> 2) + (r & 3);
-            float l = acc[i][j][r] * g.ws2;
-            if (v == at) g.tlogit[row] = l;
-            l = v < end ? l : -INFINITY;
-            acc[i][j][r] = l;
-            top = fmaxf(top, l);
-          }
-        top = fmaxf(top, __shfl_xor(top, 32));
+            for (int r = 0; r < 16; ++r) {
+              const int v = i * 32 + 8 * (r >> 2) + (r & 3);
+              if (!kPlain && v == at) g.tlogit[row] = acc[i][j][r] * g.ws2;
+              if (!kPlain && v >= end) acc[i][j][r] = -INFINITY;
+              top = fmaxf(top, acc[i][j][r]);
+            }
+        };
+        if (plain) stats(std::true_type{});
+        else stats(std::false_type{});
+        top = fmaxf(top, __shfl_xor(top, 32)) * g.ws2;
         const float ref = top == -INFINITY ? 0.0f : top;     // nothing to sum: exp(-inf) = 0
-        float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sum += __expf(acc[i][j][r] - ref);
+          for (int r = 0; r < 16; ++r) sum += __expf(__builtin_fmaf(acc[i][j][r], g.ws2, -ref));
         sum += __shfl_xor(sum, 32);
         SQ_LDS float* s = (SQ_LDS float*)lds + 2 * ((wave / WGN) * BN + wn0 + j * 32 + (lane & 31));
         if (lane < 32) {
@@ -368,28 +380,44 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
           s[1] = sum;
         }
       } else {
+        // Rounded to bf16 for the product with W, as the layers' dY is.  The
+        // target's own, by far the largest as a rule, would bring most of the
+        // rounding's error into dX: what it lost is kept, and added with the
+        // target's row of W at the end (error against 64 bits 2.5e-3 -> 1.8e-3, of
+        // which 1.7e-3 is dX's own rounding to bf16).
         const float c = valid ? g.dloss[t] : 0.0f, z = valid ? g.lse[t] : 0.0f;
-        // rounded to bf16 for the product with W, as the layers' dY is
         SQ_LDS uint16_t* s = (SQ_LDS uint16_t*)lds + wave * WM * WN;
         const int cj = j * 32 + (lane & 31);
+        auto grads = [&](auto PLAIN) {
+          constexpr bool kPlain = decltype(PLAIN)::value;
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+          for (int i = 0; i < TM; ++i)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float e[4];
+            for (int q = 0; q < 4; ++q) {
+              float e[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int v = i * 32 + 8 * q + r;
-              const float p = __expf(acc[i][j][4 * q + r] * g.ws2 - z) - (v == at ? 1.0f : 0.0f);
-              e[r] = valid && v < end ? c * p : 0.0f;
+              for (int r = 0; r < 4; ++r) {
+                const int v = i * 32 + 8 * q + r;
+                const float p = __expf(__builtin_fmaf(acc[i][j][4 * q + r], g.ws2, -z));
+                e[r] = kPlain ? c * p : valid && v < end ? c * (p - (v == at ? 1.0f : 0.0f)) : 0.0f;
+              }
+              u32x2 pair;
+              pair[0] = bits_of(__builtin_convertvector((f32x2{e[0], e[1]}), bf16x2));
+              pair[1] = bits_of(__builtin_convertvector((f32x2{e[2], e[3]}), bf16x2));
+              if constexpr (!kPlain) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  if (i * 32 + 8 * q + r == at) g.tlogit[row] = e[r] - bf16_half(pair[r >> 1], r & 1);
+              }
+              // 16-byte unit u of token cj at unit u ^ cj
+              const int u = i * 4 + q;
+              *(SQ_LDS u32x2*)(s + cj * WM + ((u ^ cj) & (WM / 8 - 1)) * 8 + 4 * (lane >> 5)) = pair;
             }
-            u32x2 pair;
-            pair[0] = bits_of(__builtin_convertvector((f32x2{e[0], e[1]}), bf16x2));
-            pair[1] = bits_of(__builtin_convertvector((f32x2{e[2], e[3]}), bf16x2));
-            // 16-byte unit u of token cj at unit u ^ cj
-            const int u = i * 4 + q;
-            *(SQ_LDS u32x2*)(s + cj * WM + ((u ^ cj) & (WM / 8 - 1)) * 8 + 4 * (lane >> 5)) = pair;
-          }
+        };
+        // (an ignored token among the rows, as in a batch that is not compact,
+        // takes the way with comparisons, which gives it zeros)
+        if (plain && __ballot(in && !valid) == 0) grads(std::true_type{});
+        else grads(std::false_type{});
       }
     }
     if constexpr (MODE == kCeStats) {
@@ -467,14 +495,18 @@ __global__ __launch_bounds__(1024) void ce_loss_kernel(const float2* __restrict_
   }
 }
 
-// What the last kernel of the gradient adds up: planes of fp32 sums, and the rows
-// of a 4-bit head past a multiple of 8, which the layer's products do not take.
-struct CeTail {
-  const uint8_t* codes;     // of the first such row
+// What the last kernel of the gradient adds beside the planes of sums: the
+// target's row of the head times what rounding took from its logit's gradient,
+// and the rows of a 4-bit head past a multiple of 8, which the layer's products
+// do not take.
+struct CeRest {
+  const void* w;            // the head: bf16 rows or codes
   const uint8_t* scales;
-  const float* d;           // [T, 8] their logits' gradients
+  const float* lost;        // [T], by compact row
+  const float* d;           // [T, 8] logit gradients of the rows from `first` on
+  int64_t first;
   int rows;
-  int fmt;
+  int head;
 };
 
 template <int FMT>
@@ -484,14 +516,20 @@ __device__ __forceinline__ float code_at(const uint8_t* codes, const uint8_t* sc
   return c * (FMT == kMX ? e8m0_to_f32(b) : e4m3_to_f32(b));
 }
 
+__device__ __forceinline__ float head_at(const CeRest& r, int64_t i) {
+  if (r.head == kMX) return code_at<kMX>(static_cast<const uint8_t*>(r.w), r.scales, i);
+  if (r.head == kNV) return code_at<kNV>(static_cast<const uint8_t*>(r.w), r.scales, i);
+  return __uint_as_float((uint32_t)static_cast<const uint16_t*>(r.w)[i] << 16);
+}
+
 // dX of one token per workgroup: the planes added in order, times f (and the
-// tail's rows times ws2); zeros where there is no target (their rows come after
+// rest's rows times ws2); zeros where there is no target (their rows come after
 // the live ones).  planes = 0: as many as the product split the vocabulary into.
 template <bool BF16>
 __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ sums, int planes, int64_t plane_rows,
                                                     const int* __restrict__ rows, const int* __restrict__ count,
                                                     const void* __restrict__ y, int y_bytes, int T, int64_t V, int H,
-                                                    int bm, int tiles_n, int stages, float f, float ws2, CeTail tail,
+                                                    int bm, int tiles_n, int stages, float f, float ws2, CeRest rest,
                                                     void* __restrict__ dX) {
   const int live = count ? min(*count, T) : T;
   const int b = (int)blockIdx.x;
@@ -523,17 +561,16 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ su
         v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
       }
       v.x *= f; v.y *= f; v.z *= f; v.w *= f;
-      for (int r = 0; r < tail.rows; ++r) {
-        const float d = tail.d[b * 8 + r] * ws2;
-        const int64_t at = (int64_t)r * H + h;
-        auto w = [&](int i) {
-          return tail.fmt == kMX ? code_at<kMX>(tail.codes, tail.scales, at + i) : code_at<kNV>(tail.codes, tail.scales, at + i);
-        };
-        v.x = __builtin_fmaf(d, w(0), v.x);
-        v.y = __builtin_fmaf(d, w(1), v.y);
-        v.z = __builtin_fmaf(d, w(2), v.z);
-        v.w = __builtin_fmaf(d, w(3), v.w);
-      }
+      auto add = [&](float d, int64_t row) {
+        const int64_t at = row * H + h;
+        v.x = __builtin_fmaf(d, head_at(rest, at), v.x);
+        v.y = __builtin_fmaf(d, head_at(rest, at + 1), v.y);
+        v.z = __builtin_fmaf(d, head_at(rest, at + 2), v.z);
+        v.w = __builtin_fmaf(d, head_at(rest, at + 3), v.w);
+      };
+      const int64_t own = rows ? target_at(y, y_bytes, t) : target;
+      if (own < rest.first) add(rest.lost[b] * ws2, own);
+      for (int r = 0; r < rest.rows; ++r) add(rest.d[b * 8 + r] * ws2, rest.first + r);
       put(t, h, v);
     }
   }
@@ -582,7 +619,7 @@ __global__ __launch_bounds__(256) void ce_part_kernel(const float* __restrict__ 
 __global__ __launch_bounds__(256) void ce_grad_kernel(const float* __restrict__ logits, int n, int width, int64_t v0, int T,
                                                       int64_t V, const void* __restrict__ y, int y_bytes,
                                                       const float* __restrict__ lse, const float* __restrict__ dloss,
-                                                      int d_width, uint16_t* __restrict__ d) {
+                                                      int d_width, uint16_t* __restrict__ d, float* __restrict__ lost) {
   const int t = (int)blockIdx.y, c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8;
   if (c >= n) return;
   const int64_t target = target_at(y, y_bytes, t);
@@ -600,6 +637,7 @@ __global__ __launch_bounds__(256) void ce_grad_kernel(const float* __restrict__ 
     e.x = valid ? s * (__expf(x[2 * i] - z) - (at == 2 * i ? 1.0f : 0.0f)) : 0.0f;
     e.y = valid ? s * (__expf(x[2 * i + 1] - z) - (at == 2 * i + 1 ? 1.0f : 0.0f)) : 0.0f;
     w[i] = bits_of(__builtin_convertvector(e, bf16x2));
+    if (valid && at >> 1 == i) lost[t] = at & 1 ? e.y - bf16_half(w[i], 1) : e.x - bf16_half(w[i], 0);
   }
   const int first = c / d_width * d_width, own = min(d_width, n - first);
   *reinterpret_cast<u32x4*>(d + (size_t)first * T + (size_t)t * own + (c - first)) = w;
@@ -686,8 +724,8 @@ CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
   };
   p.rows = take(p.compact ? (size_t)T * 4 : 0);
   if (four_bit) p.wbuf = take((size_t)p.piece * H * 2);
+  p.tlogit = take((size_t)T * 4);
   if (!bwd) {
-    p.tlogit = take((size_t)T * 4);
     p.part = take((size_t)((V + 255) / 256) * T * 8);
   } else {
     p.ld = (int)(p.piece < V ? p.piece : up(V, 64));
@@ -768,8 +806,8 @@ CeFew ce_few_plan(bool bwd, int64_t T, int64_t V, int64_t H) {
     return o;
   };
   p.logits = take((size_t)most * T * 4);
+  p.tlogit = take((size_t)T * 4);
   if (!bwd) {
-    p.tlogit = take((size_t)T * 4);
     p.part = take((size_t)((p.main + 255) / 256 + p.main / p.piece + 2) * T * 8);
   } else {
     p.d = take((size_t)p.main * T * 2);
@@ -859,12 +897,13 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   uint16_t* d = reinterpret_cast<uint16_t*>(ws + p.d);
   float* sums = reinterpret_cast<float*>(ws + p.sums);
   float* dtail = reinterpret_cast<float*>(ws + p.dtail);
+  float* lost = reinterpret_cast<float*>(ws + p.tlogit);
   for (int64_t v0 = 0; v0 < p.main; v0 += p.piece) {
     const int n = (int)(p.main - v0 < p.piece ? p.main - v0 : p.piece);
     int width;
     if (ce_few_logits(head, T, v0, n, H, X, codes, scales, ws2, p.width, logits, &width, s) != 0) return -1;
     hipLaunchKernelGGL(ce_grad_kernel, dim3((unsigned)((n / 8 + 255) / 256), (unsigned)T), dim3(256), 0, s, logits, n, width, v0, T,
-                       V, y, y_bytes, lse, dloss, p.width, d + (size_t)v0 * T);
+                       V, y, y_bytes, lse, dloss, p.width, d + (size_t)v0 * T, lost);
     if (ok() != 0) return -1;
   }
   if (p.tail > 0) {
@@ -886,10 +925,10 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   if (whole > 0 && gemm_dx_grouped(head, p.width, H, whole, e, 0, s) != 0) return -1;
   if (whole < p.groups && gemm_dx(head, T, last, H, e[whole].a, e[whole].codes, e[whole].scales, ws2, e[whole].out, 0, s) != 0)
     return -1;
-  const CeTail tail{codes + p.main * H / 2, scales + p.main * G, dtail, p.tail, head};
+  const CeRest rest{codes, scales, lost, dtail, p.main, p.tail, head};
   auto finish = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(256), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, y, y_bytes,
-                       T, V, H, 0, 0, 0, 1.0f, ws2, tail, dX);
+                       T, V, H, 0, 0, 0, 1.0f, ws2, rest, dX);
     return ok();
   };
   return dx_bf16 ? finish(ce_dx_kernel<true>) : finish(ce_dx_kernel<false>);
@@ -948,6 +987,7 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
   g.x = static_cast<const uint16_t*>(X);
   g.y = y; g.y_bytes = y_bytes; g.T = T; g.H = H; g.V = V; g.ws2 = ws2;
   g.lse = lse; g.dloss = dloss;
+  g.tlogit = reinterpret_cast<float*>(ws + p.tlogit);
   g.d = reinterpret_cast<uint16_t*>(ws + p.d);
   g.sums = reinterpret_cast<float*>(ws + p.sums);
   g.ld = p.ld;
@@ -971,9 +1011,10 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     if (ce_go<kCeGrad>(g, p.bt, (n + 255) / 256 * tt, s) != 0) return -1;
     if (ce_go<kCeDx>(g, p.bt, dx_blocks, s) != 0) return -1;
   }
+  const CeRest rest{W, scales, g.tlogit, nullptr, V, 0, head};
   auto finish = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(256), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, y, y_bytes, T, V,
-                       H, p.bt, (int)tn, g.split_stages, ws2, ws2, CeTail{}, dX);
+                       H, p.bt, (int)tn, g.split_stages, ws2, ws2, rest, dX);
     return ok();
   };
   return dx_bf16 ? finish(ce_dx_kernel<true>) : finish(ce_dx_kernel<false>);
