@@ -482,9 +482,11 @@ __global__ __launch_bounds__(1024) void ce_loss_kernel(const float2* __restrict_
     const int t = rows ? rows[row] : row;
     const int64_t v = target_at(y, y_bytes, t);
     if (v >= 0 && v < V) {
-      const float z = top + __logf(sum);
-      lse[t] = z;
-      loss[t] = z - tlogit[row];
+      // the largest logit's distance first: for a likely target little is left of
+      // lse - logit, and lse's own rounding would be most of the error
+      const float rest = __logf(sum);
+      lse[t] = top + rest;
+      loss[t] = (top - tlogit[row]) + rest;
     }
   }
   // tokens without a target (this workgroup's share of all tokens)
