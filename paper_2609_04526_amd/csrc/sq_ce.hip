@@ -105,6 +105,8 @@ struct CeArgs {
   int part_tile0;           // forward: tile of all of W that this piece starts at
   int split_stages;         // backward: 64-row stages of a whole piece
   int add;                  // backward: the sums hold earlier pieces
+  float* logits;            // fp32 planes [splits][T][ldl] of a head of few tiles
+  int ldl, splits;
   float ws2;
 };
 
@@ -144,9 +146,9 @@ __device__ __forceinline__ int ce_splits(int tiles, int stages) {
   return max(1, min(min(kCUs / max(tiles, 1), stages / 4), 64));
 }
 
-enum CeMode { kCeStats = 0, kCeGrad = 1, kCeDx = 2 };
+enum CeMode { kCeStats = 0, kCeGrad = 1, kCeDx = 2, kCeLogits = 3 };
 
-// The tile product of all three, 256 x BN (logits: W's rows by tokens, so that
+// The tile product of them all, 256 x BN (logits: W's rows by tokens, so that
 // a lane holds one token's logits and sums them without its neighbours) or BM x
 // 256 (dX: tokens by columns of W).  64-deep stages copied global -> LDS, the
 // operands of a 16-deep slice read while the slice before it multiplies, and
@@ -175,10 +177,10 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   // tile, and the stages [s_first, s_first + nk) of its contraction
   const int M = kDxMode ? live : g.Vn, N = kDxMode ? g.H : live, K = kDxMode ? g.Vn : g.H;
   const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN, tiles = tiles_m * tiles_n;
-  const int splits = kDxMode ? ce_splits(tiles, g.split_stages) : 1;
+  const int splits = kDxMode ? ce_splits(tiles, g.split_stages) : MODE == kCeLogits ? g.splits : 1;
   if ((int)blockIdx.x >= tiles * splits) return;
   const int pos = xcd_stretch((int)blockIdx.x, tiles * splits);
-  const int split = kDxMode ? pos / tiles : 0;
+  const int split = kDxMode || MODE == kCeLogits ? pos / tiles : 0;
   int tm, tn;
   tile_at<kCeGroup>(pos - split * tiles, tiles_m, tiles_n, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
@@ -333,6 +335,24 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
           sums[(size_t)row * g.H + col] = acc[i][j][r];
         }
       }
+  } else if constexpr (MODE == kCeLogits) {
+    // 4 consecutive rows of W per lane and quarter: 16 bytes of a token's logits
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int row = n0 + wn0 + j * 32 + (lane & 31);
+      if (row >= live) continue;
+      float* out = g.logits + ((size_t)split * g.T + row) * g.ldl;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int v = m0 + wm0 + i * 32 + 8 * q + 4 * (lane >> 5);
+          if (v < g.ldl)
+            *reinterpret_cast<float4*>(out + v) = 
+                make_float4(acc[i][j][4 * q] * g.ws2, acc[i][j][4 * q + 1] * g.ws2, acc[i][j][4 * q + 2] * g.ws2,
+                            acc[i][j][4 * q + 3] * g.ws2);
+        }
+    }
   } else {
     __syncthreads();                     // the operand tiles are done with
     const int vrow = m0 + wm0 + 4 * (lane >> 5);             // first row of W of this lane's registers
@@ -511,17 +531,24 @@ struct CeRest {
   int head;
 };
 
-template <int FMT>
-__device__ __forceinline__ float code_at(const uint8_t* codes, const uint8_t* scales, int64_t i) {
-  const float c = e2m1_to_f32((uint32_t)(codes[i >> 1] >> (4 * (i & 1))) & 15u);
-  const uint32_t b = scales[i / ScaleOperand<FMT>::kBlock];
-  return c * (FMT == kMX ? e8m0_to_f32(b) : e4m3_to_f32(b));
-}
-
-__device__ __forceinline__ float head_at(const CeRest& r, int64_t i) {
-  if (r.head == kMX) return code_at<kMX>(static_cast<const uint8_t*>(r.w), r.scales, i);
-  if (r.head == kNV) return code_at<kNV>(static_cast<const uint8_t*>(r.w), r.scales, i);
-  return __uint_as_float((uint32_t)static_cast<const uint16_t*>(r.w)[i] << 16);
+// 8 values of a head from element i (a multiple of 8) of its rows on.
+__device__ __forceinline__ void head8(int head, const void* w, const uint8_t* scales, int64_t i, float (&v)[8]) {
+  if (head == kCeBf16) {
+    const u32x4 q = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(w) + i);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = bf16_half(q[k >> 1], k & 1);
+    return;
+  }
+  const uint32_t q = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(w) + (i >> 1));
+  const uint32_t b = scales[i / (head == kMX ? 32 : 16)];
+  const float s = head == kMX ? e8m0_to_f32(b) : e4m3_to_f32(b);
+  const f32x2 c[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3)};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] = c[k].x * s;
+    v[2 * k + 1] = c[k].y * s;
+  }
 }
 
 // dX of one token per workgroup: the planes added in order, times f (and the
@@ -535,14 +562,16 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ su
                                                     void* __restrict__ dX) {
   const int live = count ? min(*count, T) : T;
   const int b = (int)blockIdx.x;
-  auto put = [&](int t, int h, float4 v) {
+  auto put = [&](int t, int h, const float (&v)[8]) {
     if constexpr (BF16) {
-      u32x2 w;
-      w[0] = bits_of(__builtin_convertvector((f32x2{v.x, v.y}), bf16x2));
-      w[1] = bits_of(__builtin_convertvector((f32x2{v.z, v.w}), bf16x2));
-      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(dX) + (size_t)t * H + h) = w;
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = bits_of(__builtin_convertvector((f32x2{v[2 * i], v[2 * i + 1]}), bf16x2));
+      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dX) + (size_t)t * H + h) = w;
     } else {
-      *reinterpret_cast<float4*>(static_cast<float*>(dX) + (size_t)t * H + h) = v;
+      float4* q = reinterpret_cast<float4*>(static_cast<float*>(dX) + (size_t)t * H + h);
+      q[0] = make_float4(v[0], v[1], v[2], v[3]);
+      q[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
   };
   const int64_t target = target_at(y, y_bytes, b);
@@ -555,56 +584,84 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ su
     }
     const size_t plane = (size_t)plane_rows * H;
     const int t = rows ? rows[b] : b;
-    for (int h = threadIdx.x * 4; h < H; h += 1024) {
-      float4 v = *reinterpret_cast<const float4*>(sums + (size_t)b * H + h);
-#pragma unroll 8
-      for (int s = 1; s < planes; ++s) {
-        const float4 u = *reinterpret_cast<const float4*>(sums + s * plane + (size_t)b * H + h);
-        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    const int64_t own = rows ? target_at(y, y_bytes, t) : target;
+    for (int h = threadIdx.x * 8; h < H; h += 2048) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+#pragma unroll 4
+      for (int s = 0; s < planes; ++s) {
+        const float4* q = reinterpret_cast<const float4*>(sums + s * plane + (size_t)b * H + h);
+        const float4 a = q[0], c = q[1];
+        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+        v[4] += c.x; v[5] += c.y; v[6] += c.z; v[7] += c.w;
       }
-      v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= f;
       auto add = [&](float d, int64_t row) {
-        const int64_t at = row * H + h;
-        v.x = __builtin_fmaf(d, head_at(rest, at), v.x);
-        v.y = __builtin_fmaf(d, head_at(rest, at + 1), v.y);
-        v.z = __builtin_fmaf(d, head_at(rest, at + 2), v.z);
-        v.w = __builtin_fmaf(d, head_at(rest, at + 3), v.w);
+        float w[8];
+        head8(rest.head, rest.w, rest.scales, row * H + h, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(d, w[i], v[i]);
       };
-      const int64_t own = rows ? target_at(y, y_bytes, t) : target;
       if (own < rest.first) add(rest.lost[b] * ws2, own);
       for (int r = 0; r < rest.rows; ++r) add(rest.d[b * 8 + r] * ws2, rest.first + r);
       put(t, h, v);
     }
   }
-  if (ignored)
-    for (int h = threadIdx.x * 4; h < H; h += 1024) put(b, h, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+  if (ignored) {
+    const float zero[8] = {};
+    for (int h = threadIdx.x * 8; h < H; h += 2048) put(b, h, zero);
+  }
 }
 
-// ------------------------------------------------------------------ 4-bit heads, few tokens
+// ------------------------------------------------------------------ logits in pieces
 // With few tokens the time is the head's bytes, and a 4-bit head written out in
-// bf16 first is five times its own.  There the layer's own products read the
-// codes (their few-token strips and narrow tiles), a piece of fp32 logits passes
-// through the workspace, and these kernels do the rest.
-
-// A piece's n logits lie in groups of `width` columns, each a [T, its width]
-// matrix of its own (width and n are multiples of 8, width of 256 or n itself).
+// bf16 first is five times its own: there the layer's own products read the codes.
+// And a head of few tiles leaves most of the chip idle: there the tiles' sums over
+// I are split into planes.  Either way a piece of fp32 logits passes through the
+// workspace, and these kernels do the rest.
+//
+// A piece's n logits of a token lie in groups of `width` columns, each group a
+// [T, its width] matrix of its own (width a multiple of 256), or in one matrix of
+// row length `width` >= n; in `planes` planes, `plane` values apart, that add up.
+struct CePiece {
+  const float* logits;
+  int n, width, planes;
+  int64_t plane;
+  int64_t v0;               // its first row of the head
+  const int* rows;          // as CeArgs
+  const int* count;
+  const void* y;
+  int y_bytes;
+  int T;
+  int64_t V;
+  __device__ __forceinline__ int live() const { return count ? min(*count, T) : T; }
+  __device__ __forceinline__ int token(int row) const { return rows ? rows[row] : row; }
+  // where row `row`'s logit of column c < n is, its neighbours of the group beside it
+  __device__ __forceinline__ int64_t at(int row, int c) const {
+    const int first = c / width * width, own = width < n ? min(width, n - first) : width;
+    return (int64_t)first * T + (int64_t)row * own + (c - first);
+  }
+};
 
 // (max, sum) of 256 logits of one token per wave, and the target's logit.
-__global__ __launch_bounds__(256) void ce_part_kernel(const float* __restrict__ logits, int n, int width, int64_t v0, int T,
-                                                      int64_t V, const void* __restrict__ y, int y_bytes,
-                                                      float2* __restrict__ part, float* __restrict__ tlogit) {
-  const int lane = threadIdx.x & 63, t = (int)blockIdx.y * 4 + (threadIdx.x >> 6);
-  if (t >= T) return;
+__global__ __launch_bounds__(256) void ce_part_kernel(CePiece p, float2* __restrict__ part, float* __restrict__ tlogit) {
+  const int lane = threadIdx.x & 63, row = (int)blockIdx.y * 4 + (threadIdx.x >> 6);
+  if (row >= p.live()) return;
   const int c0 = (int)blockIdx.x * 256 + lane * 4;
-  float l[4], top = -INFINITY;
-  const int64_t at = target_at(y, y_bytes, t) - v0 - c0;
-  const int first = c0 / width * width, own = min(width, n - first);
-  const float* row = logits + (int64_t)first * T + (int64_t)t * own - first;
+  const int64_t at = target_at(p.y, p.y_bytes, p.token(row)) - p.v0 - c0;
+  float l[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, top = -INFINITY;
+  if (c0 < p.n) {
+    const float* src = p.logits + p.at(row, c0);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    l[i] = c0 + i < n ? row[c0 + i] : -INFINITY;
-    if (at == i && c0 + i < n) tlogit[t] = l[i];
-    top = fmaxf(top, l[i]);
+    for (int i = 0; i < 4; ++i) {
+      if (c0 + i >= p.n) continue;
+      l[i] = src[i];
+      for (int s = 1; s < p.planes; ++s) l[i] += src[s * p.plane + i];
+      if (at == i) tlogit[row] = l[i];
+      top = fmaxf(top, l[i]);
+    }
   }
 #pragma unroll
   for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -614,110 +671,149 @@ __global__ __launch_bounds__(256) void ce_part_kernel(const float* __restrict__ 
   for (int i = 0; i < 4; ++i) sum += __expf(l[i] - ref);
 #pragma unroll
   for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  if (lane == 0) part[(size_t)blockIdx.x * T + t] = make_float2(top, sum);
+  if (lane == 0) part[(size_t)blockIdx.x * p.T + row] = make_float2(top, sum);
 }
 
-// The logits' gradients in bf16, 8 of one token per lane, in groups of d_width.
-__global__ __launch_bounds__(256) void ce_grad_kernel(const float* __restrict__ logits, int n, int width, int64_t v0, int T,
-                                                      int64_t V, const void* __restrict__ y, int y_bytes,
-                                                      const float* __restrict__ lse, const float* __restrict__ dloss,
-                                                      int d_width, uint16_t* __restrict__ d, float* __restrict__ lost) {
-  const int t = (int)blockIdx.y, c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8;
-  if (c >= n) return;
-  const int64_t target = target_at(y, y_bytes, t);
-  const bool valid = target >= 0 && target < V;
-  const float s = valid ? dloss[t] : 0.0f, z = valid ? lse[t] : 0.0f;
-  const int from = c / width * width;
-  const float4* l = reinterpret_cast<const float4*>(logits + (int64_t)from * T + (int64_t)t * min(width, n - from) + (c - from));
-  const float4 a = l[0], b = l[1];
-  const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  const int64_t at = target - v0 - c;
+// The logits' gradients in bf16, 8 of one token per lane, in groups of d_width
+// columns, each a [T, d_width] matrix; d_cols columns in all, whole groups.  The
+// last group ends where the logits end, so it begins `shift` columns inside the
+// one before it, and those columns are zeros in it; without groups (d_width =
+// d_cols, shift 0) columns from n on are zeros.  All sizes are multiples of 8 but n.
+__global__ __launch_bounds__(256) void ce_grad_kernel(CePiece p, const float* __restrict__ lse,
+                                                      const float* __restrict__ dloss, int d_cols, int d_width, int shift,
+                                                      uint16_t* __restrict__ d, float* __restrict__ lost) {
+  const int row = (int)blockIdx.y, k = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8;
+  if (row >= p.live() || k >= d_cols) return;
+  const int first = k / d_width * d_width, early = first + d_width >= d_cols ? shift : 0;
+  const int c = k - early, t = p.token(row);
+  const int64_t target = target_at(p.y, p.y_bytes, t), at = target - p.v0 - c;
+  const bool any = target >= 0 && target < p.V && c < p.n && k - first >= early;
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+  if (any) {
+    const float* src = p.logits + p.at(row, c);
+    for (int s = 0; s < p.planes; ++s) {
+      const float4* l = reinterpret_cast<const float4*>(src + s * p.plane);
+      const float4 a = l[0], b = l[1];
+      x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
+      x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+    }
+  }
+  const float f = any ? dloss[t] : 0.0f, z = any ? lse[t] : 0.0f;
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     f32x2 e;
-    e.x = valid ? s * (__expf(x[2 * i] - z) - (at == 2 * i ? 1.0f : 0.0f)) : 0.0f;
-    e.y = valid ? s * (__expf(x[2 * i + 1] - z) - (at == 2 * i + 1 ? 1.0f : 0.0f)) : 0.0f;
+    e.x = any && c + 2 * i < p.n ? f * (__expf(x[2 * i] - z) - (at == 2 * i ? 1.0f : 0.0f)) : 0.0f;
+    e.y = any && c + 2 * i + 1 < p.n ? f * (__expf(x[2 * i + 1] - z) - (at == 2 * i + 1 ? 1.0f : 0.0f)) : 0.0f;
     w[i] = bits_of(__builtin_convertvector(e, bf16x2));
-    if (valid && at >> 1 == i) lost[t] = at & 1 ? e.y - bf16_half(w[i], 1) : e.x - bf16_half(w[i], 0);
+    if (any && at >= 0 && at >> 1 == i) lost[row] = at & 1 ? e.y - bf16_half(w[i], 1) : e.x - bf16_half(w[i], 0);
   }
-  const int first = c / d_width * d_width, own = min(d_width, n - first);
-  *reinterpret_cast<u32x4*>(d + (size_t)first * T + (size_t)t * own + (c - first)) = w;
+  *reinterpret_cast<u32x4*>(d + (size_t)first * p.T + (size_t)row * d_width + (k - first)) = w;
 }
 
-// The tail's logits of one token per wave: their part and target's logit (GRAD
-// false), or their gradients in fp32.
-template <int FMT, bool GRAD>
-__global__ __launch_bounds__(64) void ce_tail_kernel(const uint16_t* __restrict__ X, const uint8_t* __restrict__ codes,
-                                                     const uint8_t* __restrict__ scales, int rows, int H, float ws2,
-                                                     int64_t v0, int T, int64_t V, const void* __restrict__ y,
-                                                     int y_bytes, const float* __restrict__ lse,
-                                                     const float* __restrict__ dloss, float2* __restrict__ part,
-                                                     float* __restrict__ tlogit, float* __restrict__ d) {
-  const int t = (int)blockIdx.x, lane = threadIdx.x;
-  float l[8];
+// The rows of a 4-bit head past a multiple of 8, fewer than 8: a workgroup takes
+// one token's logits of them, a wave two rows; their part and the target's logit
+// (GRAD false), or their gradients in fp32.
+template <bool GRAD>
+__global__ __launch_bounds__(256) void ce_tail_kernel(const uint16_t* __restrict__ X, const uint8_t* __restrict__ codes,
+                                                      const uint8_t* __restrict__ scales, int fmt, int rows, int H,
+                                                      float ws2, int64_t v0, int64_t V, const void* __restrict__ y,
+                                                      int y_bytes, const float* __restrict__ lse,
+                                                      const float* __restrict__ dloss, float2* __restrict__ part,
+                                                      float* __restrict__ tlogit, float* __restrict__ d) {
+  __shared__ float s_l[8];
+  const int t = (int)blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float sum[2] = {0.0f, 0.0f};
+  for (int h = lane * 8; h < H; h += 512) {
+    const u32x4 q = *reinterpret_cast<const u32x4*>(X + (size_t)t * H + h);
 #pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    float sum = 0.0f;
-    if (r < rows) {
-      for (int h = lane; h < H; h += 64)
-        sum = __builtin_fmaf(__uint_as_float((uint32_t)X[(size_t)t * H + h] << 16), code_at<FMT>(codes, scales, (int64_t)r * H + h), sum);
+    for (int k = 0; k < 2; ++k) {
+      const int r = min(2 * wave + k, rows - 1);              // a row past the last is not used
+      float w[8];
+      head8(fmt, codes, scales, (int64_t)r * H + h, w);
 #pragma unroll
-      for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
+      for (int i = 0; i < 8; ++i) sum[k] = __builtin_fmaf(bf16_half(q[i >> 1], i & 1), w[i], sum[k]);
     }
-    l[r] = r < rows ? sum * ws2 : -INFINITY;
   }
-  if (lane != 0) return;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+#pragma unroll
+    for (int s = 32; s; s >>= 1) sum[k] += __shfl_xor(sum[k], s);
+    if (lane == 0) s_l[2 * wave + k] = 2 * wave + k < rows ? sum[k] * ws2 : -INFINITY;
+  }
+  __syncthreads();
   const int64_t target = target_at(y, y_bytes, t), at = target - v0;
   if constexpr (GRAD) {
     const bool valid = target >= 0 && target < V;
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-      if (r < rows) d[t * 8 + r] = valid ? dloss[t] * (__expf(l[r] - lse[t]) - (at == r ? 1.0f : 0.0f)) : 0.0f;
-  } else {
-    float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      top = fmaxf(top, l[r]);
-      if (at == r && r < rows) tlogit[t] = l[r];
+    const int r = (int)threadIdx.x;
+    if (r < rows) d[t * 8 + r] = valid ? dloss[t] * (__expf(s_l[r] - lse[t]) - (at == r ? 1.0f : 0.0f)) : 0.0f;
+  } else if (threadIdx.x == 0) {
+    float top = -INFINITY, total = 0.0f;
+    for (int r = 0; r < rows; ++r) {
+      top = fmaxf(top, s_l[r]);
+      if (at == r) tlogit[t] = s_l[r];
     }
     const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-    for (int r = 0; r < 8; ++r) sum += __expf(l[r] - ref);
-    part[t] = make_float2(top, sum);
+    for (int r = 0; r < rows; ++r) total += __expf(s_l[r] - ref);
+    part[t] = make_float2(top, total);
   }
 }
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
 
 // ------------------------------------------------------------------ plan
+constexpr int64_t kCeFullTiles = 192;   // tiles below which smaller ones are taken
+constexpr int64_t kCeSplitStages = 16;  // stages of the sum over I from which few tiles are split
 constexpr int64_t kCePieceBytes = int64_t(256) << 20;        // a piece's logit gradients, and a 4-bit head's bf16 rows
 
 struct CePlan {
   int bt;                   // token extent of the tiles
   bool compact;             // rows without a target are left out
+  int splits;               // of the logits' sums over I, through fp32 planes (1: none)
   int64_t piece;            // rows of W per piece (a multiple of 256)
   int pieces;
-  int ld;                   // backward: columns of the logit gradients
-  size_t rows, tlogit, part, wbuf, d, sums, total;           // offsets in the workspace
+  int ld;                   // columns of the logit gradients (and of the planes)
+  size_t rows, tlogit, part, wbuf, logits, d, sums, total;   // offsets in the workspace
 };
 
 inline int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
 CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
   CePlan p{};
+  // The largest tiles that give most CUs one, down to 64 tokens (174 tokens of
+  // 7717 x 736 bf16, loss and gradient: 256-token tiles 115 us, 64-token ones 53).
+  const int64_t vt = (V + 255) / 256;
   p.bt = T <= 64 ? 64 : T <= 128 ? 128 : 256;
+  while (p.bt > 64 && vt * (up(T, p.bt) / p.bt) < kCeFullTiles) p.bt /= 2;
   p.compact = T > 256;
-  int64_t most = V;
+  int64_t most = up(V, 256);
   if (bwd) most = kCePieceBytes / (2 * T);
   if (four_bit || bwd) {                                     // also 32-bit offsets into a piece of W
-    const int64_t by_w = (four_bit ? kCePieceBytes : int64_t(1) << 30) / (2 * H);
+    // A 4-bit head's rows, written out and read while still in the cache at 256
+    // MiB, but at least four tiles for every CU within 1 GiB (673 tokens, half of
+    // them ignored, of 143596 x 8160 MXFP4: pieces of 256 MiB 6.6 ms, of 1 GiB 5.3)
+    int64_t by_w = (int64_t(1) << 30) / (2 * H);
+    if (four_bit) {
+      const int64_t cached = kCePieceBytes / (2 * H), fill = 4 * kCUs * 256 / (up(T, p.bt) / p.bt), rows = cached > fill ? cached : fill;
+      by_w = rows < by_w ? rows : by_w;
+    }
     most = most < by_w ? most : by_w;
   }
   most = most / 256 * 256 > 256 ? most / 256 * 256 : 256;
   p.pieces = (int)((V + most - 1) / most);
   p.piece = up((V + p.pieces - 1) / p.pieces, 256);
   p.pieces = (int)((V + p.piece - 1) / p.piece);
+  p.ld = (int)(p.piece < V ? p.piece : up(V, 64));
+  // Few tiles and a long sum: split it, at least 4 stages each (bf16, whole against
+  // split: 4 tokens of 1136 x 7296 178, 53 us; 555 of 3891 x 4864 351, 138).
+  const int64_t tiles = vt * (up(T, p.bt) / p.bt), stages = (H + kBK - 1) / kBK;
+  p.splits = 1;
+  if (p.pieces == 1 && 2 * tiles <= kCUs && stages >= kCeSplitStages) {
+    const int64_t by_cu = kCUs / tiles, by_stages = stages / 4, n = by_cu < by_stages ? by_cu : by_stages;
+    p.splits = (int)(n < 8 ? n : 8);
+  }
   size_t at = 256;                                           // the count of live rows
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -727,14 +823,14 @@ CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
   p.rows = take(p.compact ? (size_t)T * 4 : 0);
   if (four_bit) p.wbuf = take((size_t)p.piece * H * 2);
   p.tlogit = take((size_t)T * 4);
+  if (p.splits > 1) p.logits = take((size_t)p.splits * T * p.ld * 4);
   if (!bwd) {
-    p.part = take((size_t)((V + 255) / 256) * T * 8);
+    p.part = take((size_t)vt * T * 8);
   } else {
-    p.ld = (int)(p.piece < V ? p.piece : up(V, 64));
     p.d = take((size_t)T * p.ld * 2);
     // planes of whole tiles: splits x tiles <= max(CUs, tiles), or one tile row's
-    const int64_t tiles = up(T, p.bt) / p.bt * (up(H, 256) / 256);
-    p.sums = take((size_t)(tiles > kCUs ? tiles : kCUs) * p.bt * 256 * 4);
+    const int64_t dx_tiles = up(T, p.bt) / p.bt * (up(H, 256) / 256);
+    p.sums = take((size_t)(dx_tiles > kCUs ? dx_tiles : kCUs) * p.bt * 256 * 4);
   }
   p.total = at;
   return p;
@@ -773,33 +869,62 @@ int ce_weight(int head, const void* W, const uint8_t* scales, int64_t v0, int64_
   return ok();
 }
 
-// ------------------------------------------------------------------ 4-bit heads, few tokens: plan
+int ce_part_go(const CePiece& c, float2* part, float* tlogit, hipStream_t s) {
+  hipLaunchKernelGGL(ce_part_kernel, dim3((unsigned)((c.n + 255) / 256), (unsigned)((c.T + 3) / 4)), dim3(256), 0, s, c, part,
+                     tlogit);
+  return ok();
+}
+
+int ce_grad_go(const CePiece& c, const float* lse, const float* dloss, int d_cols, int d_width, int shift, uint16_t* d,
+               float* lost, hipStream_t s) {
+  hipLaunchKernelGGL(ce_grad_kernel, dim3((unsigned)((d_cols / 8 + 255) / 256), (unsigned)c.T), dim3(256), 0, s, c, lse, dloss,
+                     d_cols, d_width, shift, d, lost);
+  return ok();
+}
+
+int ce_loss_go(const float2* part, const float* tlogit, const CePiece& c, int tiles, float* loss, float* lse, hipStream_t s) {
+  hipLaunchKernelGGL(ce_loss_kernel, dim3((unsigned)((c.T + 63) / 64)), dim3(1024), 0, s, part, tlogit, c.rows, c.count, c.y,
+                     c.y_bytes, c.T, c.V, tiles, loss, lse);
+  return ok();
+}
+
+// ------------------------------------------------------------------ 4-bit heads, few tokens
 constexpr int64_t kCeLogitBytes = int64_t(64) << 20;         // a piece's fp32 logits
-constexpr int kCeGroupTokens = 128;
 
 struct CeFew {
   int64_t main;             // rows of the head that the layer's products take (a multiple of 8)
   int tail;                 // the others, fewer than 8
   int64_t piece;            // rows per piece of logits
-  int width, groups;        // backward: rows per group of dX's contraction, groups of the whole head
+  int group;                // rows per group of the logits' product (0: one product)
+  int width, groups, shift; // backward: groups of dX's contraction, as ce_grad_kernel takes them
   size_t tlogit, part, logits, d, sums, dtail, total;
 };
+
+// One product over many rows would take strips or tiles made for a layer's few; as
+// a grouped one over groups of 4096 rows it takes the grouped products' tiles
+// (131072 x 4096 MXFP4, us of loss and gradient, one product against groups: 1
+// token 318, 261; 64 tokens 503, 328; 128 tokens 694, 575; 256 tokens 939, 1063;
+// NVFP4 64 tokens 493, 439; 128 tokens 821, 663).
+constexpr int kCeGroupTokens = 128, kCeGroupRows = 4096, kCeGroupFrom = 8 * kCeGroupRows;
 
 CeFew ce_few_plan(bool bwd, int64_t T, int64_t V, int64_t H) {
   CeFew p{};
   p.main = V / 8 * 8;
   p.tail = (int)(V - p.main);
-  // groups of whole stages, so many that their 256-column tiles fill the CUs
-  const int64_t cols = (H + 255) / 256;
-  int64_t groups = (2 * kCUs + cols - 1) / cols;
-  groups = groups < 64 ? groups : 64;
-  p.width = (int)up((p.main + groups - 1) / groups, 256);
-  if (p.width < 256) p.width = 256;
-  p.groups = (int)((p.main + p.width - 1) / p.width);
+  p.group = (T <= kCeGroupTokens && p.main >= kCeGroupFrom) || p.main * H > int64_t(1) << 31 ? kCeGroupRows : 0;
   int64_t rows = kCeLogitBytes / (4 * T);
   const int64_t by_codes = (int64_t(1) << 31) / H;           // operands below 1 GiB
   rows = rows < by_codes ? rows : by_codes;
-  p.piece = rows / p.width * p.width > p.width ? rows / p.width * p.width : p.width;
+  rows = rows / kCeGroupRows * kCeGroupRows;
+  p.piece = rows > kCeGroupRows ? rows : kCeGroupRows;
+  // dX in as many groups of equal width as their 256-column tiles need to fill the
+  // CUs twice, over all of the head at once: its gradients are 2 bytes per logit
+  const int64_t cols = (H + 255) / 256, want = (2 * kCUs + cols - 1) / cols;
+  p.width = (int)up((p.main + (want < 64 ? want : 64) - 1) / (want < 64 ? want : 64), 64);
+  if (p.width < 256) p.width = 256;
+  if (p.width > p.main) p.width = (int)p.main;
+  p.groups = (int)((p.main + p.width - 1) / p.width);
+  p.shift = (int)((int64_t)p.groups * p.width - p.main);
   const int64_t most = p.piece < p.main ? p.piece : p.main;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -807,12 +932,12 @@ CeFew ce_few_plan(bool bwd, int64_t T, int64_t V, int64_t H) {
     at += (bytes + 255) & ~(size_t)255;
     return o;
   };
-  p.logits = take((size_t)most * T * 4);
+  p.logits = take((size_t)(bwd ? p.main : most) * T * 4);
   p.tlogit = take((size_t)T * 4);
   if (!bwd) {
-    p.part = take((size_t)((p.main + 255) / 256 + p.main / p.piece + 2) * T * 8);
+    p.part = take((size_t)((p.main + 255) / 256 + 1) * T * 8);
   } else {
-    p.d = take((size_t)p.main * T * 2);
+    p.d = take((size_t)p.groups * p.width * T * 2);
     p.sums = take((size_t)p.groups * T * H * 4);
     p.dtail = take((size_t)T * 32);
   }
@@ -823,71 +948,60 @@ CeFew ce_few_plan(bool bwd, int64_t T, int64_t V, int64_t H) {
 // Whether the layer's products take the head (their operands within 32 bits).
 bool ce_few(int head, int64_t T, int64_t V, int64_t H) {
   if (head == kCeBf16 || T > kCeFewTokens || V < 8) return false;
-  const int64_t width = ce_few_plan(true, T, V, H).width;
-  return width * H <= int64_t(1) << 31 && width * T * 4 <= int64_t(1) << 30;
+  const CeFew p = ce_few_plan(true, T, V, H);
+  return p.width * H <= int64_t(1) << 31 && kCeGroupRows * H <= int64_t(1) << 31 && p.width * T * 4 <= int64_t(1) << 30 &&
+         p.main * T * 4 <= int64_t(1) << 30;
 }
 
-// Logits of rows [v0, v0 + n) of the head; the width of their groups goes to
-// *width.  One product over this many rows would take strips or tiles made for a
-// layer's few; as a grouped one over groups of rows it takes the grouped
-// products' tiles (131072 x 4096 MXFP4, us of loss and gradient, one product
-// against groups: 1 token 318, 261; 64 tokens 503, 328; 128 tokens 694, 575; 256
-// tokens 939, 1063; NVFP4 64 tokens 493, 439; 128 tokens 821, 663).
+// Logits of rows [v0, v0 + n) of the head to `logits`, and how they lie in *c.
 int ce_few_logits(int head, int T, int64_t v0, int n, int H, const void* X, const uint8_t* codes, const uint8_t* scales,
-                  float ws2, int group, float* logits, int* width, hipStream_t s) {
+                  float ws2, int group, float* logits, CePiece* c, hipStream_t s) {
   const int64_t G = H / (head == kMX ? 32 : 16);
-  const uint8_t* c = codes + v0 * H / 2;
+  const uint8_t* cd = codes + v0 * H / 2;
   const uint8_t* sc = scales + v0 * G;
-  if (T > kCeGroupTokens || n <= group) {
-    *width = n;
-    return gemm_fwd(head, T, n, H, X, c, sc, ws2, logits, 0, s);
-  }
-  *width = group;
+  c->logits = logits;
+  c->v0 = v0;
+  c->n = n;
+  c->planes = 1;
+  c->width = group > 0 && n > group ? group : n;
+  if (c->width == n) return gemm_fwd(head, T, n, H, X, cd, sc, ws2, logits, 0, s);
   ExpertProblem e[kGroupMax];
   const int whole = n / group, last = n - whole * group;
   for (int k0 = 0; k0 < whole; k0 += kGroupMax) {
     const int m = whole - k0 < kGroupMax ? whole - k0 : kGroupMax;
     for (int k = 0; k < m; ++k) {
       const int64_t r = (int64_t)(k0 + k) * group;
-      e[k] = ExpertProblem{X, nullptr, c + r * H / 2, sc + r * G, logits + r * T, T, ws2};
+      e[k] = ExpertProblem{X, nullptr, cd + r * H / 2, sc + r * G, logits + r * T, T, ws2};
     }
     if (gemm_fwd_grouped(head, group, H, m, e, 0, s) != 0) return -1;
   }
   const int64_t r = (int64_t)whole * group;
-  return last == 0 ? 0 : gemm_fwd(head, T, last, H, X, c + r * H / 2, sc + r * G, ws2, logits + r * T, 0, s);
+  return last == 0 ? 0 : gemm_fwd(head, T, last, H, X, cd + r * H / 2, sc + r * G, ws2, logits + r * T, 0, s);
 }
 
 int ce_few_fwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* codes, const uint8_t* scales, float ws2,
                const void* y, int y_bytes, float* loss, float* lse, uint8_t* ws, hipStream_t s) {
   const CeFew p = ce_few_plan(false, T, V, H);
-  const int64_t G = H / (head == kMX ? 32 : 16);
   float* logits = reinterpret_cast<float*>(ws + p.logits);
   float2* part = reinterpret_cast<float2*>(ws + p.part);
   float* tlogit = reinterpret_cast<float*>(ws + p.tlogit);
+  CePiece c{};
+  c.y = y; c.y_bytes = y_bytes; c.T = T; c.V = V;
   int tiles = 0;
   for (int64_t v0 = 0; v0 < p.main; v0 += p.piece) {
     const int n = (int)(p.main - v0 < p.piece ? p.main - v0 : p.piece);
-    int width;
-    if (ce_few_logits(head, T, v0, n, H, X, codes, scales, ws2, p.width, logits, &width, s) != 0) return -1;
-    const int nt = (n + 255) / 256;
-    hipLaunchKernelGGL(ce_part_kernel, dim3((unsigned)nt, (unsigned)((T + 3) / 4)), dim3(256), 0, s, logits, n, width, v0, T, V, y,
-                       y_bytes, part + (size_t)tiles * T, tlogit);
-    if (ok() != 0) return -1;
-    tiles += nt;
+    if (ce_few_logits(head, T, v0, n, H, X, codes, scales, ws2, p.group, logits, &c, s) != 0) return -1;
+    if (ce_part_go(c, part + (size_t)tiles * T, tlogit, s) != 0) return -1;
+    tiles += (n + 255) / 256;
   }
   if (p.tail > 0) {
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(64), 0, s, static_cast<const uint16_t*>(X), codes + p.main * H / 2,
-                         scales + p.main * G, p.tail, H, ws2, p.main, T, V, y, y_bytes, nullptr, nullptr,
-                         part + (size_t)tiles * T, tlogit, nullptr);
-      return ok();
-    };
-    if ((head == kMX ? go(ce_tail_kernel<kMX, false>) : go(ce_tail_kernel<kNV, false>)) != 0) return -1;
+    hipLaunchKernelGGL(ce_tail_kernel<false>, dim3((unsigned)T), dim3(256), 0, s, static_cast<const uint16_t*>(X),
+                       codes + p.main * H / 2, scales + p.main * (H / (head == kMX ? 32 : 16)), head, p.tail, H, ws2, p.main, V,
+                       y, y_bytes, nullptr, nullptr, part + (size_t)tiles * T, tlogit, nullptr);
+    if (ok() != 0) return -1;
     ++tiles;
   }
-  hipLaunchKernelGGL(ce_loss_kernel, dim3((unsigned)((T + 63) / 64)), dim3(1024), 0, s, part, tlogit, nullptr, nullptr, y,
-                     y_bytes, T, V, tiles, loss, lse);
-  return ok();
+  return ce_loss_go(part, tlogit, c, tiles, loss, lse, s);
 }
 
 int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* codes, const uint8_t* scales, float ws2,
@@ -895,38 +1009,28 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
                hipStream_t s) {
   const CeFew p = ce_few_plan(true, T, V, H);
   const int64_t G = H / (head == kMX ? 32 : 16);
-  float* logits = reinterpret_cast<float*>(ws + p.logits);
   uint16_t* d = reinterpret_cast<uint16_t*>(ws + p.d);
   float* sums = reinterpret_cast<float*>(ws + p.sums);
   float* dtail = reinterpret_cast<float*>(ws + p.dtail);
   float* lost = reinterpret_cast<float*>(ws + p.tlogit);
-  for (int64_t v0 = 0; v0 < p.main; v0 += p.piece) {
-    const int n = (int)(p.main - v0 < p.piece ? p.main - v0 : p.piece);
-    int width;
-    if (ce_few_logits(head, T, v0, n, H, X, codes, scales, ws2, p.width, logits, &width, s) != 0) return -1;
-    hipLaunchKernelGGL(ce_grad_kernel, dim3((unsigned)((n / 8 + 255) / 256), (unsigned)T), dim3(256), 0, s, logits, n, width, v0, T,
-                       V, y, y_bytes, lse, dloss, p.width, d + (size_t)v0 * T, lost);
+  CePiece c{};
+  c.y = y; c.y_bytes = y_bytes; c.T = T; c.V = V;
+  if (ce_few_logits(head, T, 0, (int)p.main, H, X, codes, scales, ws2, p.group, reinterpret_cast<float*>(ws + p.logits), &c, s) != 0)
+    return -1;
+  if (ce_grad_go(c, lse, dloss, p.groups * p.width, p.width, p.shift, d, lost, s) != 0) return -1;
+  if (p.tail > 0) {
+    hipLaunchKernelGGL(ce_tail_kernel<true>, dim3((unsigned)T), dim3(256), 0, s, static_cast<const uint16_t*>(X),
+                       codes + p.main * H / 2, scales + p.main * G, head, p.tail, H, ws2, p.main, V, y, y_bytes, lse, dloss,
+                       nullptr, nullptr, dtail);
     if (ok() != 0) return -1;
   }
-  if (p.tail > 0) {
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(64), 0, s, static_cast<const uint16_t*>(X), codes + p.main * H / 2,
-                         scales + p.main * G, p.tail, H, ws2, p.main, T, V, y, y_bytes, lse, dloss, nullptr, nullptr, dtail);
-      return ok();
-    };
-    if ((head == kMX ? go(ce_tail_kernel<kMX, true>) : go(ce_tail_kernel<kNV, true>)) != 0) return -1;
-  }
-  // dX of every group of rows, as the layer's grouped product: groups of one width
-  // in one call, the last, narrower one in its own
+  // dX of every group of rows, as the layer's grouped product
   ExpertProblem e[64];
   for (int k = 0; k < p.groups; ++k) {
-    const int64_t v0 = (int64_t)k * p.width;
-    e[k] = ExpertProblem{d + (size_t)v0 * T, nullptr, codes + v0 * H / 2, scales + v0 * G, sums + (size_t)k * T * H, T, ws2};
+    const int64_t v0 = (int64_t)k * p.width - (k + 1 == p.groups ? p.shift : 0);
+    e[k] = ExpertProblem{d + (size_t)k * p.width * T, nullptr, codes + v0 * H / 2, scales + v0 * G, sums + (size_t)k * T * H, T, ws2};
   }
-  const int last = (int)(p.main - (int64_t)(p.groups - 1) * p.width), whole = last == p.width ? p.groups : p.groups - 1;
-  if (whole > 0 && gemm_dx_grouped(head, p.width, H, whole, e, 0, s) != 0) return -1;
-  if (whole < p.groups && gemm_dx(head, T, last, H, e[whole].a, e[whole].codes, e[whole].scales, ws2, e[whole].out, 0, s) != 0)
-    return -1;
+  if (gemm_dx_grouped(head, p.width, H, p.groups, e, 0, s) != 0) return -1;
   const CeRest rest{codes, scales, lost, dtail, p.main, p.tail, head};
   auto finish = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(256), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, y, y_bytes,
@@ -943,6 +1047,29 @@ size_t ce_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H) {
   return ce_plan(bwd != 0, head != kCeBf16, T, V, H).total;
 }
 
+// What both directions set up: the arguments, and the live rows numbered.
+static int ce_begin(const CePlan& p, int T, int64_t V, int H, const void* X, float ws2, const void* y, int y_bytes, uint8_t* ws,
+                    CeArgs* g, CePiece* c, hipStream_t s) {
+  g->x = static_cast<const uint16_t*>(X);
+  g->y = y; g->y_bytes = y_bytes; g->T = T; g->H = H; g->V = V; g->ws2 = ws2;
+  g->tlogit = reinterpret_cast<float*>(ws + p.tlogit);
+  g->ld = g->ldl = p.ld;
+  g->splits = p.splits;
+  g->logits = reinterpret_cast<float*>(ws + p.logits);
+  if (p.compact) {
+    int* count = reinterpret_cast<int*>(ws);
+    int* rows = reinterpret_cast<int*>(ws + p.rows);
+    g->count = count;
+    g->rows = rows;
+    hipLaunchKernelGGL(ce_rows_kernel, dim3(1), dim3(1024), 0, s, y, y_bytes, T, V, count, rows);
+    if (ok() != 0) return -1;
+  }
+  c->logits = g->logits;
+  c->n = (int)V; c->width = p.ld; c->planes = p.splits; c->plane = (int64_t)T * p.ld;
+  c->rows = g->rows; c->count = g->count; c->y = y; c->y_bytes = y_bytes; c->T = T; c->V = V;
+  return 0;
+}
+
 int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
                   const void* y, int y_bytes, float* loss, float* lse, void* workspace, hipStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -950,31 +1077,24 @@ int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     return ce_few_fwd(head, T, V, H, X, static_cast<const uint8_t*>(W), scales, ws2, y, y_bytes, loss, lse, ws, s);
   const CePlan p = ce_plan(false, head != kCeBf16, T, V, H);
   CeArgs g{};
-  g.x = static_cast<const uint16_t*>(X);
-  g.y = y; g.y_bytes = y_bytes; g.T = T; g.H = H; g.V = V; g.ws2 = ws2;
+  CePiece c{};
+  if (ce_begin(p, T, V, H, X, ws2, y, y_bytes, ws, &g, &c, s) != 0) return -1;
   g.part = reinterpret_cast<float*>(ws + p.part);
-  g.tlogit = reinterpret_cast<float*>(ws + p.tlogit);
-  if (p.compact) {
-    int* count = reinterpret_cast<int*>(ws);
-    int* rows = reinterpret_cast<int*>(ws + p.rows);
-    g.count = count;
-    g.rows = rows;
-    hipLaunchKernelGGL(ce_rows_kernel, dim3(1), dim3(1024), 0, s, y, y_bytes, T, V, count, rows);
-    if (ok() != 0) return -1;
-  }
+  float2* part = reinterpret_cast<float2*>(g.part);
   const int64_t tt = (T + p.bt - 1) / p.bt;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
-    const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
+    const int64_t n = V - v0 < p.piece ? V - v0 : p.piece, tiles = (n + 255) / 256 * tt;
     if (ce_weight(head, W, scales, v0, n, H, ws + p.wbuf, &g.w, s) != 0) return -1;
     g.v0 = v0;
     g.Vn = (int)n;
     g.part_tile0 = (int)(v0 / 256);
-    if (ce_go<kCeStats>(g, p.bt, (n + 255) / 256 * tt, s) != 0) return -1;
+    if (p.splits > 1) {
+      if (ce_go<kCeLogits>(g, p.bt, tiles * p.splits, s) != 0 || ce_part_go(c, part, g.tlogit, s) != 0) return -1;
+    } else if (ce_go<kCeStats>(g, p.bt, tiles, s) != 0) {
+      return -1;
+    }
   }
-  hipLaunchKernelGGL(ce_loss_kernel, dim3((unsigned)((T + 63) / 64)), dim3(1024), 0, s,
-                     reinterpret_cast<const float2*>(g.part), g.tlogit, g.rows, g.count, y, y_bytes, T, V,
-                     (int)((V + 255) / 256), loss, lse);
-  return ok();
+  return ce_loss_go(part, g.tlogit, c, (int)((V + 255) / 256), loss, lse, s);
 }
 
 int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
@@ -986,31 +1106,27 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
                       ws, s);
   const CePlan p = ce_plan(true, head != kCeBf16, T, V, H);
   CeArgs g{};
-  g.x = static_cast<const uint16_t*>(X);
-  g.y = y; g.y_bytes = y_bytes; g.T = T; g.H = H; g.V = V; g.ws2 = ws2;
+  CePiece c{};
+  if (ce_begin(p, T, V, H, X, ws2, y, y_bytes, ws, &g, &c, s) != 0) return -1;
   g.lse = lse; g.dloss = dloss;
-  g.tlogit = reinterpret_cast<float*>(ws + p.tlogit);
   g.d = reinterpret_cast<uint16_t*>(ws + p.d);
   g.sums = reinterpret_cast<float*>(ws + p.sums);
-  g.ld = p.ld;
-  g.split_stages = (int)((p.piece < V ? p.piece : V) + kBK - 1) / kBK;
-  if (p.compact) {
-    int* count = reinterpret_cast<int*>(ws);
-    int* rows = reinterpret_cast<int*>(ws + p.rows);
-    g.count = count;
-    g.rows = rows;
-    hipLaunchKernelGGL(ce_rows_kernel, dim3(1), dim3(1024), 0, s, y, y_bytes, T, V, count, rows);
-    if (ok() != 0) return -1;
-  }
+  g.split_stages = (int)(((p.piece < V ? p.piece : V) + kBK - 1) / kBK);
   const int64_t tt = (T + p.bt - 1) / p.bt, tn = (H + 255) / 256;
   const int64_t dx_blocks = tt * tn > kCUs ? tt * tn : kCUs;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
-    const int64_t n = V - v0 < p.piece ? V - v0 : p.piece;
+    const int64_t n = V - v0 < p.piece ? V - v0 : p.piece, tiles = (n + 255) / 256 * tt;
     if (ce_weight(head, W, scales, v0, n, H, ws + p.wbuf, &g.w, s) != 0) return -1;
     g.v0 = v0;
     g.Vn = (int)n;
     g.add = v0 > 0;
-    if (ce_go<kCeGrad>(g, p.bt, (n + 255) / 256 * tt, s) != 0) return -1;
+    if (p.splits > 1) {
+      if (ce_go<kCeLogits>(g, p.bt, tiles * p.splits, s) != 0 ||
+          ce_grad_go(c, lse, dloss, p.ld, p.ld, 0, g.d, g.tlogit, s) != 0)
+        return -1;
+    } else if (ce_go<kCeGrad>(g, p.bt, tiles, s) != 0) {
+      return -1;
+    }
     if (ce_go<kCeDx>(g, p.bt, dx_blocks, s) != 0) return -1;
   }
   const CeRest rest{W, scales, g.tlogit, nullptr, V, 0, head};

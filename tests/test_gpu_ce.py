@@ -223,3 +223,23 @@ def test_no_tokens(sq):
     loss, lse = sq.sq_ce_fwd("bf16", X, W, y)
     assert loss.shape == lse.shape == (0,)
     assert sq.sq_ce_bwd("bf16", X, W, y, lse, loss).shape == (0, 64)
+
+
+# few tiles and long rows: the logits' sums over I split into planes, with and without compact rows, and ignored tokens
+@pytest.mark.parametrize("T,V,I", [(1, 1, 1024), (4, 1136, 7296), (200, 700, 2080), (300, 513, 1088), (1000, 260, 4096)])
+@pytest.mark.parametrize("head", ["bf16", "nv"])
+def test_few_tiles_of_long_rows(sq, head, T, V, I):
+    y = inputs.rng(T + 1).integers(0, V, T)
+    y[1::5] = -1
+    _check(sq, head, T, V, I, T + I, y, out_dtype=BF16 if T > 200 else F32)
+
+
+# a 4-bit head's rows in groups: the last one of the gradient overlaps the one before it, the logits' in groups of 4096 with a
+# narrower last one, rows past a multiple of 8, and the target in each of these places
+@pytest.mark.parametrize("T,V,I", [(6, 2665, 704), (3, 33003, 64), (130, 33003, 64), (2, 40961, 96)])
+@pytest.mark.parametrize("head", ["mx", "nv"])
+def test_groups_of_a_4_bit_head(sq, head, T, V, I):
+    g = inputs.rng(T + 2)
+    edges = np.array([V - 1, V // 8 * 8 - 1, 0, V // 8 * 8, V // 8 * 8 - 300, -1, V])
+    y = np.where(g.random(T) < 0.5, g.choice(edges, T), g.integers(0, V, T))
+    _check(sq, head, T, V, I, T + I, y)
