@@ -35,29 +35,51 @@ __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
+// 4 pairs from p on, of a step that ends at `end` (<= N): one access where they
+// are whole, and its width is left to the ids' own alignment.
+template <typename ID>
+__device__ __forceinline__ void keys4(const ID* ids, int p, int end, int E, int (&k)[4]) {
+  struct __attribute__((packed, aligned(alignof(ID)))) Four { ID v[4]; };
+  if (p + 4 <= end) {
+    const Four f = *reinterpret_cast<const Four*>(ids + p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) k[j] = f.v[j] >= 0 && f.v[j] < (ID)E ? (int)f.v[j] : E;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) k[j] = key_of(ids, p + j, end, E);
+  }
+}
+
 // One launch, workgroup e owns key e: it counts the pairs of smaller keys (the
 // key's first slot) and its own (its waves' shares, each wave a contiguous run
-// of pairs), then walks the pairs again and numbers its own.  A lane takes 4
-// consecutive pairs, so 4 ballots order 256 pairs.  Every workgroup reads all
-// ids, which stay in L2; nothing is exchanged between workgroups.
+// of pairs), then numbers its own.  A lane takes 4 consecutive pairs of 256 and
+// keeps one bit for each that is its key's, so the ids are read once, 4 steps'
+// loads together, and 4 ballots order a step.  Every workgroup reads all ids,
+// which stay in L2; nothing is exchanged between workgroups.
 template <typename ID>
-__global__ __launch_bounds__(1024) void moe_sort_kernel(const ID* __restrict__ ids, int64_t N, int K, int E,
+__global__ __launch_bounds__(1024) void moe_sort_kernel(const ID* __restrict__ ids, int N, int K, int E,
                                                         int* __restrict__ offsets, int* __restrict__ token,
                                                         int* __restrict__ slot) {
   __shared__ int s_eq[16], s_lt[16];
   const int e = (int)blockIdx.x;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int64_t per = ((N + waves - 1) / waves + 255) & ~(int64_t)255;
-  const int64_t p0 = wave * per, p1 = p0 + per < N ? p0 + per : N;
-  int eq = 0, lt = 0;
-  for (int64_t p = p0; p < p1; p += 256) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int per = ((N + waves - 1) / waves + 255) & ~255;     // at most 16 steps
+  const int p0 = wave * per, p1 = min(p0 + per, N);
+  int lt = 0;
+  uint64_t mine = 0;                                          // bit 4 step + j
+  for (int st = 0; p0 + 256 * st < p1; st += 4) {
+    int k[4][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = key_of(ids, p + 4 * lane + j, N, E);
-      eq += k == e;
-      lt += k < e;
-    }
+    for (int u = 0; u < 4; ++u) keys4(ids, p0 + 256 * (st + u) + 4 * lane, p1, E, k[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        lt += k[u][j] < e;
+        mine |= (uint64_t)(k[u][j] == e) << (4 * (st + u) + j);
+      }
   }
+  int eq = __popcll(mine);
 #pragma unroll
   for (int d = 32; d; d >>= 1) {
     eq += __shfl_xor(eq, d);
@@ -76,26 +98,23 @@ __global__ __launch_bounds__(1024) void moe_sort_kernel(const ID* __restrict__ i
   if (threadIdx.x == 0) offsets[e] = base;       // key E, the dropped pairs: the routed count
   int next = base + before;
   if (eq == 0) return;                           // after the last barrier; uniform in the wave
-  for (int64_t p = p0; p < p1; p += 256) {
-    bool mine[4];
-    uint64_t b[4];
-    int rank = 0;
+  for (int st = 0; p0 + 256 * st < p1; ++st) {
+    const uint32_t m = (uint32_t)(mine >> (4 * st)) & 15u;
+    int rank = next;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      mine[j] = key_of(ids, p + 4 * lane + j, N, E) == e;
-      b[j] = __ballot(mine[j]);
-      rank += lanes_below(b[j]);
+      const uint64_t b = __ballot((m >> j) & 1);
+      rank += lanes_below(b);
+      next += __popcll(b);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (!mine[j]) continue;
-      const int64_t q = p + 4 * lane + j;
-      slot[q] = next + rank;
-      token[next + rank] = (int)(q / K);
+      if (!((m >> j) & 1)) continue;
+      const uint32_t q = (uint32_t)(p0 + 256 * st + 4 * lane + j);
+      slot[q] = rank;
+      token[rank] = (int)(q / (uint32_t)K);
       ++rank;
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) next += __popcll(b[j]);
   }
 }
 
@@ -401,7 +420,7 @@ int sort_go(int64_t N, int K, int E, const ID* ids, int* offsets, int* token, in
   if (moe_sort_one(N)) {
     const int64_t need = (N + 255) / 256 * 64;                // a wave orders 256 pairs per step
     const unsigned threads = (unsigned)(need >= 1024 ? 1024 : (need < 64 ? 64 : need));
-    hipLaunchKernelGGL((moe_sort_kernel<ID>), dim3((unsigned)(E + 1)), dim3(threads), 0, s, ids, N, K, E, offsets, token, slot);
+    hipLaunchKernelGGL((moe_sort_kernel<ID>), dim3((unsigned)(E + 1)), dim3(threads), 0, s, ids, (int)N, K, E, offsets, token, slot);
     return ok();
   }
   const int chunks = (int)((N + kMoeChunk - 1) / kMoeChunk);
