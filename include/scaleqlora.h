@@ -558,7 +558,8 @@ int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, const void* d
  * sq_bwd_dscale_act8: sq_bwd_dscale with x^ in the place of X, bit for bit what
  *   that call computes for the unpacked x^.  I % 32 == 0 for either weight
  *   format, O and I at most 2^23; x_codes 16-byte aligned; workspace as sq_bwd_dscale's, of
- *   sq_bwd_dscale_act8_workspace bytes; the rest as sq_bwd_dscale.
+ *   sq_bwd_dscale_act8_workspace bytes (large layers' with x^ in bf16, for the time
+ *   of the call); the rest as sq_bwd_dscale.
  *
  * sq_bwd_dscale_act8_batched: the scale gradients of E stacked experts, whose
  *   rows of dY bf16 [N, O] stand one expert after another: expert e has rows

@@ -851,6 +851,18 @@ int ds8_splits(int T, int O, int I) {
   return splits < 2 ? 1 : splits;
 }
 
+// Layers of many outputs meet each row of x^ in many tiles, and each of them would
+// turn its 8 bits into bf16: beyond 2048 outputs, once the product is long enough
+// to pay for another launch (some 20 us), x^ goes through the workspace in bf16 to
+// the bf16 product.  MXFP4, us, tiles from 8 bits (int8, E4M3) against x^ first:
+// 8192 tokens, 14336 x 4096: 926, 807 against 737, 733; 512 tokens of it: 87, 79
+// against 75, 74; 4096 tokens, 4096 x 4096: 122, 111 against 112, 110.  And where
+// the rule keeps the tiles: 8192 tokens, 2048 x 4096: 124, 114 against 121, 120;
+// 512 tokens, 4096 x 4096: 22, 21 against 24, 25.
+bool ds8_unpacks(int T, int O, int I) {
+  return O > 2048 && (int64_t)T * O >= int64_t(24000000000) / I;
+}
+
 }  // namespace
 
 int act_pack_launch(int act, int64_t T, int64_t I, const void* X, uint8_t* codes, uint8_t* scales, hipStream_t s) {
@@ -876,12 +888,17 @@ int act_unpack_launch(int act, int64_t T, int64_t I, const uint8_t* codes, const
 }
 
 size_t dscale_act8_workspace(int fmt, int T, int O, int I) {
+  if (ds8_unpacks(T, O, I)) return (size_t)T * I * 2 + gemm_dscale_workspace(fmt, T, O, I);   // I % 32 == 0
   const int splits = ds8_splits(T, O, I);
   return splits < 2 ? 0 : (size_t)splits * O * (I / (fmt == kMX ? 32 : 16)) * sizeof(float);
 }
 
 int dscale_act8(int fmt, int act, int T, int O, int I, const uint8_t* x, const uint8_t* xs, const void* dY,
                 const uint8_t* codes, float* dS, void* workspace, hipStream_t s) {
+  if (ds8_unpacks(T, O, I)) {
+    if (act_unpack_launch(act, T, I, x, xs, workspace, s) != 0) return -1;
+    return gemm_dscale(fmt, T, O, I, workspace, dY, codes, dS, static_cast<uint8_t*>(workspace) + (size_t)T * I * 2, s);
+  }
   Ds8Args g{};
   g.x = x; g.xs = xs; g.dy = static_cast<const uint16_t*>(dY); g.codes = codes;
   g.N = T; g.O = O; g.I = I; g.G = I / (fmt == kMX ? 32 : 16);

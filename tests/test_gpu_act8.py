@@ -203,3 +203,17 @@ def test_streams_and_runs_agree(sq):
         got = sq.sq_bwd_dscale_act8("nv", "e4m3", q, s, dY, codes)
     st.synchronize()
     assert torch.equal(want, got)
+
+
+# many outputs: through x^ in bf16, with and without partial planes behind it
+# and, between the two, products of whole 256 x 256 tiles too short for that
+@pytest.mark.parametrize("T,O,I", [(1025, 8192, 4096), (16400, 8200, 288), (16392, 8192, 256), (333, 4096, 4096), (1000, 2048, 8224)])
+@pytest.mark.parametrize("fmt,act", [("mx", "int8"), ("nv", "e4m3")])
+def test_dscale_of_many_outputs_equals_the_bf16_product(sq, fmt, act, T, O, I):
+    X = inputs.device_bf16_normal(6, (T, I))
+    q, s = sq.sq_act_pack(act, X)
+    dY, codes = inputs.device_bf16_normal(7, (T, O)), inputs.device_codes_uniform(8, O, I)
+    dS = torch.full((O, I // BLOCK[fmt]), float("nan"), device="cuda")
+    workspace = torch.full((sq.sq_bwd_dscale_act8_workspace(sq.FORMATS[fmt], T, O, I),), 255, dtype=torch.uint8, device="cuda")
+    sq.sq_bwd_dscale_act8(fmt, act, q, s, dY, codes, dS=dS, workspace=workspace)
+    assert torch.equal(dS, sq.sq_bwd_dscale(fmt, sq.sq_act_unpack(act, q, s), dY, codes))
