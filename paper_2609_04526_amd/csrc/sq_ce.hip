@@ -551,18 +551,19 @@ __device__ __forceinline__ void head8(int head, const void* w, const uint8_t* sc
   }
 }
 
-// dX of one token per workgroup: the planes added in order, times f (and the
+// 1024 columns of one token's dX per workgroup: the planes added in order, times f (and the
 // rest's rows times ws2); zeros where there is no target (their rows come after
 // the live ones).  planes = 0: as many as the product split the vocabulary into.
 template <bool BF16>
-__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ sums, int planes, int64_t plane_rows,
+__global__ __launch_bounds__(128) void ce_dx_kernel(const float* __restrict__ sums, int planes, int64_t plane_rows,
                                                     const int* __restrict__ rows, const int* __restrict__ count,
                                                     const void* __restrict__ y, int y_bytes, int T, int64_t V, int H,
                                                     int bm, int tiles_n, int stages, float f, float ws2, CeRest rest,
                                                     void* __restrict__ dX) {
   const int live = count ? min(*count, T) : T;
-  const int b = (int)blockIdx.x;
-  auto put = [&](int t, int h, const float (&v)[8]) {
+  const int b = (int)blockIdx.x, h = ((int)blockIdx.y * 128 + (int)threadIdx.x) * 8;
+  if (h >= H) return;
+  auto put = [&](int t, const float (&v)[8]) {
     if constexpr (BF16) {
       u32x4 w;
 #pragma unroll
@@ -585,33 +586,31 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ su
     const size_t plane = (size_t)plane_rows * H;
     const int t = rows ? rows[b] : b;
     const int64_t own = rows ? target_at(y, y_bytes, t) : target;
-    for (int h = threadIdx.x * 8; h < H; h += 2048) {
-      float v[8];
+    float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-#pragma unroll 4
-      for (int s = 0; s < planes; ++s) {
-        const float4* q = reinterpret_cast<const float4*>(sums + s * plane + (size_t)b * H + h);
-        const float4 a = q[0], c = q[1];
-        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-        v[4] += c.x; v[5] += c.y; v[6] += c.z; v[7] += c.w;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= f;
-      auto add = [&](float d, int64_t row) {
-        float w[8];
-        head8(rest.head, rest.w, rest.scales, row * H + h, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(d, w[i], v[i]);
-      };
-      if (own < rest.first) add(rest.lost[b] * ws2, own);
-      for (int r = 0; r < rest.rows; ++r) add(rest.d[b * 8 + r] * ws2, rest.first + r);
-      put(t, h, v);
+    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+#pragma unroll 8
+    for (int s = 0; s < planes; ++s) {
+      const float4* q = reinterpret_cast<const float4*>(sums + s * plane + (size_t)b * H + h);
+      const float4 a = q[0], c = q[1];
+      v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+      v[4] += c.x; v[5] += c.y; v[6] += c.z; v[7] += c.w;
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= f;
+    auto add = [&](float d, int64_t row) {
+      float w[8];
+      head8(rest.head, rest.w, rest.scales, row * H + h, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(d, w[i], v[i]);
+    };
+    if (own < rest.first) add(rest.lost[b] * ws2, own);
+    for (int r = 0; r < rest.rows; ++r) add(rest.d[b * 8 + r] * ws2, rest.first + r);
+    put(t, v);
   }
   if (ignored) {
     const float zero[8] = {};
-    for (int h = threadIdx.x * 8; h < H; h += 2048) put(b, h, zero);
+    put(b, zero);
   }
 }
 
@@ -726,6 +725,7 @@ __global__ __launch_bounds__(256) void ce_tail_kernel(const uint16_t* __restrict
   __shared__ float s_l[8];
   const int t = (int)blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float sum[2] = {0.0f, 0.0f};
+#pragma unroll 4
   for (int h = lane * 8; h < H; h += 512) {
     const u32x4 q = *reinterpret_cast<const u32x4*>(X + (size_t)t * H + h);
 #pragma unroll
@@ -764,12 +764,11 @@ __global__ __launch_bounds__(256) void ce_tail_kernel(const uint16_t* __restrict
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
 
 // ------------------------------------------------------------------ plan
-constexpr int64_t kCeFullTiles = 192;   // tiles below which smaller ones are taken
 constexpr int64_t kCeSplitStages = 16;  // stages of the sum over I from which few tiles are split
 constexpr int64_t kCePieceBytes = int64_t(256) << 20;        // a piece's logit gradients, and a 4-bit head's bf16 rows
 
 struct CePlan {
-  int bt;                   // token extent of the tiles
+  int bt, bx;               // token extent of the logits' tiles and of dX's
   bool compact;             // rows without a target are left out
   int splits;               // of the logits' sums over I, through fp32 planes (1: none)
   int64_t piece;            // rows of W per piece (a multiple of 256)
@@ -780,13 +779,43 @@ struct CePlan {
 
 inline int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
+// Token extent of the logits' tiles: the least time in rounds of the CUs, where a
+// round of 256 x 128 and 256 x 64 tiles takes 0.58 and 0.36 of one of 256 x 256
+// tiles, and a last round from three quarters of a whole one on, as it is filled.
+// us of the forward with 64-, 128- and 256-token tiles, bf16: 1024 tokens of
+// 16384 x 4096 166, 136, 122; 1024 of 8192 x 4096 87, 73, 95; 250 of 72471 x 4960
+// 402, 314, 349; 420 of 36320 x 544 45, 45, 52; 174 of 7717 x 736 15, 19, 29.
+int ce_tokens(int64_t T, int64_t vt) {
+  auto cost = [&](int bt, double round) {
+    const int64_t tiles = vt * (up(T, bt) / bt), last = tiles % kCUs;
+    return round * (double)(tiles / kCUs) + (last ? round * (0.75 + 0.25 * (double)last / kCUs) : 0.0);
+  };
+  const double c64 = cost(64, 0.36), c128 = cost(128, 0.58), c256 = cost(256, 1.0);
+  if (c64 < c128 && c64 < c256) return 64;
+  return c128 < c256 ? 128 : 256;
+}
+
+// Token extent of dX's tiles: their products' time, with the idle CUs and what
+// smaller tiles were measured to cost, and that of the fp32 planes, which double
+// with the extent (bf16, us of the gradient with 64-, 128- and 256-token tiles: 256
+// tokens of 50000 x 2048 133, 127, 142; 501 of 72471 x 4960 1437, 943, 877; 174 of
+// 7717 x 736 31, 34, 37; 3947 of 2830 x 960 86, 83, 91).
+int ce_dx_tokens(int64_t T, int64_t rows, int64_t cols) {
+  auto cost = [&](int bx, double product) {
+    const int64_t tiles = up(T, bx) / bx * cols, by_cu = kCUs / tiles, by_stages = (rows + kBK - 1) / kBK / 4;
+    const int64_t splits = by_cu < by_stages ? by_cu : by_stages, groups = tiles * (splits > 1 ? splits : 1);
+    const double us = product * 2e-9 / 1.3 * (double)up(groups, kCUs) / (double)groups * (double)(tiles * bx) * 256 * (double)rows;
+    return us + 2 * 1024 / 5e6 * (double)(groups * bx);
+  };
+  const double c64 = cost(64, 2.0), c128 = cost(128, 1.18), c256 = cost(256, 1.0);
+  if (c64 < c128 && c64 < c256) return 64;
+  return c128 < c256 ? 128 : 256;
+}
+
 CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
   CePlan p{};
-  // The largest tiles that give most CUs one, down to 64 tokens (174 tokens of
-  // 7717 x 736 bf16, loss and gradient: 256-token tiles 115 us, 64-token ones 53).
   const int64_t vt = (V + 255) / 256;
-  p.bt = T <= 64 ? 64 : T <= 128 ? 128 : 256;
-  while (p.bt > 64 && vt * (up(T, p.bt) / p.bt) < kCeFullTiles) p.bt /= 2;
+  p.bt = ce_tokens(T, vt);
   p.compact = T > 256;
   int64_t most = up(V, 256);
   if (bwd) most = kCePieceBytes / (2 * T);
@@ -828,9 +857,11 @@ CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
     p.part = take((size_t)vt * T * 8);
   } else {
     p.d = take((size_t)T * p.ld * 2);
-    // planes of whole tiles: splits x tiles <= max(CUs, tiles), or one tile row's
-    const int64_t dx_tiles = up(T, p.bt) / p.bt * (up(H, 256) / 256);
-    p.sums = take((size_t)(dx_tiles > kCUs ? dx_tiles : kCUs) * p.bt * 256 * 4);
+    const int64_t dx_cols = up(H, 256) / 256;
+    p.bx = ce_dx_tokens(T, p.piece < V ? p.piece : V, dx_cols);
+    // planes of whole tiles: splits x tiles <= max(CUs, tiles)
+    const int64_t dx_tiles = up(T, p.bx) / p.bx * dx_cols;
+    p.sums = take((size_t)(dx_tiles > kCUs ? dx_tiles : kCUs) * p.bx * 256 * 4);
   }
   p.total = at;
   return p;
@@ -1033,7 +1064,7 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   if (gemm_dx_grouped(head, p.width, H, p.groups, e, 0, s) != 0) return -1;
   const CeRest rest{codes, scales, lost, dtail, p.main, p.tail, head};
   auto finish = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(256), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, y, y_bytes,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)((H + 1023) / 1024)), dim3(128), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, y, y_bytes,
                        T, V, H, 0, 0, 0, 1.0f, ws2, rest, dX);
     return ok();
   };
@@ -1112,8 +1143,8 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
   g.d = reinterpret_cast<uint16_t*>(ws + p.d);
   g.sums = reinterpret_cast<float*>(ws + p.sums);
   g.split_stages = (int)(((p.piece < V ? p.piece : V) + kBK - 1) / kBK);
-  const int64_t tt = (T + p.bt - 1) / p.bt, tn = (H + 255) / 256;
-  const int64_t dx_blocks = tt * tn > kCUs ? tt * tn : kCUs;
+  const int64_t tt = (T + p.bt - 1) / p.bt, tn = (H + 255) / 256, dx_tiles = (T + p.bx - 1) / p.bx * tn;
+  const int64_t dx_blocks = dx_tiles > kCUs ? dx_tiles : kCUs;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece, tiles = (n + 255) / 256 * tt;
     if (ce_weight(head, W, scales, v0, n, H, ws + p.wbuf, &g.w, s) != 0) return -1;
@@ -1127,12 +1158,12 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     } else if (ce_go<kCeGrad>(g, p.bt, tiles, s) != 0) {
       return -1;
     }
-    if (ce_go<kCeDx>(g, p.bt, dx_blocks, s) != 0) return -1;
+    if (ce_go<kCeDx>(g, p.bx, dx_blocks, s) != 0) return -1;
   }
   const CeRest rest{W, scales, g.tlogit, nullptr, V, 0, head};
   auto finish = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)T), dim3(256), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, y, y_bytes, T, V,
-                       H, p.bt, (int)tn, g.split_stages, ws2, ws2, rest, dX);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)((H + 1023) / 1024)), dim3(128), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, y, y_bytes, T, V,
+                       H, p.bx, (int)tn, g.split_stages, ws2, ws2, rest, dX);
     return ok();
   };
   return dx_bf16 ? finish(ce_dx_kernel<true>) : finish(ce_dx_kernel<false>);
