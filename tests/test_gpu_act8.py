@@ -217,3 +217,33 @@ def test_dscale_of_many_outputs_equals_the_bf16_product(sq, fmt, act, T, O, I):
     workspace = torch.full((sq.sq_bwd_dscale_act8_workspace(sq.FORMATS[fmt], T, O, I),), 255, dtype=torch.uint8, device="cuda")
     sq.sq_bwd_dscale_act8(fmt, act, q, s, dY, codes, dS=dS, workspace=workspace)
     assert torch.equal(dS, sq.sq_bwd_dscale(fmt, sq.sq_act_unpack(act, q, s), dY, codes))
+
+
+# more experts than one pass over the queues holds, experts without rows between them, tiles of several per expert
+@pytest.mark.parametrize("E,O,I,T,most", [(8192, 8, 32, 500, 2), (1500, 40, 96, 300, 5), (700, 264, 288, 90, 1), (40, 520, 800, 700, 150)])
+@pytest.mark.parametrize("fmt,act", [("mx", "e4m3"), ("nv", "int8")])
+def test_dscale_batched_of_many_experts(sq, E, O, I, T, most, fmt, act):
+    g = inputs.rng(E)
+    counts = g.integers(0, most + 1, E)
+    counts[g.random(E) < 0.3] = 0
+    offsets, rows = _expert_rows(E + 1, E, counts, T)
+    q, s, _ = _layer(E + 2, T, O, I, act)
+    dY = inputs.bf16_normal(E + 3, (int(offsets[-1]), O)).cuda()
+    codes = inputs.device_codes_uniform(E + 4, E * O, I).view(E, O, I // 2)
+    rows_d, offsets_d = torch.from_numpy(rows).cuda(), torch.from_numpy(offsets).cuda()
+    dS = torch.full((E, O, I // BLOCK[fmt]), float("nan"), device="cuda")
+    sq.sq_bwd_dscale_act8_batched(fmt, act, q, s, rows_d, offsets_d, dY, codes, dS=dS)
+    again = sq.sq_bwd_dscale_act8_batched(fmt, act, q, s, rows_d, offsets_d, dY, codes)
+    assert torch.equal(dS, again)
+    x = sq.sq_act_unpack(act, q, s)[rows_d.long()]
+    filled = np.flatnonzero(counts)
+    cut = [slice(offsets[e], offsets[e + 1]) for e in filled]
+    want = torch.zeros_like(dS)
+    want[torch.from_numpy(filled).cuda()] = torch.stack(
+        sq.sq_bwd_dscale_grouped(fmt, [x[c].contiguous() for c in cut], [dY[c] for c in cut], [codes[e] for e in filled]))
+    # the two sum the same exact products in fp32, each within gamma of the sum of their sizes
+    mag = torch.zeros_like(dS)
+    mag[torch.from_numpy(filled).cuda()] = torch.stack(
+        sq.sq_bwd_dscale_grouped(fmt, [x[c].abs().contiguous() for c in cut], [dY[c].abs() for c in cut],
+                                 [(codes[e] & 0x77).contiguous() for e in filled]))
+    assert ((dS - want).abs() <= 2 * (most + BLOCK[fmt] + 10) * 2.0 ** -23 * mag).all()

@@ -193,3 +193,16 @@ def test_same_results_on_another_stream(sq):
         got = [sq.sq_moe_combine(Ys, slot, offsets, w)] + list(sq.sq_moe_combine_bwd(d, Ys, slot, offsets, w))
     s.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+# ids that begin inside an aligned group of four, the longest sort of one launch, and lengths around a wave's step
+@pytest.mark.parametrize("T,K,E", [(65536, 1, 300), (8191, 8, 64), (4097, 1, 5), (1023, 3, 17), (255, 1, 2), (1, 3, 4)])
+@pytest.mark.parametrize("skip", [1, 2, 3])
+@pytest.mark.parametrize("dtype", [np.int64, np.int32])
+def test_sort_of_unaligned_ids(sq, T, K, E, skip, dtype):
+    ids = _ids(T + skip, T, K, E, 0.1, dtype)
+    base = torch.full((T * K + skip,), -1, dtype=torch.from_numpy(ids).dtype, device="cuda")
+    base[skip:] = torch.from_numpy(ids).cuda().reshape(-1)
+    got = sq.sq_moe_sort(base[skip:].view(T, K), E)
+    for a, b in zip(got, step.moe_sort(ids, E)):
+        assert np.array_equal(a.cpu().numpy(), b)
