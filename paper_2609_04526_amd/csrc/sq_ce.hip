@@ -30,6 +30,7 @@ namespace sq {
 
 namespace {
 
+constexpr float kLog2E = 1.44269504f;
 constexpr int kCeGroup = 4;             // tile rows per group of the tile order
 
 __device__ __forceinline__ int64_t target_at(const void* y, int bytes, int64_t t) {
@@ -150,16 +151,25 @@ enum CeMode { kCeStats = 0, kCeGrad = 1, kCeDx = 2, kCeLogits = 3 };
 
 // The tile product of them all, 256 x BN (logits: W's rows by tokens, so that
 // a lane holds one token's logits and sums them without its neighbours) or BM x
-// 256 (dX: tokens by columns of W).  64-deep stages copied global -> LDS, the
-// operands of a 16-deep slice read while the slice before it multiplies, and
-// the barrier that publishes the next stage before the last slice's products:
-// the schedule of the layer's own products (sq_gemm.hip).
+// 256 (dX: tokens by columns of W).  64-deep stages copied global -> LDS, four
+// 16-deep slices each.  The chip's power bounds it: what counts is that the matrix
+// cores, at whatever clock is left, do not wait.  With a slice's reads and copies
+// in a row and the barrier between two slices the products of 4096 tokens with
+// 131072 x 4096 bf16 took 3.50 (statistics), 3.66 (gradients) and 3.45 ms (dX);
+// in this order 3.27, 3.47 and 3.21.  4 waves of 128 x 128 instead of 8 (a third
+// fewer LDS reads) took 3.44 ms and, in dX, 3.26: one wave per SIMD cannot overlap
+// its exponentials.  Stages of 32 with up to 5 in LDS were 8% slower.
+template <int... N, typename F>
+__device__ __forceinline__ void for_each(std::integer_sequence<int, N...>, F f) {
+  (f(std::integral_constant<int, N>{}), ...);
+}
+
 template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES>
 __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   constexpr int NT = 64 * WGM * WGN;
   constexpr int WM = BM / WGM, WN = BN / WGN;
   constexpr int TM = WM / 32, TN = WN / 32;
-  constexpr int kA = BM * kBK * 2, kB = BN * kBK * 2, kStage = kA + kB;
+  constexpr int kA = BM * kBK * 2, kB = BN * kBK * 2, kStage = kA + kB, kSlices = kBK / 16;
   constexpr bool kDxMode = MODE == kCeDx;
   using DA = DmaKC<BM, NT>;
   using DB = std::conditional_t<kDxMode, DmaNat<BN, NT, kBK>, DmaRows<BN, NT>>;
@@ -203,6 +213,37 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     dB.init(g.H, live, g.H, n0, tid, g.rows);
   }
 
+  // What the epilogue needs of this lane's tokens, a chain of loads that would hold
+  // it up: whether they have a target (bit j of `has`), where in the lane's registers
+  // it is, if there, and their loss's gradient and lse.
+  const int vrow = m0 + wm0 + 4 * (lane >> 5);               // first row of W of this lane's registers
+  uint32_t has = 0;
+  int own[TN];
+  float c_of[TN], z_of[TN];
+  if constexpr (MODE == kCeStats || MODE == kCeGrad) {
+    int t[TN];
+    int64_t y[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int row = n0 + wn0 + j * 32 + (lane & 31);
+      t[j] = row < live ? g.rows ? g.rows[row] : row : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j) y[j] = t[j] >= 0 ? target_at(g.y, g.y_bytes, t[j]) : -1;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const bool valid = y[j] >= 0 && y[j] < g.V;
+      // the target's row counted from this lane's first, if this lane holds it
+      const int64_t off = y[j] - g.v0 - vrow;
+      own[j] = valid && off >= 0 && off < WM && (off & 4) == 0 ? (int)off : -1;
+      has |= (uint32_t)valid << j;
+      if constexpr (MODE == kCeGrad) {
+        c_of[j] = valid ? g.dloss[t[j]] : 0.0f;
+        z_of[j] = valid ? g.lse[t[j]] * kLog2E : 0.0f;
+      }
+    }
+  }
+
   f32x16 acc[TM][TN];
   float* sums = nullptr;
   if constexpr (kDxMode) {
@@ -229,69 +270,106 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   }
 
   auto stage_at = [&](auto S) { return (SQ_LDS uint8_t*)lds + decltype(S)::value * kStage; };
-  // halves of the copy of stage kt into buffer S
-  auto dma_half = [&](auto S, int kt, auto HALF) {
-    constexpr int h = decltype(HALF)::value;
-    SQ_LDS uint16_t* a = (SQ_LDS uint16_t*)stage_at(S);
-    SQ_LDS uint16_t* b = (SQ_LDS uint16_t*)(stage_at(S) + kA);
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+
+  // copy N of half HALF of stage kt into buffer S; what lies past the matrix reads
+  // as zeros, so the copies need no condition on kt
+  auto dma = [&](auto S, int kt, auto HALF, auto N) {
+    constexpr int h = decltype(HALF)::value, n = decltype(N)::value;
+    constexpr int a0 = h ? DA::kInst / 2 : 0, an = h ? DA::kInst - a0 : DA::kInst / 2, b0 = h ? DB::kInst / 2 : 0;
     const int ka = (s_first + kt) * kBK;
-    dA.template issue_part<h * DA::kInst / 2, (h + 1) * DA::kInst / 2>(ra, a, ka, false, wave_u);
-    if constexpr (kDxMode)
-      dB.template issue_part<h * DB::kInst / 2, (h + 1) * DB::kInst / 2>(rb, b, (uint32_t)(kt * kBK) * (uint32_t)g.H * 2u, wave_u);
-    else
-      dB.template issue_part<h * DB::kInst / 2, (h + 1) * DB::kInst / 2>(rb, b, ka, wave_u);
+    if constexpr (n < an) {
+      dA.template issue_part<a0 + n, a0 + n + 1>(ra, (SQ_LDS uint16_t*)stage_at(S), ka, false, wave_u);
+    } else {
+      SQ_LDS uint16_t* b = (SQ_LDS uint16_t*)(stage_at(S) + kA);
+      constexpr int q = b0 + n - an;
+      if constexpr (kDxMode)
+        dB.template issue_part<q, q + 1>(rb, b, (uint32_t)(kt * kBK) * (uint32_t)g.H * 2u, wave_u);
+      else
+        dB.template issue_part<q, q + 1>(rb, b, ka, wave_u);
+    }
+  };
+  constexpr int kHalf[2] = {DA::kInst / 2 + DB::kInst / 2, kDma - DA::kInst / 2 - DB::kInst / 2};
+  auto dma_half = [&](auto S, int kt, auto HALF) {
+    for_each(std::make_integer_sequence<int, kHalf[decltype(HALF)::value]>{}, [&](auto N) { dma(S, kt, HALF, N); });
   };
 
+  // A slice's operands, and its products and reads in the order in which each needs
+  // the fewest before it: a0 b0 b1 .. a1 .., products row by row.
   struct Frag {
     bf16x8 a[TM];
     bf16x8 b[TN];
   };
   Frag F0, F1;
-  auto read = [&](auto S, auto KK, Frag& f) {
-    constexpr int kk = decltype(KK)::value;
-    const SQ_LDS uint16_t* a = (const SQ_LDS uint16_t*)stage_at(S);
-    const SQ_LDS uint16_t* b = (const SQ_LDS uint16_t*)(stage_at(S) + kA);
+  constexpr int kReads = TM + TN, kProducts = TM * TN, kMid = kProducts / 2, kRest = kProducts - kMid;
+  auto read = [&](auto S, auto KK, Frag& f, auto N) {
+    constexpr int n = decltype(N)::value, kk = decltype(KK)::value;
     const int chunk = 2 * kk + (lane >> 5);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) f.a[i] = *(const SQ_LDS bf16x8*)(a + kc_off(wm0 + i * 32 + (lane & 31), chunk));
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
+    if constexpr (n == 0 || n > TN) {
+      constexpr int i = n == 0 ? 0 : n - TN;
+      f.a[i] = *(const SQ_LDS bf16x8*)((const SQ_LDS uint16_t*)stage_at(S) + kc_off(wm0 + i * 32 + (lane & 31), chunk));
+    } else {
+      constexpr int j = n - 1;
+      const SQ_LDS uint16_t* b = (const SQ_LDS uint16_t*)(stage_at(S) + kA);
       if constexpr (kDxMode) f.b[j] = nat_frag<BN>(b, kk, wn0 + j * 32, lane);
       else f.b[j] = *(const SQ_LDS bf16x8*)(b + kc_off(wn0 + j * 32 + (lane & 31), chunk));
     }
   };
-  auto mma = [&](Frag& f) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+  auto product = [&](Frag& f, auto N) {
+    constexpr int i = decltype(N)::value / TN, j = decltype(N)::value % TN;
+    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
   };
-  using I0 = std::integral_constant<int, 0>;
-  using I1 = std::integral_constant<int, 1>;
-  using I2 = std::integral_constant<int, 2>;
-  using I3 = std::integral_constant<int, 3>;
+  // f of those of 0 .. ALL - 1 that fall to part N of PARTS
+  auto share = [&](auto N, auto PARTS, auto ALL, auto f) {
+    constexpr int parts = decltype(PARTS)::value, all = decltype(ALL)::value;
+    constexpr int n = decltype(N)::value < parts ? decltype(N)::value : parts, m = n < parts ? n + 1 : parts;
+    constexpr int lo = n * all / parts, hi = m * all / parts;
+    for_each(std::make_integer_sequence<int, hi - lo>{}, [&](auto K) { f(std::integral_constant<int, lo + decltype(K)::value>{}); });
+  };
+  using Products = std::make_integer_sequence<int, kProducts>;
+  using Reads = std::integral_constant<int, kReads>;
 
+  // One stage.  Between a slice's products go the reads of the next slice and the
+  // copies of the stage STAGES - 1 ahead, one at a time, so that neither holds the
+  // matrix cores up; the barrier that publishes stage kt + 1 and frees this one
+  // stands amid the last slice, whose other half covers its reads and copies.
   auto step = [&](auto S, int kt) {
     constexpr int s = decltype(S)::value;
     using SN = std::integral_constant<int, (s + 1) % STAGES>;            // stage kt + 1
     using SP = std::integral_constant<int, (s + STAGES - 1) % STAGES>;   // stage kt + STAGES - 1
-    read(S, I1{}, F1);
-    if (kt + STAGES - 1 < nk) dma_half(SP{}, kt + STAGES - 1, I1{});
-    mma(F0);
-    read(S, I2{}, F0);
-    mma(F1);
-    read(S, I3{}, F1);
-    mma(F0);
-    // stage kt + 1 has landed once only the copies of the stages after it are
-    // outstanding; in the last stages everything is waited for
-    if (kt + STAGES - 1 < nk) wait_vm_lgkm0<kAhead>();
-    else wait_vm_lgkm0<0>();
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    if (kt + 1 < nk) read(SN{}, I0{}, F0);
-    if (kt + STAGES < nk) dma_half(S, kt + STAGES, I0{});
-    mma(F1);
+    for_each(std::make_integer_sequence<int, kSlices - 1>{}, [&](auto KK) {
+      constexpr int kk = decltype(KK)::value;
+      Frag& now = kk & 1 ? F1 : F0;
+      Frag& next = kk & 1 ? F0 : F1;
+      for_each(Products{}, [&](auto N) {
+        product(now, N);
+        share(N, std::integral_constant<int, (kReads < kProducts ? kReads : kProducts)>{}, Reads{},
+              [&](auto R) { read(S, std::integral_constant<int, kk + 1>{}, next, R); });
+        if constexpr (kk == 0)
+          share(N, std::integral_constant<int, kProducts>{}, std::integral_constant<int, kHalf[1]>{},
+                [&](auto C) { dma(SP{}, kt + STAGES - 1, I1{}, C); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+    for_each(Products{}, [&](auto N) {
+      constexpr int n = decltype(N)::value;
+      if constexpr (n == kMid) {
+        // stage kt + 1 has landed once only the copies of the stages after it are
+        // outstanding
+        wait_vm_lgkm0<kAhead>();
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      product(F1, N);
+      if constexpr (n >= kMid) {
+        using At = std::integral_constant<int, n - kMid>;
+        using Rest = std::integral_constant<int, kRest>;
+        share(At{}, Rest{}, Reads{}, [&](auto R) { read(SN{}, I0{}, F0, R); });
+        share(At{}, Rest{}, std::integral_constant<int, kHalf[0]>{}, [&](auto C) { dma(S, kt + STAGES, I0{}, C); });
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
   };
   // prologue: stage 0 whole and its first operands, then stages 1 .. STAGES - 2
   // and the first half of stage STAGES - 1
@@ -301,22 +379,18 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     wait_vm_lgkm0<0>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    read(I0{}, I0{}, F0);
+    for_each(std::make_integer_sequence<int, kReads>{}, [&](auto R) { read(I0{}, I0{}, F0, R); });
     if constexpr (STAGES > 2) {
-      if (1 < nk) {
-        dma_half(I1{}, 1, I0{});
-        dma_half(I1{}, 1, I1{});
-      }
+      dma_half(I1{}, 1, I0{});
+      dma_half(I1{}, 1, I1{});
     }
-    if (STAGES - 1 < nk) dma_half(std::integral_constant<int, STAGES - 1>{}, STAGES - 1, I0{});
+    dma_half(std::integral_constant<int, STAGES - 1>{}, STAGES - 1, I0{});
   }
-  for (int kt0 = 0; kt0 < nk; kt0 += STAGES) {
-    step(I0{}, kt0);
-    if (kt0 + 1 < nk) step(I1{}, kt0 + 1);
-    if constexpr (STAGES > 2) {
-      if (kt0 + 2 < nk) step(I2{}, kt0 + 2);
-    }
-  }
+  for (int kt0 = 0; kt0 < nk; kt0 += STAGES)
+    for_each(std::make_integer_sequence<int, STAGES>{}, [&](auto S) {
+      constexpr int s = decltype(S)::value;
+      if (s == 0 || kt0 + s < nk) step(S, kt0 + s);
+    });
   wait_vm_lgkm0<0>();
 
   // ---------------------------------------------------------------- epilogue
@@ -355,45 +429,47 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     }
   } else {
     __syncthreads();                     // the operand tiles are done with
-    const int vrow = m0 + wm0 + 4 * (lane >> 5);             // first row of W of this lane's registers
     const int end = g.Vn - vrow;                              // rows of W from it on
     const bool whole = m0 + BM <= g.Vn;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const int row = n0 + wn0 + j * 32 + (lane & 31);       // compact token row
-      const bool in = row < live;
-      const int t = in ? (g.rows ? g.rows[row] : row) : 0;
-      const int64_t y = in ? target_at(g.y, g.y_bytes, t) : -1;
-      const bool valid = y >= 0 && y < g.V;
-      // the target's row counted from this lane's first, or one that no register holds
-      const int64_t off = y - g.v0 - vrow;
-      const int at = valid && off >= 0 && off < WM ? (int)off : -1;
+      const bool valid = (has >> j) & 1;
+      const int at = own[j];
       // most waves hold whole tiles and no token's target: their registers need
       // no comparison
       const bool plain = whole && __ballot(at >= 0) == 0;
       if constexpr (MODE == kCeStats) {
-        float top = -INFINITY, sum = 0.0f;
+        // 4 running maxima and sums, so that none waits for the one before it
+        float top, sum;
         auto stats = [&](auto PLAIN) {
           constexpr bool kPlain = decltype(PLAIN)::value;
+          float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, sums[4] = {0.0f, 0.0f, 0.0f, 0.0f}, l = 0.0f;
 #pragma unroll
           for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
               const int v = i * 32 + 8 * (r >> 2) + (r & 3);
-              if (!kPlain && v == at) g.tlogit[row] = acc[i][j][r] * g.ws2;
-              if (!kPlain && v >= end) acc[i][j][r] = -INFINITY;
-              top = fmaxf(top, acc[i][j][r]);
+              if (!kPlain) l = v == at ? acc[i][j][r] : l;
+              tops[r & 3] = kPlain || v < end ? fmaxf(tops[r & 3], acc[i][j][r]) : tops[r & 3];
             }
+          if (!kPlain && at >= 0) g.tlogit[row] = l * g.ws2;
+          top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+          top = fmaxf(top, __shfl_xor(top, 32)) * g.ws2;
+          const float ref = top == -INFINITY ? 0.0f : top * kLog2E;   // nothing to sum: exp(-inf) = 0
+          const float scale = g.ws2 * kLog2E;
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], scale, -ref));
+              sums[r & 3] += kPlain || i * 32 + 8 * (r >> 2) + (r & 3) < end ? p : 0.0f;
+            }
+          sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+          sum += __shfl_xor(sum, 32);
         };
         if (plain) stats(std::true_type{});
         else stats(std::false_type{});
-        top = fmaxf(top, __shfl_xor(top, 32)) * g.ws2;
-        const float ref = top == -INFINITY ? 0.0f : top;     // nothing to sum: exp(-inf) = 0
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sum += __expf(__builtin_fmaf(acc[i][j][r], g.ws2, -ref));
-        sum += __shfl_xor(sum, 32);
         SQ_LDS float* s = (SQ_LDS float*)lds + 2 * ((wave / WGN) * BN + wn0 + j * 32 + (lane & 31));
         if (lane < 32) {
           s[0] = top;
@@ -405,11 +481,12 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
         // rounding's error into dX: what it lost is kept, and added with the
         // target's row of W at the end (error against 64 bits 2.5e-3 -> 1.8e-3, of
         // which 1.7e-3 is dX's own rounding to bf16).
-        const float c = valid ? g.dloss[t] : 0.0f, z = valid ? g.lse[t] : 0.0f;
+        const float c = c_of[j], z = z_of[j], scale = g.ws2 * kLog2E;
         SQ_LDS uint16_t* s = (SQ_LDS uint16_t*)lds + wave * WM * WN;
         const int cj = j * 32 + (lane & 31);
         auto grads = [&](auto PLAIN) {
           constexpr bool kPlain = decltype(PLAIN)::value;
+          float lost = 0.0f;
 #pragma unroll
           for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -418,7 +495,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const int v = i * 32 + 8 * q + r;
-                const float p = __expf(__builtin_fmaf(acc[i][j][4 * q + r], g.ws2, -z));
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + r], scale, -z));
                 e[r] = kPlain ? c * p : valid && v < end ? c * (p - (v == at ? 1.0f : 0.0f)) : 0.0f;
               }
               u32x2 pair;
@@ -426,17 +503,17 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
               pair[1] = bits_of(__builtin_convertvector((f32x2{e[2], e[3]}), bf16x2));
               if constexpr (!kPlain) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                  if (i * 32 + 8 * q + r == at) g.tlogit[row] = e[r] - bf16_half(pair[r >> 1], r & 1);
+                for (int r = 0; r < 4; ++r) lost = i * 32 + 8 * q + r == at ? e[r] - bf16_half(pair[r >> 1], r & 1) : lost;
               }
               // 16-byte unit u of token cj at unit u ^ cj
               const int u = i * 4 + q;
               *(SQ_LDS u32x2*)(s + cj * WM + ((u ^ cj) & (WM / 8 - 1)) * 8 + 4 * (lane >> 5)) = pair;
             }
+          if (!kPlain && at >= 0) g.tlogit[row] = lost;
         };
         // (an ignored token among the rows, as in a batch that is not compact,
         // takes the way with comparisons, which gives it zeros)
-        if (plain && __ballot(in && !valid) == 0) grads(std::true_type{});
+        if (plain && __ballot(row < live && !valid) == 0) grads(std::true_type{});
         else grads(std::false_type{});
       }
     }
