@@ -854,6 +854,15 @@ def sq_byte_diff(a, b, counts=None):
     return counts
 
 
+def _out(t, name, shape, dtype, device, dtypes=None):
+    """The caller's buffer, checked, or a new one (of one of dtypes, where the caller names its dtype)."""
+    if t is not None:
+        return _need(t, name, dtypes or dtype, shape)
+    if dtypes is not None and dtype not in dtypes:
+        raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {dtype}")
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _scratch(workspace, need, device):
     """The caller's workspace, or a fresh one of `need` bytes."""
     if workspace is None:
@@ -884,18 +893,13 @@ def sq_moe_sort(ids, n_experts, offsets=None, token=None, slot=None, workspace=N
     """(offsets int32 [E+1], token int32 [T*K], slot int32 [T, K]) of the pairs of ids [T, K] by expert."""
     T, K = _dims2(ids, "ids")
     _need(ids, "ids", _IDS)
-    if offsets is None:
-        offsets = torch.empty(n_experts + 1, dtype=_I32, device=ids.device)
-    if token is None:
-        token = torch.empty(T * K, dtype=_I32, device=ids.device)
-    if slot is None:
-        slot = torch.empty((T, K), dtype=_I32, device=ids.device)
-    _need(offsets, "offsets", _I32, (n_experts + 1,))
-    _need(token, "token", _I32, (T * K,))
-    _need(slot, "slot", _I32, (T, K))
-    workspace = _scratch(workspace, int(load().sq_moe_sort_workspace(T, K, n_experts)), ids.device)
+    device, lib = ids.device, load()
+    offsets = _out(offsets, "offsets", (n_experts + 1,), _I32, device)
+    token = _out(token, "token", (T * K,), _I32, device)
+    slot = _out(slot, "slot", (T, K), _I32, device)
+    workspace = _scratch(workspace, lib.sq_moe_sort_workspace(T, K, n_experts), device)
     _dev(ids, offsets, token, slot, workspace)
-    _check("sq_moe_sort", load().sq_moe_sort(T, K, n_experts, _ptr(ids), ids.element_size(), _ptr(offsets), _ptr(token),
+    _check("sq_moe_sort", lib.sq_moe_sort(T, K, n_experts, _ptr(ids), ids.element_size(), _ptr(offsets), _ptr(token),
                                              _ptr(slot), _ptr(workspace), 0 if workspace is None else workspace.numel(),
                                              _stream()))
     return offsets, token, slot
@@ -910,9 +914,7 @@ def sq_moe_gather(X, slot, offsets, Xs=None):
     T, K, E = _slots(slot, offsets)
     H = _dims2(X, "X")[1]
     _need(X, "X", _OUT, (T, H))
-    if Xs is None:
-        Xs = torch.empty((T * K, H), dtype=X.dtype, device=X.device)
-    _need(Xs, "Xs", X.dtype, (T * K, H))
+    Xs = _out(Xs, "Xs", (T * K, H), X.dtype, X.device)
     _dev(X, slot, offsets, Xs)
     _check("sq_moe_gather", load().sq_moe_gather(T, K, E, H, _ptr(X), _dtype_of(X), _ptr(slot), _ptr(offsets), _ptr(Xs),
                                                  _stream()))
@@ -926,9 +928,7 @@ def sq_moe_combine(Ys, slot, offsets, weights=None, out_dtype=torch.float32, out
     _need(Ys, "Ys", _OUT, (T * K, H))
     if weights is not None:
         _need(weights, "weights", _F32, (T, K))
-    if out is None:
-        out = torch.empty((T, H), dtype=out_dtype, device=Ys.device)
-    _need(out, "out", _OUT, (T, H))
+    out = _out(out, "out", (T, H), out_dtype, Ys.device, _OUT)
     _dev(Ys, slot, offsets, weights, out)
     _check("sq_moe_combine", load().sq_moe_combine(T, K, E, H, _ptr(Ys), _dtype_of(Ys), _ptr(slot), _ptr(offsets),
                                                    _ptr(weights), _ptr(out), _dtype_of(out), _stream()))
@@ -942,12 +942,8 @@ def sq_moe_combine_bwd(dOut, Ys, slot, offsets, weights, out_dtype=None, dYs=Non
     _need(Ys, "Ys", _OUT, (T * K, H))
     _need(dOut, "dOut", _OUT, (T, H))
     _need(weights, "weights", _F32, (T, K))
-    if dYs is None:
-        dYs = torch.empty((T * K, H), dtype=Ys.dtype if out_dtype is None else out_dtype, device=Ys.device)
-    if dweights is None:
-        dweights = torch.empty((T, K), dtype=_F32, device=Ys.device)
-    _need(dYs, "dYs", _OUT, (T * K, H))
-    _need(dweights, "dweights", _F32, (T, K))
+    dYs = _out(dYs, "dYs", (T * K, H), Ys.dtype if out_dtype is None else out_dtype, Ys.device, _OUT)
+    dweights = _out(dweights, "dweights", (T, K), _F32, Ys.device)
     _dev(dOut, Ys, slot, offsets, weights, dYs, dweights)
     _check("sq_moe_combine_bwd", load().sq_moe_combine_bwd(T, K, E, H, _ptr(dOut), _dtype_of(dOut), _ptr(Ys),
                                                            _dtype_of(Ys), _ptr(slot), _ptr(offsets), _ptr(weights),
@@ -974,12 +970,10 @@ def sq_act_pack(act, X, codes=None, scales=None):
     act = ACTS.get(act, act)
     T, I = _dims2(X, "X")
     _need(X, "X", _BF16)
-    if codes is None:
-        codes = torch.empty((T, I), dtype=_U8, device=X.device)
-    if scales is None:
-        scales = torch.empty((T, I // ACT_BLOCK), dtype=_U8, device=X.device)
-    if _kept(codes, scales) != (T, I):
-        raise ValueError(f"codes has shape {tuple(codes.shape)}, expected {(T, I)}")
+    if I % ACT_BLOCK:
+        raise ValueError(f"the width {I} is not a multiple of the block {ACT_BLOCK}")
+    codes = _out(codes, "codes", (T, I), _U8, X.device)
+    scales = _out(scales, "scales", (T, I // ACT_BLOCK), _U8, X.device)
     _dev(X, codes, scales)
     _check("sq_act_pack", load().sq_act_pack(act, T, I, _ptr(X), _ptr(codes), _ptr(scales), _stream()))
     return codes, scales
@@ -989,9 +983,7 @@ def sq_act_unpack(act, codes, scales, X=None):
     """The kept values as bf16 [T, I]."""
     act = ACTS.get(act, act)
     T, I = _kept(codes, scales)
-    if X is None:
-        X = torch.empty((T, I), dtype=_BF16, device=codes.device)
-    _need(X, "X", _BF16, (T, I))
+    X = _out(X, "X", (T, I), _BF16, codes.device)
     _dev(codes, scales, X)
     _check("sq_act_unpack", load().sq_act_unpack(act, T, I, _ptr(codes), _ptr(scales), _ptr(X), _stream()))
     return X
@@ -1008,10 +1000,8 @@ def sq_bwd_dscale_act8(fmt, act, x_codes, x_scales, dY, codes, dS=None, workspac
     O = _dims2(dY, "dY")[1]
     _need(dY, "dY", _BF16, (T, O))
     G = _layer(fmt, O, I, codes)
-    if dS is None:
-        dS = torch.empty((O, G), dtype=_F32, device=dY.device)
-    _need(dS, "dS", _F32, (O, G))
-    workspace = _scratch(workspace, int(load().sq_bwd_dscale_act8_workspace(fmt, T, O, I)), dY.device)
+    dS = _out(dS, "dS", (O, G), _F32, dY.device)
+    workspace = _scratch(workspace, load().sq_bwd_dscale_act8_workspace(fmt, T, O, I), dY.device)
     _dev(x_codes, x_scales, dY, codes, dS, workspace)
     _check("sq_bwd_dscale_act8", load().sq_bwd_dscale_act8(
         fmt, act, T, O, I, _ptr(x_codes), _ptr(x_scales), _ptr(dY), _ptr(codes), _ptr(dS), _ptr(workspace),
@@ -1038,10 +1028,8 @@ def sq_bwd_dscale_act8_batched(fmt, act, x_codes, x_scales, rows, offsets, dY, c
     _need(offsets, "offsets", _I32, (E + 1,))
     if rows is not None:
         _need(rows, "rows", _I32, (N,))
-    if dS is None:
-        dS = torch.empty((E, O, G), dtype=_F32, device=dY.device)
-    _need(dS, "dS", _F32, (E, O, G))
-    workspace = _scratch(workspace, int(load().sq_bwd_dscale_act8_batched_workspace(E, T, I)), dY.device)
+    dS = _out(dS, "dS", (E, O, G), _F32, dY.device)
+    workspace = _scratch(workspace, load().sq_bwd_dscale_act8_batched_workspace(E, T, I), dY.device)
     _dev(x_codes, x_scales, rows, offsets, dY, codes, dS, workspace)
     _check("sq_bwd_dscale_act8_batched", load().sq_bwd_dscale_act8_batched(
         fmt, act, E, T, N, O, I, _ptr(x_codes), _ptr(x_scales), _ptr(rows), _ptr(offsets), _ptr(dY), _ptr(codes),
@@ -1078,13 +1066,9 @@ def sq_ce_fwd(head, X, W, targets, scales=None, ws2=1.0, loss=None, lse=None, wo
     uint8 [V, I/2], with scales and ws2); targets outside 0 .. V-1 are ignored."""
     head = HEADS.get(head, head)
     T, V, I = _head(head, X, W, targets, scales)
-    if loss is None:
-        loss = torch.empty(T, dtype=_F32, device=X.device)
-    if lse is None:
-        lse = torch.empty(T, dtype=_F32, device=X.device)
-    _need(loss, "loss", _F32, (T,))
-    _need(lse, "lse", _F32, (T,))
-    workspace = _scratch(workspace, int(load().sq_ce_fwd_workspace(head, T, V, I)), X.device)
+    loss = _out(loss, "loss", (T,), _F32, X.device)
+    lse = _out(lse, "lse", (T,), _F32, X.device)
+    workspace = _scratch(workspace, load().sq_ce_fwd_workspace(head, T, V, I), X.device)
     _dev(X, W, targets, scales, loss, lse, workspace)
     _check("sq_ce_fwd", load().sq_ce_fwd(head, T, V, I, _ptr(X), _ptr(W), _ptr(scales), float(ws2), _ptr(targets),
                                          targets.element_size(), _ptr(loss), _ptr(lse), _ptr(workspace),
@@ -1098,10 +1082,8 @@ def sq_ce_bwd(head, X, W, targets, lse, dloss, scales=None, ws2=1.0, out_dtype=t
     T, V, I = _head(head, X, W, targets, scales)
     _need(lse, "lse", _F32, (T,))
     _need(dloss, "dloss", _F32, (T,))
-    if dX is None:
-        dX = torch.empty((T, I), dtype=out_dtype, device=X.device)
-    _need(dX, "dX", _OUT, (T, I))
-    workspace = _scratch(workspace, int(load().sq_ce_bwd_workspace(head, T, V, I)), X.device)
+    dX = _out(dX, "dX", (T, I), out_dtype, X.device, _OUT)
+    workspace = _scratch(workspace, load().sq_ce_bwd_workspace(head, T, V, I), X.device)
     _dev(X, W, targets, scales, lse, dloss, dX, workspace)
     _check("sq_ce_bwd", load().sq_ce_bwd(head, T, V, I, _ptr(X), _ptr(W), _ptr(scales), float(ws2), _ptr(targets),
                                          targets.element_size(), _ptr(lse), _ptr(dloss), _ptr(dX), _dtype_of(dX),

@@ -129,7 +129,8 @@ def test_dscale_act8_refusals(lib, kw, status):
 
 
 def test_dscale_act8_workspace(lib):
-    assert lib.sq_bwd_dscale_act8_workspace(0, 4096, 4096, 4096) == 0
+    assert lib.sq_bwd_dscale_act8_workspace(0, 1024, 4096, 4096) == 0
+    assert lib.sq_bwd_dscale_act8_workspace(0, 4096, 4096, 4096) == 4096 * 4096 * 2 + lib.sq_bwd_dscale_workspace(0, 4096, 4096, 4096)
     assert lib.sq_bwd_dscale_act8_workspace(0, 4096, 1024, 4096) == lib.sq_bwd_dscale_workspace(0, 4096, 1024, 4096) > 0
     assert lib.sq_bwd_dscale_act8_workspace(1, 4096, 1024, 4112) == 0          # not whole blocks of 32
 
