@@ -588,7 +588,8 @@ size_t sq_bwd_dscale_act8_batched_workspace(int64_t E, int64_t T, int64_t I);
 
 /*
  * Softmax cross entropy of a language-model head over its whole vocabulary and
- * the gradient of the head's input; the logits are never kept.  The head is
+ * the gradient of the head's input; no logits pass from one call to the other,
+ * and the logits of large products never reach memory.  The head is
  * frozen (it has no gradient of its own): W bf16 [V, I] (SQ_HEAD_BF16), or codes
  * uint8 [V, I/2] with scales uint8 [V, G] and ws2 as the layer stores them
  * (SQ_HEAD_MXFP4, SQ_HEAD_NVFP4; scales and ws2 are ignored for SQ_HEAD_BF16).
@@ -616,8 +617,9 @@ size_t sq_bwd_dscale_act8_batched_workspace(int64_t E, int64_t T, int64_t I);
  * sq_ce_fwd_workspace / sq_ce_bwd_workspace bytes (0 when T = 0), contents
  * irrelevant: the row statistics (8 bytes per token and 256 entries of the
  * vocabulary), or one piece's logit gradients (about 256 MiB at most; one of 256
- * entries at least) and fp32 sums; and for a 4-bit head one piece of it as bf16 (256
- * MiB at most).  Deterministic.
+ * entries at least) and fp32 sums; for a 4-bit head one piece of it as bf16 (1 GiB
+ * at most); for products too small to fill the GPU, and a 4-bit head of up to 256
+ * tokens, fp32 logits (1 GiB at most).  Deterministic.
  */
 size_t sq_ce_fwd_workspace(int head, int64_t T, int64_t V, int64_t I);
 size_t sq_ce_bwd_workspace(int head, int64_t T, int64_t V, int64_t I);

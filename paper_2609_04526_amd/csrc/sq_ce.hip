@@ -1,5 +1,5 @@
 // Softmax cross entropy of a language-model head over its whole vocabulary and
-// the gradient of the head's input, without the logits in memory.
+// the gradient of the head's input; large products' logits never reach memory.
 //
 //   l[t,v]  = X[t] . W[v]                       W bf16, or codes x scales
 //   lse[t]  = log sum_v exp l[t,v]              loss[t] = lse[t] - l[t,y_t]
@@ -13,9 +13,18 @@
 // piece is written out as bf16 before it is used (code x scale is exact in
 // bf16; NVFP4's ws2 goes to the fp32 sums).
 //
+// Few tiles, whose sums are split, and a 4-bit head of few tokens, read by the
+// layer's own products, pass fp32 logits through the workspace instead.
+//
 // Rows without a target in the vocabulary cost nothing beyond 256 tokens: the
 // rows that have one are numbered first, and tiles past the last of them end at
 // once.  The number stays on the device.
+//
+// The three products bound it (the forward's logits, the same again, dX), and the
+// matrix cores' power bounds them: 4096 tokens of 131072 x 4096 bf16 10.2 ms, 1.29
+// PFLOP/s; 1999 tokens, 40% of them ignored, of 50001 x 4096 MXFP4 1.5 ms, of which
+// 0.17 write the head out.  One token of 131072 x 4096 bf16 takes 530 us, three
+// reads of the head at 6.1 TB/s, of MXFP4 243.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
