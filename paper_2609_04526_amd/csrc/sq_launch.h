@@ -164,6 +164,7 @@ int byte_diff_launch(int64_t n, const uint8_t* a, const uint8_t* b, uint64_t* co
 // number of routed pairs (the sort's offsets[E]).
 constexpr int kMoeChunk = 4096;           // pairs per workgroup of the sort over many pairs
 constexpr int kMoeWaveTokens = 2048;      // tokens from which the combine's gradients take a wave per token
+constexpr int64_t kMoeStreamBytes = int64_t(64) << 20;   // rows of a combine from which they are read past the caches
 // One launch sorts up to this many pairs.
 constexpr bool moe_sort_one(int64_t N) { return N <= 65536; }
 int moe_sort_launch(int64_t T, int K, int E, const void* ids, int id_bytes, int32_t* offsets, int32_t* token,

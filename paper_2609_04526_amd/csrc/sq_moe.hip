@@ -43,7 +43,7 @@ __device__ __forceinline__ void keys4(const ID* ids, int p, int end, int E, int 
   if (p + 4 <= end) {
     const Four f = *reinterpret_cast<const Four*>(ids + p);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) k[j] = f.v[j] >= 0 && f.v[j] < (ID)E ? (int)f.v[j] : E;
+    for (int j = 0; j < 4; ++j) k[j] = (int)min((std::make_unsigned_t<ID>)f.v[j], (std::make_unsigned_t<ID>)E);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) k[j] = key_of(ids, p + j, end, E);
@@ -73,13 +73,15 @@ __global__ __launch_bounds__(1024) void moe_sort_kernel(const ID* __restrict__ i
     int k[4][4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) keys4(ids, p0 + 256 * (st + u) + 4 * lane, p1, E, k[u]);
+    uint32_t bits = 0;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         lt += k[u][j] < e;
-        mine |= (uint64_t)(k[u][j] == e) << (4 * (st + u) + j);
+        bits |= k[u][j] == e ? 1u << (4 * u + j) : 0u;
       }
+    mine |= (uint64_t)bits << (4 * st);
   }
   int eq = __popcll(mine);
 #pragma unroll
@@ -244,10 +246,11 @@ __global__ __launch_bounds__(256) void moe_number_kernel(const ID* __restrict__ 
 template <bool BF16>
 struct Raw8 {
   u32x4m w[BF16 ? 1 : 2];
+  template <bool STREAM = false>
   __device__ __forceinline__ void load(const void* base, int64_t at) {
     const u32x4m* q = reinterpret_cast<const u32x4m*>(static_cast<const uint8_t*>(base) + at * (BF16 ? 2 : 4));
 #pragma unroll
-    for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = q[i];
+    for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = STREAM ? __builtin_nontemporal_load(q + i) : q[i];
   }
   __device__ __forceinline__ float at(int i) const {
     if constexpr (BF16) return __uint_as_float(i & 1 ? w[0][i >> 1] & 0xFFFF0000u : w[0][i >> 1] << 16);
@@ -295,8 +298,10 @@ constexpr int kPairs = 8;
 
 // Workgroup t: out[t] = sum over k of w[t,k] Ys[slot[t,k]] in k order, fp32,
 // over the routed pairs.  Bound by memory: 8 rows of 2048 bf16 each to 16384 tokens
-// 119 us (5.1 TB/s), 143 with the rows' last writes still on their way to memory.
-template <bool YB, bool OB, bool WEIGHTED>
+// 106 us (5.7 TB/s), weighted 113.  STREAM: rows that do not fit the caches, read
+// past them, do not wait for what was written last to leave (120 and 143 us there
+// without; 333 tokens, 2 rows of 4104 fp32, which fit: 4.9 us, with it 6.0).
+template <bool YB, bool OB, bool WEIGHTED, bool STREAM>
 __global__ __launch_bounds__(256) void moe_combine_kernel(const void* __restrict__ Ys, const int* __restrict__ slot,
                                                           const int* __restrict__ routed,
                                                           const float* __restrict__ weights, int K, int H, int64_t N,
@@ -318,7 +323,7 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const void* __restrict
         if (k0 + k >= K) continue;
         at[k] = (uint32_t)slot[t * K + k0 + k];
         if (WEIGHTED) w[k] = weights[t * K + k0 + k];
-        v[k].load(Ys, (int64_t)(at[k] < R ? at[k] : 0u) * H + c);
+        v[k].template load<STREAM>(Ys, (int64_t)(at[k] < R ? at[k] : 0u) * H + c);
       }
 #pragma unroll
       for (int k = 0; k < kPairs; ++k) {
@@ -464,9 +469,13 @@ int moe_gather_launch(int64_t T, int K, int H, int bf16, const void* X, const in
 int moe_combine_launch(int64_t T, int K, int H, const void* Ys, int y_bf16, const int32_t* slot, const int32_t* routed,
                        const float* weights, void* out, int out_bf16, hipStream_t s) {
   const dim3 grid((unsigned)T), block(row_threads(H / 8));
+  const bool stream = T * K * H * (y_bf16 ? 2 : 4) >= kMoeStreamBytes;
   auto go = [&](auto YB, auto OB, auto W) {
-    hipLaunchKernelGGL((moe_combine_kernel<decltype(YB)::value, decltype(OB)::value, decltype(W)::value>), grid, block, 0,
-                       s, Ys, slot, routed, weights, K, H, T * K, out);
+    constexpr bool y = decltype(YB)::value, o = decltype(OB)::value, w = decltype(W)::value;
+    if (stream)
+      hipLaunchKernelGGL((moe_combine_kernel<y, o, w, true>), grid, block, 0, s, Ys, slot, routed, weights, K, H, T * K, out);
+    else
+      hipLaunchKernelGGL((moe_combine_kernel<y, o, w, false>), grid, block, 0, s, Ys, slot, routed, weights, K, H, T * K, out);
     return ok();
   };
   using Y = std::true_type;

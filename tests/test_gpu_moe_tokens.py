@@ -206,3 +206,25 @@ def test_sort_of_unaligned_ids(sq, T, K, E, skip, dtype):
     got = sq.sq_moe_sort(base[skip:].view(T, K), E)
     for a, b in zip(got, step.moe_sort(ids, E)):
         assert np.array_equal(a.cpu().numpy(), b)
+
+
+# rows beyond what the caches hold are read past them
+@pytest.mark.parametrize("weighted", [True, False])
+@pytest.mark.parametrize("y_dtype,out_dtype", [(BF16, BF16), (F32, F32)])
+def test_combine_of_many_bytes(sq, weighted, y_dtype, out_dtype):
+    T, K, E, H = 5003, 4, 37, 2056
+    offsets, _, slot = sq.sq_moe_sort(torch.from_numpy(_ids(5, T, K, E, 0.2)).cuda(), E)
+    Ys = torch.randn((T * K, H), generator=torch.Generator("cuda").manual_seed(6), device="cuda").to(y_dtype)
+    w = torch.rand((T, K), generator=torch.Generator("cuda").manual_seed(7), device="cuda") - 0.5 if weighted else None
+    out = torch.full((T, H), float("nan"), dtype=out_dtype, device="cuda")
+    sq.sq_moe_combine(Ys, slot, offsets, w, out=out)
+    live = (slot < offsets[-1]).double()
+    f = live * w.double() if weighted else live
+    ref, mag = torch.zeros((2, T, H), dtype=torch.float64, device="cuda")
+    for k in range(K):
+        rows = Ys[slot[:, k].long()].double() * f[:, k, None]
+        ref += rows
+        mag += rows.abs()
+    # K fused steps in fp32, and the rounding of the result
+    bound = K * 2.0 ** -24 * 1.01 * mag + (2.0 ** -8 if out_dtype == BF16 else 0.0) * (ref.abs() + K * 2.0 ** -23 * mag)
+    assert ((out.double() - ref).abs() <= bound).all()
