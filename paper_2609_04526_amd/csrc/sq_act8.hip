@@ -27,8 +27,8 @@ enum Act { kInt8 = 0, kE4M3 = 1 };
 
 // ------------------------------------------------------------------ pack
 // One lane takes 8 columns (16 bytes of bf16), four lanes a block.  Streams
-// 3.03 bytes per value: 8192 x 14336 in 79 us (4.5 TB/s), and back in 53 (6.6 TB/s,
-// mostly writes that the cache takes).
+// 3.03 bytes per value: 8192 x 14336 to E4M3 in 58 us (6.1 TB/s), and back in 53
+// (6.6 TB/s, mostly writes that the cache takes).
 template <int ACT>
 __device__ __forceinline__ void pack8(const u32x4& w, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                       int64_t at) {
@@ -74,7 +74,11 @@ __device__ __forceinline__ void pack8(const u32x4& w, uint8_t* __restrict__ code
 
 constexpr int kActSteps = 4;                                  // 8-column pieces per lane, all loaded first
 
-template <int ACT>
+// STREAM: an X that the caches do not hold is read past them (58 us there, 78
+// without); one that they do is read from them (12106 x 2432 and back: 29, 31).
+constexpr int64_t kActStreamBytes = int64_t(128) << 20;
+
+template <int ACT, bool STREAM>
 __global__ __launch_bounds__(256) void act_pack_kernel(const u32x4* __restrict__ X, int64_t pieces,
                                                        uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
   const int64_t p0 = (int64_t)blockIdx.x * (256 * kActSteps) + threadIdx.x;
@@ -82,7 +86,8 @@ __global__ __launch_bounds__(256) void act_pack_kernel(const u32x4* __restrict__
 #pragma unroll
   for (int i = 0; i < kActSteps; ++i) {
     const int64_t p = p0 + i * 256;
-    w[i] = X[p < pieces ? p : pieces - 1];
+    const u32x4* x = X + (p < pieces ? p : pieces - 1);
+    w[i] = STREAM ? __builtin_nontemporal_load(x) : *x;
   }
 #pragma unroll
   for (int i = 0; i < kActSteps; ++i)                         // whole blocks: pieces is a multiple of 4
@@ -869,10 +874,10 @@ bool ds8_unpacks(int T, int O, int I) {
 int act_pack_launch(int act, int64_t T, int64_t I, const void* X, uint8_t* codes, uint8_t* scales, hipStream_t s) {
   const int64_t pieces = T * I / 8, blocks = (pieces + 256 * kActSteps - 1) / (256 * kActSteps);
   const u32x4* x = static_cast<const u32x4*>(X);
-  if (act == kInt8)
-    hipLaunchKernelGGL((act_pack_kernel<kInt8>), dim3((unsigned)blocks), dim3(256), 0, s, x, pieces, codes, scales);
-  else
-    hipLaunchKernelGGL((act_pack_kernel<kE4M3>), dim3((unsigned)blocks), dim3(256), 0, s, x, pieces, codes, scales);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, x, pieces, codes, scales); };
+  const bool stream = T * I * 2 >= kActStreamBytes;
+  if (act == kInt8) stream ? go(act_pack_kernel<kInt8, true>) : go(act_pack_kernel<kInt8, false>);
+  else stream ? go(act_pack_kernel<kE4M3, true>) : go(act_pack_kernel<kE4M3, false>);
   return ok();
 }
 

@@ -247,3 +247,14 @@ def test_dscale_batched_of_many_experts(sq, E, O, I, T, most, fmt, act):
         sq.sq_bwd_dscale_grouped(fmt, [x[c].abs().contiguous() for c in cut], [dY[c].abs() for c in cut],
                                  [(codes[e] & 0x77).contiguous() for e in filled]))
     assert ((dS - want).abs() <= 2 * (most + BLOCK[fmt] + 10) * 2.0 ** -23 * mag).all()
+
+
+@pytest.mark.parametrize("act", ["int8", "e4m3"])
+def test_pack_of_many_bytes_equals_its_parts(sq, act):
+    """An X beyond the caches, read past them, against the same rows in calls that fit."""
+    X = inputs.device_bf16_normal(11, (9001, 8224))
+    X[::97, 5] = float("inf")
+    q, s = sq.sq_act_pack(act, X)
+    for a in range(0, 9001, 1000):
+        qa, sa = sq.sq_act_pack(act, X[a:a + 1000].contiguous())
+        assert torch.equal(q[a:a + 1000], qa) and torch.equal(s[a:a + 1000], sa)
