@@ -614,33 +614,33 @@ struct CeRest {
   const float* d;           // [T, 8] logit gradients of the rows from `first` on
   int64_t first;
   int rows;
-  int head;
 };
 
 // 8 values of a head from element i (a multiple of 8) of its rows on.
-__device__ __forceinline__ void head8(int head, const void* w, const uint8_t* scales, int64_t i, float (&v)[8]) {
-  if (head == kCeBf16) {
+template <int HEAD>
+__device__ __forceinline__ void head8(const void* w, const uint8_t* scales, int64_t i, float (&v)[8]) {
+  if constexpr (HEAD == kCeBf16) {
     const u32x4 q = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(w) + i);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = bf16_half(q[k >> 1], k & 1);
-    return;
-  }
-  const uint32_t q = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(w) + (i >> 1));
-  const uint32_t b = scales[i / (head == kMX ? 32 : 16)];
-  const float s = head == kMX ? e8m0_to_f32(b) : e4m3_to_f32(b);
-  const f32x2 c[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
-                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3)};
+  } else {
+    const uint32_t q = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(w) + (i >> 1));
+    const uint32_t b = scales[i / (HEAD == kMX ? 32 : 16)];
+    const float s = HEAD == kMX ? e8m0_to_f32(b) : e4m3_to_f32(b);
+    const f32x2 c[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3)};
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    v[2 * k] = c[k].x * s;
-    v[2 * k + 1] = c[k].y * s;
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = c[k].x * s;
+      v[2 * k + 1] = c[k].y * s;
+    }
   }
 }
 
 // 1024 columns of one token's dX per workgroup: the planes added in order, times f (and the
 // rest's rows times ws2); zeros where there is no target (their rows come after
 // the live ones).  planes = 0: as many as the product split the vocabulary into.
-template <bool BF16>
+template <bool BF16, int HEAD>
 __global__ __launch_bounds__(128) void ce_dx_kernel(const float* __restrict__ sums, int planes, int64_t plane_rows,
                                                     const int* __restrict__ rows, const int* __restrict__ count,
                                                     const void* __restrict__ y, int y_bytes, int T, int64_t V, int H,
@@ -686,7 +686,7 @@ __global__ __launch_bounds__(128) void ce_dx_kernel(const float* __restrict__ su
     for (int i = 0; i < 8; ++i) v[i] *= f;
     auto add = [&](float d, int64_t row) {
       float w[8];
-      head8(rest.head, rest.w, rest.scales, row * H + h, w);
+      head8<HEAD>(rest.w, rest.scales, row * H + h, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = __builtin_fmaf(d, w[i], v[i]);
     };
@@ -707,9 +707,10 @@ __global__ __launch_bounds__(128) void ce_dx_kernel(const float* __restrict__ su
 // I are split into planes.  Either way a piece of fp32 logits passes through the
 // workspace, and these kernels do the rest.
 //
-// A piece's n logits of a token lie in groups of `width` columns, each group a
-// [T, its width] matrix of its own (width a multiple of 256), or in one matrix of
-// row length `width` >= n; in `planes` planes, `plane` values apart, that add up.
+// A piece's n logits of a token lie in groups of `width` columns, each group a [T,
+// width] matrix of its own (width a multiple of 256; the last ends where the logits
+// end, so it holds some of the one before it again), or in one matrix of row length
+// `width` >= n; in `planes` planes, `plane` values apart, that add up.
 struct CePiece {
   const float* logits;
   int n, width, planes;
@@ -723,15 +724,78 @@ struct CePiece {
   int64_t V;
   __device__ __forceinline__ int live() const { return count ? min(*count, T) : T; }
   __device__ __forceinline__ int token(int row) const { return rows ? rows[row] : row; }
-  // where row `row`'s logit of column c < n is, its neighbours of the group beside it
+  // where row `row`'s logit of column c < n is, those of the next columns beside it
+  // as far as c's group goes
   __device__ __forceinline__ int64_t at(int row, int c) const {
-    const int first = c / width * width, own = width < n ? min(width, n - first) : width;
-    return (int64_t)first * T + (int64_t)row * own + (c - first);
+    const int first = c / width * width, early = first > 0 && first + width > n ? first + width - n : 0;
+    return (int64_t)first * T + (int64_t)row * width + (c - first + early);
   }
 };
 
-// (max, sum) of 256 logits of one token per wave, and the target's logit.
-__global__ __launch_bounds__(256) void ce_part_kernel(CePiece p, float2* __restrict__ part, float* __restrict__ tlogit) {
+// The rows of a 4-bit head past a multiple of 8, fewer than 8, which the layer's
+// products do not take: workgroups of their own in the two kernels below, each
+// with one token (launches of their own cost 115 tokens of 16301 x 3648 24 us of 152).
+struct CeTail {
+  const uint16_t* x;        // X [T, H]
+  const uint8_t* codes;     // from the first such row on
+  const uint8_t* scales;
+  int rows, H;              // 0: none
+  float ws2;
+  int64_t v0;
+  float2* part;             // forward
+  float* d;                 // backward: fp32 gradients [T, 8]
+};
+
+// Token t's logits of these rows, 2 per wave, to s_l; rows that are not there -inf.
+template <int HEAD>
+__device__ __forceinline__ void tail_logits(const CeTail& g, int t, float* s_l) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float sum[2] = {0.0f, 0.0f};
+#pragma unroll 4
+  for (int h = lane * 8; h < g.H; h += 512) {
+    const u32x4 q = *reinterpret_cast<const u32x4*>(g.x + (size_t)t * g.H + h);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int r = min(2 * wave + k, g.rows - 1);            // a row past the last is not used
+      float w[8];
+      head8<HEAD>(g.codes, g.scales, (int64_t)r * g.H + h, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[k] = __builtin_fmaf(bf16_half(q[i >> 1], i & 1), w[i], sum[k]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+#pragma unroll
+    for (int s = 32; s; s >>= 1) sum[k] += __shfl_xor(sum[k], s);
+    if (lane == 0) s_l[2 * wave + k] = 2 * wave + k < g.rows ? sum[k] * g.ws2 : -INFINITY;
+  }
+  __syncthreads();
+}
+
+// (max, sum) of 256 logits of one token per wave, and the target's logit; past the
+// n logits, a workgroup per token for the tail (HEAD a 4-bit format).
+template <int HEAD>
+__global__ __launch_bounds__(256) void ce_part_kernel(CePiece p, float2* __restrict__ part, float* __restrict__ tlogit,
+                                                      CeTail tail) {
+  const int extra = (int)blockIdx.x - (p.n + 255) / 256;
+  if (HEAD != kCeBf16 && extra >= 0) {
+    __shared__ float s_l[8];
+    const int t = (int)blockIdx.y * 4 + extra;
+    if (t >= p.T) return;
+    tail_logits<HEAD>(tail, t, s_l);
+    if (threadIdx.x == 0) {
+      const int64_t at = target_at(p.y, p.y_bytes, t) - tail.v0;
+      float top = -INFINITY, total = 0.0f;
+      for (int r = 0; r < tail.rows; ++r) {
+        top = fmaxf(top, s_l[r]);
+        if (at == r) tlogit[t] = s_l[r];
+      }
+      const float ref = top == -INFINITY ? 0.0f : top;
+      for (int r = 0; r < tail.rows; ++r) total += __expf(s_l[r] - ref);
+      tail.part[t] = make_float2(top, total);
+    }
+    return;
+  }
   const int lane = threadIdx.x & 63, row = (int)blockIdx.y * 4 + (threadIdx.x >> 6);
   if (row >= p.live()) return;
   const int c0 = (int)blockIdx.x * 256 + lane * 4;
@@ -764,9 +828,20 @@ __global__ __launch_bounds__(256) void ce_part_kernel(CePiece p, float2* __restr
 // last group ends where the logits end, so it begins `shift` columns inside the
 // one before it, and those columns are zeros in it; without groups (d_width =
 // d_cols, shift 0) columns from n on are zeros.  All sizes are multiples of 8 but n.
+// Past the columns, a workgroup per token for the tail (HEAD a 4-bit format).
+template <int HEAD>
 __global__ __launch_bounds__(256) void ce_grad_kernel(CePiece p, const float* __restrict__ lse,
                                                       const float* __restrict__ dloss, int d_cols, int d_width, int shift,
-                                                      uint16_t* __restrict__ d, float* __restrict__ lost) {
+                                                      uint16_t* __restrict__ d, float* __restrict__ lost, CeTail tail) {
+  if (HEAD != kCeBf16 && (int)blockIdx.x * 2048 >= d_cols) {
+    __shared__ float s_l[8];
+    const int t = (int)blockIdx.y, r = (int)threadIdx.x;
+    tail_logits<HEAD>(tail, t, s_l);
+    const int64_t y = target_at(p.y, p.y_bytes, t);
+    if (r < tail.rows)
+      tail.d[t * 8 + r] = y >= 0 && y < p.V ? dloss[t] * (__expf(s_l[r] - lse[t]) - (y - tail.v0 == r ? 1.0f : 0.0f)) : 0.0f;
+    return;
+  }
   const int row = (int)blockIdx.y, k = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8;
   if (row >= p.live() || k >= d_cols) return;
   const int first = k / d_width * d_width, early = first + d_width >= d_cols ? shift : 0;
@@ -796,55 +871,6 @@ __global__ __launch_bounds__(256) void ce_grad_kernel(CePiece p, const float* __
     if (any && at >= 0 && at >> 1 == i) lost[row] = at & 1 ? e.y - bf16_half(w[i], 1) : e.x - bf16_half(w[i], 0);
   }
   *reinterpret_cast<u32x4*>(d + (size_t)first * p.T + (size_t)row * d_width + (k - first)) = w;
-}
-
-// The rows of a 4-bit head past a multiple of 8, fewer than 8: a workgroup takes
-// one token's logits of them, a wave two rows; their part and the target's logit
-// (GRAD false), or their gradients in fp32.
-template <bool GRAD>
-__global__ __launch_bounds__(256) void ce_tail_kernel(const uint16_t* __restrict__ X, const uint8_t* __restrict__ codes,
-                                                      const uint8_t* __restrict__ scales, int fmt, int rows, int H,
-                                                      float ws2, int64_t v0, int64_t V, const void* __restrict__ y,
-                                                      int y_bytes, const float* __restrict__ lse,
-                                                      const float* __restrict__ dloss, float2* __restrict__ part,
-                                                      float* __restrict__ tlogit, float* __restrict__ d) {
-  __shared__ float s_l[8];
-  const int t = (int)blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float sum[2] = {0.0f, 0.0f};
-#pragma unroll 4
-  for (int h = lane * 8; h < H; h += 512) {
-    const u32x4 q = *reinterpret_cast<const u32x4*>(X + (size_t)t * H + h);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int r = min(2 * wave + k, rows - 1);              // a row past the last is not used
-      float w[8];
-      head8(fmt, codes, scales, (int64_t)r * H + h, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum[k] = __builtin_fmaf(bf16_half(q[i >> 1], i & 1), w[i], sum[k]);
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-#pragma unroll
-    for (int s = 32; s; s >>= 1) sum[k] += __shfl_xor(sum[k], s);
-    if (lane == 0) s_l[2 * wave + k] = 2 * wave + k < rows ? sum[k] * ws2 : -INFINITY;
-  }
-  __syncthreads();
-  const int64_t target = target_at(y, y_bytes, t), at = target - v0;
-  if constexpr (GRAD) {
-    const bool valid = target >= 0 && target < V;
-    const int r = (int)threadIdx.x;
-    if (r < rows) d[t * 8 + r] = valid ? dloss[t] * (__expf(s_l[r] - lse[t]) - (at == r ? 1.0f : 0.0f)) : 0.0f;
-  } else if (threadIdx.x == 0) {
-    float top = -INFINITY, total = 0.0f;
-    for (int r = 0; r < rows; ++r) {
-      top = fmaxf(top, s_l[r]);
-      if (at == r) tlogit[t] = s_l[r];
-    }
-    const float ref = top == -INFINITY ? 0.0f : top;
-    for (int r = 0; r < rows; ++r) total += __expf(s_l[r] - ref);
-    part[t] = make_float2(top, total);
-  }
 }
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
@@ -986,17 +1012,31 @@ int ce_weight(int head, const void* W, const uint8_t* scales, int64_t v0, int64_
   return ok();
 }
 
-int ce_part_go(const CePiece& c, float2* part, float* tlogit, hipStream_t s) {
-  hipLaunchKernelGGL(ce_part_kernel, dim3((unsigned)((c.n + 255) / 256), (unsigned)((c.T + 3) / 4)), dim3(256), 0, s, c, part,
-                     tlogit);
+int ce_part_go(int head, const CePiece& c, float2* part, float* tlogit, const CeTail& tail, hipStream_t s) {
+  const dim3 grid((unsigned)((c.n + 255) / 256 + (tail.rows > 0 ? 4 : 0)), (unsigned)((c.T + 3) / 4));
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, c, part, tlogit, tail); };
+  if (tail.rows == 0) go(ce_part_kernel<kCeBf16>);
+  else head == kMX ? go(ce_part_kernel<kMX>) : go(ce_part_kernel<kNV>);
   return ok();
 }
 
-int ce_grad_go(const CePiece& c, const float* lse, const float* dloss, int d_cols, int d_width, int shift, uint16_t* d,
-               float* lost, hipStream_t s) {
-  hipLaunchKernelGGL(ce_grad_kernel, dim3((unsigned)((d_cols / 8 + 255) / 256), (unsigned)c.T), dim3(256), 0, s, c, lse, dloss,
-                     d_cols, d_width, shift, d, lost);
+int ce_grad_go(int head, const CePiece& c, const float* lse, const float* dloss, int d_cols, int d_width, int shift,
+               uint16_t* d, float* lost, const CeTail& tail, hipStream_t s) {
+  const dim3 grid((unsigned)((d_cols / 8 + 255) / 256 + (tail.rows > 0 ? 1 : 0)), (unsigned)c.T);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, c, lse, dloss, d_cols, d_width, shift, d, lost, tail);
+  };
+  if (tail.rows == 0) go(ce_grad_kernel<kCeBf16>);
+  else head == kMX ? go(ce_grad_kernel<kMX>) : go(ce_grad_kernel<kNV>);
   return ok();
+}
+
+// The last step of the gradient, for each head and output type.
+template <typename F>
+int ce_dx_by(int head, int dx_bf16, F finish) {
+  if (head == kMX) return dx_bf16 ? finish(ce_dx_kernel<true, kMX>) : finish(ce_dx_kernel<false, kMX>);
+  if (head == kNV) return dx_bf16 ? finish(ce_dx_kernel<true, kNV>) : finish(ce_dx_kernel<false, kNV>);
+  return dx_bf16 ? finish(ce_dx_kernel<true, kCeBf16>) : finish(ce_dx_kernel<false, kCeBf16>);
 }
 
 int ce_loss_go(const float2* part, const float* tlogit, const CePiece& c, int tiles, float* loss, float* lse, hipStream_t s) {
@@ -1042,14 +1082,14 @@ CeFew ce_few_plan(bool bwd, int64_t T, int64_t V, int64_t H) {
   if (p.width > p.main) p.width = (int)p.main;
   p.groups = (int)((p.main + p.width - 1) / p.width);
   p.shift = (int)((int64_t)p.groups * p.width - p.main);
-  const int64_t most = p.piece < p.main ? p.piece : p.main;
+  const int64_t most = bwd || p.piece > p.main ? p.main : p.piece;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
     at += (bytes + 255) & ~(size_t)255;
     return o;
   };
-  p.logits = take((size_t)(bwd ? p.main : most) * T * 4);
+  p.logits = take((size_t)(p.group > 0 ? up(most, p.group) : most) * T * 4);
   p.tlogit = take((size_t)T * 4);
   if (!bwd) {
     p.part = take((size_t)((p.main + 255) / 256 + 1) * T * 8);
@@ -1083,17 +1123,21 @@ int ce_few_logits(int head, int T, int64_t v0, int n, int H, const void* X, cons
   c->width = group > 0 && n > group ? group : n;
   if (c->width == n) return gemm_fwd(head, T, n, H, X, cd, sc, ws2, logits, 0, s);
   ExpertProblem e[kGroupMax];
-  const int whole = n / group, last = n - whole * group;
-  for (int k0 = 0; k0 < whole; k0 += kGroupMax) {
-    const int m = whole - k0 < kGroupMax ? whole - k0 : kGroupMax;
+  const int groups = (n + group - 1) / group;
+  for (int k0 = 0; k0 < groups; k0 += kGroupMax) {
+    const int m = groups - k0 < kGroupMax ? groups - k0 : kGroupMax;
     for (int k = 0; k < m; ++k) {
-      const int64_t r = (int64_t)(k0 + k) * group;
-      e[k] = ExpertProblem{X, nullptr, cd + r * H / 2, sc + r * G, logits + r * T, T, ws2};
+      const int64_t at = (int64_t)(k0 + k) * group, r = at + group < n ? at : n - group;
+      e[k] = ExpertProblem{X, nullptr, cd + r * H / 2, sc + r * G, logits + at * T, T, ws2};
     }
     if (gemm_fwd_grouped(head, group, H, m, e, 0, s) != 0) return -1;
   }
-  const int64_t r = (int64_t)whole * group;
-  return last == 0 ? 0 : gemm_fwd(head, T, last, H, X, cd + r * H / 2, sc + r * G, ws2, logits + r * T, 0, s);
+  return 0;
+}
+
+CeTail ce_tail(const CeFew& p, int head, const void* X, const uint8_t* codes, const uint8_t* scales, int H, float ws2) {
+  return CeTail{static_cast<const uint16_t*>(X), codes + p.main * H / 2, scales + p.main * (H / (head == kMX ? 32 : 16)),
+                p.tail, H, ws2, p.main, nullptr, nullptr};
 }
 
 int ce_few_fwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* codes, const uint8_t* scales, float ws2,
@@ -1108,15 +1152,13 @@ int ce_few_fwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   for (int64_t v0 = 0; v0 < p.main; v0 += p.piece) {
     const int n = (int)(p.main - v0 < p.piece ? p.main - v0 : p.piece);
     if (ce_few_logits(head, T, v0, n, H, X, codes, scales, ws2, p.group, logits, &c, s) != 0) return -1;
-    if (ce_part_go(c, part + (size_t)tiles * T, tlogit, s) != 0) return -1;
-    tiles += (n + 255) / 256;
-  }
-  if (p.tail > 0) {
-    hipLaunchKernelGGL(ce_tail_kernel<false>, dim3((unsigned)T), dim3(256), 0, s, static_cast<const uint16_t*>(X),
-                       codes + p.main * H / 2, scales + p.main * (H / (head == kMX ? 32 : 16)), head, p.tail, H, ws2, p.main, V,
-                       y, y_bytes, nullptr, nullptr, part + (size_t)tiles * T, tlogit, nullptr);
-    if (ok() != 0) return -1;
-    ++tiles;
+    const bool last = v0 + n == p.main;
+    const int own = (n + 255) / 256;
+    CeTail tail{};
+    if (last && p.tail > 0) tail = ce_tail(p, head, X, codes, scales, H, ws2);
+    tail.part = part + (size_t)(tiles + own) * T;
+    if (ce_part_go(head, c, part + (size_t)tiles * T, tlogit, tail, s) != 0) return -1;
+    tiles += own + (tail.rows > 0);
   }
   return ce_loss_go(part, tlogit, c, tiles, loss, lse, s);
 }
@@ -1134,13 +1176,10 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   c.y = y; c.y_bytes = y_bytes; c.T = T; c.V = V;
   if (ce_few_logits(head, T, 0, (int)p.main, H, X, codes, scales, ws2, p.group, reinterpret_cast<float*>(ws + p.logits), &c, s) != 0)
     return -1;
-  if (ce_grad_go(c, lse, dloss, p.groups * p.width, p.width, p.shift, d, lost, s) != 0) return -1;
-  if (p.tail > 0) {
-    hipLaunchKernelGGL(ce_tail_kernel<true>, dim3((unsigned)T), dim3(256), 0, s, static_cast<const uint16_t*>(X),
-                       codes + p.main * H / 2, scales + p.main * G, head, p.tail, H, ws2, p.main, V, y, y_bytes, lse, dloss,
-                       nullptr, nullptr, dtail);
-    if (ok() != 0) return -1;
-  }
+  CeTail tail{};
+  if (p.tail > 0) tail = ce_tail(p, head, X, codes, scales, H, ws2);
+  tail.d = dtail;
+  if (ce_grad_go(head, c, lse, dloss, p.groups * p.width, p.width, p.shift, d, lost, tail, s) != 0) return -1;
   // dX of every group of rows, as the layer's grouped product
   ExpertProblem e[64];
   for (int k = 0; k < p.groups; ++k) {
@@ -1148,13 +1187,13 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
     e[k] = ExpertProblem{d + (size_t)k * p.width * T, nullptr, codes + v0 * H / 2, scales + v0 * G, sums + (size_t)k * T * H, T, ws2};
   }
   if (gemm_dx_grouped(head, p.width, H, p.groups, e, 0, s) != 0) return -1;
-  const CeRest rest{codes, scales, lost, dtail, p.main, p.tail, head};
+  const CeRest rest{codes, scales, lost, dtail, p.main, p.tail};
   auto finish = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)((H + 1023) / 1024)), dim3(128), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, y, y_bytes,
                        T, V, H, 0, 0, 0, 1.0f, ws2, rest, dX);
     return ok();
   };
-  return dx_bf16 ? finish(ce_dx_kernel<true>) : finish(ce_dx_kernel<false>);
+  return ce_dx_by(head, dx_bf16, finish);
 }
 
 }  // namespace
@@ -1206,7 +1245,7 @@ int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     g.Vn = (int)n;
     g.part_tile0 = (int)(v0 / 256);
     if (p.splits > 1) {
-      if (ce_go<kCeLogits>(g, p.bt, tiles * p.splits, s) != 0 || ce_part_go(c, part, g.tlogit, s) != 0) return -1;
+      if (ce_go<kCeLogits>(g, p.bt, tiles * p.splits, s) != 0 || ce_part_go(head, c, part, g.tlogit, CeTail{}, s) != 0) return -1;
     } else if (ce_go<kCeStats>(g, p.bt, tiles, s) != 0) {
       return -1;
     }
@@ -1239,20 +1278,20 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     g.add = v0 > 0;
     if (p.splits > 1) {
       if (ce_go<kCeLogits>(g, p.bt, tiles * p.splits, s) != 0 ||
-          ce_grad_go(c, lse, dloss, p.ld, p.ld, 0, g.d, g.tlogit, s) != 0)
+          ce_grad_go(head, c, lse, dloss, p.ld, p.ld, 0, g.d, g.tlogit, CeTail{}, s) != 0)
         return -1;
     } else if (ce_go<kCeGrad>(g, p.bt, tiles, s) != 0) {
       return -1;
     }
     if (ce_go<kCeDx>(g, p.bx, dx_blocks, s) != 0) return -1;
   }
-  const CeRest rest{W, scales, g.tlogit, nullptr, V, 0, head};
+  const CeRest rest{W, scales, g.tlogit, nullptr, V, 0};
   auto finish = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)((H + 1023) / 1024)), dim3(128), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, y, y_bytes, T, V,
                        H, p.bx, (int)tn, g.split_stages, ws2, ws2, rest, dX);
     return ok();
   };
-  return dx_bf16 ? finish(ce_dx_kernel<true>) : finish(ce_dx_kernel<false>);
+  return ce_dx_by(head, dx_bf16, finish);
 }
 
 }  // namespace sq
