@@ -243,3 +243,29 @@ def test_groups_of_a_4_bit_head(sq, head, T, V, I):
     edges = np.array([V - 1, V // 8 * 8 - 1, 0, V // 8 * 8, V // 8 * 8 - 300, -1, V])
     y = np.where(g.random(T) < 0.5, g.choice(edges, T), g.integers(0, V, T))
     _check(sq, head, T, V, I, T + I, y)
+
+
+@pytest.mark.parametrize("T,V,I", [(3, 37, 64), (70, 300, 160), (290, 1001, 96)])
+@pytest.mark.parametrize("head", ["bf16", "mx", "nv"])
+def test_gradient_by_differences(sq, head, T, V, I):
+    """loss(X + U) - loss(X - U) against 2 <dX, U>, X and U on a grid of bf16 that holds X +- U.
+
+    Per token the third derivative along U is a third central moment of the logits' changes, (2 m)^3 at most for changes up to m,
+    so the difference is off by (2 m)^3 / 3; each loss by its own bound, dX by the rounding of the logits' gradients, 2^-8 of
+    sum |p - hot| <= 2 against changes up to m, and its fp32 sums."""
+    W, scales, w = _head(head, T, V, I, 0.2)
+    g = inputs.rng(T + 5)
+    x, u = g.integers(-16, 17, (T, I)) / 8.0, g.integers(-1, 2, (T, I)) / 64.0
+    y = torch.from_numpy(g.integers(0, V, T)).cuda()
+    dev = lambda a: torch.from_numpy(a).to(BF16).cuda()
+    assert torch.equal(dev(x + u).double().cpu(), torch.from_numpy(x + u))
+    up, down = (sq.sq_ce_fwd(head, dev(a), W, y, scales=scales, ws2=WS2)[0].double().cpu().numpy() for a in (x + u, x - u))
+    lse = sq.sq_ce_fwd(head, dev(x), W, y, scales=scales, ws2=WS2)[1]
+    dX = sq.sq_ce_bwd(head, dev(x), W, y, lse, torch.ones(T, device="cuda"), scales=scales, ws2=WS2).double().cpu().numpy()
+    change = np.abs(u @ w.T).max(1)
+    mag = (np.abs(x) + np.abs(u)) @ np.abs(w).T
+    one = 4 * gamma(I + 2) * mag.max(1) + 2 * (mag.max(1) + 64) * 2.0 ** -22
+    sums = 2 * gamma(V + 70) * 2 * (np.abs(u) @ np.abs(w).T).max(1)
+    bound = (2 * change) ** 3 / 3 + 2 * one + 2 * (2.0 ** -8 + 2.0 ** -18) * 2 * change + 2 * sums
+    assert (np.abs((up - down) - 2 * (dX * u).sum(1)) <= bound).all()
+    assert (bound < 0.2 * np.abs(up - down).max()).all()        # the bound says something
