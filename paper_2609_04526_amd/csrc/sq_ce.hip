@@ -98,7 +98,8 @@ __global__ __launch_bounds__(256) void ce_dequant_kernel(const uint8_t* __restri
 // ------------------------------------------------------------------ products
 struct CeArgs {
   const uint16_t* x;        // X [T, H]
-  const uint16_t* w;        // rows [v0, v0 + Vn) of W as bf16, [Vn, H]
+  const uint16_t* w;        // rows [v0, v0 + Vn) of W as bf16, [Vn, H] (with CODES their MXFP4 codes)
+  const uint8_t* scales;    // with CODES: their scales
   uint16_t* d;              // gradients of the logits [T, ld], piece columns
   float* part;              // forward: (max, sum) [tile of all of W][T]
   float* tlogit;            // forward: the target's logit [T]; backward: what rounding took from its gradient
@@ -150,6 +151,25 @@ struct DmaRows {
   }
 };
 
+// The copies of a 4-bit tile of R = NT / 2 rows, two 16-byte chunks each: 64 codes
+// of a row and stage, chunk c of row r at place c ^ (r / 8 & 1) (a wave's reads of 8
+// codes then meet each bank twice at most), or 32 scales of a row.
+template <int NT, bool SCALES>
+struct DmaPairs {
+  static constexpr int kInst = 1;
+  uint32_t off;
+  int chunk;
+  __device__ __forceinline__ void init(int row_bytes, int live, int tid) {
+    const int r = tid >> 1;
+    chunk = SCALES ? tid & 1 : (tid & 1) ^ ((r >> 3) & 1);
+    off = r < live ? (uint32_t)r * (uint32_t)row_bytes + 16u * (uint32_t)chunk : kOOB;
+  }
+  // the 32 bytes of every row from byte `first` on; past the row's end zeros
+  __device__ __forceinline__ void issue(DmaRsrc rs, SQ_LDS uint8_t* s, int first, int row_bytes, int wave) const {
+    dma16(rs, s + wave * 1024, off == kOOB || first + 16 * chunk >= row_bytes ? kOOB : off + (uint32_t)first);
+  }
+};
+
 // Split of the vocabulary rows of dX's contraction over workgroups, where the
 // live rows' tiles leave compute units idle (at least 4 stages each).
 __device__ __forceinline__ int ce_splits(int tiles, int stages) {
@@ -157,6 +177,12 @@ __device__ __forceinline__ int ce_splits(int tiles, int stages) {
 }
 
 enum CeMode { kCeStats = 0, kCeGrad = 1, kCeDx = 2, kCeLogits = 3 };
+
+// f(0), f(1), .. with constants, in this order.
+template <int... N, typename F>
+__device__ __forceinline__ void for_each(std::integer_sequence<int, N...>, F f) {
+  (f(std::integral_constant<int, N>{}), ...);
+}
 
 // The tile product of them all, 256 x BN (logits: W's rows by tokens, so that
 // a lane holds one token's logits and sums them without its neighbours) or BM x
@@ -168,24 +194,23 @@ enum CeMode { kCeStats = 0, kCeGrad = 1, kCeDx = 2, kCeLogits = 3 };
 // in this order 3.27, 3.47 and 3.21.  4 waves of 128 x 128 instead of 8 (a third
 // fewer LDS reads) took 3.44 ms and, in dX, 3.26: one wave per SIMD cannot overlap
 // its exponentials.  Stages of 32 with up to 5 in LDS were 8% slower.
-template <int... N, typename F>
-__device__ __forceinline__ void for_each(std::integer_sequence<int, N...>, F f) {
-  (f(std::integral_constant<int, N>{}), ...);
-}
-
-template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES>
+template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool CODES = false>
 __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   constexpr int NT = 64 * WGM * WGN;
   constexpr int WM = BM / WGM, WN = BN / WGN;
   constexpr int TM = WM / 32, TN = WN / 32;
-  constexpr int kA = BM * kBK * 2, kB = BN * kBK * 2, kStage = kA + kB, kSlices = kBK / 16;
+  constexpr int kA = CODES ? BM * kBK / 2 : BM * kBK * 2, kB = BN * kBK * 2, kStage = kA + kB, kSlices = kBK / 16;
   constexpr bool kDxMode = MODE == kCeDx;
-  using DA = DmaKC<BM, NT>;
+  constexpr int kGroup = 16;                                  // stages of a row's 32 scales
+  using DA = std::conditional_t<CODES, DmaPairs<NT, false>, DmaKC<BM, NT>>;
   using DB = std::conditional_t<kDxMode, DmaNat<BN, NT, kBK>, DmaRows<BN, NT>>;
   constexpr int kDma = DA::kInst + DB::kInst;
-  constexpr int kAhead = (STAGES - 2) * kDma;
+  // with CODES a stage is published a step before it is multiplied: its codes become
+  // operands in the vector units meanwhile
+  constexpr int kAhead = (STAGES - (CODES ? 3 : 2)) * kDma;
+  static_assert(!CODES || (MODE == kCeStats && BM == NT / 2 && STAGES == 3), "4-bit tiles");
   static_assert(STAGES >= 2 && STAGES <= 3 && kAhead < 63, "stages");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[STAGES * kStage];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[STAGES * kStage + (CODES ? 2 * BM * 32 : 0)];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = tid >> 6;
@@ -215,6 +240,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     rb = make_dma_rsrc(g.w + (size_t)s_first * kBK * g.H, (uint32_t)((size_t)(K - min(s_first * kBK, K)) * g.H * 2));
     dA.init(g.ld, min(BM, M - m0), g.ld, 0, tid);
     dB.init(g.H, g.H, n0, tid);
+  } else if constexpr (CODES) {
+    ra = make_dma_rsrc(reinterpret_cast<const uint8_t*>(g.w) + (size_t)m0 * (g.H / 2), (uint32_t)(min(BM, M - m0) * (g.H / 2)));
+    rb = make_dma_rsrc(g.x, (uint32_t)((size_t)g.T * g.H * 2));
+    dA.init(g.H / 2, min(BM, M - m0), tid);
+    dB.init(g.H, live, g.H, n0, tid, g.rows);
   } else {
     ra = make_dma_rsrc(g.w + (size_t)m0 * g.H, (uint32_t)((size_t)min(BM, M - m0) * g.H * 2));
     rb = make_dma_rsrc(g.x, (uint32_t)((size_t)g.T * g.H * 2));
@@ -289,7 +319,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     constexpr int a0 = h ? DA::kInst / 2 : 0, an = h ? DA::kInst - a0 : DA::kInst / 2, b0 = h ? DB::kInst / 2 : 0;
     const int ka = (s_first + kt) * kBK;
     if constexpr (n < an) {
-      dA.template issue_part<a0 + n, a0 + n + 1>(ra, (SQ_LDS uint16_t*)stage_at(S), ka, false, wave_u);
+      if constexpr (CODES) dA.issue(ra, stage_at(S), ka / 2, g.H / 2, wave_u);
+      else dA.template issue_part<a0 + n, a0 + n + 1>(ra, (SQ_LDS uint16_t*)stage_at(S), ka, false, wave_u);
     } else {
       SQ_LDS uint16_t* b = (SQ_LDS uint16_t*)(stage_at(S) + kA);
       constexpr int q = b0 + n - an;
@@ -316,6 +347,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     constexpr int n = decltype(N)::value, kk = decltype(KK)::value;
     const int chunk = 2 * kk + (lane >> 5);
     if constexpr (n == 0 || n > TN) {
+      static_assert(!CODES, "operands from codes are converted");
       constexpr int i = n == 0 ? 0 : n - TN;
       f.a[i] = *(const SQ_LDS bf16x8*)((const SQ_LDS uint16_t*)stage_at(S) + kc_off(wm0 + i * 32 + (lane & 31), chunk));
     } else {
@@ -328,6 +360,33 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   auto product = [&](Frag& f, auto N) {
     constexpr int i = decltype(N)::value / TN, j = decltype(N)::value % TN;
     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+  };
+  // CODES: this lane's codes and scales of a stage, 8 codes per row tile and slice,
+  // and the operand made of them
+  DmaPairs<NT, true> dS;
+  DmaRsrc rscale;
+  uint32_t cw[TM][4], sc[TM];
+  SQ_LDS uint8_t* const scales = (SQ_LDS uint8_t*)lds + STAGES * kStage;
+  if constexpr (CODES) {
+    rscale = make_dma_rsrc(g.scales + (size_t)m0 * (g.H / 32), (uint32_t)(min(BM, M - m0) * (g.H / 32)));
+    dS.init(g.H / 32, min(BM, M - m0), tid);
+  }
+  auto dma_scales = [&](int group) { dS.issue(rscale, scales + (group & 1) * (BM * 32), group * 32, g.H / 32, wave_u); };
+  auto read_codes = [&](auto S, int kt, auto I) {
+    constexpr int i = decltype(I)::value;
+    const int row = wm0 + i * 32 + (lane & 31), swap = (lane >> 3) & 1;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const SQ_LDS uint32_t* p = (const SQ_LDS uint32_t*)(stage_at(S) + row * 32 + (c ^ swap) * 16 + (lane >> 5) * 4);
+      cw[i][2 * c] = p[0];
+      cw[i][2 * c + 1] = p[2];
+    }
+    sc[i] = *(const SQ_LDS uint16_t*)(scales + ((kt / kGroup) & 1) * (BM * 32) + row * 32 + kt % kGroup * 2);
+  };
+  auto convert = [&](Frag& f, auto KK, auto I) {
+    constexpr int i = decltype(I)::value, kk = decltype(KK)::value;
+    const uint4 v = ScaleOperand<kMX>::dequant8(cw[i][kk], ScaleOperand<kMX>::of((sc[i] >> (kk >= 2 ? 8 : 0)) & 0xFFu));
+    f.a[i] = __builtin_bit_cast(bf16x8, v);
   };
   // f of those of 0 .. ALL - 1 that fall to part N of PARTS
   auto share = [&](auto N, auto PARTS, auto ALL, auto f) {
@@ -380,25 +439,89 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
       __builtin_amdgcn_sched_barrier(0);
     });
   };
+  // The same with CODES: the operands of the next slice are made of the codes that the
+  // lane holds; the next stage's codes are read once the present ones are used up.
+  auto step_codes = [&](auto S, int kt) {
+    constexpr int s = decltype(S)::value;
+    using SN = std::integral_constant<int, (s + 1) % STAGES>;
+    using SP = std::integral_constant<int, (s + STAGES - 1) % STAGES>;
+    using Parts = std::integral_constant<int, kProducts>;
+    using Mid = std::integral_constant<int, kMid>;
+    using Rest = std::integral_constant<int, kRest>;
+    using Rows = std::integral_constant<int, TM>;
+    using Cols = std::integral_constant<int, TN>;
+    for_each(std::make_integer_sequence<int, kSlices - 1>{}, [&](auto KK) {
+      constexpr int kk = decltype(KK)::value;
+      using Next = std::integral_constant<int, kk + 1>;
+      Frag& now = kk & 1 ? F1 : F0;
+      Frag& next = kk & 1 ? F0 : F1;
+      for_each(Products{}, [&](auto N) {
+        constexpr int n = decltype(N)::value;
+        product(now, N);
+        share(N, Parts{}, Cols{}, [&](auto J) { read(S, Next{}, next, std::integral_constant<int, decltype(J)::value + 1>{}); });
+        if constexpr (kk == kSlices - 2) {
+          share(N, Mid{}, Rows{}, [&](auto I) { convert(next, Next{}, I); });
+          if constexpr (n >= kMid)
+            share(std::integral_constant<int, n - kMid>{}, Rest{}, Rows{}, [&](auto I) { read_codes(SN{}, kt + 1, I); });
+        } else {
+          share(N, Parts{}, Rows{}, [&](auto I) { convert(next, Next{}, I); });
+        }
+        if constexpr (kk == 0) share(N, Parts{}, std::integral_constant<int, kHalf[1]>{}, [&](auto C) { dma(SP{}, kt + STAGES - 1, I1{}, C); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+    for_each(Products{}, [&](auto N) {
+      constexpr int n = decltype(N)::value;
+      if constexpr (n == kMid) {
+        wait_vm_lgkm0<kAhead>();
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      product(F1, N);
+      share(N, Mid{}, Cols{}, [&](auto J) { read(SN{}, I0{}, F0, std::integral_constant<int, decltype(J)::value + 1>{}); });
+      if constexpr (n >= kMid) {
+        using At = std::integral_constant<int, n - kMid>;
+        share(At{}, Rest{}, Rows{}, [&](auto I) { convert(F0, I0{}, I); });
+        share(At{}, Rest{}, std::integral_constant<int, kHalf[0]>{}, [&](auto C) { dma(S, kt + STAGES, I0{}, C); });
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (kt % kGroup == 0) dma_scales(kt / kGroup + 1);
+  };
   // prologue: stage 0 whole and its first operands, then stages 1 .. STAGES - 2
   // and the first half of stage STAGES - 1
   if (nk > 0) {
     dma_half(I0{}, 0, I0{});
     dma_half(I0{}, 0, I1{});
+    if constexpr (CODES) {
+      dma_scales(0);
+      dma_half(I1{}, 1, I0{});
+      dma_half(I1{}, 1, I1{});
+    }
     wait_vm_lgkm0<0>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    for_each(std::make_integer_sequence<int, kReads>{}, [&](auto R) { read(I0{}, I0{}, F0, R); });
-    if constexpr (STAGES > 2) {
-      dma_half(I1{}, 1, I0{});
-      dma_half(I1{}, 1, I1{});
+    if constexpr (CODES) {
+      for_each(std::make_integer_sequence<int, TM>{}, [&](auto I) {
+        read_codes(I0{}, 0, I);
+        convert(F0, I0{}, I);
+      });
+      for_each(std::make_integer_sequence<int, TN>{}, [&](auto J) { read(I0{}, I0{}, F0, std::integral_constant<int, decltype(J)::value + 1>{}); });
+    } else {
+      for_each(std::make_integer_sequence<int, kReads>{}, [&](auto R) { read(I0{}, I0{}, F0, R); });
+      if constexpr (STAGES > 2) {
+        dma_half(I1{}, 1, I0{});
+        dma_half(I1{}, 1, I1{});
+      }
     }
     dma_half(std::integral_constant<int, STAGES - 1>{}, STAGES - 1, I0{});
   }
   for (int kt0 = 0; kt0 < nk; kt0 += STAGES)
     for_each(std::make_integer_sequence<int, STAGES>{}, [&](auto S) {
       constexpr int s = decltype(S)::value;
-      if (s == 0 || kt0 + s < nk) step(S, kt0 + s);
+      if (s > 0 && kt0 + s >= nk) return;
+      if constexpr (CODES) step_codes(S, kt0 + s);
+      else step(S, kt0 + s);
     });
   wait_vm_lgkm0<0>();
 
@@ -995,6 +1118,26 @@ int ce_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
   return ok();
 }
 
+// The logits' statistics of an MXFP4 head straight from its codes: rows that its
+// 16-byte copies of codes and scales end with, and tiles enough.  Each value is
+// converted by the two waves that multiply it, which costs the products 6% over
+// bf16 operands but saves writing the head out, or the logits of the layer's own
+// products (us of the forward, 131072 x 4096: 256 tokens 283 -> 225, 64 tokens 109 ->
+// 88; of loss and gradient: 512 tokens of it 2055 -> 1821, 1999 of 50001 x 4096 2521
+// -> 2407, 4096 of 131072 x 2048 5666 either way; with 2 x 4 waves, four of which
+// convert each value, 1888, 2544, 6062).
+bool ce_codes(int head, int64_t T, int64_t V, int64_t H) {
+  return head == kMX && H % 512 == 0 && V * T > 0 && ce_plan(false, false, T, V, H).splits == 1;
+}
+
+int ce_codes_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
+  const dim3 grid((unsigned)blocks), block(512);
+  if (bt == 64) hipLaunchKernelGGL((ce_kernel<kCeStats, 256, 64, 8, 1, 3, true>), grid, block, 0, s, g);
+  else if (bt == 128) hipLaunchKernelGGL((ce_kernel<kCeStats, 256, 128, 4, 2, 3, true>), grid, block, 0, s, g);
+  else hipLaunchKernelGGL((ce_kernel<kCeStats, 256, 256, 4, 2, 3, true>), grid, block, 0, s, g);
+  return ok();
+}
+
 // The bf16 rows [v0, v0 + n) of the head: its own, or a 4-bit piece written out.
 int ce_weight(int head, const void* W, const uint8_t* scales, int64_t v0, int64_t n, int64_t H, void* buf,
               const uint16_t** out, hipStream_t s) {
@@ -1199,8 +1342,10 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
 }  // namespace
 
 size_t ce_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H) {
-  if (ce_few(head, T, V, H)) return ce_few_plan(bwd != 0, T, V, H).total;
-  return ce_plan(bwd != 0, head != kCeBf16, T, V, H).total;
+  const size_t n = ce_few(head, T, V, H) ? ce_few_plan(bwd != 0, T, V, H).total : ce_plan(bwd != 0, head != kCeBf16, T, V, H).total;
+  if (bwd || !ce_codes(head, T, V, H)) return n;
+  const size_t codes = ce_plan(false, false, T, V, H).total;     // either way: what decides is where the operands are
+  return n > codes ? n : codes;
 }
 
 // What both directions set up: the arguments, and the live rows numbered.
@@ -1229,6 +1374,19 @@ static int ce_begin(const CePlan& p, int T, int64_t V, int H, const void* X, flo
 int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
                   const void* y, int y_bytes, float* loss, float* lse, void* workspace, hipStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
+  if (ce_codes(head, T, V, H) && ((uintptr_t)W | (uintptr_t)scales) % 16 == 0) {
+    const CePlan p = ce_plan(false, false, T, V, H);
+    CeArgs g{};
+    CePiece c{};
+    if (ce_begin(p, T, V, H, X, ws2, y, y_bytes, ws, &g, &c, s) != 0) return -1;
+    g.w = static_cast<const uint16_t*>(W);
+    g.scales = scales;
+    g.Vn = (int)V;
+    g.part = reinterpret_cast<float*>(ws + p.part);
+    const int tiles = (int)((V + 255) / 256);
+    if (ce_codes_go(g, p.bt, (int64_t)tiles * ((T + p.bt - 1) / p.bt), s) != 0) return -1;
+    return ce_loss_go(reinterpret_cast<float2*>(g.part), g.tlogit, c, tiles, loss, lse, s);
+  }
   if (ce_few(head, T, V, H))
     return ce_few_fwd(head, T, V, H, X, static_cast<const uint8_t*>(W), scales, ws2, y, y_bytes, loss, lse, ws, s);
   const CePlan p = ce_plan(false, head != kCeBf16, T, V, H);
