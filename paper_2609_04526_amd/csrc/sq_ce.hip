@@ -199,18 +199,22 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   constexpr int NT = 64 * WGM * WGN;
   constexpr int WM = BM / WGM, WN = BN / WGN;
   constexpr int TM = WM / 32, TN = WN / 32;
-  constexpr int kA = CODES ? BM * kBK / 2 : BM * kBK * 2, kB = BN * kBK * 2, kStage = kA + kB, kSlices = kBK / 16;
+  constexpr int kA = CODES && MODE != kCeDx ? BM * kBK / 2 : BM * kBK * 2, kB = BN * kBK * 2, kStage = kA + kB, kSlices = kBK / 16;
   constexpr bool kDxMode = MODE == kCeDx;
   constexpr int kGroup = 16;                                  // stages of a row's 32 scales
-  using DA = std::conditional_t<CODES, DmaPairs<NT, false>, DmaKC<BM, NT>>;
+  constexpr bool kRowCodes = CODES && !kDxMode;               // W's codes through LDS
+  using DA = std::conditional_t<kRowCodes, DmaPairs<NT, false>, DmaKC<BM, NT>>;
   using DB = std::conditional_t<kDxMode, DmaNat<BN, NT, kBK>, DmaRows<BN, NT>>;
-  constexpr int kDma = DA::kInst + DB::kInst;
+  constexpr bool kItems = kDxMode && CODES;                   // W's codes through registers
+  constexpr int kDmaB = kItems ? 0 : DB::kInst;
+  constexpr int kDma = DA::kInst + kDmaB;
   // with CODES a stage is published a step before it is multiplied: its codes become
   // operands in the vector units meanwhile
-  constexpr int kAhead = (STAGES - (CODES ? 3 : 2)) * kDma;
-  static_assert(!CODES || (MODE == kCeStats && BM == NT / 2 && STAGES == 3), "4-bit tiles");
+  constexpr int kAhead = kItems ? 0 : (STAGES - (CODES ? 3 : 2)) * kDma;
+  static_assert(!kRowCodes || (MODE != kCeLogits && BM == NT / 2 && STAGES == 3), "4-bit tiles");
+  static_assert(!kItems || (BN == 256 && NT == 512 && STAGES == 2), "an item of 32 columns per thread");
   static_assert(STAGES >= 2 && STAGES <= 3 && kAhead < 63, "stages");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[STAGES * kStage + (CODES ? 2 * BM * 32 : 0)];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[STAGES * kStage + (kRowCodes ? 2 * BM * 32 : 0)];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = tid >> 6;
@@ -237,10 +241,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   DB dB;
   if constexpr (kDxMode) {
     ra = make_dma_rsrc(g.d + (size_t)m0 * g.ld, (uint32_t)((size_t)min(BM, M - m0) * g.ld * 2));
-    rb = make_dma_rsrc(g.w + (size_t)s_first * kBK * g.H, (uint32_t)((size_t)(K - min(s_first * kBK, K)) * g.H * 2));
+    if constexpr (!kItems)
+      rb = make_dma_rsrc(g.w + (size_t)s_first * kBK * g.H, (uint32_t)((size_t)(K - min(s_first * kBK, K)) * g.H * 2));
     dA.init(g.ld, min(BM, M - m0), g.ld, 0, tid);
-    dB.init(g.H, g.H, n0, tid);
-  } else if constexpr (CODES) {
+    if constexpr (!kItems) dB.init(g.H, g.H, n0, tid);
+  } else if constexpr (kRowCodes) {
     ra = make_dma_rsrc(reinterpret_cast<const uint8_t*>(g.w) + (size_t)m0 * (g.H / 2), (uint32_t)(min(BM, M - m0) * (g.H / 2)));
     rb = make_dma_rsrc(g.x, (uint32_t)((size_t)g.T * g.H * 2));
     dA.init(g.H / 2, min(BM, M - m0), tid);
@@ -316,10 +321,10 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   // as zeros, so the copies need no condition on kt
   auto dma = [&](auto S, int kt, auto HALF, auto N) {
     constexpr int h = decltype(HALF)::value, n = decltype(N)::value;
-    constexpr int a0 = h ? DA::kInst / 2 : 0, an = h ? DA::kInst - a0 : DA::kInst / 2, b0 = h ? DB::kInst / 2 : 0;
+    constexpr int a0 = h ? DA::kInst / 2 : 0, an = h ? DA::kInst - a0 : DA::kInst / 2, b0 = h ? kDmaB / 2 : 0;
     const int ka = (s_first + kt) * kBK;
     if constexpr (n < an) {
-      if constexpr (CODES) dA.issue(ra, stage_at(S), ka / 2, g.H / 2, wave_u);
+      if constexpr (kRowCodes) dA.issue(ra, stage_at(S), ka / 2, g.H / 2, wave_u);
       else dA.template issue_part<a0 + n, a0 + n + 1>(ra, (SQ_LDS uint16_t*)stage_at(S), ka, false, wave_u);
     } else {
       SQ_LDS uint16_t* b = (SQ_LDS uint16_t*)(stage_at(S) + kA);
@@ -330,7 +335,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
         dB.template issue_part<q, q + 1>(rb, b, ka, wave_u);
     }
   };
-  constexpr int kHalf[2] = {DA::kInst / 2 + DB::kInst / 2, kDma - DA::kInst / 2 - DB::kInst / 2};
+  constexpr int kHalf[2] = {DA::kInst / 2 + kDmaB / 2, kDma - DA::kInst / 2 - kDmaB / 2};
   auto dma_half = [&](auto S, int kt, auto HALF) {
     for_each(std::make_integer_sequence<int, kHalf[decltype(HALF)::value]>{}, [&](auto N) { dma(S, kt, HALF, N); });
   };
@@ -347,7 +352,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     constexpr int n = decltype(N)::value, kk = decltype(KK)::value;
     const int chunk = 2 * kk + (lane >> 5);
     if constexpr (n == 0 || n > TN) {
-      static_assert(!CODES, "operands from codes are converted");
+      static_assert(!kRowCodes, "operands from codes are converted");
       constexpr int i = n == 0 ? 0 : n - TN;
       f.a[i] = *(const SQ_LDS bf16x8*)((const SQ_LDS uint16_t*)stage_at(S) + kc_off(wm0 + i * 32 + (lane & 31), chunk));
     } else {
@@ -367,7 +372,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   DmaRsrc rscale;
   uint32_t cw[TM][4], sc[TM];
   SQ_LDS uint8_t* const scales = (SQ_LDS uint8_t*)lds + STAGES * kStage;
-  if constexpr (CODES) {
+  if constexpr (kRowCodes) {
     rscale = make_dma_rsrc(g.scales + (size_t)m0 * (g.H / 32), (uint32_t)(min(BM, M - m0) * (g.H / 32)));
     dS.init(g.H / 32, min(BM, M - m0), tid);
   }
@@ -387,6 +392,28 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     constexpr int i = decltype(I)::value, kk = decltype(KK)::value;
     const uint4 v = ScaleOperand<kMX>::dequant8(cw[i][kk], ScaleOperand<kMX>::of((sc[i] >> (kk >= 2 ? 8 : 0)) & 0xFFu));
     f.a[i] = __builtin_bit_cast(bf16x8, v);
+  };
+  // dX from codes: a thread's item of a stage is a block of 32 columns of one row of
+  // W, its codes and their scale loaded a step before it is written out as bf16
+  const int irow = tid >> 3, icol = (tid & 7) * 32;
+  const bool icol_in = n0 + icol < g.H;
+  u32x4 iq = {0u, 0u, 0u, 0u};
+  uint32_t isc = 0;
+  auto load_item = [&](int kt) {
+    const int first = min((s_first + kt) * kBK, K), left = min(K - first, kBK);
+    const size_t row0 = (size_t)first;
+    const __amdgpu_buffer_rsrc_t rc = make_rsrc(reinterpret_cast<const uint8_t*>(g.w) + row0 * (g.H / 2), (uint32_t)(left * (g.H / 2)));
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(g.scales + row0 * (g.H / 32), (uint32_t)(left * (g.H / 32)));
+    const uint32_t at = icol_in ? (uint32_t)irow * (uint32_t)(g.H / 2) + (uint32_t)((n0 + icol) / 2) : kOOB;
+    const uint32_t as = icol_in ? (uint32_t)irow * (uint32_t)(g.H / 32) + (uint32_t)((n0 + icol) / 32) : kOOB;
+    iq = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, (int)at, 0, 0));
+    isc = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)as, 0, 0);
+  };
+  auto write_item = [&](auto S, auto C) {                     // columns 8 C .. 8 C + 7 of it
+    constexpr int c = decltype(C)::value;
+    SQ_LDS uint16_t* b = (SQ_LDS uint16_t*)(stage_at(S) + kA);
+    const uint4 v = ScaleOperand<kMX>::dequant8(iq[c], ScaleOperand<kMX>::of(isc));
+    *(SQ_LDS u32x4*)(b + nat_off<BN>(irow, icol + 8 * c)) = __builtin_bit_cast(u32x4, v);
   };
   // f of those of 0 .. ALL - 1 that fall to part N of PARTS
   auto share = [&](auto N, auto PARTS, auto ALL, auto f) {
@@ -417,6 +444,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
         if constexpr (kk == 0)
           share(N, std::integral_constant<int, kProducts>{}, std::integral_constant<int, kHalf[1]>{},
                 [&](auto C) { dma(SP{}, kt + STAGES - 1, I1{}, C); });
+        if constexpr (kItems && kk == 0 && decltype(N)::value == 0) load_item(kt + 2);
         __builtin_amdgcn_sched_barrier(0);
       });
     });
@@ -435,6 +463,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
         using Rest = std::integral_constant<int, kRest>;
         share(At{}, Rest{}, Reads{}, [&](auto R) { read(SN{}, I0{}, F0, R); });
         share(At{}, Rest{}, std::integral_constant<int, kHalf[0]>{}, [&](auto C) { dma(S, kt + STAGES, I0{}, C); });
+        if constexpr (kItems) share(At{}, Rest{}, std::integral_constant<int, 4>{}, [&](auto C) { write_item(S, C); });
       }
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -493,7 +522,13 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
   if (nk > 0) {
     dma_half(I0{}, 0, I0{});
     dma_half(I0{}, 0, I1{});
-    if constexpr (CODES) {
+    if constexpr (kItems) {
+      load_item(0);
+      for_each(std::make_integer_sequence<int, 4>{}, [&](auto C) { write_item(I0{}, C); });
+      load_item(1);
+      for_each(std::make_integer_sequence<int, 4>{}, [&](auto C) { write_item(I1{}, C); });
+    }
+    if constexpr (kRowCodes) {
       dma_scales(0);
       dma_half(I1{}, 1, I0{});
       dma_half(I1{}, 1, I1{});
@@ -501,7 +536,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     wait_vm_lgkm0<0>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (CODES) {
+    if constexpr (kRowCodes) {
       for_each(std::make_integer_sequence<int, TM>{}, [&](auto I) {
         read_codes(I0{}, 0, I);
         convert(F0, I0{}, I);
@@ -520,7 +555,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
     for_each(std::make_integer_sequence<int, STAGES>{}, [&](auto S) {
       constexpr int s = decltype(S)::value;
       if (s > 0 && kt0 + s >= nk) return;
-      if constexpr (CODES) step_codes(S, kt0 + s);
+      if constexpr (kRowCodes) step_codes(S, kt0 + s);
       else step(S, kt0 + s);
     });
   wait_vm_lgkm0<0>();
@@ -1118,23 +1153,34 @@ int ce_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
   return ok();
 }
 
-// The logits' statistics of an MXFP4 head straight from its codes: rows that its
-// 16-byte copies of codes and scales end with, and tiles enough.  Each value is
-// converted by the two waves that multiply it, which costs the products 6% over
-// bf16 operands but saves writing the head out, or the logits of the layer's own
-// products (us of the forward, 131072 x 4096: 256 tokens 283 -> 225, 64 tokens 109 ->
-// 88; of loss and gradient: 512 tokens of it 2055 -> 1821, 1999 of 50001 x 4096 2521
-// -> 2407, 4096 of 131072 x 2048 5666 either way; with 2 x 4 waves, four of which
-// convert each value, 1888, 2544, 6062).
+// An MXFP4 head straight from its codes: rows that its 16-byte copies of codes and
+// scales end with, and tiles enough.  Of the logits' tiles two waves convert each
+// value, of dX's one thread, on its way to LDS: 6% over bf16 operands or less, and
+// neither the head in bf16 nor the logits of the layer's own products go through
+// memory (us, without against with: loss and gradient of 512 tokens of 131072 x
+// 4096 2055, 1576; 300 of 50000 x 4096 806, 473; 1999 of 50001 x 4096 2521, 2208;
+// 4096 of 131072 x 2048 5666, 5657; forward of 64 and 256 tokens of 131072 x 4096
+// 109, 88 and 283, 225).  The gradient of up to 64 tokens stays with the layer's
+// products (64 tokens of 131072 x 4096 307, from codes 326; 128 tokens 573, 490).
+constexpr int kCeCodesTokens = 64;
+
 bool ce_codes(int head, int64_t T, int64_t V, int64_t H) {
   return head == kMX && H % 512 == 0 && V * T > 0 && ce_plan(false, false, T, V, H).splits == 1;
 }
 
+template <int MODE>
 int ce_codes_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
+  if (blocks == 0) return 0;
   const dim3 grid((unsigned)blocks), block(512);
-  if (bt == 64) hipLaunchKernelGGL((ce_kernel<kCeStats, 256, 64, 8, 1, 3, true>), grid, block, 0, s, g);
-  else if (bt == 128) hipLaunchKernelGGL((ce_kernel<kCeStats, 256, 128, 4, 2, 3, true>), grid, block, 0, s, g);
-  else hipLaunchKernelGGL((ce_kernel<kCeStats, 256, 256, 4, 2, 3, true>), grid, block, 0, s, g);
+  if constexpr (MODE == kCeDx) {
+    if (bt == 64) hipLaunchKernelGGL((ce_kernel<MODE, 64, 256, 1, 8, 2, true>), grid, block, 0, s, g);
+    else if (bt == 128) hipLaunchKernelGGL((ce_kernel<MODE, 128, 256, 2, 4, 2, true>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((ce_kernel<MODE, 256, 256, 2, 4, 2, true>), grid, block, 0, s, g);
+  } else {
+    if (bt == 64) hipLaunchKernelGGL((ce_kernel<MODE, 256, 64, 8, 1, 3, true>), grid, block, 0, s, g);
+    else if (bt == 128) hipLaunchKernelGGL((ce_kernel<MODE, 256, 128, 4, 2, 3, true>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((ce_kernel<MODE, 256, 256, 4, 2, 3, true>), grid, block, 0, s, g);
+  }
   return ok();
 }
 
@@ -1343,8 +1389,8 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
 
 size_t ce_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H) {
   const size_t n = ce_few(head, T, V, H) ? ce_few_plan(bwd != 0, T, V, H).total : ce_plan(bwd != 0, head != kCeBf16, T, V, H).total;
-  if (bwd || !ce_codes(head, T, V, H)) return n;
-  const size_t codes = ce_plan(false, false, T, V, H).total;     // either way: what decides is where the operands are
+  if (!ce_codes(head, T, V, H)) return n;
+  const size_t codes = ce_plan(bwd != 0, false, T, V, H).total;  // either way: what decides is where the operands are
   return n > codes ? n : codes;
 }
 
@@ -1384,7 +1430,7 @@ int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     g.Vn = (int)V;
     g.part = reinterpret_cast<float*>(ws + p.part);
     const int tiles = (int)((V + 255) / 256);
-    if (ce_codes_go(g, p.bt, (int64_t)tiles * ((T + p.bt - 1) / p.bt), s) != 0) return -1;
+    if (ce_codes_go<kCeStats>(g, p.bt, (int64_t)tiles * ((T + p.bt - 1) / p.bt), s) != 0) return -1;
     return ce_loss_go(reinterpret_cast<float2*>(g.part), g.tlogit, c, tiles, loss, lse, s);
   }
   if (ce_few(head, T, V, H))
@@ -1415,10 +1461,11 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
                   const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16,
                   void* workspace, hipStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  if (ce_few(head, T, V, H))
+  const bool codes = T > kCeCodesTokens && ce_codes(head, T, V, H) && ((uintptr_t)W | (uintptr_t)scales) % 16 == 0;
+  if (!codes && ce_few(head, T, V, H))
     return ce_few_bwd(head, T, V, H, X, static_cast<const uint8_t*>(W), scales, ws2, y, y_bytes, lse, dloss, dX, dx_bf16,
                       ws, s);
-  const CePlan p = ce_plan(true, head != kCeBf16, T, V, H);
+  const CePlan p = ce_plan(true, head != kCeBf16 && !codes, T, V, H);
   CeArgs g{};
   CePiece c{};
   if (ce_begin(p, T, V, H, X, ws2, y, y_bytes, ws, &g, &c, s) != 0) return -1;
@@ -1430,10 +1477,16 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
   const int64_t dx_blocks = dx_tiles > kCUs ? dx_tiles : kCUs;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece, tiles = (n + 255) / 256 * tt;
-    if (ce_weight(head, W, scales, v0, n, H, ws + p.wbuf, &g.w, s) != 0) return -1;
     g.v0 = v0;
     g.Vn = (int)n;
     g.add = v0 > 0;
+    if (codes) {
+      g.w = reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(W) + v0 * (H / 2));
+      g.scales = scales + v0 * (H / 32);
+      if (ce_codes_go<kCeGrad>(g, p.bt, tiles, s) != 0 || ce_codes_go<kCeDx>(g, p.bx, dx_blocks, s) != 0) return -1;
+      continue;
+    }
+    if (ce_weight(head, W, scales, v0, n, H, ws + p.wbuf, &g.w, s) != 0) return -1;
     if (p.splits > 1) {
       if (ce_go<kCeLogits>(g, p.bt, tiles * p.splits, s) != 0 ||
           ce_grad_go(head, c, lse, dloss, p.ld, p.ld, 0, g.d, g.tlogit, CeTail{}, s) != 0)

@@ -297,3 +297,35 @@ def test_statistics_of_codes_of_few_tokens(sq, T, V, I):
     got = sq.sq_ce_fwd("mx", X, codes, y, scales=scales)
     want = sq.sq_ce_fwd("bf16", X, torch.from_numpy(w).to(BF16).cuda(), y)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# the gradient straight from MXFP4 codes: dX tiles of 64, 128 and 256 tokens, splits of the vocabulary, ragged edges, and codes
+# that are not aligned for it, which go through bf16 in memory
+@pytest.mark.parametrize("T,V,I", [(300, 3003, 512), (257, 17000, 1024), (700, 9001, 1536), (1030, 16399, 2048), (2100, 9000, 1024)])
+@pytest.mark.parametrize("offset", [0, 4])
+def test_gradient_of_codes_equals_that_of_bf16_values(sq, T, V, I, offset):
+    codes, scales, w = _head("mx", V, V, I)
+    base = torch.zeros(codes.numel() + 16, dtype=torch.uint8, device="cuda")
+    base[offset:offset + codes.numel()] = codes.reshape(-1)
+    codes = base[offset:offset + codes.numel()].view(V, I // 2)
+    g = inputs.rng(T)
+    y = torch.from_numpy(g.integers(0, V, T)).cuda()
+    y[::5] = -1
+    dloss = torch.from_numpy(g.standard_normal(T).astype(np.float32)).cuda()
+    X, W = inputs.device_bf16_normal(T, (T, I)), torch.from_numpy(w).to(BF16).cuda()
+    _, lse = sq.sq_ce_fwd("bf16", X, W, y)
+    got = sq.sq_ce_bwd("mx", X, codes, y, lse, dloss, scales=scales)
+    assert torch.equal(got, sq.sq_ce_bwd("bf16", X, W, y, lse, dloss))
+
+
+@pytest.mark.parametrize("T,V,I", [(100, 34001, 512), (256, 33333, 512), (65, 40008, 1024)])
+def test_gradient_of_codes_of_few_tokens(sq, T, V, I):
+    codes, scales, w = _head("mx", V, V, I)
+    g = inputs.rng(T)
+    y = torch.from_numpy(g.integers(0, V, T)).cuda()
+    y[::7] = V
+    dloss = torch.from_numpy(g.standard_normal(T).astype(np.float32)).cuda()
+    X, W = inputs.device_bf16_normal(T, (T, I)), torch.from_numpy(w).to(BF16).cuda()
+    _, lse = sq.sq_ce_fwd("bf16", X, W, y)
+    got = sq.sq_ce_bwd("mx", X, codes, y, lse, dloss, scales=scales)
+    assert torch.equal(got, sq.sq_ce_bwd("bf16", X, W, y, lse, dloss))
