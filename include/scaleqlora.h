@@ -618,7 +618,8 @@ size_t sq_bwd_dscale_act8_batched_workspace(int64_t E, int64_t T, int64_t I);
  * irrelevant: the row statistics (8 bytes per token and 256 entries of the
  * vocabulary), or one piece's logit gradients (about 256 MiB at most; one of 256
  * entries at least) and fp32 sums; for a 4-bit head one piece of it as bf16 (1 GiB
- * at most); for products too small to fill the GPU, and a 4-bit head of up to 256
+ * at most; an MXFP4 head of I % 512 == 0 at 16-byte aligned addresses is read as it
+ * is, but the size does not know the addresses); for products too small to fill the GPU, and a 4-bit head of up to 256
  * tokens, fp32 logits (1 GiB at most).  Deterministic.
  */
 size_t sq_ce_fwd_workspace(int head, int64_t T, int64_t V, int64_t I);

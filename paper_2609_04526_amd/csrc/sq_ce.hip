@@ -9,9 +9,10 @@
 // token's maximum and sum of exponentials over the tile; a second kernel joins
 // them.  Backward: pieces of the vocabulary; a piece's logits are formed again
 // and leave as bf16 gradients of the logits, [tokens, piece], which the next
-// product contracts with the same rows of W into fp32 sums.  A 4-bit head's
-// piece is written out as bf16 before it is used (code x scale is exact in
-// bf16; NVFP4's ws2 goes to the fp32 sums).
+// product contracts with the same rows of W into fp32 sums.  Up to 4096 tokens
+// an MXFP4 head of whole 512s is read as codes by all three products; other 4-bit heads' pieces are written
+// out as bf16 before they are used (code x scale is exact in bf16; NVFP4's ws2 goes
+// to the fp32 sums).
 //
 // Few tiles, whose sums are split, and a 4-bit head of few tokens, read by the
 // layer's own products, pass fp32 logits through the workspace instead.
@@ -21,10 +22,10 @@
 // once.  The number stays on the device.
 //
 // The three products bound it (the forward's logits, the same again, dX), and the
-// matrix cores' power bounds them: 4096 tokens of 131072 x 4096 bf16 10.2 ms, 1.29
-// PFLOP/s; 1999 tokens, 40% of them ignored, of 50001 x 4096 MXFP4 1.5 ms, of which
-// 0.17 write the head out.  One token of 131072 x 4096 bf16 takes 530 us, three
-// reads of the head at 6.1 TB/s, of MXFP4 243.
+// matrix cores' power bounds them: 4096 tokens of 131072 x 4096 bf16 10.0-10.6 ms,
+// 1.24-1.32 PFLOP/s; 1999 tokens, 40% of them ignored, of 50001 x 4096 MXFP4 1.33 ms.
+// One token of 131072 x 4096 bf16 takes 530 us, three reads of the head at 6.1 TB/s,
+// of MXFP4 245.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -1155,17 +1156,18 @@ int ce_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
 
 // An MXFP4 head straight from its codes: rows that its 16-byte copies of codes and
 // scales end with, and tiles enough.  Of the logits' tiles two waves convert each
-// value, of dX's one thread, on its way to LDS: 6% over bf16 operands or less, and
-// neither the head in bf16 nor the logits of the layer's own products go through
-// memory (us, without against with: loss and gradient of 512 tokens of 131072 x
-// 4096 2055, 1576; 300 of 50000 x 4096 806, 473; 1999 of 50001 x 4096 2521, 2208;
-// 4096 of 131072 x 2048 5666, 5657; forward of 64 and 256 tokens of 131072 x 4096
-// 109, 88 and 283, 225).  The gradient of up to 64 tokens stays with the layer's
+// value, of dX's one thread, on its way to LDS, which costs the products up to 8%
+// over bf16 operands; neither the head in bf16 nor the logits of the layer's own
+// products go through memory, which counts for less with more tokens.  us of loss
+// and gradient, without against with: 300 tokens of 50000 x 4096 806, 473; 1024 of
+// 131072 x 4096 3318, 2879; 2048 of 50001 x 4096 2510, 2178; 4096 of it 4260, 4268;
+// 8192 of 50001 x 2048 4322, 4504.  The forward of 64 and 256 tokens of 131072 x 4096:
+// 109, 88 and 283, 225.  The gradient of up to 64 tokens stays with the layer's
 // products (64 tokens of 131072 x 4096 307, from codes 326; 128 tokens 573, 490).
-constexpr int kCeCodesTokens = 64;
+constexpr int kCeCodesTokens = 64, kCeCodesMost = 4096;
 
 bool ce_codes(int head, int64_t T, int64_t V, int64_t H) {
-  return head == kMX && H % 512 == 0 && V * T > 0 && ce_plan(false, false, T, V, H).splits == 1;
+  return head == kMX && H % 512 == 0 && T > 0 && T <= kCeCodesMost && ce_plan(false, false, T, V, H).splits == 1;
 }
 
 template <int MODE>
