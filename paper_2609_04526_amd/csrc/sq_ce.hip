@@ -171,10 +171,28 @@ struct DmaPairs {
   }
 };
 
-// Split of the vocabulary rows of dX's contraction over workgroups, where the
-// live rows' tiles leave compute units idle (at least 4 stages each).
-__device__ __forceinline__ int ce_splits(int tiles, int stages) {
-  return max(1, min(min(kCUs / max(tiles, 1), stages / 4), 64));
+// Split of the vocabulary rows of dX's contraction over workgroups: few tiles as often
+// as they go into the CUs (at least 4 stages each); tiles that would leave the last
+// round of the CUs poorly filled up to 6 times, by the time of the rounds and of the
+// planes (tenths of us: 16 a stage, 1 a tile's plane).  4097 tokens of 131072 x 2048
+// make 136 tiles: the gradient with one split 4.92 ms, with 5 4.39 (bf16).
+constexpr int kCeMostGroups = 768;      // tiles times splits, where there are splits
+__host__ __device__ inline int ce_splits(int tiles, int stages) {
+  const int most = stages / 4;
+  if (tiles < 1 || most < 2 || 2 * tiles > kCeMostGroups) return 1;
+  if (3 * tiles <= kCUs) {
+    const int n = kCUs / tiles < most ? kCUs / tiles : most;
+    return n < 64 ? n : 64;
+  }
+  int best = 1, least = 0x7FFFFFFF;
+  for (int s = 1; s <= 6 && s <= most && s * tiles <= kCeMostGroups; ++s) {
+    const int cost = (s * tiles + kCUs - 1) / kCUs * ((stages + s - 1) / s) * 16 + s * tiles;
+    if (cost < least) {
+      least = cost;
+      best = s;
+    }
+  }
+  return best;
 }
 
 enum CeMode { kCeStats = 0, kCeGrad = 1, kCeDx = 2, kCeLogits = 3 };
@@ -1045,6 +1063,7 @@ struct CePlan {
   int64_t piece;            // rows of W per piece (a multiple of 256)
   int pieces;
   int ld;                   // columns of the logit gradients (and of the planes)
+  int64_t groups;           // tiles times splits of dX, at most
   size_t rows, tlogit, part, wbuf, logits, d, sums, total;   // offsets in the workspace
 };
 
@@ -1073,12 +1092,12 @@ int ce_tokens(int64_t T, int64_t vt) {
 // 7717 x 736 31, 34, 37; 3947 of 2830 x 960 86, 83, 91).
 int ce_dx_tokens(int64_t T, int64_t rows, int64_t cols) {
   auto cost = [&](int bx, double product) {
-    const int64_t tiles = up(T, bx) / bx * cols, by_cu = kCUs / tiles, by_stages = (rows + kBK - 1) / kBK / 4;
-    const int64_t splits = by_cu < by_stages ? by_cu : by_stages, groups = tiles * (splits > 1 ? splits : 1);
+    const int64_t tiles = up(T, bx) / bx * cols;
+    const int64_t groups = tiles > kCUs * 16 ? tiles : tiles * ce_splits((int)tiles, (int)((rows + kBK - 1) / kBK));
     const double us = product * 2e-9 / 1.3 * (double)up(groups, kCUs) / (double)groups * (double)(tiles * bx) * 256 * (double)rows;
     return us + 2 * 1024 / 5e6 * (double)(groups * bx);
   };
-  const double c64 = cost(64, 2.0), c128 = cost(128, 1.18), c256 = cost(256, 1.0);
+  const double c64 = cost(64, 2.0), c128 = cost(128, 1.25), c256 = cost(256, 1.0);
   if (c64 < c128 && c64 < c256) return 64;
   return c128 < c256 ? 128 : 256;
 }
@@ -1130,9 +1149,15 @@ CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
     p.d = take((size_t)T * p.ld * 2);
     const int64_t dx_cols = up(H, 256) / 256;
     p.bx = ce_dx_tokens(T, p.piece < V ? p.piece : V, dx_cols);
-    // planes of whole tiles: splits x tiles <= max(CUs, tiles)
-    const int64_t dx_tiles = up(T, p.bx) / p.bx * dx_cols;
-    p.sums = take((size_t)(dx_tiles > kCUs ? dx_tiles : kCUs) * p.bx * 256 * 4);
+    // planes of whole tiles, for as many live rows as need the most
+    const int64_t tt = up(T, p.bx) / p.bx;
+    const int stages = (int)(((p.piece < V ? p.piece : V) + kBK - 1) / kBK);
+    p.groups = tt * dx_cols;
+    for (int64_t t = dx_cols; t <= tt * dx_cols && t <= kCeMostGroups; t += dx_cols) {
+      const int64_t n = t * ce_splits((int)t, stages);
+      p.groups = p.groups > n ? p.groups : n;
+    }
+    p.sums = take((size_t)p.groups * p.bx * 256 * 4);
   }
   p.total = at;
   return p;
@@ -1475,8 +1500,7 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
   g.d = reinterpret_cast<uint16_t*>(ws + p.d);
   g.sums = reinterpret_cast<float*>(ws + p.sums);
   g.split_stages = (int)(((p.piece < V ? p.piece : V) + kBK - 1) / kBK);
-  const int64_t tt = (T + p.bt - 1) / p.bt, tn = (H + 255) / 256, dx_tiles = (T + p.bx - 1) / p.bx * tn;
-  const int64_t dx_blocks = dx_tiles > kCUs ? dx_tiles : kCUs;
+  const int64_t tt = (T + p.bt - 1) / p.bt, tn = (H + 255) / 256;
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece, tiles = (n + 255) / 256 * tt;
     g.v0 = v0;
@@ -1485,7 +1509,7 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     if (codes) {
       g.w = reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(W) + v0 * (H / 2));
       g.scales = scales + v0 * (H / 32);
-      if (ce_codes_go<kCeGrad>(g, p.bt, tiles, s) != 0 || ce_codes_go<kCeDx>(g, p.bx, dx_blocks, s) != 0) return -1;
+      if (ce_codes_go<kCeGrad>(g, p.bt, tiles, s) != 0 || ce_codes_go<kCeDx>(g, p.bx, p.groups, s) != 0) return -1;
       continue;
     }
     if (ce_weight(head, W, scales, v0, n, H, ws + p.wbuf, &g.w, s) != 0) return -1;
@@ -1496,7 +1520,7 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     } else if (ce_go<kCeGrad>(g, p.bt, tiles, s) != 0) {
       return -1;
     }
-    if (ce_go<kCeDx>(g, p.bx, dx_blocks, s) != 0) return -1;
+    if (ce_go<kCeDx>(g, p.bx, p.groups, s) != 0) return -1;
   }
   const CeRest rest{W, scales, g.tlogit, nullptr, V, 0};
   auto finish = [&](auto kernel) {

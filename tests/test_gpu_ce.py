@@ -234,6 +234,16 @@ def test_few_tiles_of_long_rows(sq, head, T, V, I):
     _check(sq, head, T, V, I, T + I, y, out_dtype=BF16 if T > 200 else F32)
 
 
+# tiles of dX that would leave the last round of the compute units poorly filled, in splits of the vocabulary, with live rows
+# that need more groups than all of the rows would
+@pytest.mark.parametrize("T,V,I,ignored", [(2200, 1300, 2560, 0), (1100, 1700, 4600, 3), (1900, 1100, 1096, 2)])
+def test_splits_of_many_tiles(sq, T, V, I, ignored):
+    y = inputs.rng(T + 1).integers(0, V, T)
+    if ignored:
+        y[::ignored] = V
+    _check(sq, "bf16", T, V, I, T + I, y, out_dtype=BF16)
+
+
 # a 4-bit head's rows in groups: the last one of the gradient overlaps the one before it, the logits' in groups of 4096 with a
 # narrower last one, rows past a multiple of 8, and the target in each of these places
 @pytest.mark.parametrize("T,V,I", [(6, 2665, 704), (3, 33003, 64), (130, 33003, 64), (2, 40961, 96)])
