@@ -185,8 +185,10 @@ __host__ __device__ inline int ce_splits(int tiles, int stages) {
     return n < 64 ? n : 64;
   }
   int best = 1, least = 0x7FFFFFFF;
-  for (int s = 1; s <= 6 && s <= most && s * tiles <= kCeMostGroups; ++s) {
-    const int cost = (s * tiles + kCUs - 1) / kCUs * ((stages + s - 1) / s) * 16 + s * tiles;
+#pragma unroll                            // divisions by constants: every workgroup works this out
+  for (int s = 1; s <= 6; ++s) {
+    if (s > most || s * tiles > kCeMostGroups) continue;
+    const int cost = (s * tiles + kCUs - 1) / kCUs * (int)((unsigned)(stages + s - 1) / s) * 16 + s * tiles;
     if (cost < least) {
       least = cost;
       best = s;
