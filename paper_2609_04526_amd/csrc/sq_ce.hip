@@ -1075,8 +1075,10 @@ inline int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 // round of 256 x 128 and 256 x 64 tiles takes 0.58 and 0.36 of one of 256 x 256
 // tiles, and a last round from three quarters of a whole one on, as it is filled.
 // us of the forward with 64-, 128- and 256-token tiles, bf16: 1024 tokens of
-// 16384 x 4096 166, 136, 122; 1024 of 8192 x 4096 87, 73, 95; 250 of 72471 x 4960
-// 402, 314, 349; 420 of 36320 x 544 45, 45, 52; 174 of 7717 x 736 15, 19, 29.
+// 16384 x 4096 146, 123, 115; 180 of 72000 x 5120 277, 252, 279; 300 of 131072 x 4096
+// 494, 434, 455; 420 of 36320 x 544 41, 44, 49; 130 of 40000 x 1024 26, 34, 32.  From
+// codes: 180 of 72000 x 5120 165, 227, 224; 300 of 131072 x 4096 417, 444, 448.  The
+// rule is the same for both, so that codes give bit for bit what their bf16 values do.
 int ce_tokens(int64_t T, int64_t vt) {
   auto cost = [&](int bt, double round) {
     const int64_t tiles = vt * (up(T, bt) / bt), last = tiles % kCUs;
@@ -1165,6 +1167,10 @@ CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
   return p;
 }
 
+// 256 x 64 tiles: where there are more than CUs two workgroups share one, with two
+// stages each, otherwise one with three (us of the forward, bf16, three stages against
+// two: 300 tokens of 50000 x 4096 226, 202; 420 of 36320 x 544 46, 42; 250 of 8000 x
+// 4096 36, 42; 40 of 50000 x 2048 36, 39).
 template <int MODE>
 int ce_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
   if (blocks == 0) return 0;
@@ -1174,7 +1180,8 @@ int ce_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
     else if (bt == 128) hipLaunchKernelGGL((ce_kernel<MODE, 128, 256, 2, 4, 3>), grid, block, 0, s, g);
     else hipLaunchKernelGGL((ce_kernel<MODE, 256, 256, 2, 4, 2>), grid, block, 0, s, g);
   } else {
-    if (bt == 64) hipLaunchKernelGGL((ce_kernel<MODE, 256, 64, 8, 1, 3>), grid, block, 0, s, g);
+    if (bt == 64 && blocks > kCUs) hipLaunchKernelGGL((ce_kernel<MODE, 256, 64, 8, 1, 2>), grid, block, 0, s, g);
+    else if (bt == 64) hipLaunchKernelGGL((ce_kernel<MODE, 256, 64, 8, 1, 3>), grid, block, 0, s, g);
     else if (bt == 128) hipLaunchKernelGGL((ce_kernel<MODE, 256, 128, 4, 2, 3>), grid, block, 0, s, g);
     else hipLaunchKernelGGL((ce_kernel<MODE, 256, 256, 2, 4, 2>), grid, block, 0, s, g);
   }
