@@ -152,18 +152,19 @@ struct Ds8Args {
   int groups, rows_per;
 };
 
-// Conversion of 8 kept values to bf16: int8 as (q + 128) s - 128 s, exact in
-// one fused step; E4M3 by the scaled converts.
+// Conversion of 8 kept values to bf16, as unpack8 does it: int8 as q s, whose 7 bits
+// pack_hi16 keeps; E4M3 by the scaled converts.  ((q + 128) s - 128 s would be one
+// instruction shorter, but 128 s overflows where q s does not: under byte 248, which
+// blocks of 2^127 and more have.)
 template <int ACT>
 __device__ __forceinline__ u32x4 kept8(u32x2 q, uint32_t sb) {
   u32x4 r;
   if constexpr (ACT == kInt8) {
-    const float s = e8m0_to_f32(sb), z = -128.0f * s;
+    const float s = e8m0_to_f32(sb);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t u = q[h] ^ 0x80808080u;
-      const float a = __builtin_fmaf((float)(u & 0xFFu), s, z), b = __builtin_fmaf((float)((u >> 8) & 0xFFu), s, z);
-      const float c = __builtin_fmaf((float)((u >> 16) & 0xFFu), s, z), d = __builtin_fmaf((float)(u >> 24), s, z);
+      const float a = (float)((int)(q[h] << 24) >> 24) * s, b = (float)((int)(q[h] << 16) >> 24) * s;
+      const float c = (float)((int)(q[h] << 8) >> 24) * s, d = (float)((int)q[h] >> 24) * s;
       r[2 * h] = pack_hi16(a, b);
       r[2 * h + 1] = pack_hi16(c, d);
     }
