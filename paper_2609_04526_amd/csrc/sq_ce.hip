@@ -304,7 +304,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
       has |= (uint32_t)valid << j;
       if constexpr (MODE == kCeGrad) {
         c_of[j] = valid ? g.dloss[t[j]] : 0.0f;
-        z_of[j] = valid ? g.lse[t[j]] * kLog2E : 0.0f;
+        z_of[j] = valid ? g.lse[t[j]] : 0.0f;
       }
     }
   }
@@ -643,18 +643,21 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
             }
           if (!kPlain && at >= 0) g.tlogit[row] = l * g.ws2;
           top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-          top = fmaxf(top, __shfl_xor(top, 32)) * g.ws2;
-          const float ref = top == -INFINITY ? 0.0f : top * kLog2E;   // nothing to sum: exp(-inf) = 0
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float ref = top == -INFINITY ? 0.0f : top;     // nothing to sum: exp(-inf) = 0
           const float scale = g.ws2 * kLog2E;
 #pragma unroll
           for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], scale, -ref));
+              // the distance first: scaled by log2(e) before, logits from 1e4 on lost
+              // their last bits and those from 2.36e38 on were infinite
+              const float p = __builtin_amdgcn_exp2f((acc[i][j][r] - ref) * scale);
               sums[r & 3] += kPlain || i * 32 + 8 * (r >> 2) + (r & 3) < end ? p : 0.0f;
             }
           sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
           sum += __shfl_xor(sum, 32);
+          top *= g.ws2;
         };
         if (plain) stats(std::true_type{});
         else stats(std::false_type{});
@@ -669,7 +672,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
         // rounding's error into dX: what it lost is kept, and added with the
         // target's row of W at the end (error against 64 bits 2.5e-3 -> 1.8e-3, of
         // which 1.7e-3 is dX's own rounding to bf16).
-        const float c = c_of[j], z = z_of[j], scale = g.ws2 * kLog2E;
+        const float c = c_of[j], z = z_of[j];
         SQ_LDS uint16_t* s = (SQ_LDS uint16_t*)lds + wave * WM * WN;
         const int cj = j * 32 + (lane & 31);
         auto grads = [&](auto PLAIN) {
@@ -683,7 +686,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ce_kernel(CeArgs g) {
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const int v = i * 32 + 8 * q + r;
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + r], scale, -z));
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + r], g.ws2, -z) * kLog2E);
                 e[r] = kPlain ? c * p : valid && v < end ? c * (p - (v == at ? 1.0f : 0.0f)) : 0.0f;
               }
               u32x2 pair;
