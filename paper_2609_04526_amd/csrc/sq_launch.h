@@ -160,6 +160,10 @@ int applied_launch(int fmt, int64_t n, const uint8_t* before, const uint8_t* aft
 int rollback_launch(int fmt, int64_t n, uint8_t* scales, const float* applied, hipStream_t s);
 int byte_diff_launch(int64_t n, const uint8_t* a, const uint8_t* b, uint64_t* counts, hipStream_t s);
 
+// Workgroups in x of a launch whose count goes with the tokens.  One that asks for
+// 2^32 work-items in a dimension, or for more, is cut short without an error.
+constexpr int64_t kGroupsX = int64_t(1) << 22;   // of up to 512 threads: 2^31 work-items
+
 // Tokens to experts and back (sq_moe.hip).  routed: device pointer to the
 // number of routed pairs (the sort's offsets[E]).
 constexpr int kMoeChunk = 4096;           // pairs per workgroup of the sort over many pairs

@@ -274,13 +274,20 @@ __device__ __forceinline__ void store8(const float (&v)[8], void* base, int64_t 
   }
 }
 
+// Workgroups by token, on in y where x is full.
+__device__ __forceinline__ int64_t group_at() { return (int64_t)blockIdx.y * kGroupsX + blockIdx.x; }
+inline dim3 groups_of(int64_t n) {
+  return dim3((unsigned)(n < kGroupsX ? n : kGroupsX), (unsigned)((n + kGroupsX - 1) / kGroupsX));
+}
+
 // Workgroup t: row t of X (units 16-byte pieces) to the slots of its K pairs;
 // dropped pairs' rows are zeros.  Bound by memory: 4096 x 2048 bf16 to 8 rows each
 // 22.9 us, 6.6 TB/s of reads and writes.
 __global__ __launch_bounds__(256) void moe_gather_kernel(const u32x4m* __restrict__ X, const int* __restrict__ slot,
-                                                         const int* __restrict__ routed, int K, int units, int64_t N,
-                                                         u32x4m* __restrict__ Xs) {
-  const int64_t t = blockIdx.x;
+                                                         const int* __restrict__ routed, int64_t T, int K, int units,
+                                                         int64_t N, u32x4m* __restrict__ Xs) {
+  const int64_t t = group_at();
+  if (t >= T) return;
   const int R = *routed;
   for (int c = threadIdx.x; c < units; c += blockDim.x) {
     const u32x4m v = X[t * units + c], zero = {0u, 0u, 0u, 0u};
@@ -304,9 +311,10 @@ constexpr int kPairs = 8;
 template <bool YB, bool OB, bool WEIGHTED, bool STREAM>
 __global__ __launch_bounds__(256) void moe_combine_kernel(const void* __restrict__ Ys, const int* __restrict__ slot,
                                                           const int* __restrict__ routed,
-                                                          const float* __restrict__ weights, int K, int H, int64_t N,
-                                                          void* __restrict__ out) {
-  const int64_t t = blockIdx.x;
+                                                          const float* __restrict__ weights, int64_t T, int K, int H,
+                                                          int64_t N, void* __restrict__ out) {
+  const int64_t t = group_at();
+  if (t >= T) return;
   const uint32_t R = (uint32_t)min((int64_t)max(*routed, 0), N);
   for (int c = threadIdx.x * 8; c < H; c += blockDim.x * 8) {
     float acc[8];
@@ -352,7 +360,7 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const void* __rest
   __shared__ float s_part[4][kPairs];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
-  const int64_t t = (int64_t)blockIdx.x * kTokens + wave_u / WAVES;
+  const int64_t t = group_at() * kTokens + wave_u / WAVES;
   const int in = (wave % WAVES) * 64 + lane;                  // of the token's 64 WAVES lanes
   const uint32_t R = (uint32_t)min((int64_t)max(*routed, 0), N);
   for (int k0 = 0; k0 < K; k0 += kPairs) {
@@ -461,21 +469,21 @@ int moe_sort_launch(int64_t T, int K, int E, const void* ids, int id_bytes, int3
 int moe_gather_launch(int64_t T, int K, int H, int bf16, const void* X, const int32_t* slot, const int32_t* routed,
                       void* Xs, hipStream_t s) {
   const int units = H / (bf16 ? 8 : 4);
-  hipLaunchKernelGGL(moe_gather_kernel, dim3((unsigned)T), dim3(row_threads(units)), 0, s,
-                     static_cast<const u32x4m*>(X), slot, routed, K, units, T * K, static_cast<u32x4m*>(Xs));
+  hipLaunchKernelGGL(moe_gather_kernel, groups_of(T), dim3(row_threads(units)), 0, s,
+                     static_cast<const u32x4m*>(X), slot, routed, T, K, units, T * K, static_cast<u32x4m*>(Xs));
   return ok();
 }
 
 int moe_combine_launch(int64_t T, int K, int H, const void* Ys, int y_bf16, const int32_t* slot, const int32_t* routed,
                        const float* weights, void* out, int out_bf16, hipStream_t s) {
-  const dim3 grid((unsigned)T), block(row_threads(H / 8));
+  const dim3 grid = groups_of(T), block(row_threads(H / 8));
   const bool stream = T * K * H * (y_bf16 ? 2 : 4) >= kMoeStreamBytes;
   auto go = [&](auto YB, auto OB, auto W) {
     constexpr bool y = decltype(YB)::value, o = decltype(OB)::value, w = decltype(W)::value;
     if (stream)
-      hipLaunchKernelGGL((moe_combine_kernel<y, o, w, true>), grid, block, 0, s, Ys, slot, routed, weights, K, H, T * K, out);
+      hipLaunchKernelGGL((moe_combine_kernel<y, o, w, true>), grid, block, 0, s, Ys, slot, routed, weights, T, K, H, T * K, out);
     else
-      hipLaunchKernelGGL((moe_combine_kernel<y, o, w, false>), grid, block, 0, s, Ys, slot, routed, weights, K, H, T * K, out);
+      hipLaunchKernelGGL((moe_combine_kernel<y, o, w, false>), grid, block, 0, s, Ys, slot, routed, weights, T, K, H, T * K, out);
     return ok();
   };
   using Y = std::true_type;
@@ -491,10 +499,10 @@ int moe_combine_bwd_launch(int64_t T, int K, int H, const void* dOut, int d_bf16
   auto go = [&](auto DB, auto YB, auto GB) {
     constexpr bool d = decltype(DB)::value, y = decltype(YB)::value, g = decltype(GB)::value;
     if (T >= kMoeWaveTokens)
-      hipLaunchKernelGGL((moe_combine_bwd_kernel<d, y, g, 1>), dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, dOut, Ys,
+      hipLaunchKernelGGL((moe_combine_bwd_kernel<d, y, g, 1>), groups_of((T + 3) / 4), dim3(256), 0, s, dOut, Ys,
                          slot, routed, weights, T, K, H, T * K, dYs, dw);
     else
-      hipLaunchKernelGGL((moe_combine_bwd_kernel<d, y, g, 4>), dim3((unsigned)T), dim3(256), 0, s, dOut, Ys, slot, routed,
+      hipLaunchKernelGGL((moe_combine_bwd_kernel<d, y, g, 4>), groups_of(T), dim3(256), 0, s, dOut, Ys, slot, routed,
                          weights, T, K, H, T * K, dYs, dw);
     return ok();
   };
