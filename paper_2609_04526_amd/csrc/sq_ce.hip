@@ -829,8 +829,9 @@ __global__ __launch_bounds__(128) void ce_dx_kernel(const float* __restrict__ su
                                                     int bm, int tiles_n, int stages, float f, float ws2, CeRest rest,
                                                     void* __restrict__ dX) {
   const int live = count ? min(*count, T) : T;
-  const int b = (int)blockIdx.x, h = ((int)blockIdx.y * 128 + (int)threadIdx.x) * 8;
-  if (h >= H) return;
+  const int64_t at = (int64_t)blockIdx.z * kGroupsX + blockIdx.x;
+  const int b = (int)at, h = ((int)blockIdx.y * 128 + (int)threadIdx.x) * 8;
+  if (at >= T || h >= H) return;
   auto put = [&](int t, const float (&v)[8]) {
     if constexpr (BF16) {
       u32x4 w;
@@ -1127,6 +1128,8 @@ CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
     }
     most = most < by_w ? most : by_w;
   }
+  const int64_t by_grid = kGroupsX / (up(T, p.bt) / p.bt) * 256;   // the tiles of a launch
+  most = most < by_grid ? most : by_grid;
   most = most / 256 * 256 > 256 ? most / 256 * 256 : 256;
   p.pieces = (int)((V + most - 1) / most);
   p.piece = up((V + p.pieces - 1) / p.pieces, 256);
@@ -1204,7 +1207,9 @@ int ce_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
 constexpr int kCeCodesTokens = 64, kCeCodesMost = 4096;
 
 bool ce_codes(int head, int64_t T, int64_t V, int64_t H) {
-  return head == kMX && H % 512 == 0 && T > 0 && T <= kCeCodesMost && ce_plan(false, false, T, V, H).splits == 1;
+  if (head != kMX || H % 512 != 0 || T < 1 || T > kCeCodesMost) return false;
+  const CePlan p = ce_plan(false, false, T, V, H);
+  return p.splits == 1 && p.pieces == 1;
 }
 
 template <int MODE>
@@ -1257,6 +1262,11 @@ int ce_grad_go(int head, const CePiece& c, const float* lse, const float* dloss,
   if (tail.rows == 0) go(ce_grad_kernel<kCeBf16>);
   else head == kMX ? go(ce_grad_kernel<kMX>) : go(ce_grad_kernel<kNV>);
   return ok();
+}
+
+// Workgroups of the gradient's last step.
+inline dim3 ce_dx_grid(int T, int H) {
+  return dim3((unsigned)(T < kGroupsX ? T : kGroupsX), (unsigned)((H + 1023) / 1024), (unsigned)((T + kGroupsX - 1) / kGroupsX));
 }
 
 // The last step of the gradient, for each head and output type.
@@ -1417,7 +1427,7 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   if (gemm_dx_grouped(head, p.width, H, p.groups, e, 0, s) != 0) return -1;
   const CeRest rest{codes, scales, lost, dtail, p.main, p.tail};
   auto finish = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)((H + 1023) / 1024)), dim3(128), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, y, y_bytes,
+    hipLaunchKernelGGL(kernel, ce_dx_grid(T, H), dim3(128), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, y, y_bytes,
                        T, V, H, 0, 0, 0, 1.0f, ws2, rest, dX);
     return ok();
   };
@@ -1536,7 +1546,7 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
   }
   const CeRest rest{W, scales, g.tlogit, nullptr, V, 0};
   auto finish = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)((H + 1023) / 1024)), dim3(128), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, y, y_bytes, T, V,
+    hipLaunchKernelGGL(kernel, ce_dx_grid(T, H), dim3(128), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, y, y_bytes, T, V,
                        H, p.bx, (int)tn, g.split_stages, ws2, ws2, rest, dX);
     return ok();
   };
