@@ -553,7 +553,7 @@ int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, const void* d
  * sq_act_pack: X bf16 [T, I] -> codes_out uint8 [T, I], scales_out uint8
  *   [T, I/32].  sq_act_unpack: the values x^ as bf16 [T, I] (q 2^k is exact in
  *   bf16; values below its range are rounded to nearest even).  I % 32 == 0; X
- *   and codes 16-byte aligned; T*I <= 2^40.
+ *   and codes 16-byte aligned; T*I <= 2^36.
  *
  * sq_bwd_dscale_act8: sq_bwd_dscale with x^ in the place of X, bit for bit what
  *   that call computes for the unpacked x^.  I % 32 == 0 for either weight

@@ -98,7 +98,8 @@ bool act_ok(int act) { return act == SQ_ACT_INT8 || act == SQ_ACT_E4M3; }
 
 int check_act(int act, int64_t T, int64_t I, const void* X, const uint8_t* codes, const uint8_t* scales) {
   if (!act_ok(act)) return SQ_ERR_ARG;
-  if (T < 0 || I < 1 || T > kDimMax || I > kDimMax || I % 32 != 0 || T > (int64_t(1) << 40) / I) return SQ_ERR_SHAPE;
+  // 32 values a work-item: a launch of 2^32 of them would be cut short
+  if (T < 0 || I < 1 || T > kDimMax || I > kDimMax || I % 32 != 0 || T > (int64_t(1) << 36) / I) return SQ_ERR_SHAPE;
   if (T > 0 && (!X || !codes || !scales)) return SQ_ERR_ARG;
   return aligned(X, 16) && aligned(codes, 16) ? SQ_OK : SQ_ERR_ALIGN;
 }

@@ -109,6 +109,11 @@ def test_act_refusals(lib, name, kw, status):
     assert _call(getattr(lib, name), args, dict(T=0, a=None, b=None, c=None)) == 0
 
 
+@pytest.mark.parametrize("name", ["sq_act_pack", "sq_act_unpack"])
+@pytest.mark.parametrize("T,I", [(1 << 21, 1 << 16), ((1 << 26) + 1, 1 << 10), (1 << 30, 128)])
+def test_more_values_than_a_launch_holds(lib, name, T, I):
+    assert getattr(lib, name)(0, T, I, FAKE, FAKE, FAKE, None) == SHAPE
+
 def test_act_alignment_of_the_second_plane(lib):
     assert lib.sq_act_pack(0, 16, 64, FAKE, OFF, FAKE, None) == ALIGN
     assert lib.sq_act_unpack(0, 16, 64, FAKE, FAKE, OFF, None) == ALIGN
