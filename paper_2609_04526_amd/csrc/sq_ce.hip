@@ -1135,11 +1135,11 @@ CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
   p.piece = up((V + p.pieces - 1) / p.pieces, 256);
   p.pieces = (int)((V + p.piece - 1) / p.piece);
   p.ld = (int)(p.piece < V ? p.piece : up(V, 64));
-  // Few tiles and a long sum: split it, at least 4 stages each (bf16, whole against
+  // Few tiles (64-token ones then, by ce_tokens) and a long sum: split it, at least 4 stages each (bf16, whole against
   // split: 4 tokens of 1136 x 7296 178, 53 us; 555 of 3891 x 4864 351, 138).
   const int64_t tiles = vt * (up(T, p.bt) / p.bt), stages = (H + kBK - 1) / kBK;
   p.splits = 1;
-  if (p.pieces == 1 && 2 * tiles <= kCUs && stages >= kCeSplitStages) {
+  if (p.pieces == 1 && p.bt == 64 && 2 * tiles <= kCUs && stages >= kCeSplitStages) {
     const int64_t by_cu = kCUs / tiles, by_stages = stages / 4, n = by_cu < by_stages ? by_cu : by_stages;
     p.splits = (int)(n < 8 ? n : 8);
   }
@@ -1181,7 +1181,9 @@ template <int MODE>
 int ce_go(const CeArgs& g, int bt, int64_t blocks, hipStream_t s) {
   if (blocks == 0) return 0;
   const dim3 grid((unsigned)blocks), block(512);
-  if constexpr (MODE == kCeDx) {
+  if constexpr (MODE == kCeLogits) {                          // of 64 tokens, as many as the CUs at most
+    hipLaunchKernelGGL((ce_kernel<MODE, 256, 64, 8, 1, 3>), grid, block, 0, s, g);
+  } else if constexpr (MODE == kCeDx) {
     if (bt == 64) hipLaunchKernelGGL((ce_kernel<MODE, 64, 256, 1, 8, 3>), grid, block, 0, s, g);
     else if (bt == 128) hipLaunchKernelGGL((ce_kernel<MODE, 128, 256, 2, 4, 3>), grid, block, 0, s, g);
     else hipLaunchKernelGGL((ce_kernel<MODE, 256, 256, 2, 4, 2>), grid, block, 0, s, g);
