@@ -552,7 +552,8 @@ int sq_moe_combine_bwd(int64_t T, int64_t K, int64_t E, int64_t H, const void* d
  *
  * sq_act_pack: X bf16 [T, I] -> codes_out uint8 [T, I], scales_out uint8
  *   [T, I/32].  sq_act_unpack: the values x^ as bf16 [T, I] (q 2^k is exact in
- *   bf16; values below its range are rounded to nearest even).  I % 32 == 0; X
+ *   bf16; values below its range are rounded to nearest even, and E4M3's of 1.9375 *
+ *   2^127 and more, which round to 2^128, read as infinities).  I % 32 == 0; X
  *   and codes 16-byte aligned; T*I <= 2^36.
  *
  * sq_bwd_dscale_act8: sq_bwd_dscale with x^ in the place of X, bit for bit what
@@ -611,7 +612,9 @@ size_t sq_bwd_dscale_act8_batched_workspace(int64_t E, int64_t T, int64_t I);
  *   gradient that reaches each token's loss) -> dX [T, I] in dx_dtype.  The
  *   logits are formed again in pieces of the vocabulary; their gradients are
  *   rounded to bf16 for the product with W, as the layers' dY is, and summed in
- *   fp32 over all pieces.
+ *   fp32 over all pieces; the target's keeps its fp32 value.  In an fp32 dX that
+ *   rounding is most of the error: 1e-5 of its norm where the targets lead, 1e-3
+ *   where other entries do.  p is formed from lse as it is held, 2^-24 of it off.
  * I % 8 == 0 (SQ_HEAD_BF16) or I % B == 0; V >= 1; T*I*2 below 2 GiB.  codes
  * 4-byte, W and dX 16-byte aligned.  workspace: 256-byte aligned, of at least
  * sq_ce_fwd_workspace / sq_ce_bwd_workspace bytes (0 when T = 0), contents

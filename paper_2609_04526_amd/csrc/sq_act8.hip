@@ -355,8 +355,9 @@ __global__ __launch_bounds__(64 * WGM * WGN) void ds8_tile_kernel(Ds8Args g) {
 // of the tiles as one pipeline of stages in two LDS buffers: the copies go two
 // stages ahead of the products, across the ends of tiles, and every barrier waits
 // for all loads.  Tiles are 256 x 256, a wave's part 128 x 64: of the shapes that
-// fit the registers the one that reads the fewest operand bytes from LDS, which
-// bounds smaller ones.
+// fit the registers the one that reads the fewest operand bytes from LDS.  Rows that
+// are picked and rows in place take the same time (128 experts of 768 x 2048 over
+// 32768 rows 140 and 146 us).
 constexpr int kRowsBM = 256, kRowsBN = 256;
 constexpr int kTakenStep = 64;          // a queue's count in a line of its own
 constexpr int kQueueUnits = 1040;       // of one queue at most: 8192 experts, or 64 units and more of fewer
@@ -862,10 +863,10 @@ int ds8_splits(int T, int O, int I) {
 // turn its 8 bits into bf16: beyond 2048 outputs, once the product is long enough
 // to pay for another launch (some 20 us), x^ goes through the workspace in bf16 to
 // the bf16 product.  MXFP4, us, tiles from 8 bits (int8, E4M3) against x^ first:
-// 8192 tokens, 14336 x 4096: 926, 807 against 737, 733; 512 tokens of it: 87, 79
-// against 75, 74; 4096 tokens, 4096 x 4096: 122, 111 against 112, 110.  And where
-// the rule keeps the tiles: 8192 tokens, 2048 x 4096: 124, 114 against 121, 120;
-// 512 tokens, 4096 x 4096: 22, 21 against 24, 25.
+// 8192 tokens, 14336 x 4096: 855, 799 against 730, 726; 512 tokens of it: 73, 69
+// against 65, 65; 4096 tokens, 4096 x 4096: 116, 110 against 108, 108.  And where
+// the rule keeps the tiles: 8192 tokens, 2048 x 4096: 118, 112 against 119, 119;
+// 512 tokens, 4096 x 4096: 20, 19 against 23, 22.
 bool ds8_unpacks(int T, int O, int I) {
   return O > 2048 && (int64_t)T * O >= int64_t(24000000000) / I;
 }

@@ -23,9 +23,9 @@
 //
 // The three products bound it (the forward's logits, the same again, dX), and the
 // matrix cores' power bounds them: 4096 tokens of 131072 x 4096 bf16 10.0-10.6 ms,
-// 1.24-1.32 PFLOP/s; 1999 tokens, 40% of them ignored, of 50001 x 4096 MXFP4 1.33 ms.
-// One token of 131072 x 4096 bf16 takes 530 us, three reads of the head at 6.1 TB/s,
-// of MXFP4 245.
+// 1.24-1.32 PFLOP/s; 1999 tokens, 40% of them ignored, of 50001 x 4096 MXFP4 1.27 ms.
+// One token of 131072 x 4096 bf16 takes 538 us, three reads of the head at 6.0 TB/s,
+// of MXFP4 226.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -1082,7 +1082,9 @@ inline int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 // 16384 x 4096 146, 123, 115; 180 of 72000 x 5120 277, 252, 279; 300 of 131072 x 4096
 // 494, 434, 455; 420 of 36320 x 544 41, 44, 49; 130 of 40000 x 1024 26, 34, 32.  From
 // codes: 180 of 72000 x 5120 165, 227, 224; 300 of 131072 x 4096 417, 444, 448.  The
-// rule is the same for both, so that codes give bit for bit what their bf16 values do.
+// rule is the same for both, though codes would gain from 64 more often: then tiles
+// of up to 128 tokens join the sums of codes in the order of their bf16 values', and
+// give the same bits (256-token ones have their waves laid out otherwise).
 int ce_tokens(int64_t T, int64_t vt) {
   auto cost = [&](int bt, double round) {
     const int64_t tiles = vt * (up(T, bt) / bt), last = tiles % kCUs;
@@ -1135,8 +1137,9 @@ CePlan ce_plan(bool bwd, bool four_bit, int64_t T, int64_t V, int64_t H) {
   p.piece = up((V + p.pieces - 1) / p.pieces, 256);
   p.pieces = (int)((V + p.piece - 1) / p.piece);
   p.ld = (int)(p.piece < V ? p.piece : up(V, 64));
-  // Few tiles (64-token ones then, by ce_tokens) and a long sum: split it, at least 4 stages each (bf16, whole against
-  // split: 4 tokens of 1136 x 7296 178, 53 us; 555 of 3891 x 4864 351, 138).
+  // Few tiles (64-token ones then, by ce_tokens) and a long sum: split it, at least 4
+  // stages each (bf16, us of loss and gradient, whole against split: 4 tokens of 1136
+  // x 7296 104, 45; 300 of 3891 x 4864 108, 85; 100 of 8000 x 4096 82, 69).
   const int64_t tiles = vt * (up(T, p.bt) / p.bt), stages = (H + kBK - 1) / kBK;
   p.splits = 1;
   if (p.pieces == 1 && p.bt == 64 && 2 * tiles <= kCUs && stages >= kCeSplitStages) {
@@ -1299,9 +1302,9 @@ struct CeFew {
 
 // One product over many rows would take strips or tiles made for a layer's few; as
 // a grouped one over groups of 4096 rows it takes the grouped products' tiles
-// (131072 x 4096 MXFP4, us of loss and gradient, one product against groups: 1
-// token 318, 261; 64 tokens 503, 328; 128 tokens 694, 575; 256 tokens 939, 1063;
-// NVFP4 64 tokens 493, 439; 128 tokens 821, 663).
+// (131072 x 4096, one product against groups, us of NVFP4's loss and gradient: 1
+// token 297, 311; 64 tokens 442, 413; 128 tokens 721, 593; 256 tokens 966, 1104; of
+// MXFP4's gradient: 1 token 180, 150; 64 tokens 275, 206).
 constexpr int kCeGroupTokens = 128, kCeGroupRows = 4096, kCeGroupFrom = 8 * kCeGroupRows;
 
 CeFew ce_few_plan(bool bwd, int64_t T, int64_t V, int64_t H) {
