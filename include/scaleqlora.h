@@ -634,6 +634,113 @@ int sq_ce_bwd(int head, int64_t T, int64_t V, int64_t I, const void* X, const vo
               const void* targets, int target_bytes, const float* lse, const float* dloss, void* dX, int dx_dtype,
               void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Activations in the layer's own 4-bit storage, and the products of two 4-bit
+ * operands: what the deployed layer computes where its input is quantised too.
+ *
+ * sq_act4_pack: X bf16 [T, I] -> codes_out uint8 [T, I/2], scales_out uint8
+ *   [T, G].  Scales and codes are those of rtn_quantize with SQ_TIE_EVEN (for
+ *   NVFP4 with the given ws2 > 0: activations share one calibrated scalar), but
+ *   a block that holds an Inf or NaN gets the NaN scale (0xFF; 0x7F) and zero
+ *   codes, and reads as NaN.
+ * sq_act4_unpack: the values x^ = code * eff as bf16 [T, I], rounded to nearest
+ *   even (exact for MXFP4 but below bf16's range and from 2^128 on, where they
+ *   read as infinities).  The backward products of a layer whose forward took
+ *   x^ are the layer's own: sq_bwd_dx, and sq_bwd_dscale with x^ for X.
+ *   X 16-byte, codes 4-byte aligned; T*I <= 2^36.
+ *
+ * sq_fwd_act4: Y[t,o] = sum_i x^[t,i] W[o,i] from x_codes [T, I/2], x_scales
+ *   [T, G] and the layer's codes [O, I/2], scales [O, G]; y_dtype as sq_fwd's.
+ *   Products are exact and sums fp32.  MXFP4 runs on the matrix cores' scaled
+ *   4-bit products; an NVFP4 x^ goes through the workspace in bf16 (without
+ *   x_ws2, exact) to sq_fwd, with x_ws2 * ws2 on the fp32 sums.  Both scalars
+ *   and their product finite and > 0 (ignored for MXFP4).
+ * sq_fwd_act4_batched: the same for E stacked experts (codes [E, O, I/2],
+ *   scales [E, O, G]; MXFP4 only, NVFP4 returns SQ_ERR_UNIMPLEMENTED): expert e
+ *   has rows [offsets[e], offsets[e+1]) of Y [N, O], offsets int32 [E+1] on the
+ *   DEVICE (as sq_moe_sort writes them).  Row s of Y is row rows[s] of x^ [T, I]
+ *   (sq_moe_sort's token) times the expert's weight, or row s with rows NULL
+ *   (then N == T).  Rows that no expert has, before offsets[0] and from
+ *   offsets[E] on, are zeros; a row number outside 0 .. T-1 reads as a row of
+ *   zeros, and offsets are held to 0 .. N.  E <= 8192; (N/16 + min(E, N) + 1)
+ *   ceil(O/16) <= 2^22.
+ * x_codes and codes 16-byte, x_scales and scales 4-byte aligned; workspace: at
+ * least the bytes of the _workspace call, 256-byte aligned (NULL where that is
+ * 0), contents irrelevant.  Deterministic.
+ */
+int sq_act4_pack(int fmt, int64_t T, int64_t I, const void* X, float ws2, uint8_t* codes_out, uint8_t* scales_out, void* stream);
+int sq_act4_unpack(int fmt, int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, float ws2, void* X, void* stream);
+size_t sq_fwd_act4_workspace(int fmt, int64_t T, int64_t O, int64_t I);
+int sq_fwd_act4(int fmt, int64_t T, int64_t O, int64_t I, const uint8_t* x_codes, const uint8_t* x_scales, float x_ws2,
+                const uint8_t* codes, const uint8_t* scales, float ws2, void* Y, int y_dtype, void* workspace,
+                size_t workspace_bytes, void* stream);
+size_t sq_fwd_act4_batched_workspace(int fmt, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I);
+int sq_fwd_act4_batched(int fmt, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I, const uint8_t* x_codes,
+                        const uint8_t* x_scales, const int32_t* rows, const int32_t* offsets, const uint8_t* codes,
+                        const uint8_t* scales, void* Y, int y_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Distillation of a language-model head from a teacher's top logits, in the
+ * place of sq_ce_fwd / sq_ce_bwd where a teacher answers.  The teacher gives K
+ * entries per token: ids int32 or int64 [T, K] (id_bytes 4 or 8) and its logits
+ * fp32 or bf16 [T, K].  With tau = temperature and l the head's logits:
+ *
+ *   s[t,v]  = l[t,v] / tau               lse[t] = log sum_v exp s[t,v]
+ *   q[t,k]  = softmax over the token's entries of logits[t,k] / tau
+ *   loss[t] = tau^2 sum_k q[t,k] (log q[t,k] - s[t, ids[t,k]] + lse[t])
+ *   dX[t]   = dloss[t] tau sum_v (exp(s[t,v] - lse[t]) - sum_{k: ids[t,k] = v} q[t,k]) W[v]
+ *
+ * An entry counts if its id lies in 0 .. V-1 (say -1 to leave it out) and its
+ * logit is not -inf; an id may come twice.  A token without an entry that
+ * counts is ignored: loss, lse and its row of dX are 0, and from 257 tokens on
+ * it takes no part in the products.  NaN and +inf among a token's logits
+ * give NaN.
+ *
+ * sq_distill_fwd -> loss, lse fp32 [T] and picked fp32 [T, K], the student's
+ *   s[t, ids[t,k]] (0 for entries that do not count).
+ * sq_distill_bwd: the same arguments with lse and picked as sq_distill_fwd wrote
+ *   them and dloss fp32 [T] -> dX [T, I] in dx_dtype.  Logit gradients are
+ *   rounded to bf16 for the product with W; those of the entries are formed in
+ *   fp32 from picked first.
+ * 1 <= K <= 256; 2^-20 <= temperature <= 2^20.  Head formats, shapes, alignment
+ * and workspace otherwise as sq_ce_fwd / sq_ce_bwd.  Deterministic.
+ */
+size_t sq_distill_fwd_workspace(int head, int64_t T, int64_t V, int64_t I);
+size_t sq_distill_bwd_workspace(int head, int64_t T, int64_t V, int64_t I);
+int sq_distill_fwd(int head, int64_t T, int64_t V, int64_t I, int64_t K, const void* X, const void* W, const uint8_t* scales,
+                   float ws2, const void* ids, int id_bytes, const void* logits, int logit_dtype, float temperature, float* loss,
+                   float* lse, float* picked, void* workspace, size_t workspace_bytes, void* stream);
+int sq_distill_bwd(int head, int64_t T, int64_t V, int64_t I, int64_t K, const void* X, const void* W, const uint8_t* scales,
+                   float ws2, const void* ids, int id_bytes, const void* logits, int logit_dtype, float temperature,
+                   const float* lse, const float* picked, const float* dloss, void* dX, int dx_dtype, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/*
+ * Embedding lookup of a table that is bf16 [V, I] (SQ_HEAD_BF16) or stored as the
+ * layer's weights (codes, scales, ws2), and the gradient of what is trained of it.
+ *
+ * sq_embed_fwd: out[t] = factor * W[ids[t]] in out_dtype, fp32 products rounded
+ *   once; ids int32 or int64 [T] (id_bytes 4 or 8).  An id outside 0 .. V-1 gives
+ *   a row of zeros and has no gradient.
+ * sq_embed_bwd: dW[v] = factor * sum over t with ids[t] = v of dOut[t], [V, I] in
+ *   dw_dtype, every row written (zeros for an id without a token).
+ * sq_embed_bwd_dscale: the gradient of a 4-bit table's effective scales, as
+ *   sq_bwd_dscale's: dS[v,g] = factor * sum_{j in g} code[v,j] sum_t dOut[t,j],
+ *   fp32 [V, G], every row written.
+ * dOut [T, I] fp32 or bf16 by d_dtype; fp32 sums in token order (an id with many
+ * tokens: in runs of 32 and more), the same bits on every run.  factor finite;
+ * I % 8 == 0 (bf16) or I % B == 0; W (bf16), out, dOut, dW, dS 16-byte, codes
+ * 4-byte aligned.  workspace: at least sq_embed_bwd_workspace bytes (0 when T =
+ * 0), 256-byte aligned, contents irrelevant.
+ */
+int sq_embed_fwd(int head, int64_t T, int64_t V, int64_t I, const void* ids, int id_bytes, const void* W, const uint8_t* scales,
+                 float ws2, float factor, void* out, int out_dtype, void* stream);
+size_t sq_embed_bwd_workspace(int64_t T, int64_t V, int64_t I);
+int sq_embed_bwd(int64_t T, int64_t V, int64_t I, const void* ids, int id_bytes, const void* dOut, int d_dtype, float factor,
+                 void* dW, int dw_dtype, void* workspace, size_t workspace_bytes, void* stream);
+int sq_embed_bwd_dscale(int fmt, int64_t T, int64_t V, int64_t I, const void* ids, int id_bytes, const void* dOut, int d_dtype,
+                        float factor, const uint8_t* codes, float* dS, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Human-readable name of a status code (static storage). */
 const char* sq_status_str(int status);
 

@@ -1,0 +1,347 @@
+// Activations in the layer's own 4-bit storage, and the products of two 4-bit
+// operands: one layer, or stacked experts on rows whose ranges stay on the device.
+//
+//   x^[t,i] = code[t,i] sx[t, i/B]          block scale and code as the layer's
+//   Y[t,o]  = sum_b sx[t,b] sw[o,b] sum_{i in b} cx[t,i] cw[o,i]
+//
+// MXFP4's blocks are the matrix cores' own: a scaled product takes 32 codes and
+// one E8M0 byte per lane and operand and sums exact products in fp32, at four times
+// the rate of bf16 from a quarter of its bytes.  NVFP4's blocks of 16 with E4M3
+// scales are not, so its kept rows go through bf16 (code x scale is exact there)
+// and the layer's bf16 product.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "sq_device.h"
+#include "sq_gemm_args.h"
+#include "sq_launch.h"
+#include "sq_rtn.h"
+
+namespace sq {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
+
+// ------------------------------------------------------------------ pack, unpack
+constexpr int kSteps = 4;               // pieces of 8 values in flight per lane
+
+// The codes and the scale byte of piece p (8 values; B / 8 adjacent lanes share a
+// block): exactly the re-quantiser's nearest rule, but a block that holds an Inf or
+// NaN gets the NaN scale and zero codes.
+template <int FMT>
+__device__ __forceinline__ void pack8(u32x4 h, float ws2, const RcpDivisor& wd, uint8_t* codes, uint8_t* scales, int64_t p) {
+  constexpr int kLanes = ScaleOperand<FMT>::kBlock / 8;
+  uint32_t am = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) am = max(am, max(h[k] & 0x7FFFu, (h[k] >> 16) & 0x7FFFu));
+  am = max(am, (uint32_t)__shfl_xor((int)am, 1));
+  if (kLanes == 4) am = max(am, (uint32_t)__shfl_xor((int)am, 2));
+  const bool bad = am >= 0x7F80u;
+  const float sixth = sixth_of(bad ? 0.0f : __uint_as_float(am << 16));
+  uint32_t byte;
+  float f = 0.0f;                                             // MXFP4: 2^-k
+  RcpDivisor ed{};
+  if constexpr (FMT == kMX) {
+    byte = mx_scale_byte(sixth, &f);
+  } else {
+    byte = e4m3_encode_rne_sat(div_exact(sixth, wd));
+    ed = make_rcp_divisor(__fmul_rn(e4m3_to_f32(byte), ws2));
+  }
+  uint32_t c = 0, sign = 0;
+  float q[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float x = __uint_as_float((h[k >> 1] >> (16 * (k & 1))) << 16);
+    if constexpr (FMT == kMX) q[k] = __fmul_rn(x, f);
+    else q[k] = ed.d == 0.0f ? 0.0f : div_exact(x, ed);
+    sign |= ((h[k >> 1] >> (12 + 16 * (k & 1))) & 8u) << (4 * k);
+  }
+  // nearest E2M1, ties to even, held to 6
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[0], q[1], 1.0f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[2], q[3], 1.0f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[4], q[5], 1.0f, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[6], q[7], 1.0f, 3);
+  c = bad ? 0u : (c & 0x77777777u) | sign;
+  reinterpret_cast<uint32_t*>(codes)[p] = c;
+  if (p % kLanes == 0) scales[p / kLanes] = (uint8_t)(bad ? (FMT == kMX ? 0xFFu : 0x7Fu) : byte);
+}
+
+template <int FMT>
+__global__ __launch_bounds__(256) void act4_pack_kernel(const u32x4* __restrict__ X, int64_t pieces, float ws2,
+                                                        uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  const int64_t p0 = (int64_t)blockIdx.x * (256 * kSteps) + threadIdx.x;
+  u32x4 w[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) w[i] = X[min(p0 + i * 256, pieces - 1)];
+  const RcpDivisor wd = make_rcp_divisor(ws2);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)                            // whole blocks: pieces is a multiple of their lanes
+    if (p0 + i * 256 < pieces) pack8<FMT>(w[i], ws2, wd, codes, scales, p0 + i * 256);
+}
+
+// 8 codes times their scale as bf16: exact but below bf16's range, at 2^128 and
+// more (infinite) and, with NVFP4, by the tensor's ws2 (rounded once).
+template <int FMT>
+__device__ __forceinline__ u32x4 unpack8(uint32_t c, uint32_t byte, float ws2) {
+  const float s = FMT == kMX ? e8m0_to_f32(byte) : e4m3_to_f32(byte);
+  const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3)};
+  u32x4 r;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float a = FMT == kMX ? v[k].x * s : v[k].x * s * ws2, b = FMT == kMX ? v[k].y * s : v[k].y * s * ws2;
+    r[k] = bits_of(__builtin_convertvector((f32x2{a, b}), bf16x2));
+  }
+  return r;
+}
+
+template <int FMT>
+__global__ __launch_bounds__(256) void act4_unpack_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                          int64_t pieces, float ws2, u32x4* __restrict__ X) {
+  const int64_t p0 = (int64_t)blockIdx.x * (256 * kSteps) + threadIdx.x;
+  uint32_t c[kSteps], b[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int64_t p = min(p0 + i * 256, pieces - 1);
+    c[i] = codes[p];
+    b[i] = scales[p / (ScaleOperand<FMT>::kBlock / 8)];
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+    if (p0 + i * 256 < pieces) X[p0 + i * 256] = unpack8<FMT>(c[i], b[i], ws2);
+}
+
+// ------------------------------------------------------------------ products
+struct Act4Args {
+  const uint8_t* x;         // codes [T, I/2] and scales [T, G] of the kept rows
+  const uint8_t* xs;
+  const uint8_t* w;         // codes [E, O, I/2] and scales [E, O, G]
+  const uint8_t* ws;
+  const int* rows;          // row of Y -> kept row, or null
+  const int* offsets;       // [E + 1], or null: one layer, rows [0, N)
+  void* out;                // [N, O]
+  int T, N, E, O, I, G;
+  int chunks;               // workgroups along the rows
+};
+
+// Which rows of Y a workgroup takes: chunk c of the experts' ranges, each cut into
+// chunks of `per` rows.  Ranges are held to 0 .. N.  e < 0: past the last chunk, then
+// n = c minus their number, and r0 .. r1 are the rows that no expert has at the end,
+// with those before the first range counted in front.
+struct Chunk {
+  int e, r0, r1, n;
+};
+__device__ __forceinline__ Chunk chunk_at(const int* offsets, int E, int N, int per, int c) {
+  if (!offsets) {
+    const int r0 = c * per;
+    return r0 < N ? Chunk{0, r0, min(r0 + per, N), 0} : Chunk{-1, N, N, c - (N + per - 1) / per};
+  }
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int e0 = 0; e0 < E; e0 += 64) {
+    const int e = e0 + lane;
+    const int a = e < E ? min(max(offsets[e], 0), N) : 0, b = e < E ? min(max(offsets[e + 1], 0), N) : 0;
+    const int n = max(b - a, 0), t = (n + per - 1) / per;
+    int upto = t;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int v = __shfl_up(upto, d);
+      upto += lane >= d ? v : 0;
+    }
+    const uint64_t in = __ballot(before + upto > c);
+    if (in) {
+      const int l = __builtin_ctzll(in);
+      const int at = __builtin_amdgcn_readfirstlane(c - before - __shfl(upto - t, l));
+      const int first = __builtin_amdgcn_readfirstlane(__shfl(a, l)), end = __builtin_amdgcn_readfirstlane(__shfl(b, l));
+      return Chunk{e0 + l, first + at * per, min(first + (at + 1) * per, end), 0};
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return Chunk{-1, min(max(offsets[E], 0), N), N, c - before};
+}
+
+// 4 consecutive outputs of one row.
+template <bool BF16>
+__device__ __forceinline__ void put4(void* out, size_t at, f32x4 v) {
+  if constexpr (BF16) {
+    u32x2 w;
+    w[0] = bits_of(__builtin_convertvector((f32x2{v[0], v[1]}), bf16x2));
+    w[1] = bits_of(__builtin_convertvector((f32x2{v[2], v[3]}), bf16x2));
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) = w;
+  } else {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
+  }
+}
+
+// Zeros in columns [o0, o0 + cols) of the rows that no expert has: this workgroup's
+// share of them, the chunks past the last taking turns.
+template <bool BF16>
+__device__ __forceinline__ void zero_rows(const Act4Args& g, const Chunk& c, int chunk, int o0, int cols) {
+  if (!g.offsets) return;
+  const int step = g.chunks - (chunk - c.n);                  // chunks past the last
+  const int front = min(min(max(g.offsets[0], 0), g.N), c.r0), all = front + c.r1 - c.r0;
+  const int quads = (min(o0 + cols, g.O) - o0) / 4;           // O is a multiple of 8
+  for (int r = c.n; r < all; r += step) {
+    const int row = r < front ? r : c.r0 + r - front;
+    for (int q = threadIdx.x; q < quads; q += blockDim.x) put4<BF16>(g.out, (size_t)row * g.O + o0 + 4 * q, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+  }
+}
+
+__device__ __forceinline__ i32x8 codes_operand(u32x4 c) {
+  return i32x8{(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0};
+}
+
+// Few rows: the weight's codes go from memory into the operand registers, each once
+// per chunk of 16 NT rows.  A workgroup takes 16 RM outputs; its waves share the
+// steps of 128 inputs in turn, and their sums meet in LDS in wave order.
+template <int RM, int NT, bool BF16>
+__global__ __launch_bounds__(512) void act4_thin_kernel(Act4Args g) {
+  constexpr int kWaves = 8, kUnroll = 4;
+  __shared__ f32x4 part[kWaves][RM * NT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int groups = (g.O + 16 * RM - 1) / (16 * RM);
+  const int o0 = (int)(blockIdx.x % groups) * 16 * RM;
+  const int chunk = (int)(blockIdx.x / groups);
+  const Chunk c = chunk_at(g.offsets, g.E, g.N, 16 * NT, chunk);
+  if (c.e < 0) {
+    zero_rows<BF16>(g, c, chunk, o0, 16 * RM);
+    return;
+  }
+  const int half = g.I / 2, steps = (g.I + 127) / 128, kb = lane >> 4;
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(g.w + (size_t)c.e * g.O * half, (uint32_t)((size_t)g.O * half));
+  const __amdgpu_buffer_rsrc_t rws = make_rsrc(g.ws + (size_t)c.e * g.O * g.G, (uint32_t)((size_t)g.O * g.G));
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(g.x, (uint32_t)((size_t)g.T * half));
+  const __amdgpu_buffer_rsrc_t rxs = make_rsrc(g.xs, (uint32_t)((size_t)g.T * g.G));
+  uint32_t w_row[RM], x_row[NT];
+#pragma unroll
+  for (int m = 0; m < RM; ++m) {
+    const int o = o0 + 16 * m + (lane & 15);
+    w_row[m] = o < g.O ? (uint32_t)o : kOOB;
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int r = c.r0 + 16 * j + (lane & 15);
+    x_row[j] = kOOB;
+    if (r < c.r1) {
+      const int t = g.rows ? g.rows[r] : r;
+      if (t >= 0 && t < g.T) x_row[j] = (uint32_t)t;
+    }
+  }
+  f32x4 acc[RM][NT];
+#pragma unroll
+  for (int m = 0; m < RM; ++m)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[m][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = wave; s0 < steps; s0 += kWaves * kUnroll) {
+    u32x4 wc[kUnroll][RM], xc[kUnroll][NT];
+    int wb[kUnroll][RM], xb[kUnroll][NT];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const uint32_t b = (uint32_t)(s0 + u * kWaves) * 4 + kb;      // this lane's block of 32 inputs
+      const bool in = b < (uint32_t)g.G;
+      auto load = [&](__amdgpu_buffer_rsrc_t rc, __amdgpu_buffer_rsrc_t rs, uint32_t row, u32x4& codes, int& byte) {
+        const bool live = in && row != kOOB;
+        codes = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, (int)(live ? row * (uint32_t)half + 16u * b : kOOB), 0, 0));
+        byte = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(live ? row * (uint32_t)g.G + b : kOOB), 0, 0);
+      };
+#pragma unroll
+      for (int m = 0; m < RM; ++m) load(rw, rws, w_row[m], wc[u][m], wb[u][m]);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) load(rx, rxs, x_row[j], xc[u][j], xb[u][j]);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int m = 0; m < RM; ++m)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes_operand(wc[u][m]), codes_operand(xc[u][j]), acc[m][j], 4, 4, 0,
+                                                                       wb[u][m], 0, xb[u][j]);
+  }
+#pragma unroll
+  for (int m = 0; m < RM; ++m)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) part[wave][m * NT + j][lane] = acc[m][j];
+  __syncthreads();
+  // a 16 x 16 result: lane l holds outputs 4 (l / 16) + 0..3 of row l % 16
+  for (int i = threadIdx.x; i < RM * NT * 64; i += 512) {
+    const int f = i >> 6, l = i & 63;
+    f32x4 v = part[0][f][l];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v += part[w][f][l];
+    const int o = o0 + 16 * (f / NT) + 4 * (l >> 4), r = c.r0 + 16 * (f % NT) + (l & 15);
+    if (o < g.O && r < c.r1) put4<BF16>(g.out, (size_t)r * g.O + o, v);
+  }
+}
+
+template <int RM, int NT>
+int thin_go(Act4Args g, int bf16, hipStream_t s) {
+  // every range's last chunk may be short, and one more chunk for the rows of no expert
+  g.chunks = g.offsets ? (int)(g.N / (16 * NT) + (g.E < g.N ? g.E : g.N) + 1) : (g.N + 16 * NT - 1) / (16 * NT);
+  const int64_t groups = (g.O + 16 * RM - 1) / (16 * RM);
+  if (groups * g.chunks > kGroupsX) return -1;
+  const dim3 grid((unsigned)(groups * g.chunks)), block(512);
+  if (bf16) hipLaunchKernelGGL((act4_thin_kernel<RM, NT, true>), grid, block, 0, s, g);
+  else hipLaunchKernelGGL((act4_thin_kernel<RM, NT, false>), grid, block, 0, s, g);
+  return ok();
+}
+
+int product(Act4Args g, int bf16, hipStream_t s) {
+  const int64_t avg = (g.N + g.E - 1) / g.E;
+  if (avg <= 16) return thin_go<1, 1>(g, bf16, s);
+  return thin_go<2, 4>(g, bf16, s);
+}
+
+}  // namespace
+
+int act4_pack_launch(int fmt, int64_t T, int64_t I, const void* X, float ws2, uint8_t* codes, uint8_t* scales, hipStream_t s) {
+  const int64_t pieces = T * I / 8;
+  const dim3 grid((unsigned)((pieces + 256 * kSteps - 1) / (256 * kSteps))), block(256);
+  const u32x4* x = static_cast<const u32x4*>(X);
+  if (fmt == kMX) hipLaunchKernelGGL((act4_pack_kernel<kMX>), grid, block, 0, s, x, pieces, 1.0f, codes, scales);
+  else hipLaunchKernelGGL((act4_pack_kernel<kNV>), grid, block, 0, s, x, pieces, ws2, codes, scales);
+  return ok();
+}
+
+int act4_unpack_launch(int fmt, int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, float ws2, void* X, hipStream_t s) {
+  const int64_t pieces = T * I / 8;
+  const dim3 grid((unsigned)((pieces + 256 * kSteps - 1) / (256 * kSteps))), block(256);
+  const uint32_t* c = reinterpret_cast<const uint32_t*>(codes);
+  u32x4* x = static_cast<u32x4*>(X);
+  if (fmt == kMX) hipLaunchKernelGGL((act4_unpack_kernel<kMX>), grid, block, 0, s, c, scales, pieces, 1.0f, x);
+  else hipLaunchKernelGGL((act4_unpack_kernel<kNV>), grid, block, 0, s, c, scales, pieces, ws2, x);
+  return ok();
+}
+
+size_t act4_workspace(int fmt, int64_t T, int64_t O, int64_t I) { return fmt == kMX ? 0 : (size_t)T * I * 2; }
+
+int act4_fwd(int fmt, int T, int O, int I, const uint8_t* x, const uint8_t* xs, float x_ws2, const uint8_t* codes,
+             const uint8_t* scales, float ws2, void* Y, int y_bf16, void* workspace, hipStream_t s) {
+  if (fmt == kNV) {
+    if (act4_unpack_launch(fmt, T, I, x, xs, 1.0f, workspace, s) != 0) return -1;
+    return gemm_fwd(fmt, T, O, I, workspace, codes, scales, x_ws2 * ws2, Y, y_bf16, s);
+  }
+  Act4Args g{};
+  g.x = x; g.xs = xs; g.w = codes; g.ws = scales; g.out = Y;
+  g.T = g.N = T; g.E = 1; g.O = O; g.I = I; g.G = I / 32;
+  return product(g, y_bf16, s);
+}
+
+size_t act4_batched_workspace(int64_t E, int64_t T, int64_t O, int64_t I) { return 0; }
+
+int act4_fwd_batched(int E, int T, int N, int O, int I, const uint8_t* x, const uint8_t* xs, const int* rows,
+                     const int* offsets, const uint8_t* codes, const uint8_t* scales, void* Y, int y_bf16, void* workspace,
+                     hipStream_t s) {
+  Act4Args g{};
+  g.x = x; g.xs = xs; g.w = codes; g.ws = scales; g.out = Y; g.rows = rows; g.offsets = offsets;
+  g.T = T; g.N = N; g.E = E; g.O = O; g.I = I; g.G = I / 32;
+  return product(g, y_bf16, s);
+}
+
+}  // namespace sq

@@ -32,6 +32,7 @@
 #include <type_traits>
 
 #include "sq_device.h"
+#include "sq_distill.h"
 #include "sq_gemm_args.h"
 #include "sq_launch.h"
 #include "sq_tiles.h"
@@ -905,6 +906,7 @@ struct CePiece {
   int y_bytes;
   int T;
   int64_t V;
+  float f;                  // times the logits as they lie there
   __device__ __forceinline__ int live() const { return count ? min(*count, T) : T; }
   __device__ __forceinline__ int token(int row) const { return rows ? rows[row] : row; }
   // where row `row`'s logit of column c < n is, those of the next columns beside it
@@ -991,6 +993,7 @@ __global__ __launch_bounds__(256) void ce_part_kernel(CePiece p, float2* __restr
       if (c0 + i >= p.n) continue;
       l[i] = src[i];
       for (int s = 1; s < p.planes; ++s) l[i] += src[s * p.plane + i];
+      l[i] *= p.f;
       if (at == i) tlogit[row] = l[i];
       top = fmaxf(top, l[i]);
     }
@@ -1042,6 +1045,8 @@ __global__ __launch_bounds__(256) void ce_grad_kernel(CePiece p, const float* __
       x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
       x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= p.f;
   }
   const float f = any ? dloss[t] : 0.0f, z = any ? lse[t] : 0.0f;
   u32x4 w;
@@ -1378,19 +1383,37 @@ int ce_few_logits(int head, int T, int64_t v0, int n, int H, const void* X, cons
   return 0;
 }
 
+// The loss of a call: of targets, or against a teacher's entries (k).  `classes`: the
+// targets' range, V, or V + 1 where the tokens that count stand at V, an entry that no
+// row of the head is.
+struct CeCall {
+  const Distill* k;
+  int64_t classes;
+  const void* y;
+  int y_bytes;
+  float f;                  // of the logits, 1 / temperature
+};
+
+int ce_join(const CeCall& call, const float2* part, const float* tlogit, const CePiece& c, int tiles, float* loss, float* lse,
+            hipStream_t s) {
+  if (!call.k) return ce_loss_go(part, tlogit, c, tiles, loss, lse, s);
+  return distill_loss_launch(*call.k, part, c.rows, c.count, static_cast<const int*>(c.y), c.T, (int)call.classes - 1, tiles,
+                             loss, lse, s);
+}
+
 CeTail ce_tail(const CeFew& p, int head, const void* X, const uint8_t* codes, const uint8_t* scales, int H, float ws2) {
   return CeTail{static_cast<const uint16_t*>(X), codes + p.main * H / 2, scales + p.main * (H / (head == kMX ? 32 : 16)),
                 p.tail, H, ws2, p.main, nullptr, nullptr};
 }
 
 int ce_few_fwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* codes, const uint8_t* scales, float ws2,
-               const void* y, int y_bytes, float* loss, float* lse, uint8_t* ws, hipStream_t s) {
+               const CeCall& call, float* loss, float* lse, uint8_t* ws, hipStream_t s) {
   const CeFew p = ce_few_plan(false, T, V, H);
   float* logits = reinterpret_cast<float*>(ws + p.logits);
   float2* part = reinterpret_cast<float2*>(ws + p.part);
   float* tlogit = reinterpret_cast<float*>(ws + p.tlogit);
   CePiece c{};
-  c.y = y; c.y_bytes = y_bytes; c.T = T; c.V = V;
+  c.y = call.y; c.y_bytes = call.y_bytes; c.T = T; c.V = call.classes; c.f = call.f;
   int tiles = 0;
   for (int64_t v0 = 0; v0 < p.main; v0 += p.piece) {
     const int n = (int)(p.main - v0 < p.piece ? p.main - v0 : p.piece);
@@ -1398,17 +1421,16 @@ int ce_few_fwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
     const bool last = v0 + n == p.main;
     const int own = (n + 255) / 256;
     CeTail tail{};
-    if (last && p.tail > 0) tail = ce_tail(p, head, X, codes, scales, H, ws2);
+    if (last && p.tail > 0) tail = ce_tail(p, head, X, codes, scales, H, ws2 * call.f);
     tail.part = part + (size_t)(tiles + own) * T;
     if (ce_part_go(head, c, part + (size_t)tiles * T, tlogit, tail, s) != 0) return -1;
     tiles += own + (tail.rows > 0);
   }
-  return ce_loss_go(part, tlogit, c, tiles, loss, lse, s);
+  return ce_join(call, part, tlogit, c, tiles, loss, lse, s);
 }
 
 int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* codes, const uint8_t* scales, float ws2,
-               const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16, uint8_t* ws,
-               hipStream_t s) {
+               const CeCall& call, const float* lse, const float* dloss, void* dX, int dx_bf16, uint8_t* ws, hipStream_t s) {
   const CeFew p = ce_few_plan(true, T, V, H);
   const int64_t G = H / (head == kMX ? 32 : 16);
   uint16_t* d = reinterpret_cast<uint16_t*>(ws + p.d);
@@ -1416,13 +1438,17 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   float* dtail = reinterpret_cast<float*>(ws + p.dtail);
   float* lost = reinterpret_cast<float*>(ws + p.tlogit);
   CePiece c{};
-  c.y = y; c.y_bytes = y_bytes; c.T = T; c.V = V;
+  c.y = call.y; c.y_bytes = call.y_bytes; c.T = T; c.V = call.classes; c.f = call.f;
   if (ce_few_logits(head, T, 0, (int)p.main, H, X, codes, scales, ws2, p.group, reinterpret_cast<float*>(ws + p.logits), &c, s) != 0)
     return -1;
   CeTail tail{};
-  if (p.tail > 0) tail = ce_tail(p, head, X, codes, scales, H, ws2);
+  if (p.tail > 0) tail = ce_tail(p, head, X, codes, scales, H, ws2 * call.f);
   tail.d = dtail;
   if (ce_grad_go(head, c, lse, dloss, p.groups * p.width, p.width, p.shift, d, lost, tail, s) != 0) return -1;
+  if (call.k) {
+    const DistillPiece piece{d, 0, (int)p.main, p.width, p.groups, p.shift, dtail, p.main, nullptr, nullptr, T, (int)V};
+    if (distill_put_launch(*call.k, piece, lse, dloss, s) != 0) return -1;
+  }
   // dX of every group of rows, as the layer's grouped product
   ExpertProblem e[64];
   for (int k = 0; k < p.groups; ++k) {
@@ -1431,9 +1457,10 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   }
   if (gemm_dx_grouped(head, p.width, H, p.groups, e, 0, s) != 0) return -1;
   const CeRest rest{codes, scales, lost, dtail, p.main, p.tail};
+  const float f = call.k ? call.k->tau : 1.0f;
   auto finish = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, ce_dx_grid(T, H), dim3(128), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, y, y_bytes,
-                       T, V, H, 0, 0, 0, 1.0f, ws2, rest, dX);
+    hipLaunchKernelGGL(kernel, ce_dx_grid(T, H), dim3(128), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, call.y,
+                       call.y_bytes, T, call.classes, H, 0, 0, 0, f, ws2 * f, rest, dX);
     return ok();
   };
   return ce_dx_by(head, dx_bf16, finish);
@@ -1449,10 +1476,10 @@ size_t ce_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H) {
 }
 
 // What both directions set up: the arguments, and the live rows numbered.
-static int ce_begin(const CePlan& p, int T, int64_t V, int H, const void* X, float ws2, const void* y, int y_bytes, uint8_t* ws,
+static int ce_begin(const CePlan& p, int T, int64_t V, int H, const void* X, float ws2, const CeCall& call, uint8_t* ws,
                     CeArgs* g, CePiece* c, hipStream_t s) {
   g->x = static_cast<const uint16_t*>(X);
-  g->y = y; g->y_bytes = y_bytes; g->T = T; g->H = H; g->V = V; g->ws2 = ws2;
+  g->y = call.y; g->y_bytes = call.y_bytes; g->T = T; g->H = H; g->V = call.classes; g->ws2 = ws2 * call.f;
   g->tlogit = reinterpret_cast<float*>(ws + p.tlogit);
   g->ld = g->ldl = p.ld;
   g->splits = p.splits;
@@ -1462,37 +1489,37 @@ static int ce_begin(const CePlan& p, int T, int64_t V, int H, const void* X, flo
     int* rows = reinterpret_cast<int*>(ws + p.rows);
     g->count = count;
     g->rows = rows;
-    hipLaunchKernelGGL(ce_rows_kernel, dim3(1), dim3(1024), 0, s, y, y_bytes, T, V, count, rows);
+    hipLaunchKernelGGL(ce_rows_kernel, dim3(1), dim3(1024), 0, s, call.y, call.y_bytes, T, call.classes, count, rows);
     if (ok() != 0) return -1;
   }
   c->logits = g->logits;
   c->n = (int)V; c->width = p.ld; c->planes = p.splits; c->plane = (int64_t)T * p.ld;
-  c->rows = g->rows; c->count = g->count; c->y = y; c->y_bytes = y_bytes; c->T = T; c->V = V;
+  c->rows = g->rows; c->count = g->count; c->y = call.y; c->y_bytes = call.y_bytes; c->T = T; c->V = call.classes;
+  c->f = 1.0f;                                                // g->ws2 holds the call's factor
   return 0;
 }
 
-int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
-                  const void* y, int y_bytes, float* loss, float* lse, void* workspace, hipStream_t s) {
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
+static int ce_fwd(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                  const CeCall& call, float* loss, float* lse, uint8_t* ws, hipStream_t s) {
   if (ce_codes(head, T, V, H) && ((uintptr_t)W | (uintptr_t)scales) % 16 == 0) {
     const CePlan p = ce_plan(false, false, T, V, H);
     CeArgs g{};
     CePiece c{};
-    if (ce_begin(p, T, V, H, X, ws2, y, y_bytes, ws, &g, &c, s) != 0) return -1;
+    if (ce_begin(p, T, V, H, X, ws2, call, ws, &g, &c, s) != 0) return -1;
     g.w = static_cast<const uint16_t*>(W);
     g.scales = scales;
     g.Vn = (int)V;
     g.part = reinterpret_cast<float*>(ws + p.part);
     const int tiles = (int)((V + 255) / 256);
     if (ce_codes_go<kCeStats>(g, p.bt, (int64_t)tiles * ((T + p.bt - 1) / p.bt), s) != 0) return -1;
-    return ce_loss_go(reinterpret_cast<float2*>(g.part), g.tlogit, c, tiles, loss, lse, s);
+    return ce_join(call, reinterpret_cast<float2*>(g.part), g.tlogit, c, tiles, loss, lse, s);
   }
   if (ce_few(head, T, V, H))
-    return ce_few_fwd(head, T, V, H, X, static_cast<const uint8_t*>(W), scales, ws2, y, y_bytes, loss, lse, ws, s);
+    return ce_few_fwd(head, T, V, H, X, static_cast<const uint8_t*>(W), scales, ws2, call, loss, lse, ws, s);
   const CePlan p = ce_plan(false, head != kCeBf16, T, V, H);
   CeArgs g{};
   CePiece c{};
-  if (ce_begin(p, T, V, H, X, ws2, y, y_bytes, ws, &g, &c, s) != 0) return -1;
+  if (ce_begin(p, T, V, H, X, ws2, call, ws, &g, &c, s) != 0) return -1;
   g.part = reinterpret_cast<float*>(ws + p.part);
   float2* part = reinterpret_cast<float2*>(g.part);
   const int64_t tt = (T + p.bt - 1) / p.bt;
@@ -1508,26 +1535,28 @@ int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
       return -1;
     }
   }
-  return ce_loss_go(part, g.tlogit, c, (int)((V + 255) / 256), loss, lse, s);
+  return ce_join(call, part, g.tlogit, c, (int)((V + 255) / 256), loss, lse, s);
 }
 
-int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
-                  const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16,
-                  void* workspace, hipStream_t s) {
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
+static int ce_bwd(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                  const CeCall& call, const float* lse, const float* dloss, void* dX, int dx_bf16, uint8_t* ws, hipStream_t s) {
   const bool codes = T > kCeCodesTokens && ce_codes(head, T, V, H) && ((uintptr_t)W | (uintptr_t)scales) % 16 == 0;
   if (!codes && ce_few(head, T, V, H))
-    return ce_few_bwd(head, T, V, H, X, static_cast<const uint8_t*>(W), scales, ws2, y, y_bytes, lse, dloss, dX, dx_bf16,
-                      ws, s);
+    return ce_few_bwd(head, T, V, H, X, static_cast<const uint8_t*>(W), scales, ws2, call, lse, dloss, dX, dx_bf16, ws, s);
   const CePlan p = ce_plan(true, head != kCeBf16 && !codes, T, V, H);
   CeArgs g{};
   CePiece c{};
-  if (ce_begin(p, T, V, H, X, ws2, y, y_bytes, ws, &g, &c, s) != 0) return -1;
+  if (ce_begin(p, T, V, H, X, ws2, call, ws, &g, &c, s) != 0) return -1;
   g.lse = lse; g.dloss = dloss;
   g.d = reinterpret_cast<uint16_t*>(ws + p.d);
   g.sums = reinterpret_cast<float*>(ws + p.sums);
   g.split_stages = (int)(((p.piece < V ? p.piece : V) + kBK - 1) / kBK);
   const int64_t tt = (T + p.bt - 1) / p.bt, tn = (H + 255) / 256;
+  auto put = [&]() {                     // a teacher's entries among the piece's gradients
+    if (!call.k) return 0;
+    const DistillPiece piece{g.d, g.v0, g.Vn, g.ld, 1, 0, nullptr, V, g.rows, g.count, T, (int)V};
+    return distill_put_launch(*call.k, piece, lse, dloss, s);
+  };
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
     const int64_t n = V - v0 < p.piece ? V - v0 : p.piece, tiles = (n + 255) / 256 * tt;
     g.v0 = v0;
@@ -1536,7 +1565,7 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     if (codes) {
       g.w = reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(W) + v0 * (H / 2));
       g.scales = scales + v0 * (H / 32);
-      if (ce_codes_go<kCeGrad>(g, p.bt, tiles, s) != 0 || ce_codes_go<kCeDx>(g, p.bx, p.groups, s) != 0) return -1;
+      if (ce_codes_go<kCeGrad>(g, p.bt, tiles, s) != 0 || put() != 0 || ce_codes_go<kCeDx>(g, p.bx, p.groups, s) != 0) return -1;
       continue;
     }
     if (ce_weight(head, W, scales, v0, n, H, ws + p.wbuf, &g.w, s) != 0) return -1;
@@ -1547,15 +1576,60 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
     } else if (ce_go<kCeGrad>(g, p.bt, tiles, s) != 0) {
       return -1;
     }
-    if (ce_go<kCeDx>(g, p.bx, p.groups, s) != 0) return -1;
+    if (put() != 0 || ce_go<kCeDx>(g, p.bx, p.groups, s) != 0) return -1;
   }
   const CeRest rest{W, scales, g.tlogit, nullptr, V, 0};
+  const float f = call.k ? ws2 * call.k->tau : ws2;
   auto finish = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, ce_dx_grid(T, H), dim3(128), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, y, y_bytes, T, V,
-                       H, p.bx, (int)tn, g.split_stages, ws2, ws2, rest, dX);
+    hipLaunchKernelGGL(kernel, ce_dx_grid(T, H), dim3(128), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, call.y, call.y_bytes,
+                       T, call.classes, H, p.bx, (int)tn, g.split_stages, f, f, rest, dX);
     return ok();
   };
   return ce_dx_by(head, dx_bf16, finish);
+}
+
+int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                  const void* y, int y_bytes, float* loss, float* lse, void* workspace, hipStream_t s) {
+  return ce_fwd(head, T, V, H, X, W, scales, ws2, CeCall{nullptr, V, y, y_bytes, 1.0f}, loss, lse, static_cast<uint8_t*>(workspace), s);
+}
+
+int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                  const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16,
+                  void* workspace, hipStream_t s) {
+  return ce_bwd(head, T, V, H, X, W, scales, ws2, CeCall{nullptr, V, y, y_bytes, 1.0f}, lse, dloss, dX, dx_bf16,
+                static_cast<uint8_t*>(workspace), s);
+}
+
+// ------------------------------------------------------------------ distillation
+// The same products with a teacher's entries in the place of the targets.  Behind
+// their workspace, a target for each token: V where it has an entry that counts (no
+// row of the head), else -1.
+size_t distill_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H) {
+  return ((ce_workspace(bwd, head, T, V, H) + 255) & ~(size_t)255) + (size_t)T * 4;
+}
+
+static int distill_begin(int bwd, int head, int T, int64_t V, int H, const Distill& k, uint8_t* ws, CeCall* call, hipStream_t s) {
+  int* y = reinterpret_cast<int*>(ws + distill_workspace(bwd, head, T, V, H) - (size_t)T * 4);
+  *call = CeCall{&k, V + 1, y, 4, 1.0f / k.tau};
+  return distill_live_launch(k, T, (int)V, y, s);
+}
+
+int distill_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                       const Distill& k, float* loss, float* lse, void* workspace, hipStream_t s) {
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  CeCall call;
+  if (distill_begin(0, head, T, V, H, k, ws, &call, s) != 0) return -1;
+  if (distill_pick_launch(k, head, T, (int)V, H, X, W, scales, ws2 * call.f, s) != 0) return -1;
+  return ce_fwd(head, T, V, H, X, W, scales, ws2, call, loss, lse, ws, s);
+}
+
+int distill_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                       const Distill& k, const float* lse, const float* dloss, void* dX, int dx_bf16, void* workspace,
+                       hipStream_t s) {
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  CeCall call;
+  if (distill_begin(1, head, T, V, H, k, ws, &call, s) != 0) return -1;
+  return ce_bwd(head, T, V, H, X, W, scales, ws2, call, lse, dloss, dX, dx_bf16, ws, s);
 }
 
 }  // namespace sq

@@ -1,0 +1,275 @@
+// Distillation of a head from a teacher's top logits: what differs from the cross
+// entropy, whose products over the vocabulary (sq_ce.hip) it shares.
+//
+//   s[t,v]  = l[t,v] / tau                       lse[t] = log sum_v exp s[t,v]
+//   q[t,k]  = softmax over the entries k that count of z[t,k] / tau
+//   loss[t] = tau^2 sum_k q[t,k] (log q[t,k] - s[t,ids[t,k]] + lse[t])
+//   dX[t]   = dloss[t] tau sum_v (exp(s[t,v] - lse[t]) - sum_{k : ids[t,k] = v} q[t,k]) W[v]
+//
+// An entry counts if its id is in the vocabulary and its logit is not -inf; a token
+// without one is ignored.  The entries touch K of V columns: the forward takes their
+// logits as products of their own with K rows of the head, which the backward uses
+// again to write (p - q) over the p of its piece before the product with W, in one
+// rounding.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "sq_device.h"
+#include "sq_distill.h"
+#include "sq_gemm_args.h"
+#include "sq_launch.h"
+#include "sq_rows.h"
+
+namespace sq {
+
+namespace {
+
+inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
+
+constexpr int kPer = kDistillMax / 64;  // entries per lane
+
+// Workgroups by token (or by 4), on in y where x is full.
+__device__ __forceinline__ int64_t group_at() { return (int64_t)blockIdx.y * kGroupsX + blockIdx.x; }
+inline dim3 groups_of(int64_t n) {
+  return dim3((unsigned)(n < kGroupsX ? n : kGroupsX), (unsigned)((n + kGroupsX - 1) / kGroupsX));
+}
+
+__device__ __forceinline__ float max_of(float v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ __forceinline__ float sum_of(float v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// Entry k of token t: its row of the head, or -1 where it does not count.
+__device__ __forceinline__ int entry_at(const Distill& g, int64_t t, int k, int V, float* z) {
+  if (k >= g.K) return -1;
+  const int64_t at = t * g.K + k, v = id_at(g.ids, g.id_bytes, at);
+  *z = g.z_bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(g.z)[at] << 16) : static_cast<const float*>(g.z)[at];
+  return v >= 0 && v < V && *z != -INFINITY ? (int)v : -1;
+}
+
+// A token's entries, one wave's: lane l has entries l, l + 64, ..; the teacher's
+// probabilities and their logarithms (0 where an entry does not count).
+struct Entries {
+  int id[kPer];
+  float q[kPer], log_q[kPer];
+};
+__device__ __forceinline__ Entries entries_of(const Distill& g, int64_t t, int V) {
+  const int lane = threadIdx.x & 63;
+  Entries e;
+  float z[kPer], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    z[i] = -INFINITY;
+    e.id[i] = entry_at(g, t, i * 64 + lane, V, &z[i]);
+    // a NaN stays: fmax would drop it
+    if (e.id[i] >= 0) top = z[i] != z[i] || top != top ? z[i] + top : fmaxf(top, z[i]);
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    const float o = __shfl_xor(top, d);
+    top = o != o || top != top ? o + top : fmaxf(top, o);
+  }
+  const float f = 1.0f / g.tau;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    e.log_q[i] = e.id[i] >= 0 ? (z[i] - top) * f : 0.0f;
+    e.q[i] = e.id[i] >= 0 ? __expf(e.log_q[i]) : 0.0f;
+    sum += e.q[i];
+  }
+  sum = sum_of(sum);
+  const float log_sum = __logf(sum);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (e.id[i] < 0) continue;
+    e.q[i] /= sum;
+    e.log_q[i] -= log_sum;
+  }
+  return e;
+}
+
+// ------------------------------------------------------------------ live tokens
+__global__ __launch_bounds__(256) void distill_live_kernel(Distill g, int T, int V, int* __restrict__ y) {
+  const int64_t t = group_at() * 4 + (threadIdx.x >> 6);
+  if (t >= T) return;
+  const int lane = threadIdx.x & 63;
+  bool any = false;
+  for (int k = lane; k < g.K; k += 64) {
+    float z;
+    any |= entry_at(g, t, k, V, &z) >= 0;
+  }
+  const bool live = __ballot(any) != 0;
+  if (lane == 0) y[t] = live ? V : -1;
+}
+
+// ------------------------------------------------------------------ their logits
+// One token per workgroup; a wave takes 4 entries at a time, 8 columns per lane.
+template <int HEAD>
+__global__ __launch_bounds__(256) void distill_pick_kernel(Distill g, int T, int V, int H, const uint16_t* __restrict__ X,
+                                                           const void* __restrict__ W, const uint8_t* __restrict__ scales,
+                                                           float f) {
+  const int64_t t = group_at();
+  if (t >= T) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int k0 = wave * 4; k0 < g.K; k0 += 16) {
+    int id[4];
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f}, z;
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      id[i] = __builtin_amdgcn_readfirstlane(entry_at(g, t, k0 + i, V, &z));
+      any |= id[i] >= 0;
+    }
+    if (any) {
+      for (int h = lane * 8; h < H; h += 512) {
+        float x[8];
+        load8<true>(X, t * H + h, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float w[8];
+          table8<HEAD>(W, scales, 1.0f, (int64_t)max(id[i], 0) * H + h, w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum[i] = __builtin_fmaf(x[j], w[j], sum[i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float v = sum_of(sum[i]) * f;
+      if (lane == 0 && k0 + i < g.K) g.picked[t * g.K + k0 + i] = id[i] >= 0 ? v : 0.0f;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ loss
+// 64 tokens per workgroup: 16 waves share the tiles' pairs, then take 4 tokens each.
+__global__ __launch_bounds__(1024) void distill_loss_kernel(Distill g, const float2* __restrict__ part, const int* __restrict__ rows,
+                                                            const int* __restrict__ count, const int* __restrict__ y, int T, int V,
+                                                            int tiles, float* __restrict__ loss, float* __restrict__ lse) {
+  __shared__ float s_top[16][64], s_sum[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int live = count ? min(*count, T) : T;
+  const int row = (int)blockIdx.x * 64 + lane;
+  float top = -INFINITY, sum = 0.0f;
+  if (row < live) {
+#pragma unroll 4
+    for (int i = wave; i < tiles; i += 16) {
+      const float2 p = part[(size_t)i * T + row];
+      const float m = fmaxf(top, p.x), ref = m == -INFINITY ? 0.0f : m;
+      sum = sum * __expf(top - ref) + p.y * __expf(p.x - ref);
+      top = m;
+    }
+  }
+  s_top[wave][lane] = top;
+  s_sum[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0) {
+    for (int w = 1; w < 16; ++w) {
+      const float b = s_top[w][lane], m = fmaxf(top, b), ref = m == -INFINITY ? 0.0f : m;
+      sum = sum * __expf(top - ref) + s_sum[w][lane] * __expf(b - ref);
+      top = m;
+    }
+    s_top[0][lane] = top;
+    s_sum[0][lane] = __logf(sum);
+  }
+  __syncthreads();
+  for (int i = wave; i < 64; i += 16) {
+    const int r = (int)blockIdx.x * 64 + i;
+    if (r >= live) continue;
+    const int t = rows ? rows[r] : r;
+    if (y[t] < 0) continue;
+    const Entries e = entries_of(g, t, V);
+    const float most = s_top[0][i], rest = s_sum[0][i];
+    float v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      // the distance to the largest logit first, as the cross entropy takes it
+      const int at = k * 64 + lane;
+      if (e.id[k] >= 0) v += e.q[k] != 0.0f ? e.q[k] * (e.log_q[k] + ((most - g.picked[(int64_t)t * g.K + at]) + rest)) : 0.0f;
+    }
+    v = sum_of(v);
+    if (lane == 0) {
+      loss[t] = g.tau * g.tau * v;
+      lse[t] = most + rest;
+    }
+  }
+  const int t = (int)blockIdx.x * 64 + lane;                  // tokens that are ignored
+  if (wave == 0 && t < T && y[t] < 0) loss[t] = lse[t] = 0.0f;
+}
+
+// ------------------------------------------------------------------ gradient
+// A wave per live token.  Entries of one id are one column: each writes the same
+// value, with all their probabilities taken off.
+__global__ __launch_bounds__(256) void distill_put_kernel(Distill g, DistillPiece p, const float* __restrict__ lse,
+                                                          const float* __restrict__ dloss) {
+  __shared__ int s_id[4][kDistillMax];
+  __shared__ float s_q[4][kDistillMax];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = group_at() * 4 + wave;
+  if (row >= (p.count ? min(*p.count, p.T) : p.T)) return;                                    // no barrier below: a wave's LDS is its own
+  const int64_t t = p.rows ? p.rows[row] : row;
+  const Entries e = entries_of(g, t, p.V);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    s_id[wave][i * 64 + lane] = e.id[i];
+    s_q[wave][i * 64 + lane] = e.q[i];
+  }
+  __builtin_amdgcn_wave_barrier();
+  const float z = lse[t], c = dloss[t];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int k = i * 64 + lane;
+    if (e.id[i] < 0) continue;
+    const int64_t at = e.id[i] - p.v0;
+    const bool tail = p.dtail && e.id[i] >= p.main;
+    if (!tail && (at < 0 || at >= p.n)) continue;
+    float q = 0.0f;
+    for (int j = 0; j < g.K; ++j) q += s_id[wave][j] == e.id[i] ? s_q[wave][j] : 0.0f;
+    const float d = c * (__expf(g.picked[t * g.K + k] - z) - q);
+    if (tail) {
+      p.dtail[t * 8 + (e.id[i] - p.main)] = d;
+      continue;
+    }
+    const int group = min((int)(at / p.width), p.groups - 1);
+    const int64_t last = (int64_t)(p.groups - 1) * p.width - p.shift;     // the last group's first column
+    const bool in_last = p.groups > 1 ? group == p.groups - 1 : true;
+    const int64_t col = in_last ? at - last : at - (int64_t)group * p.width;
+    const bf16x2 b = __builtin_convertvector((f32x2{d, d}), bf16x2);
+    p.d[(int64_t)group * p.width * p.T + row * p.width + col] = (uint16_t)bits_of(b);
+  }
+}
+
+}  // namespace
+
+int distill_live_launch(const Distill& k, int T, int V, int* y, hipStream_t s) {
+  hipLaunchKernelGGL(distill_live_kernel, groups_of((T + 3) / 4), dim3(256), 0, s, k, T, V, y);
+  return ok();
+}
+
+int distill_pick_launch(const Distill& k, int head, int T, int V, int H, const void* X, const void* W, const uint8_t* scales,
+                        float f, hipStream_t s) {
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, groups_of(T), dim3(256), 0, s, k, T, V, H, static_cast<const uint16_t*>(X), W, scales, f);
+    return ok();
+  };
+  return head == kMX ? go(distill_pick_kernel<kMX>) : head == kNV ? go(distill_pick_kernel<kNV>) : go(distill_pick_kernel<kCeBf16>);
+}
+
+int distill_loss_launch(const Distill& k, const float2* part, const int* rows, const int* count, const int* y, int T, int V,
+                        int tiles, float* loss, float* lse, hipStream_t s) {
+  hipLaunchKernelGGL(distill_loss_kernel, dim3((unsigned)((T + 63) / 64)), dim3(1024), 0, s, k, part, rows, count, y, T, V,
+                     tiles, loss, lse);
+  return ok();
+}
+
+int distill_put_launch(const Distill& k, const DistillPiece& piece, const float* lse, const float* dloss, hipStream_t s) {
+  hipLaunchKernelGGL(distill_put_kernel, groups_of((piece.T + 3) / 4), dim3(256), 0, s, k, piece, lse, dloss);
+  return ok();
+}
+
+}  // namespace sq

@@ -206,4 +206,42 @@ int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* 
                   const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16,
                   void* workspace, hipStream_t s);
 
+// Activations in the layer's 4-bit storage and products of two 4-bit operands (sq_act4.hip).
+int act4_pack_launch(int fmt, int64_t T, int64_t I, const void* X, float ws2, uint8_t* codes, uint8_t* scales, hipStream_t s);
+int act4_unpack_launch(int fmt, int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, float ws2, void* X,
+                       hipStream_t s);
+size_t act4_workspace(int fmt, int64_t T, int64_t O, int64_t I);
+int act4_fwd(int fmt, int T, int O, int I, const uint8_t* x, const uint8_t* xs, float x_ws2, const uint8_t* codes,
+             const uint8_t* scales, float ws2, void* Y, int y_bf16, void* workspace, hipStream_t s);
+size_t act4_batched_workspace(int64_t E, int64_t T, int64_t O, int64_t I);
+int act4_fwd_batched(int E, int T, int N, int O, int I, const uint8_t* x, const uint8_t* xs, const int* rows,
+                     const int* offsets, const uint8_t* codes, const uint8_t* scales, void* Y, int y_bf16,
+                     void* workspace, hipStream_t s);
+
+// Distillation from a teacher's top logits: the loss's products with these in the
+// place of the targets (sq_ce.hip, sq_distill.hip).
+constexpr int kDistillMax = 256;          // entries per token
+struct Distill {
+  const void* ids;          // [T, K]
+  const void* z;            // [T, K], fp32 or bf16
+  float* picked;            // [T, K], written by the forward
+  int id_bytes, z_bf16, K;
+  float tau;
+};
+size_t distill_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H);
+int distill_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                       const Distill& k, float* loss, float* lse, void* workspace, hipStream_t s);
+int distill_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
+                       const Distill& k, const float* lse, const float* dloss, void* dX, int dx_bf16, void* workspace,
+                       hipStream_t s);
+
+// Embedding lookup and its gradients (sq_embed.hip).  head as the loss's.
+constexpr int kEmbedRankTokens = 16384;   // up to these one launch sorts the tokens
+constexpr int kEmbedDigitBits = 9, kEmbedDigits = 1 << kEmbedDigitBits;
+int embed_launch(int head, int64_t T, int V, int H, const void* ids, int id_bytes, const void* W, const uint8_t* scales,
+                 float ws2, float factor, void* out, int out_bf16, hipStream_t s);
+size_t embed_workspace(int64_t T, int64_t V, int64_t H);
+int embed_bwd_launch(int head, int T, int V, int H, const void* ids, int id_bytes, const void* dOut, int d_bf16, float factor,
+                     const uint8_t* codes, void* grad, int grad_bf16, void* workspace, hipStream_t s);
+
 }  // namespace sq

@@ -171,6 +171,29 @@ def _load():
                                      ctypes.c_int, _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]),
         "sq_ce_bwd": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p, ctypes.c_float, _c_p,
                                      ctypes.c_int, _c_p, _c_p, _c_p, ctypes.c_int, _c_p, ctypes.c_size_t, _c_p]),
+        "sq_act4_pack": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_p, ctypes.c_float, _c_p, _c_p, _c_p]),
+        "sq_act4_unpack": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_p, _c_p, ctypes.c_float, _c_p, _c_p]),
+        "sq_fwd_act4_workspace": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64]),
+        "sq_fwd_act4": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, ctypes.c_float, _c_p, _c_p,
+                                       ctypes.c_float, _c_p, ctypes.c_int, _c_p, ctypes.c_size_t, _c_p]),
+        "sq_fwd_act4_batched_workspace": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i64, _c_i64]),
+        "sq_fwd_act4_batched": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
+                                               _c_p, _c_p, _c_p, _c_p, ctypes.c_int, _c_p, ctypes.c_size_t, _c_p]),
+        "sq_distill_fwd_workspace": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64]),
+        "sq_distill_bwd_workspace": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64]),
+        "sq_distill_fwd": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p, ctypes.c_float,
+                                          _c_p, ctypes.c_int, _c_p, ctypes.c_int, ctypes.c_float, _c_p, _c_p, _c_p,
+                                          _c_p, ctypes.c_size_t, _c_p]),
+        "sq_distill_bwd": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p, ctypes.c_float,
+                                          _c_p, ctypes.c_int, _c_p, ctypes.c_int, ctypes.c_float, _c_p, _c_p, _c_p,
+                                          _c_p, ctypes.c_int, _c_p, ctypes.c_size_t, _c_p]),
+        "sq_embed_fwd": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_p, _c_p,
+                                        ctypes.c_float, ctypes.c_float, _c_p, ctypes.c_int, _c_p]),
+        "sq_embed_bwd_workspace": (ctypes.c_size_t, [_c_i64, _c_i64, _c_i64]),
+        "sq_embed_bwd": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_p, ctypes.c_int, ctypes.c_float,
+                                        _c_p, ctypes.c_int, _c_p, ctypes.c_size_t, _c_p]),
+        "sq_embed_bwd_dscale": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_p,
+                                               ctypes.c_int, ctypes.c_float, _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]),
         "sq_status_str": (ctypes.c_char_p, [ctypes.c_int]),
         "sq_abi_version": (ctypes.c_int, []),
     }
@@ -1089,6 +1112,216 @@ def sq_ce_bwd(head, X, W, targets, lse, dloss, scales=None, ws2=1.0, out_dtype=t
                                          targets.element_size(), _ptr(lse), _ptr(dloss), _ptr(dX), _dtype_of(dX),
                                          _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
     return dX
+
+
+# ---------------------------------------------------------------- 4-bit activations
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel()
+
+
+def _kept4(fmt, codes, scales, names=("codes", "scales")):
+    """T, I of an activation in the layer's storage: codes uint8 [T, I/2], scales uint8 [T, I/B]."""
+    T, half = _dims2(codes, names[0])
+    G = _block(fmt, 2 * half)
+    _need(codes, names[0], _U8)
+    _need(scales, names[1], _U8, (T, G))
+    return T, 2 * half
+
+
+def sq_act4_pack(fmt, X, ws2=1.0, codes=None, scales=None):
+    """(codes uint8 [T, I/2], scales uint8 [T, I/B]) of X bf16 [T, I]; ws2 the NVFP4 scalar of the activation."""
+    fmt = _fmt(fmt)
+    T, I = _dims2(X, "X")
+    _need(X, "X", _BF16)
+    G = _block(fmt, I)
+    codes = _out(codes, "codes", (T, I // 2), _U8, X.device)
+    scales = _out(scales, "scales", (T, G), _U8, X.device)
+    _dev(X, codes, scales)
+    _check("sq_act4_pack", load().sq_act4_pack(fmt, T, I, _ptr(X), float(ws2), _ptr(codes), _ptr(scales), _stream()))
+    return codes, scales
+
+
+def sq_act4_unpack(fmt, codes, scales, ws2=1.0, X=None):
+    """The kept values as bf16 [T, I]."""
+    fmt = _fmt(fmt)
+    T, I = _kept4(fmt, codes, scales)
+    X = _out(X, "X", (T, I), _BF16, codes.device)
+    _dev(codes, scales, X)
+    _check("sq_act4_unpack", load().sq_act4_unpack(fmt, T, I, _ptr(codes), _ptr(scales), float(ws2), _ptr(X), _stream()))
+    return X
+
+
+def sq_fwd_act4_workspace(fmt, T, O, I):
+    return int(load().sq_fwd_act4_workspace(_fmt(fmt), T, O, I))
+
+
+def sq_fwd_act4(fmt, x_codes, x_scales, codes, scales, x_ws2=1.0, ws2=1.0, out_dtype=torch.float32, Y=None, workspace=None):
+    """Y = X^ W^T of a kept X (sq_act4_pack) and a layer: codes uint8 [O, I/2], scales uint8 [O, I/B]."""
+    fmt = _fmt(fmt)
+    T, I = _kept4(fmt, x_codes, x_scales, ("x_codes", "x_scales"))
+    O = _dims2(codes, "codes")[0]
+    _layer(fmt, O, I, codes, scales)
+    Y = _out(Y, "Y", (T, O), out_dtype, x_codes.device, _OUT)
+    workspace = _scratch(workspace, load().sq_fwd_act4_workspace(fmt, T, O, I), x_codes.device)
+    _dev(x_codes, x_scales, codes, scales, Y, workspace)
+    _check("sq_fwd_act4", load().sq_fwd_act4(fmt, T, O, I, _ptr(x_codes), _ptr(x_scales), float(x_ws2), _ptr(codes),
+                                             _ptr(scales), float(ws2), _ptr(Y), _dtype_of(Y), _ptr(workspace),
+                                             _bytes(workspace), _stream()))
+    return Y
+
+
+def sq_fwd_act4_batched_workspace(fmt, E, T, N, O, I):
+    return int(load().sq_fwd_act4_batched_workspace(_fmt(fmt), E, T, N, O, I))
+
+
+def sq_fwd_act4_batched(fmt, x_codes, x_scales, rows, offsets, codes, scales, out_dtype=torch.float32, Y=None, workspace=None):
+    """Y [N, O] of E stacked experts (codes uint8 [E, O, I/2], scales uint8 [E, O, I/B]): rows [offsets[e], offsets[e+1])
+    are rows rows[s] of the kept X (None: row s) times expert e; rows that no expert has are zeros."""
+    fmt = _fmt(fmt)
+    T, I = _kept4(fmt, x_codes, x_scales, ("x_codes", "x_scales"))
+    if not isinstance(codes, torch.Tensor) or codes.dim() != 3:
+        raise ValueError("codes must be a 3-D tensor")
+    E, O, _ = codes.shape
+    _need(codes, "codes", _U8, (E, O, I // 2))
+    _need(scales, "scales", _U8, (E, O, _block(fmt, I)))
+    _need(offsets, "offsets", _I32, (E + 1,))
+    N = T
+    if rows is not None:
+        if not isinstance(rows, torch.Tensor) or rows.dim() != 1:
+            raise ValueError("rows must be a 1-D tensor")
+        _need(rows, "rows", _I32)
+        N = rows.numel()
+    Y = _out(Y, "Y", (N, O), out_dtype, x_codes.device, _OUT)
+    workspace = _scratch(workspace, load().sq_fwd_act4_batched_workspace(fmt, E, T, N, O, I), x_codes.device)
+    _dev(x_codes, x_scales, rows, offsets, codes, scales, Y, workspace)
+    _check("sq_fwd_act4_batched", load().sq_fwd_act4_batched(
+        fmt, E, T, N, O, I, _ptr(x_codes), _ptr(x_scales), _ptr(rows), _ptr(offsets), _ptr(codes), _ptr(scales), _ptr(Y),
+        _dtype_of(Y), _ptr(workspace), _bytes(workspace), _stream()))
+    return Y
+
+
+# ---------------------------------------------------------------- distillation
+def sq_distill_fwd_workspace(head, T, V, I):
+    return int(load().sq_distill_fwd_workspace(HEADS.get(head, head), T, V, I))
+
+
+def sq_distill_bwd_workspace(head, T, V, I):
+    return int(load().sq_distill_bwd_workspace(HEADS.get(head, head), T, V, I))
+
+
+def _teacher(head, X, W, ids, logits, scales):
+    """T, V, I, K of a head's operands and a teacher's entries."""
+    T, I = _dims2(X, "X")
+    V = _dims2(W, "W")[0]
+    _need(X, "X", _BF16)
+    if head == HEAD_BF16:
+        _need(W, "W", _BF16, (V, I))
+    else:
+        G = _block(head, I)
+        _need(W, "W", _U8, (V, I // 2))
+        _need(scales, "scales", _U8, (V, G))
+    K = _dims2(ids, "ids")[1]
+    _need(ids, "ids", _IDS, (T, K))
+    _need(logits, "logits", _OUT, (T, K))
+    return T, V, I, K
+
+
+def sq_distill_fwd(head, X, W, ids, logits, temperature=1.0, scales=None, ws2=1.0, loss=None, lse=None, picked=None,
+                   workspace=None):
+    """(loss, lse fp32 [T], picked fp32 [T, K]) of X bf16 [T, I] through the head (as sq_ce_fwd's) against a teacher's
+    entries: ids int32 or int64 [T, K] (outside 0 .. V-1: left out) and logits fp32 or bf16 [T, K]."""
+    head = HEADS.get(head, head)
+    T, V, I, K = _teacher(head, X, W, ids, logits, scales)
+    loss = _out(loss, "loss", (T,), _F32, X.device)
+    lse = _out(lse, "lse", (T,), _F32, X.device)
+    picked = _out(picked, "picked", (T, K), _F32, X.device)
+    workspace = _scratch(workspace, load().sq_distill_fwd_workspace(head, T, V, I), X.device)
+    _dev(X, W, ids, logits, scales, loss, lse, picked, workspace)
+    _check("sq_distill_fwd", load().sq_distill_fwd(
+        head, T, V, I, K, _ptr(X), _ptr(W), _ptr(scales), float(ws2), _ptr(ids), ids.element_size(), _ptr(logits),
+        _dtype_of(logits), float(temperature), _ptr(loss), _ptr(lse), _ptr(picked), _ptr(workspace), _bytes(workspace),
+        _stream()))
+    return loss, lse, picked
+
+
+def sq_distill_bwd(head, X, W, ids, logits, lse, picked, dloss, temperature=1.0, scales=None, ws2=1.0,
+                   out_dtype=torch.float32, dX=None, workspace=None):
+    """dX [T, I] of sq_distill_fwd for dloss fp32 [T]; lse and picked as it returned them."""
+    head = HEADS.get(head, head)
+    T, V, I, K = _teacher(head, X, W, ids, logits, scales)
+    _need(lse, "lse", _F32, (T,))
+    _need(picked, "picked", _F32, (T, K))
+    _need(dloss, "dloss", _F32, (T,))
+    dX = _out(dX, "dX", (T, I), out_dtype, X.device, _OUT)
+    workspace = _scratch(workspace, load().sq_distill_bwd_workspace(head, T, V, I), X.device)
+    _dev(X, W, ids, logits, scales, lse, picked, dloss, dX, workspace)
+    _check("sq_distill_bwd", load().sq_distill_bwd(
+        head, T, V, I, K, _ptr(X), _ptr(W), _ptr(scales), float(ws2), _ptr(ids), ids.element_size(), _ptr(logits),
+        _dtype_of(logits), float(temperature), _ptr(lse), _ptr(picked), _ptr(dloss), _ptr(dX), _dtype_of(dX),
+        _ptr(workspace), _bytes(workspace), _stream()))
+    return dX
+
+
+# ---------------------------------------------------------------- embedding
+def _ids1(ids):
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        raise ValueError("ids must be a 1-D tensor")
+    _need(ids, "ids", _IDS)
+    return ids.numel()
+
+
+def sq_embed_fwd(head, ids, W, scales=None, ws2=1.0, factor=1.0, out_dtype=torch.bfloat16, out=None):
+    """out [T, I] = factor W[ids] of a table "bf16" (W bf16 [V, I]), "mx" or "nv" (W the codes uint8 [V, I/2], with
+    scales and ws2); ids int32 or int64 [T], rows of ids outside 0 .. V-1 are zeros."""
+    head = HEADS.get(head, head)
+    T = _ids1(ids)
+    V, I = _dims2(W, "W")
+    if head == HEAD_BF16:
+        _need(W, "W", _BF16)
+    else:
+        I *= 2
+        _need(W, "W", _U8)
+        _need(scales, "scales", _U8, (V, _block(head, I)))
+    out = _out(out, "out", (T, I), out_dtype, W.device, _OUT)
+    _dev(ids, W, scales, out)
+    _check("sq_embed_fwd", load().sq_embed_fwd(head, T, V, I, _ptr(ids), ids.element_size(), _ptr(W), _ptr(scales),
+                                               float(ws2), float(factor), _ptr(out), _dtype_of(out), _stream()))
+    return out
+
+
+def sq_embed_bwd_workspace(T, V, I):
+    return int(load().sq_embed_bwd_workspace(T, V, I))
+
+
+def sq_embed_bwd(ids, dOut, V, factor=1.0, out_dtype=torch.float32, dW=None, workspace=None):
+    """dW [V, I] of sq_embed_fwd's bf16 table for dOut [T, I] (fp32 or bf16); zeros where an id has no token."""
+    T = _ids1(ids)
+    I = _dims2(dOut, "dOut")[1]
+    _need(dOut, "dOut", _OUT, (T, I))
+    dW = _out(dW, "dW", (V, I), out_dtype, dOut.device, _OUT)
+    workspace = _scratch(workspace, load().sq_embed_bwd_workspace(T, V, I), dOut.device)
+    _dev(ids, dOut, dW, workspace)
+    _check("sq_embed_bwd", load().sq_embed_bwd(T, V, I, _ptr(ids), ids.element_size(), _ptr(dOut), _dtype_of(dOut),
+                                               float(factor), _ptr(dW), _dtype_of(dW), _ptr(workspace),
+                                               _bytes(workspace), _stream()))
+    return dW
+
+
+def sq_embed_bwd_dscale(fmt, ids, dOut, codes, factor=1.0, dS=None, workspace=None):
+    """dS fp32 [V, I/B] of sq_embed_fwd's 4-bit table (codes uint8 [V, I/2]) for dOut [T, I] (fp32 or bf16)."""
+    fmt = _fmt(fmt)
+    T = _ids1(ids)
+    I = _dims2(dOut, "dOut")[1]
+    _need(dOut, "dOut", _OUT, (T, I))
+    V = _dims2(codes, "codes")[0]
+    G = _layer(fmt, V, I, codes)
+    dS = _out(dS, "dS", (V, G), _F32, dOut.device)
+    workspace = _scratch(workspace, load().sq_embed_bwd_workspace(T, V, I), dOut.device)
+    _dev(ids, dOut, codes, dS, workspace)
+    _check("sq_embed_bwd_dscale", load().sq_embed_bwd_dscale(fmt, T, V, I, _ptr(ids), ids.element_size(), _ptr(dOut),
+                                                             _dtype_of(dOut), float(factor), _ptr(codes), _ptr(dS),
+                                                             _ptr(workspace), _bytes(workspace), _stream()))
+    return dS
 
 
 def abi_version():
