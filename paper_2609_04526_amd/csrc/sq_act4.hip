@@ -18,6 +18,7 @@
 #include "sq_gemm_args.h"
 #include "sq_launch.h"
 #include "sq_rtn.h"
+#include "sq_tiles.h"
 
 namespace sq {
 
@@ -127,6 +128,7 @@ struct Act4Args {
   const int* offsets;       // [E + 1], or null: one layer, rows [0, N)
   void* out;                // [N, O]
   int T, N, E, O, I, G;
+  int Gs;                   // bytes from one row's scales to the next
   int chunks;               // workgroups along the rows
 };
 
@@ -292,10 +294,355 @@ int thin_go(Act4Args g, int bf16, hipStream_t s) {
   return ok();
 }
 
-int product(Act4Args g, int bf16, hipStream_t s) {
-  const int64_t avg = (g.N + g.E - 1) / g.E;
-  if (avg <= 16) return thin_go<1, 1>(g, bf16, s);
-  return thin_go<2, 4>(g, bf16, s);
+// 4 bytes per lane, global -> LDS; lane l writes dst + 4 l.  As dma16.
+__device__ __forceinline__ void dma4(DmaRsrc r, SQ_LDS void* dst, uint32_t voff) {
+  const int lds = __builtin_amdgcn_readfirstlane((int)(uint32_t)reinterpret_cast<uintptr_t>(dst));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(r.v)
+               : "memory", "m0");
+}
+
+// f(0), f(1), .. with constants, in this order.
+template <int... N, typename F>
+__device__ __forceinline__ void for_each(std::integer_sequence<int, N...>, F f) {
+  (f(std::integral_constant<int, N>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void times(F f) {
+  for_each(std::make_integer_sequence<int, N>{}, f);
+}
+
+// Many rows: tiles of 256 outputs by BT rows of Y, so that a lane holds one row's
+// outputs.  A stage is 256 inputs: 128 bytes of codes and 8 scales of each row, copied
+// to LDS with the 16-byte chunks placed as a bf16 tile's (a chunk is one lane's 32
+// codes of a product).  Between a slice's products go the reads of the next slice and
+// the copies of a later stage, and the barrier that publishes the next stage stands
+// amid the last slice.
+template <int BT, int WGM, int WGN, int STAGES, bool BF16>
+__global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
+  constexpr int BM = 256, kStageI = 256, kRow = kStageI / 2, kSlices = 4;
+  constexpr int WM = BM / WGM, WN = BT / WGN, TM = WM / 32, TN = WN / 32;
+  static_assert(WGM * WGN == 8 && TM >= 1 && TN >= 1, "8 waves");
+  constexpr int kA = BM * kRow, kB = BT * kRow, kSa = BM * 8, kSb = BT * 8, kStage = kA + kB + kSa + kSb;
+  static_assert(STAGES * kStage <= 160 * 1024, "LDS");
+  constexpr int kInstA = BM / 64, kInstB = BT / 64, kDma = kInstA + kInstB + 2;
+  constexpr int kAhead = (STAGES - 2) * kDma;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[STAGES * kStage];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+  const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
+
+  // the tile: chunks of one expert's rows beside each other, or groups of 4 x n tiles
+  const int tiles_m = (g.O + BM - 1) / BM;
+  int chunk, tm;
+  if (g.offsets) {
+    const int pos = xcd_stretch((int)blockIdx.x, tiles_m * g.chunks);
+    chunk = pos / tiles_m;
+    tm = pos - chunk * tiles_m;
+  } else {
+    tile_of<4>((int)blockIdx.x, tiles_m * g.chunks, tiles_m, g.chunks, tm, chunk);
+  }
+  const int m0 = tm * BM;
+  const Chunk c = chunk_at(g.offsets, g.E, g.N, BT, chunk);
+  if (c.e < 0) {
+    zero_rows<BF16>(g, c, chunk, m0, BM);
+    return;
+  }
+  const int half = g.I / 2, nk = (g.I + kStageI - 1) / kStageI;
+  const int live_m = min(BM, g.O - m0);
+  const size_t row0 = (size_t)c.e * g.O + m0;
+  const DmaRsrc ra = make_dma_rsrc(g.w + row0 * half, (uint32_t)((size_t)live_m * half));
+  const DmaRsrc rb = make_dma_rsrc(g.x, (uint32_t)((size_t)g.T * half));
+  const DmaRsrc rsa = make_dma_rsrc(g.ws + row0 * g.Gs, (uint32_t)((size_t)live_m * g.Gs));
+  const DmaRsrc rsb = make_dma_rsrc(g.xs, (uint32_t)((size_t)g.T * g.Gs));
+
+  // a copy instruction fills 8 rows of codes, or 32 rows of scales (2 words each)
+  auto kept_row = [&](int r) -> uint32_t {                    // of Y's row c.r0 + r
+    if (c.r0 + r >= c.r1) return kOOB;
+    const int t = g.rows ? g.rows[c.r0 + r] : c.r0 + r;
+    return t >= 0 && t < g.T ? (uint32_t)t : kOOB;
+  };
+  // (rows past the weight's last lie behind the buffer's end)
+  uint32_t off_a, off_b[kInstB];
+  int lim;                                                    // bytes of a row from this lane's chunk on: rows r and r + 64 have the same
+  {
+    const int r = wave * 8 + (lane >> 3), ch = (lane & 7) ^ swz_kc(r);
+    lim = half - 16 * ch;
+    off_a = (uint32_t)r * (uint32_t)half + 16u * ch;
+#pragma unroll
+    for (int q = 0; q < kInstB; ++q) {
+      const uint32_t t = kept_row(q * 64 + r);
+      off_b[q] = t == kOOB ? kOOB : t * (uint32_t)half + 16u * ch;
+    }
+  }
+  // (where the rows have fewer words of scales than there are lanes, waves copy the same)
+  const int sr = wave * 32 + (lane >> 1), srb = sr % BT;
+  const uint32_t off_sa = (uint32_t)sr * (uint32_t)g.Gs + 4u * (lane & 1);
+  const uint32_t t_sb = kept_row(srb);
+  const uint32_t off_sb = t_sb == kOOB ? kOOB : t_sb * (uint32_t)g.Gs + 4u * (lane & 1);
+  const int lim_s = g.Gs - 4 * (lane & 1);
+
+  // each operand's buffers lie beside each other, so that their places are one
+  // register's and a constant
+  constexpr int kAtB = STAGES * kA, kAtSa = kAtB + STAGES * kB, kAtSb = kAtSa + STAGES * kSa;
+  SQ_LDS uint8_t* const lp = (SQ_LDS uint8_t*)lds;
+  // copy n of stage kt into buffer S; what lies past the matrix reads as zeros
+  auto dma = [&](auto S, int kt, auto N) {
+    constexpr int n = decltype(N)::value;
+    constexpr int st = decltype(S)::value;
+    const int k = kt * kRow, ks = kt * 8;
+    if constexpr (n == 0) {
+      dma4(rsa, lp + kAtSa + st * kSa + wave_u * 256, ks >= lim_s ? kOOB : off_sa + (uint32_t)ks);
+    } else if constexpr (n == 1) {
+      dma4(rsb, lp + kAtSb + st * kSb + wave_u * 256 % kSb, off_sb == kOOB || ks >= lim_s ? kOOB : off_sb + (uint32_t)ks);
+    } else if constexpr (n < 2 + kInstA) {
+      constexpr int q = n - 2;
+      dma16(ra, lp + st * kA + (q * 64 + wave_u * 8) * kRow, k >= lim ? kOOB : off_a + (uint32_t)(q * 64 * half + k));
+    } else {
+      constexpr int q = n - 2 - kInstA;
+      dma16(rb, lp + kAtB + st * kB + (q * 64 + wave_u * 8) * kRow, off_b[q] == kOOB || k >= lim ? kOOB : off_b[q] + (uint32_t)k);
+    }
+  };
+  constexpr int kFirst = kDma / 2, kSecond = kDma - kFirst;
+  auto dma_all = [&](auto S, int kt) { times<kDma>([&](auto N) { dma(S, kt, N); }); };
+  auto dma_first = [&](auto S, int kt) { times<kFirst>([&](auto N) { dma(S, kt, N); }); };
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  struct Frag {
+    u32x4 a[TM], b[TN];
+  };
+  Frag F0, F1;
+  // scales of a stage, word w for slices 2 w and 2 w + 1: this lane's byte of the
+  // first in byte 0, of the second in byte 2
+  struct Scales {
+    int a[TM][2], b[TN][2];
+  };
+  Scales sc[2];
+  // Where a slice's chunk of this lane's row is, for row tiles of even number; 32 rows
+  // on, the placement turns bit 2 of the chunk, which is bit 1 of the slice.
+  uint32_t a_at[kSlices], b_at[kSlices];
+#pragma unroll
+  for (int kk = 0; kk < kSlices; ++kk) {
+    const int ra0 = wm0 + (lane & 31), rb0 = wn0 + (lane & 31), ch = 2 * kk + (lane >> 5);
+    a_at[kk] = (uint32_t)(ra0 * kRow + ((ch ^ swz_kc(ra0)) << 4));
+    b_at[kk] = (uint32_t)(kAtB + rb0 * kRow + ((ch ^ swz_kc(rb0)) << 4));
+  }
+  constexpr int kReads = TM + TN, kProducts = TM * TN, kMid = kProducts / 2, kRest = kProducts - kMid;
+  auto read = [&](auto S, auto KK, Frag& f, auto N) {
+    constexpr int n = decltype(N)::value, kk = decltype(KK)::value, st = decltype(S)::value;
+    // a0 b0 b1 .. a1 ..: the order in which the products need them
+    if constexpr (n == 0 || n > TN) {
+      constexpr int i = n == 0 ? 0 : n - TN;
+      f.a[i] = *(const SQ_LDS u32x4*)(lp + a_at[kk ^ (2 * (i & 1))] + st * kA + i * 32 * kRow);
+    } else {
+      constexpr int j = n - 1;
+      f.b[j] = *(const SQ_LDS u32x4*)(lp + b_at[kk ^ (2 * (j & 1))] + st * kB + j * 32 * kRow);
+    }
+  };
+  auto read_scales = [&](auto S, Scales& v, auto N) {
+    constexpr int n = decltype(N)::value;
+    constexpr int st = decltype(S)::value;
+    const int shift = 8 * (lane >> 5);
+    if constexpr (n < TM) {
+      const u32x2 w = *(const SQ_LDS u32x2*)(lp + kAtSa + st * kSa + (wm0 + n * 32 + (lane & 31)) * 8);
+      v.a[n][0] = (int)(w[0] >> shift);
+      v.a[n][1] = (int)(w[1] >> shift);
+    } else {
+      constexpr int j = n - TM;
+      const u32x2 w = *(const SQ_LDS u32x2*)(lp + kAtSb + st * kSb + (wn0 + j * 32 + (lane & 31)) * 8);
+      v.b[j][0] = (int)(w[0] >> shift);
+      v.b[j][1] = (int)(w[1] >> shift);
+    }
+  };
+  auto product = [&](Frag& f, const Scales& v, auto KK, auto N) {
+    constexpr int i = decltype(N)::value / TN, j = decltype(N)::value % TN, kk = decltype(KK)::value, w = kk >> 1, byte = 2 * (kk & 1);
+    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes_operand(f.a[i]), codes_operand(f.b[j]), acc[i][j], 4, 4, byte,
+                                                                v.a[i][w], byte, v.b[j][w]);
+  };
+  // f of those of 0 .. ALL - 1 that fall to part N of PARTS
+  auto share = [&](auto N, auto PARTS, auto ALL, auto f) {
+    constexpr int parts = decltype(PARTS)::value, all = decltype(ALL)::value;
+    constexpr int n = decltype(N)::value < parts ? decltype(N)::value : parts, m = n < parts ? n + 1 : parts;
+    constexpr int lo = n * all / parts, hi = m * all / parts;
+    times<hi - lo>([&](auto K) { f(std::integral_constant<int, lo + decltype(K)::value>{}); });
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using Reads = std::integral_constant<int, kReads>;
+  using Parts = std::integral_constant<int, (kReads < kProducts ? kReads : kProducts)>;
+
+  // V: which of the two sets of scales the stage has
+  auto step = [&](auto S, auto V, int kt) {
+    constexpr int st = decltype(S)::value, v = decltype(V)::value;
+    using SN = std::integral_constant<int, (st + 1) % STAGES>;            // stage kt + 1
+    using SP = std::integral_constant<int, (st + STAGES - 1) % STAGES>;   // stage kt + STAGES - 1
+    times<kSlices - 1>([&](auto KK) {
+      constexpr int kk = decltype(KK)::value;
+      Frag& now = kk & 1 ? F1 : F0;
+      Frag& next = kk & 1 ? F0 : F1;
+      times<kProducts>([&](auto N) {
+        product(now, sc[v], KK, N);
+        share(N, Parts{}, Reads{}, [&](auto R) { read(S, std::integral_constant<int, kk + 1>{}, next, R); });
+        if constexpr (kk == 0)
+          share(N, std::integral_constant<int, kProducts>{}, std::integral_constant<int, kSecond>{},
+                [&](auto C) { dma(SP{}, kt + STAGES - 1, std::integral_constant<int, kFirst + decltype(C)::value>{}); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+    times<kProducts>([&](auto N) {
+      constexpr int n = decltype(N)::value;
+      if constexpr (n == kMid) {
+        // stage kt + 1 has landed once only the copies of the stages after it are
+        // outstanding
+        wait_vm_lgkm0<kAhead>();
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      product(F1, sc[v], std::integral_constant<int, kSlices - 1>{}, N);
+      if constexpr (n >= kMid) {
+        using At = std::integral_constant<int, n - kMid>;
+        using Rest = std::integral_constant<int, kRest>;
+        share(At{}, Rest{}, Reads{}, [&](auto R) {
+          read(SN{}, I0{}, F0, R);
+          read_scales(SN{}, sc[1 - v], R);
+        });
+        share(At{}, Rest{}, std::integral_constant<int, kFirst>{}, [&](auto C) { dma(S, kt + STAGES, C); });
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+
+  // prologue: stage 0 whole and its first operands, then stages 1 .. STAGES - 2 and
+  // the first half of stage STAGES - 1
+  dma_all(I0{}, 0);
+  wait_vm_lgkm0<0>();
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  times<kReads>([&](auto R) {
+    read(I0{}, I0{}, F0, R);
+    read_scales(I0{}, sc[0], R);
+  });
+  if constexpr (STAGES > 2) dma_all(std::integral_constant<int, 1>{}, 1);
+  dma_first(std::integral_constant<int, STAGES - 1>{}, STAGES - 1);
+  // rings of STAGES buffers and 2 sets of scales turn together
+  constexpr int kTurn = STAGES % 2 ? 2 * STAGES : STAGES;
+  for (int kt0 = 0; kt0 < nk; kt0 += kTurn)
+    times<kTurn>([&](auto U) {
+      constexpr int u = decltype(U)::value;
+      if (u > 0 && kt0 + u >= nk) return;
+      step(std::integral_constant<int, u % STAGES>{}, std::integral_constant<int, u % 2>{}, kt0 + u);
+    });
+  wait_vm_lgkm0<0>();
+
+  // 32 x 32 result: lane l, register r holds output 8 (r / 4) + 4 (l / 32) + r % 4 of
+  // row l % 32.
+  if constexpr (BF16) {
+    // through LDS, so that a row's outputs leave together: 16-byte unit u of row n at
+    // unit u ^ n
+    __syncthreads();
+    SQ_LDS uint16_t* s = (SQ_LDS uint16_t*)lds + wave * WM * WN;
+    constexpr int kLanes = WM / 8, kTok = 64 / kLanes;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          u32x2 w;
+          w[0] = bits_of(__builtin_convertvector((f32x2{acc[i][j][4 * q], acc[i][j][4 * q + 1]}), bf16x2));
+          w[1] = bits_of(__builtin_convertvector((f32x2{acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}), bf16x2));
+          const int n = j * 32 + (lane & 31), u = i * 4 + q;
+          *(SQ_LDS u32x2*)(s + n * WM + ((u ^ n) & (kLanes - 1)) * 8 + 4 * (lane >> 5)) = w;
+        }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int it = 0; it < WN / kTok; ++it) {
+      const int n = it * kTok + lane / kLanes, u = lane % kLanes;
+      const u32x4 v = *(const SQ_LDS u32x4*)(s + n * WM + ((u ^ n) & (kLanes - 1)) * 8);
+      const int row = c.r0 + wn0 + n, o = m0 + wm0 + 8 * u;
+      if (row < c.r1 && o < g.O) *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(g.out) + (size_t)row * g.O + o) = v;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int row = c.r0 + wn0 + j * 32 + (lane & 31);
+      if (row >= c.r1) continue;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int o = m0 + wm0 + i * 32 + 8 * q + 4 * (lane >> 5);
+          if (o < g.O)
+            put4<false>(g.out, (size_t)row * g.O + o, f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+        }
+    }
+  }
+}
+
+// Scale rows of G bytes laid out in whole words.
+__global__ __launch_bounds__(256) void act4_words_kernel(const uint8_t* __restrict__ from, int64_t rows, int G, int words,
+                                                         uint32_t* __restrict__ to) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * words) return;
+  const int64_t r = i / words;
+  const int k = (int)(i - r * words) * 4;
+  uint32_t v = 0;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) v |= k + b < G ? (uint32_t)from[r * G + k + b] << (8 * b) : 0u;
+  to[i] = v;
+}
+
+template <int BT, int WGM, int WGN, int STAGES>
+int tile_go(Act4Args g, int bf16, hipStream_t s) {
+  g.chunks = g.offsets ? g.N / BT + (g.E < g.N ? g.E : g.N) + 1 : (g.N + BT - 1) / BT;
+  const dim3 grid((unsigned)((g.O + 255) / 256 * g.chunks)), block(512);
+  if (bf16) hipLaunchKernelGGL((act4_tile_kernel<BT, WGM, WGN, STAGES, true>), grid, block, 0, s, g);
+  else hipLaunchKernelGGL((act4_tile_kernel<BT, WGM, WGN, STAGES, false>), grid, block, 0, s, g);
+  return ok();
+}
+
+// Rows per tile (0: the few rows' kernel), by the rows of a layer or of an expert on average.
+int tile_rows(int64_t E, int64_t N, int64_t O) {
+#ifdef SQ_ACT4_BT
+  return SQ_ACT4_BT;
+#endif
+  const int64_t avg = (N + E - 1) / E, tiles = (O + 255) / 256 * E;
+  if (avg <= 16) return 0;
+  // the largest tiles that still fill the CUs
+  if (tiles * ((avg + 255) / 256) >= kCUs) return 256;
+  return tiles * ((avg + 127) / 128) >= kCUs ? 128 : 64;
+}
+
+// Scales whose rows are not whole words: bytes of their copies for the tiles.
+size_t scale_words(int64_t E, int64_t T, int64_t N, int64_t O, int64_t I) {
+  const int64_t G = I / 32;
+  return G % 4 == 0 || tile_rows(E, N, O) == 0 ? 0 : (size_t)((T + E * O) * ((G + 3) / 4 * 4));
+}
+
+int product(Act4Args g, int bf16, void* workspace, hipStream_t s) {
+  const int bt = tile_rows(g.E, g.N, g.O);
+  g.Gs = g.G;
+  if (bt == 0) return (g.N + g.E - 1) / g.E <= 16 ? thin_go<1, 1>(g, bf16, s) : thin_go<2, 4>(g, bf16, s);
+  if (g.G % 4 != 0) {
+    const int words = (g.G + 3) / 4;
+    uint32_t* to = static_cast<uint32_t*>(workspace);
+    auto lay = [&](const uint8_t* from, int64_t rows, uint32_t* at) {
+      hipLaunchKernelGGL(act4_words_kernel, dim3((unsigned)((rows * words + 255) / 256)), dim3(256), 0, s, from, rows, g.G, words, at);
+      return ok();
+    };
+    uint32_t* ws = to + (size_t)g.T * words;
+    if (lay(g.xs, g.T, to) != 0 || lay(g.ws, (int64_t)g.E * g.O, ws) != 0) return -1;
+    g.xs = reinterpret_cast<uint8_t*>(to);
+    g.ws = reinterpret_cast<uint8_t*>(ws);
+    g.Gs = 4 * words;
+  }
+  if (bt == 64) return tile_go<64, 8, 1, 3>(g, bf16, s);
+  return bt == 128 ? tile_go<128, 4, 2, 3>(g, bf16, s) : tile_go<256, 2, 4, 2>(g, bf16, s);
 }
 
 }  // namespace
@@ -319,7 +666,9 @@ int act4_unpack_launch(int fmt, int64_t T, int64_t I, const uint8_t* codes, cons
   return ok();
 }
 
-size_t act4_workspace(int fmt, int64_t T, int64_t O, int64_t I) { return fmt == kMX ? 0 : (size_t)T * I * 2; }
+size_t act4_workspace(int fmt, int64_t T, int64_t O, int64_t I) {
+  return fmt == kMX ? scale_words(1, T, T, O, I) : (size_t)T * I * 2;
+}
 
 int act4_fwd(int fmt, int T, int O, int I, const uint8_t* x, const uint8_t* xs, float x_ws2, const uint8_t* codes,
              const uint8_t* scales, float ws2, void* Y, int y_bf16, void* workspace, hipStream_t s) {
@@ -330,10 +679,10 @@ int act4_fwd(int fmt, int T, int O, int I, const uint8_t* x, const uint8_t* xs, 
   Act4Args g{};
   g.x = x; g.xs = xs; g.w = codes; g.ws = scales; g.out = Y;
   g.T = g.N = T; g.E = 1; g.O = O; g.I = I; g.G = I / 32;
-  return product(g, y_bf16, s);
+  return product(g, y_bf16, workspace, s);
 }
 
-size_t act4_batched_workspace(int64_t E, int64_t T, int64_t O, int64_t I) { return 0; }
+size_t act4_batched_workspace(int64_t E, int64_t T, int64_t N, int64_t O, int64_t I) { return scale_words(E, T, N, O, I); }
 
 int act4_fwd_batched(int E, int T, int N, int O, int I, const uint8_t* x, const uint8_t* xs, const int* rows,
                      const int* offsets, const uint8_t* codes, const uint8_t* scales, void* Y, int y_bf16, void* workspace,
@@ -341,7 +690,7 @@ int act4_fwd_batched(int E, int T, int N, int O, int I, const uint8_t* x, const 
   Act4Args g{};
   g.x = x; g.xs = xs; g.w = codes; g.ws = scales; g.out = Y; g.rows = rows; g.offsets = offsets;
   g.T = T; g.N = N; g.E = E; g.O = O; g.I = I; g.G = I / 32;
-  return product(g, y_bf16, s);
+  return product(g, y_bf16, workspace, s);
 }
 
 }  // namespace sq

@@ -85,7 +85,7 @@ SQ_EXPORT int sq_fwd_act4(int fmt, int64_t T, int64_t O, int64_t I, const uint8_
 }
 
 SQ_EXPORT size_t sq_fwd_act4_batched_workspace(int fmt, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I) {
-  return check_batched(fmt, E, T, N, O, I) != SQ_OK || N == 0 ? 0 : act4_batched_workspace(E, T, O, I);
+  return check_batched(fmt, E, T, N, O, I) != SQ_OK || N == 0 ? 0 : act4_batched_workspace(E, T, N, O, I);
 }
 
 SQ_EXPORT int sq_fwd_act4_batched(int fmt, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I, const uint8_t* x_codes,
@@ -98,7 +98,7 @@ SQ_EXPORT int sq_fwd_act4_batched(int fmt, int64_t E, int64_t T, int64_t N, int6
   if (!offsets || (N > 0 && !rows && N != T)) return SQ_ERR_ARG;
   if (!aligned(rows, 4) || !aligned(offsets, 4)) return SQ_ERR_ALIGN;
   if (N == 0) return SQ_OK;
-  st = check_workspace(act4_batched_workspace(E, T, O, I), workspace, workspace_bytes);
+  st = check_workspace(act4_batched_workspace(E, T, N, O, I), workspace, workspace_bytes);
   if (st != SQ_OK) return st;
   return hip_status(act4_fwd_batched((int)E, (int)T, (int)N, (int)O, (int)I, x_codes, x_scales, rows, offsets, codes, scales, Y,
                                      y_dtype == SQ_OUT_BF16, workspace, static_cast<hipStream_t>(stream)));

@@ -213,7 +213,7 @@ int act4_unpack_launch(int fmt, int64_t T, int64_t I, const uint8_t* codes, cons
 size_t act4_workspace(int fmt, int64_t T, int64_t O, int64_t I);
 int act4_fwd(int fmt, int T, int O, int I, const uint8_t* x, const uint8_t* xs, float x_ws2, const uint8_t* codes,
              const uint8_t* scales, float ws2, void* Y, int y_bf16, void* workspace, hipStream_t s);
-size_t act4_batched_workspace(int64_t E, int64_t T, int64_t O, int64_t I);
+size_t act4_batched_workspace(int64_t E, int64_t T, int64_t N, int64_t O, int64_t I);
 int act4_fwd_batched(int E, int T, int N, int O, int I, const uint8_t* x, const uint8_t* xs, const int* rows,
                      const int* offsets, const uint8_t* codes, const uint8_t* scales, void* Y, int y_bf16,
                      void* workspace, hipStream_t s);
