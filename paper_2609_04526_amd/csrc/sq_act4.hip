@@ -294,13 +294,6 @@ int thin_go(Act4Args g, int bf16, hipStream_t s) {
   return ok();
 }
 
-// 4 bytes per lane, global -> LDS; lane l writes dst + 4 l.  As dma16.
-__device__ __forceinline__ void dma4(DmaRsrc r, SQ_LDS void* dst, uint32_t voff) {
-  const int lds = __builtin_amdgcn_readfirstlane((int)(uint32_t)reinterpret_cast<uintptr_t>(dst));
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(r.v)
-               : "memory", "m0");
-}
-
 // f(0), f(1), .. with constants, in this order.
 template <int... N, typename F>
 __device__ __forceinline__ void for_each(std::integer_sequence<int, N...>, F f) {
@@ -312,32 +305,39 @@ __device__ __forceinline__ void times(F f) {
 }
 
 // Many rows: tiles of 256 outputs by BT rows of Y, so that a lane holds one row's
-// outputs.  A stage is 256 inputs: 128 bytes of codes and 8 scales of each row, copied
-// to LDS with the 16-byte chunks placed as a bf16 tile's (a chunk is one lane's 32
-// codes of a product).  Between a slice's products go the reads of the next slice and
-// the copies of a later stage, and the barrier that publishes the next stage stands
-// amid the last slice.
+// outputs.  A stage is 256 inputs: the 128 bytes of codes of each row, a cache line,
+// copied to LDS with the 16-byte chunks placed as a bf16 tile's (a chunk is one lane's
+// 32 codes of a product); the scales come for two stages at a time, 16 bytes of each
+// row.  Between a slice's products go the reads of the next slice and the copies of a
+// later stage, and the barrier that publishes the next stage stands amid the last
+// slice.
 template <int BT, int WGM, int WGN, int STAGES, bool BF16>
 __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   constexpr int BM = 256, kStageI = 256, kRow = kStageI / 2, kSlices = 4;
   constexpr int WM = BM / WGM, WN = BT / WGN, TM = WM / 32, TN = WN / 32;
   static_assert(WGM * WGN == 8 && TM >= 1 && TN >= 1, "8 waves");
-  constexpr int kA = BM * kRow, kB = BT * kRow, kSa = BM * 8, kSb = BT * 8, kStage = kA + kB + kSa + kSb;
-  static_assert(STAGES * kStage <= 160 * 1024, "LDS");
-  constexpr int kInstA = BM / 64, kInstB = BT / 64, kDma = kInstA + kInstB + 2;
+  constexpr int kA = BM * kRow, kB = BT * kRow, kSa = BM * 16, kSb = BT * 16;
+  constexpr int kInstA = BM / 64, kInstB = BT / 64, kDma = kInstA + kInstB;
   constexpr int kAhead = (STAGES - 2) * kDma;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[STAGES * kStage];
+  // each operand's buffers lie beside each other, so that their places are one
+  // register's and a constant
+  constexpr int kAtB = STAGES * kA, kAtSa = kAtB + STAGES * kB, kAtSb = kAtSa + 2 * kSa, kAll = kAtSb + 2 * kSb;
+  static_assert(kAll <= 160 * 1024 && BM * BT * 2 <= kAll, "LDS, of the loop and of the outputs in bf16");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kAll];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
 
-  // the tile: chunks of one expert's rows beside each other, or groups of 4 x n tiles
+  // the tile: chunks of the experts' rows dealt to the XCDs in turn (those past the
+  // last are spread as well), with their tiles of outputs beside each other, or groups
+  // of 4 x n tiles
   const int tiles_m = (g.O + BM - 1) / BM;
   int chunk, tm;
   if (g.offsets) {
-    const int pos = xcd_stretch((int)blockIdx.x, tiles_m * g.chunks);
-    chunk = pos / tiles_m;
-    tm = pos - chunk * tiles_m;
+    const int at = (int)blockIdx.x / kXcds;
+    chunk = at / tiles_m * kXcds + (int)blockIdx.x % kXcds;
+    tm = at % tiles_m;
+    if (chunk >= g.chunks) return;
   } else {
     tile_of<4>((int)blockIdx.x, tiles_m * g.chunks, tiles_m, g.chunks, tm, chunk);
   }
@@ -352,10 +352,15 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   const size_t row0 = (size_t)c.e * g.O + m0;
   const DmaRsrc ra = make_dma_rsrc(g.w + row0 * half, (uint32_t)((size_t)live_m * half));
   const DmaRsrc rb = make_dma_rsrc(g.x, (uint32_t)((size_t)g.T * half));
-  const DmaRsrc rsa = make_dma_rsrc(g.ws + row0 * g.Gs, (uint32_t)((size_t)live_m * g.Gs));
-  const DmaRsrc rsb = make_dma_rsrc(g.xs, (uint32_t)((size_t)g.T * g.Gs));
+  // a wave copies the scales of 64 rows: the first four the weight's, the others Y's
+  // (where those are fewer, several waves the same)
+  const bool weights = wave_u < 4;
+  const DmaRsrc rs = weights ? make_dma_rsrc(g.ws + row0 * g.Gs, (uint32_t)((size_t)live_m * g.Gs))
+                             : make_dma_rsrc(g.xs, (uint32_t)((size_t)g.T * g.Gs));
+  const int s_row = wave_u * 64 % (weights ? BM : BT);
+  const int s_to = (weights ? kAtSa : kAtSb) + s_row * 16, s_group = weights ? kSa : kSb;
 
-  // a copy instruction fills 8 rows of codes, or 32 rows of scales (2 words each)
+  // a copy instruction fills 8 rows of codes
   auto kept_row = [&](int r) -> uint32_t {                    // of Y's row c.r0 + r
     if (c.r0 + r >= c.r1) return kOOB;
     const int t = g.rows ? g.rows[c.r0 + r] : c.r0 + r;
@@ -374,33 +379,26 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
       off_b[q] = t == kOOB ? kOOB : t * (uint32_t)half + 16u * ch;
     }
   }
-  // (where the rows have fewer words of scales than there are lanes, waves copy the same)
-  const int sr = wave * 32 + (lane >> 1), srb = sr % BT;
-  const uint32_t off_sa = (uint32_t)sr * (uint32_t)g.Gs + 4u * (lane & 1);
-  const uint32_t t_sb = kept_row(srb);
-  const uint32_t off_sb = t_sb == kOOB ? kOOB : t_sb * (uint32_t)g.Gs + 4u * (lane & 1);
-  const int lim_s = g.Gs - 4 * (lane & 1);
+  const uint32_t t_s = weights ? (uint32_t)(s_row + lane) : kept_row(s_row + lane);
+  const uint32_t off_s = t_s == kOOB ? kOOB : t_s * (uint32_t)g.Gs;
 
-  // each operand's buffers lie beside each other, so that their places are one
-  // register's and a constant
-  constexpr int kAtB = STAGES * kA, kAtSa = kAtB + STAGES * kB, kAtSb = kAtSa + STAGES * kSa;
   SQ_LDS uint8_t* const lp = (SQ_LDS uint8_t*)lds;
   // copy n of stage kt into buffer S; what lies past the matrix reads as zeros
   auto dma = [&](auto S, int kt, auto N) {
     constexpr int n = decltype(N)::value;
     constexpr int st = decltype(S)::value;
-    const int k = kt * kRow, ks = kt * 8;
-    if constexpr (n == 0) {
-      dma4(rsa, lp + kAtSa + st * kSa + wave_u * 256, ks >= lim_s ? kOOB : off_sa + (uint32_t)ks);
-    } else if constexpr (n == 1) {
-      dma4(rsb, lp + kAtSb + st * kSb + wave_u * 256 % kSb, off_sb == kOOB || ks >= lim_s ? kOOB : off_sb + (uint32_t)ks);
-    } else if constexpr (n < 2 + kInstA) {
-      constexpr int q = n - 2;
-      dma16(ra, lp + st * kA + (q * 64 + wave_u * 8) * kRow, k >= lim ? kOOB : off_a + (uint32_t)(q * 64 * half + k));
+    const int k = kt * kRow;
+    if constexpr (n < kInstA) {
+      dma16(ra, lp + st * kA + (n * 64 + wave_u * 8) * kRow, k >= lim ? kOOB : off_a + (uint32_t)(n * 64 * half + k));
     } else {
-      constexpr int q = n - 2 - kInstA;
+      constexpr int q = n - kInstA;
       dma16(rb, lp + kAtB + st * kB + (q * 64 + wave_u * 8) * kRow, off_b[q] == kOOB || k >= lim ? kOOB : off_b[q] + (uint32_t)k);
     }
+  };
+  // the scales of stages 2 p and 2 p + 1 into set p % 2; where a row ends inside its 16
+  // bytes, the next row's follow
+  auto dma_scales = [&](int p) {
+    dma16(rs, lp + s_to + (p & 1) * s_group, off_s == kOOB || p * 16 >= g.Gs ? kOOB : off_s + (uint32_t)(p * 16));
   };
   constexpr int kFirst = kDma / 2, kSecond = kDma - kFirst;
   auto dma_all = [&](auto S, int kt) { times<kDma>([&](auto N) { dma(S, kt, N); }); };
@@ -445,20 +443,17 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
       f.b[j] = *(const SQ_LDS u32x4*)(lp + b_at[kk ^ (2 * (j & 1))] + st * kB + j * 32 * kRow);
     }
   };
-  auto read_scales = [&](auto S, Scales& v, auto N) {
-    constexpr int n = decltype(N)::value;
-    constexpr int st = decltype(S)::value;
-    const int shift = 8 * (lane >> 5);
-    if constexpr (n < TM) {
-      const u32x2 w = *(const SQ_LDS u32x2*)(lp + kAtSa + st * kSa + (wm0 + n * 32 + (lane & 31)) * 8);
-      v.a[n][0] = (int)(w[0] >> shift);
-      v.a[n][1] = (int)(w[1] >> shift);
-    } else {
-      constexpr int j = n - TM;
-      const u32x2 w = *(const SQ_LDS u32x2*)(lp + kAtSb + st * kSb + (wn0 + j * 32 + (lane & 31)) * 8);
-      v.b[j][0] = (int)(w[0] >> shift);
-      v.b[j][1] = (int)(w[1] >> shift);
-    }
+  const uint32_t sa_at = (uint32_t)(kAtSa + (wm0 + (lane & 31)) * 16), sb_at = (uint32_t)(kAtSb + (wn0 + (lane & 31)) * 16);
+  auto read_scales = [&](int kt, auto ODD, Scales& v, auto N) {
+    constexpr int n = decltype(N)::value, odd = decltype(ODD)::value;
+    const int shift = 8 * (lane >> 5), set = (kt >> 1) & 1;
+    // blocks past the row's end have zero codes, and the next row's scales may be NaN
+    const uint32_t in0 = kt * 8 < g.Gs ? ~0u : 0u, in1 = kt * 8 + 4 < g.Gs ? ~0u : 0u;
+    const u32x2 w = n < TM ? *(const SQ_LDS u32x2*)(lp + sa_at + set * kSa + n * 512 + odd * 8)
+                           : *(const SQ_LDS u32x2*)(lp + sb_at + set * kSb + (n - TM) * 512 + odd * 8);
+    int* to = n < TM ? v.a[n < TM ? n : 0] : v.b[n < TM ? 0 : n - TM];
+    to[0] = (int)((w[0] & in0) >> shift);
+    to[1] = (int)((w[1] & in1) >> shift);
   };
   auto product = [&](Frag& f, const Scales& v, auto KK, auto N) {
     constexpr int i = decltype(N)::value / TN, j = decltype(N)::value % TN, kk = decltype(KK)::value, w = kk >> 1, byte = 2 * (kk & 1);
@@ -491,6 +486,7 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
         if constexpr (kk == 0)
           share(N, std::integral_constant<int, kProducts>{}, std::integral_constant<int, kSecond>{},
                 [&](auto C) { dma(SP{}, kt + STAGES - 1, std::integral_constant<int, kFirst + decltype(C)::value>{}); });
+        if constexpr (kk == 0 && v == 0 && decltype(N)::value == kProducts - 1) dma_scales((kt >> 1) + 1);
         __builtin_amdgcn_sched_barrier(0);
       });
     });
@@ -498,8 +494,8 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
       constexpr int n = decltype(N)::value;
       if constexpr (n == kMid) {
         // stage kt + 1 has landed once only the copies of the stages after it are
-        // outstanding
-        wait_vm_lgkm0<kAhead>();
+        // outstanding; in an even one also the scales of the two stages after that
+        wait_vm_lgkm0<kAhead + (v == 0)>();
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -509,7 +505,7 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
         using Rest = std::integral_constant<int, kRest>;
         share(At{}, Rest{}, Reads{}, [&](auto R) {
           read(SN{}, I0{}, F0, R);
-          read_scales(SN{}, sc[1 - v], R);
+          read_scales(kt + 1, std::integral_constant<int, 1 - v>{}, sc[1 - v], R);
         });
         share(At{}, Rest{}, std::integral_constant<int, kFirst>{}, [&](auto C) { dma(S, kt + STAGES, C); });
       }
@@ -520,12 +516,13 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   // prologue: stage 0 whole and its first operands, then stages 1 .. STAGES - 2 and
   // the first half of stage STAGES - 1
   dma_all(I0{}, 0);
+  dma_scales(0);
   wait_vm_lgkm0<0>();
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_sched_barrier(0);
   times<kReads>([&](auto R) {
     read(I0{}, I0{}, F0, R);
-    read_scales(I0{}, sc[0], R);
+    read_scales(0, I0{}, sc[0], R);
   });
   if constexpr (STAGES > 2) dma_all(std::integral_constant<int, 1>{}, 1);
   dma_first(std::integral_constant<int, STAGES - 1>{}, STAGES - 1);
@@ -600,7 +597,8 @@ __global__ __launch_bounds__(256) void act4_words_kernel(const uint8_t* __restri
 template <int BT, int WGM, int WGN, int STAGES>
 int tile_go(Act4Args g, int bf16, hipStream_t s) {
   g.chunks = g.offsets ? g.N / BT + (g.E < g.N ? g.E : g.N) + 1 : (g.N + BT - 1) / BT;
-  const dim3 grid((unsigned)((g.O + 255) / 256 * g.chunks)), block(512);
+  const int along = g.offsets ? (g.chunks + kXcds - 1) / kXcds * kXcds : g.chunks;
+  const dim3 grid((unsigned)((g.O + 255) / 256 * along)), block(512);
   if (bf16) hipLaunchKernelGGL((act4_tile_kernel<BT, WGM, WGN, STAGES, true>), grid, block, 0, s, g);
   else hipLaunchKernelGGL((act4_tile_kernel<BT, WGM, WGN, STAGES, false>), grid, block, 0, s, g);
   return ok();
