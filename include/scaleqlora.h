@@ -662,8 +662,8 @@ int sq_ce_bwd(int head, int64_t T, int64_t V, int64_t I, const void* X, const vo
  *   (sq_moe_sort's token) times the expert's weight, or row s with rows NULL
  *   (then N == T).  Rows that no expert has, before offsets[0] and from
  *   offsets[E] on, are zeros; a row number outside 0 .. T-1 reads as a row of
- *   zeros, and offsets are held to 0 .. N.  E <= 8192; (N/16 + min(E, N) + 1)
- *   ceil(O/16) <= 2^22.
+ *   zeros, and offsets are held to 0 .. N.  E <= 8192; (N/64 + min(E, N) + 8)
+ *   ceil(O/128) <= 2^22.
  * x_codes and codes 16-byte, x_scales and scales 4-byte aligned; workspace: at
  * least the bytes of the _workspace call, 256-byte aligned (NULL where that is
  * 0), contents irrelevant.  Deterministic.

@@ -130,6 +130,7 @@ struct Act4Args {
   int T, N, E, O, I, G;
   int Gs;                   // bytes from one row's scales to the next
   int chunks;               // workgroups along the rows
+  int splits, per;          // of the sum over the inputs: planes [N, O] of `per` stages each (an even number), one layer only
 };
 
 // Which rows of Y a workgroup takes: chunk c of the experts' ranges, each cut into
@@ -200,22 +201,23 @@ __device__ __forceinline__ i32x8 codes_operand(u32x4 c) {
 }
 
 // Few rows: the weight's codes go from memory into the operand registers, each once
-// per chunk of 16 NT rows.  A workgroup takes 16 RM outputs; its waves share the
-// steps of 128 inputs in turn, and their sums meet in LDS in wave order.
-template <int RM, int NT, bool BF16>
+// per chunk of 16 NT rows.  A workgroup takes 16 RM outputs; its waves take a stretch of
+// the inputs each, in steps of 128, and their sums meet in LDS in wave order.  WORDS:
+// scale rows are whole words, and 4 steps' scales of a row come in one load.
+template <int RM, int NT, bool WORDS, bool BF16>
 __global__ __launch_bounds__(512) void act4_thin_kernel(Act4Args g) {
-  constexpr int kWaves = 8, kUnroll = 4;
+  constexpr int kWaves = 8, kUnroll = WORDS && RM * NT <= 8 ? 4 : 2;
   __shared__ f32x4 part[kWaves][RM * NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int groups = (g.O + 16 * RM - 1) / (16 * RM);
-  const int o0 = (int)(blockIdx.x % groups) * 16 * RM;
-  const int chunk = (int)(blockIdx.x / groups);
+  const int chunk = (int)(blockIdx.x / groups), o0 = (int)(blockIdx.x % groups) * 16 * RM;
   const Chunk c = chunk_at(g.offsets, g.E, g.N, 16 * NT, chunk);
   if (c.e < 0) {
     zero_rows<BF16>(g, c, chunk, o0, 16 * RM);
     return;
   }
   const int half = g.I / 2, steps = (g.I + 127) / 128, kb = lane >> 4;
+  const int per = (steps + kWaves - 1) / kWaves, first = wave * per, end = min(first + per, steps);
   const __amdgpu_buffer_rsrc_t rw = make_rsrc(g.w + (size_t)c.e * g.O * half, (uint32_t)((size_t)g.O * half));
   const __amdgpu_buffer_rsrc_t rws = make_rsrc(g.ws + (size_t)c.e * g.O * g.G, (uint32_t)((size_t)g.O * g.G));
   const __amdgpu_buffer_rsrc_t rx = make_rsrc(g.x, (uint32_t)((size_t)g.T * half));
@@ -240,31 +242,49 @@ __global__ __launch_bounds__(512) void act4_thin_kernel(Act4Args g) {
   for (int m = 0; m < RM; ++m)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[m][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s0 = wave; s0 < steps; s0 += kWaves * kUnroll) {
+  for (int s0 = first; s0 < end; s0 += kUnroll) {
     u32x4 wc[kUnroll][RM], xc[kUnroll][NT];
-    int wb[kUnroll][RM], xb[kUnroll][NT];
+    uint32_t wb[kUnroll][RM], xb[kUnroll][NT];
+    // of one row: this lane's codes of each step (zeros past the inputs), and the
+    // steps' scales; with WORDS those past the row's end are another's, of steps that
+    // are not taken
+    auto load = [&](__amdgpu_buffer_rsrc_t rc, __amdgpu_buffer_rsrc_t rs, uint32_t row, auto put) {
+      u32x4 words = {0u, 0u, 0u, 0u};
+      if constexpr (WORDS) {
+        const int at = (int)(row == kOOB ? kOOB : row * (uint32_t)g.G + 4u * (uint32_t)s0);
+        if constexpr (kUnroll == 4) {
+          words = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0));
+        } else {
+          const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0));
+          words[0] = v[0];
+          words[1] = v[1];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint32_t b = (uint32_t)(s0 + u) * 4 + kb;       // this lane's block of 32 inputs
+        const bool in = s0 + u < end && b < (uint32_t)g.G && row != kOOB;
+        const u32x4 q = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, (int)(in ? row * (uint32_t)half + 16u * b : kOOB), 0, 0));
+        uint32_t s;
+        if constexpr (WORDS) s = words[u] >> (8 * kb);
+        else s = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(in ? row * (uint32_t)g.G + b : kOOB), 0, 0);
+        put(u, q, s);
+      }
+    };
+#pragma unroll
+    for (int m = 0; m < RM; ++m) load(rw, rws, w_row[m], [&](int u, u32x4 q, uint32_t s) { wc[u][m] = q; wb[u][m] = s; });
+#pragma unroll
+    for (int j = 0; j < NT; ++j) load(rx, rxs, x_row[j], [&](int u, u32x4 q, uint32_t s) { xc[u][j] = q; xb[u][j] = s; });
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const uint32_t b = (uint32_t)(s0 + u * kWaves) * 4 + kb;      // this lane's block of 32 inputs
-      const bool in = b < (uint32_t)g.G;
-      auto load = [&](__amdgpu_buffer_rsrc_t rc, __amdgpu_buffer_rsrc_t rs, uint32_t row, u32x4& codes, int& byte) {
-        const bool live = in && row != kOOB;
-        codes = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, (int)(live ? row * (uint32_t)half + 16u * b : kOOB), 0, 0));
-        byte = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(live ? row * (uint32_t)g.G + b : kOOB), 0, 0);
-      };
-#pragma unroll
-      for (int m = 0; m < RM; ++m) load(rw, rws, w_row[m], wc[u][m], wb[u][m]);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) load(rx, rxs, x_row[j], xc[u][j], xb[u][j]);
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
+      if (s0 + u >= end) break;
 #pragma unroll
       for (int m = 0; m < RM; ++m)
 #pragma unroll
         for (int j = 0; j < NT; ++j)
           acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes_operand(wc[u][m]), codes_operand(xc[u][j]), acc[m][j], 4, 4, 0,
-                                                                       wb[u][m], 0, xb[u][j]);
+                                                                       (int)wb[u][m], 0, (int)xb[u][j]);
+    }
   }
 #pragma unroll
   for (int m = 0; m < RM; ++m)
@@ -286,12 +306,24 @@ template <int RM, int NT>
 int thin_go(Act4Args g, int bf16, hipStream_t s) {
   // every range's last chunk may be short, and one more chunk for the rows of no expert
   g.chunks = g.offsets ? (int)(g.N / (16 * NT) + (g.E < g.N ? g.E : g.N) + 1) : (g.N + 16 * NT - 1) / (16 * NT);
-  const int64_t groups = (g.O + 16 * RM - 1) / (16 * RM);
-  if (groups * g.chunks > kGroupsX) return -1;
-  const dim3 grid((unsigned)(groups * g.chunks)), block(512);
-  if (bf16) hipLaunchKernelGGL((act4_thin_kernel<RM, NT, true>), grid, block, 0, s, g);
-  else hipLaunchKernelGGL((act4_thin_kernel<RM, NT, false>), grid, block, 0, s, g);
-  return ok();
+  const dim3 grid((unsigned)((g.O + 16 * RM - 1) / (16 * RM) * g.chunks)), block(512);
+  const bool words = g.G % 4 == 0;
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, g);
+    return ok();
+  };
+  if (words) return bf16 ? go(act4_thin_kernel<RM, NT, true, true>) : go(act4_thin_kernel<RM, NT, true, false>);
+  return bf16 ? go(act4_thin_kernel<RM, NT, false, true>) : go(act4_thin_kernel<RM, NT, false, false>);
+}
+
+// Outputs per workgroup: the more, the less often the rows are read, but a workgroup
+// for every CU.
+template <int NT>
+int thin_by(const Act4Args& g, int bf16, hipStream_t s) {
+  const int64_t chunks = g.offsets ? (g.E < g.N ? g.E : g.N) : 1;
+  const int64_t groups = (g.O + 63) / 64 * chunks;
+  if (groups >= kCUs * 3 / 4) return thin_go<4, NT>(g, bf16, s);
+  return 2 * groups >= kCUs * 3 / 4 ? thin_go<2, NT>(g, bf16, s) : thin_go<1, NT>(g, bf16, s);
 }
 
 // f(0), f(1), .. with constants, in this order.
@@ -311,17 +343,21 @@ __device__ __forceinline__ void times(F f) {
 // row.  Between a slice's products go the reads of the next slice and the copies of a
 // later stage, and the barrier that publishes the next stage stands amid the last
 // slice.
-template <int BT, int WGM, int WGN, int STAGES, bool BF16>
+template <int BM, int BT, int WGM, int WGN, int STAGES, bool BF16>
 __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
-  constexpr int BM = 256, kStageI = 256, kRow = kStageI / 2, kSlices = 4;
+  constexpr int kStageI = 256, kRow = kStageI / 2, kSlices = 4;
   constexpr int WM = BM / WGM, WN = BT / WGN, TM = WM / 32, TN = WN / 32;
   static_assert(WGM * WGN == 8 && TM >= 1 && TN >= 1, "8 waves");
   constexpr int kA = BM * kRow, kB = BT * kRow, kSa = BM * 16, kSb = BT * 16;
   constexpr int kInstA = BM / 64, kInstB = BT / 64, kDma = kInstA + kInstB;
   constexpr int kAhead = (STAGES - 2) * kDma;
+  // Scales of stages 2 p and 2 p + 1 are copied behind the codes of stage 2 p - 1 (2 p
+  // with three stages), in the first slice of an even stage, kLead pairs ahead of it.
+  static_assert(STAGES == 2 || STAGES == 3 || STAGES == 4 || STAGES == 6, "stages");
+  constexpr int kLead = STAGES == 3 ? 1 : STAGES / 2, kSets = STAGES <= 3 ? 2 : 4;
   // each operand's buffers lie beside each other, so that their places are one
   // register's and a constant
-  constexpr int kAtB = STAGES * kA, kAtSa = kAtB + STAGES * kB, kAtSb = kAtSa + 2 * kSa, kAll = kAtSb + 2 * kSb;
+  constexpr int kAtB = STAGES * kA, kAtSa = kAtB + STAGES * kB, kAtSb = kAtSa + kSets * kSa, kAll = kAtSb + kSets * kSb;
   static_assert(kAll <= 160 * 1024 && BM * BT * 2 <= kAll, "LDS, of the loop and of the outputs in bf16");
   __shared__ __attribute__((aligned(16))) uint8_t lds[kAll];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -332,14 +368,16 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   // last are spread as well), with their tiles of outputs beside each other, or groups
   // of 4 x n tiles
   const int tiles_m = (g.O + BM - 1) / BM;
-  int chunk, tm;
+  int chunk, tm, split = 0;
   if (g.offsets) {
     const int at = (int)blockIdx.x / kXcds;
     chunk = at / tiles_m * kXcds + (int)blockIdx.x % kXcds;
     tm = at % tiles_m;
     if (chunk >= g.chunks) return;
   } else {
-    tile_of<4>((int)blockIdx.x, tiles_m * g.chunks, tiles_m, g.chunks, tm, chunk);
+    const int tiles = tiles_m * g.chunks, pos = xcd_stretch((int)blockIdx.x, tiles * g.splits);
+    split = pos / tiles;
+    tile_at<4>(pos - split * tiles, tiles_m, g.chunks, tm, chunk);
   }
   const int m0 = tm * BM;
   const Chunk c = chunk_at(g.offsets, g.E, g.N, BT, chunk);
@@ -347,7 +385,8 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
     zero_rows<BF16>(g, c, chunk, m0, BM);
     return;
   }
-  const int half = g.I / 2, nk = (g.I + kStageI - 1) / kStageI;
+  const int half = g.I / 2, kt_first = split * g.per;
+  const int nk = min((g.I + kStageI - 1) / kStageI - kt_first, g.per);
   const int live_m = min(BM, g.O - m0);
   const size_t row0 = (size_t)c.e * g.O + m0;
   const DmaRsrc ra = make_dma_rsrc(g.w + row0 * half, (uint32_t)((size_t)live_m * half));
@@ -387,7 +426,7 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   auto dma = [&](auto S, int kt, auto N) {
     constexpr int n = decltype(N)::value;
     constexpr int st = decltype(S)::value;
-    const int k = kt * kRow;
+    const int k = (kt_first + kt) * kRow;
     if constexpr (n < kInstA) {
       dma16(ra, lp + st * kA + (n * 64 + wave_u * 8) * kRow, k >= lim ? kOOB : off_a + (uint32_t)(n * 64 * half + k));
     } else {
@@ -395,10 +434,11 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
       dma16(rb, lp + kAtB + st * kB + (q * 64 + wave_u * 8) * kRow, off_b[q] == kOOB || k >= lim ? kOOB : off_b[q] + (uint32_t)k);
     }
   };
-  // the scales of stages 2 p and 2 p + 1 into set p % 2; where a row ends inside its 16
+  // the scales of stages 2 p and 2 p + 1 into set p % kSets; where a row ends inside its 16
   // bytes, the next row's follow
   auto dma_scales = [&](int p) {
-    dma16(rs, lp + s_to + (p & 1) * s_group, off_s == kOOB || p * 16 >= g.Gs ? kOOB : off_s + (uint32_t)(p * 16));
+    const int at = kt_first * 8 + p * 16;
+    dma16(rs, lp + s_to + p % kSets * s_group, off_s == kOOB || at >= g.Gs ? kOOB : off_s + (uint32_t)at);
   };
   constexpr int kFirst = kDma / 2, kSecond = kDma - kFirst;
   auto dma_all = [&](auto S, int kt) { times<kDma>([&](auto N) { dma(S, kt, N); }); };
@@ -446,9 +486,10 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   const uint32_t sa_at = (uint32_t)(kAtSa + (wm0 + (lane & 31)) * 16), sb_at = (uint32_t)(kAtSb + (wn0 + (lane & 31)) * 16);
   auto read_scales = [&](int kt, auto ODD, Scales& v, auto N) {
     constexpr int n = decltype(N)::value, odd = decltype(ODD)::value;
-    const int shift = 8 * (lane >> 5), set = (kt >> 1) & 1;
+    const int shift = 8 * (lane >> 5), set = (kt >> 1) % kSets;
     // blocks past the row's end have zero codes, and the next row's scales may be NaN
-    const uint32_t in0 = kt * 8 < g.Gs ? ~0u : 0u, in1 = kt * 8 + 4 < g.Gs ? ~0u : 0u;
+    const int at = (kt_first + kt) * 8;
+    const uint32_t in0 = at < g.Gs ? ~0u : 0u, in1 = at + 4 < g.Gs ? ~0u : 0u;
     const u32x2 w = n < TM ? *(const SQ_LDS u32x2*)(lp + sa_at + set * kSa + n * 512 + odd * 8)
                            : *(const SQ_LDS u32x2*)(lp + sb_at + set * kSb + (n - TM) * 512 + odd * 8);
     int* to = n < TM ? v.a[n < TM ? n : 0] : v.b[n < TM ? 0 : n - TM];
@@ -486,7 +527,7 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
         if constexpr (kk == 0)
           share(N, std::integral_constant<int, kProducts>{}, std::integral_constant<int, kSecond>{},
                 [&](auto C) { dma(SP{}, kt + STAGES - 1, std::integral_constant<int, kFirst + decltype(C)::value>{}); });
-        if constexpr (kk == 0 && v == 0 && decltype(N)::value == kProducts - 1) dma_scales((kt >> 1) + 1);
+        if constexpr (kk == 0 && v == 0 && decltype(N)::value == kProducts - 1) dma_scales((kt >> 1) + kLead);
         __builtin_amdgcn_sched_barrier(0);
       });
     });
@@ -494,8 +535,8 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
       constexpr int n = decltype(N)::value;
       if constexpr (n == kMid) {
         // stage kt + 1 has landed once only the copies of the stages after it are
-        // outstanding; in an even one also the scales of the two stages after that
-        wait_vm_lgkm0<kAhead + (v == 0)>();
+        // outstanding, and the scales copied among them
+        wait_vm_lgkm0<kAhead + kLead - v>();
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -513,19 +554,21 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
     });
   };
 
-  // prologue: stage 0 whole and its first operands, then stages 1 .. STAGES - 2 and
-  // the first half of stage STAGES - 1
-  dma_all(I0{}, 0);
+  // prologue: stages 0 .. STAGES - 2 and the first half of stage STAGES - 1 on their
+  // way, with their scales in the order of the loop; the first operands of stage 0
   dma_scales(0);
-  wait_vm_lgkm0<0>();
+  times<STAGES - 1>([&](auto S) {
+    dma_all(S, decltype(S)::value);
+    if constexpr (decltype(S)::value % 2 == 1 && decltype(S)::value / 2 + 1 < kLead) dma_scales(decltype(S)::value / 2 + 1);
+  });
+  dma_first(std::integral_constant<int, STAGES - 1>{}, STAGES - 1);
+  wait_vm_lgkm0<kAhead + kFirst + kLead - 1>();
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_sched_barrier(0);
   times<kReads>([&](auto R) {
     read(I0{}, I0{}, F0, R);
     read_scales(0, I0{}, sc[0], R);
   });
-  if constexpr (STAGES > 2) dma_all(std::integral_constant<int, 1>{}, 1);
-  dma_first(std::integral_constant<int, STAGES - 1>{}, STAGES - 1);
   // rings of STAGES buffers and 2 sets of scales turn together
   constexpr int kTurn = STAGES % 2 ? 2 * STAGES : STAGES;
   for (int kt0 = 0; kt0 < nk; kt0 += kTurn)
@@ -575,7 +618,7 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
         for (int q = 0; q < 4; ++q) {
           const int o = m0 + wm0 + i * 32 + 8 * q + 4 * (lane >> 5);
           if (o < g.O)
-            put4<false>(g.out, (size_t)row * g.O + o, f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+            put4<false>(g.out, ((size_t)split * g.N + row) * g.O + o, f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
         }
     }
   }
@@ -594,38 +637,96 @@ __global__ __launch_bounds__(256) void act4_words_kernel(const uint8_t* __restri
   to[i] = v;
 }
 
-template <int BT, int WGM, int WGN, int STAGES>
+// 8 outputs per lane: the planes added in order.
+template <bool BF16>
+__global__ __launch_bounds__(256) void act4_join_kernel(const f32x4* __restrict__ planes, int splits, int64_t items, void* __restrict__ out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= items) return;
+  f32x4 a = planes[2 * i], b = planes[2 * i + 1];
+  for (int s = 1; s < splits; ++s) {
+    a += planes[2 * ((int64_t)s * items + i)];
+    b += planes[2 * ((int64_t)s * items + i) + 1];
+  }
+  put4<BF16>(out, 8 * i, a);
+  put4<BF16>(out, 8 * i + 4, b);
+}
+
+template <int BM, int BT, int WGM, int WGN, int STAGES>
 int tile_go(Act4Args g, int bf16, hipStream_t s) {
   g.chunks = g.offsets ? g.N / BT + (g.E < g.N ? g.E : g.N) + 1 : (g.N + BT - 1) / BT;
   const int along = g.offsets ? (g.chunks + kXcds - 1) / kXcds * kXcds : g.chunks;
-  const dim3 grid((unsigned)((g.O + 255) / 256 * along)), block(512);
-  if (bf16) hipLaunchKernelGGL((act4_tile_kernel<BT, WGM, WGN, STAGES, true>), grid, block, 0, s, g);
-  else hipLaunchKernelGGL((act4_tile_kernel<BT, WGM, WGN, STAGES, false>), grid, block, 0, s, g);
+  const dim3 grid((unsigned)((g.O + BM - 1) / BM * along * g.splits)), block(512);
+  if (bf16) hipLaunchKernelGGL((act4_tile_kernel<BM, BT, WGM, WGN, STAGES, true>), grid, block, 0, s, g);
+  else hipLaunchKernelGGL((act4_tile_kernel<BM, BT, WGM, WGN, STAGES, false>), grid, block, 0, s, g);
   return ok();
 }
 
-// Rows per tile (0: the few rows' kernel), by the rows of a layer or of an expert on average.
-int tile_rows(int64_t E, int64_t N, int64_t O) {
-#ifdef SQ_ACT4_BT
-  return SQ_ACT4_BT;
-#endif
-  const int64_t avg = (N + E - 1) / E, tiles = (O + 255) / 256 * E;
-  if (avg <= 16) return 0;
-  // the largest tiles that still fill the CUs
-  if (tiles * ((avg + 255) / 256) >= kCUs) return 256;
-  return tiles * ((avg + 127) / 128) >= kCUs ? 128 : 64;
+// How a product runs: tiles of bm outputs by bt rows (bt = 0: the few rows' kernel), and
+// the splits of one layer's sums.
+struct Act4Plan {
+  int bm, bt, splits, per;
+};
+
+// The smallest tiles that one round of the CUs holds, or else the largest that the rows
+// fill.  us in a graph, of 128 x 64, 128 x 128, 256 x 64, 256 x 128 and 256 x 256 tiles:
+// 512 rows of 4096 x 4096 10.7, 11.9, 12.8, 15.5, 23.1; 512 of 14336 x 4096 40.9, 28.5,
+// 30.0, 24.7, 28.7; 2000 of 4096 x 4096 40.7, 31.1, 30.7, 26.7, 29.4; 128 experts of 768
+// x 2048 with 16 rows each 26.3, 27.3, 23.0, 25.7, 33.0, with 64 41.6, 37.7, 35.9, 30.4,
+// 36.2; 128 of 1536 x 2048 with 256 212, 155, 168, 137, 116.  The few rows' kernel against
+// 128 x 64 (one layer) and 256 x 64 tiles (experts): 16 rows of 4096 x 4096 4.8, 8.7; 64
+// 8.6, 9.0; 64 of 14336 x 4096 15.0, 10.4; 8 experts of 1536 x 2048 with 4 rows each 5.8,
+// 8.0; 128 of 768 x 2048 with 1 14.1, 12.8.
+// Few tiles and a long sum: split it, at least 8 stages each, since planes and their
+// join cost 5 us (64 rows of 4096 x 14336 26.7, in two 19.8).
+Act4Plan act4_plan(bool batched, int64_t E, int64_t N, int64_t O, int64_t I) {
+  const int64_t live = E < N ? E : N, avg = (N + live - 1) / live, stages = (I + 255) / 256;
+  Act4Plan p{256, 256, 1, (int)stages};
+  if (avg <= 16 && (!batched || live * O <= 64 * 256)) p.bt = 0;
+  if (!batched && avg <= 64 && O <= 16 * kCUs) p.bt = 0;
+  if (p.bt == 0) return p;
+  const int tiles[5][2] = {{128, 64}, {256, 64}, {128, 128}, {256, 128}, {256, 256}};
+  bool found = false;
+  for (const auto& t : tiles) {
+    if (found || (!batched && t[0] == 256 && t[1] == 64)) continue;
+    const int64_t along = (O + t[0] - 1) / t[0];
+    // of many experts each range's last chunk is half full on average; chunks go to XCDs
+    const int64_t chunks = batched ? live * (2 * avg + t[1]) / (2 * t[1]) : (N + t[1] - 1) / t[1];
+    found = batched ? ((chunks > live ? chunks : live) + kXcds - 1) / kXcds * along <= kCUs / kXcds : chunks * along <= kCUs;
+    if (found) {
+      p.bm = t[0];
+      p.bt = t[1];
+    }
+  }
+  if (batched && !found) p.bt = avg <= 48 ? 64 : avg <= 160 ? 128 : 256;
+  const int64_t t = (O + p.bm - 1) / p.bm * ((N + p.bt - 1) / p.bt);
+  if (!batched && 2 * t <= kCUs && stages >= 24) {
+    int64_t n = kCUs / t < stages / 8 ? kCUs / t : stages / 8;
+    n = n < 8 ? n : 8;
+    p.per = (int)(((stages + n - 1) / n + 1) / 2 * 2);
+    p.splits = (int)((stages + p.per - 1) / p.per);
+  }
+  return p;
 }
 
-// Scales whose rows are not whole words: bytes of their copies for the tiles.
-size_t scale_words(int64_t E, int64_t T, int64_t N, int64_t O, int64_t I) {
+// Bytes of the workspace: scales whose rows are not whole words, laid out anew for the
+// tiles, and the planes of split sums behind them.
+size_t words_bytes(const Act4Plan& p, int64_t E, int64_t T, int64_t O, int64_t I) {
   const int64_t G = I / 32;
-  return G % 4 == 0 || tile_rows(E, N, O) == 0 ? 0 : (size_t)((T + E * O) * ((G + 3) / 4 * 4));
+  return G % 4 == 0 || p.bt == 0 ? 0 : ((size_t)((T + E * O) * ((G + 3) / 4 * 4)) + 255) & ~(size_t)255;
+}
+size_t plan_bytes(const Act4Plan& p, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I) {
+  return words_bytes(p, E, T, O, I) + (p.splits > 1 ? (size_t)p.splits * N * O * 4 : 0);
 }
 
 int product(Act4Args g, int bf16, void* workspace, hipStream_t s) {
-  const int bt = tile_rows(g.E, g.N, g.O);
+  const Act4Plan p = act4_plan(g.offsets != nullptr, g.E, g.N, g.O, g.I);
   g.Gs = g.G;
-  if (bt == 0) return (g.N + g.E - 1) / g.E <= 16 ? thin_go<1, 1>(g, bf16, s) : thin_go<2, 4>(g, bf16, s);
+  g.splits = p.splits;
+  g.per = p.per;
+  if (p.bt == 0) {
+    if (g.offsets || g.N <= 16) return thin_by<1>(g, bf16, s);
+    return g.N <= 32 ? thin_by<2>(g, bf16, s) : thin_by<4>(g, bf16, s);
+  }
   if (g.G % 4 != 0) {
     const int words = (g.G + 3) / 4;
     uint32_t* to = static_cast<uint32_t*>(workspace);
@@ -639,8 +740,20 @@ int product(Act4Args g, int bf16, void* workspace, hipStream_t s) {
     g.ws = reinterpret_cast<uint8_t*>(ws);
     g.Gs = 4 * words;
   }
-  if (bt == 64) return tile_go<64, 8, 1, 3>(g, bf16, s);
-  return bt == 128 ? tile_go<128, 4, 2, 3>(g, bf16, s) : tile_go<256, 2, 4, 2>(g, bf16, s);
+  void* const out = g.out;
+  if (p.splits > 1) g.out = static_cast<uint8_t*>(workspace) + words_bytes(p, g.E, g.T, g.O, g.I);
+  const int as_bf16 = bf16 && p.splits == 1;
+  int rc;
+  if (p.bm == 128) rc = p.bt == 64 ? tile_go<128, 64, 4, 2, 6>(g, as_bf16, s) : tile_go<128, 128, 4, 2, 4>(g, as_bf16, s);
+  else if (p.bt == 64) rc = tile_go<256, 64, 8, 1, 3>(g, as_bf16, s);
+  else rc = p.bt == 128 ? tile_go<256, 128, 4, 2, 3>(g, as_bf16, s) : tile_go<256, 256, 2, 4, 2>(g, as_bf16, s);
+  if (rc != 0 || p.splits == 1) return rc;
+  const int64_t items = (int64_t)g.N * g.O / 8;
+  auto join = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, static_cast<const f32x4*>(g.out), p.splits, items, out);
+    return ok();
+  };
+  return bf16 ? join(act4_join_kernel<true>) : join(act4_join_kernel<false>);
 }
 
 }  // namespace
@@ -665,7 +778,7 @@ int act4_unpack_launch(int fmt, int64_t T, int64_t I, const uint8_t* codes, cons
 }
 
 size_t act4_workspace(int fmt, int64_t T, int64_t O, int64_t I) {
-  return fmt == kMX ? scale_words(1, T, T, O, I) : (size_t)T * I * 2;
+  return fmt == kMX ? plan_bytes(act4_plan(false, 1, T, O, I), 1, T, T, O, I) : (size_t)T * I * 2;
 }
 
 int act4_fwd(int fmt, int T, int O, int I, const uint8_t* x, const uint8_t* xs, float x_ws2, const uint8_t* codes,
@@ -680,7 +793,9 @@ int act4_fwd(int fmt, int T, int O, int I, const uint8_t* x, const uint8_t* xs, 
   return product(g, y_bf16, workspace, s);
 }
 
-size_t act4_batched_workspace(int64_t E, int64_t T, int64_t N, int64_t O, int64_t I) { return scale_words(E, T, N, O, I); }
+size_t act4_batched_workspace(int64_t E, int64_t T, int64_t N, int64_t O, int64_t I) {
+  return plan_bytes(act4_plan(true, E, N, O, I), E, T, N, O, I);
+}
 
 int act4_fwd_batched(int E, int T, int N, int O, int I, const uint8_t* x, const uint8_t* xs, const int* rows,
                      const int* offsets, const uint8_t* codes, const uint8_t* scales, void* Y, int y_bf16, void* workspace,

@@ -16,6 +16,7 @@ bool fmt_ok(int fmt) { return fmt == SQ_MXFP4 || fmt == SQ_NVFP4; }
 
 // ---------------------------------------------------------------- 4-bit activations
 constexpr int64_t kExpertsMax = 8192;
+constexpr int64_t kXcds = 8;                // the experts' chunks are dealt to them in turn
 
 // X bf16 [T, I] and its 4-bit form; code_align: 4 bytes as a layer's codes.
 int check_act4(int fmt, int64_t T, int64_t I, const void* X, float ws2, const uint8_t* codes, const uint8_t* scales) {
@@ -39,9 +40,10 @@ int check_batched(int fmt, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I
   if (st != SQ_OK) return st;
   if (fmt != SQ_MXFP4) return SQ_ERR_UNIMPLEMENTED;
   if (E < 1 || E > kExpertsMax || N < 0 || N > kDimMax) return SQ_ERR_SHAPE;
-  // the workgroups of a launch: 16 rows by 16 outputs each at least
-  const int64_t chunks = N / 16 + (E < N ? E : N) + 1;
-  return chunks > kGroupsX || chunks * ((O + 15) / 16) > kGroupsX ? SQ_ERR_SHAPE : SQ_OK;
+  // the workgroups of a launch: 64 rows by 128 outputs each at least (and 16 by 16 for the
+  // fewest rows, of which there are fewer)
+  const int64_t chunks = N / 64 + (E < N ? E : N) + kXcds;
+  return chunks > kGroupsX || chunks * ((O + 127) / 128) > kGroupsX ? SQ_ERR_SHAPE : SQ_OK;
 }
 
 int check_workspace(size_t need, const void* workspace, size_t bytes) {

@@ -131,6 +131,56 @@ def test_products(sq, fmt, T, O, I, out_dtype):
     _check(Y, x @ w.T, np.abs(x) @ np.abs(w).T, I, 4)
 
 
+def _dequant(codes, scales):
+    """MXFP4 values in 64 bits on the device."""
+    table = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, 0, -.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device="cuda")
+    v = table[torch.stack((codes & 15, codes >> 4), -1).long()].view(scales.shape + (32,))
+    return (v * torch.exp2(scales.double() - 127)[..., None]).view(codes.shape[:-1] + (-1,))
+
+
+def _check_device(Y, ref, mag, depth):
+    bound = 2 * depth * 2.0 ** -24 / (1 - depth * 2.0 ** -24) * mag + 1e-38
+    if Y.dtype == BF16:
+        bound = bound * (1 + 2.0 ** -7) + 2.0 ** -8 * ref.abs()
+    bad = ~((Y.double() - ref).abs() <= bound)
+    assert not bad.any(), (bad.nonzero()[:5].tolist(), bad.double().mean().item())
+
+
+# several rounds of the largest tiles; one round of each other kind; sums split over workgroups, of whole and of odd inputs
+@pytest.mark.parametrize("T,O,I", [(4100, 4104, 544), (8200, 2056, 160), (2000, 4096, 288), (1030, 4096, 512), (600, 14336, 96),
+                                   (70, 264, 6176), (100, 256, 8192), (65, 1032, 14336), (300, 136, 7200), (63, 4104, 6144)])
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+def test_larger_products(sq, T, O, I, out_dtype):
+    codes, scales = _dev(*_layer("mx", T + O, O, I))
+    xc, xs, _ = _rows("mx", T % 97, min(T, 500), I)
+    xc, xs = (torch.from_numpy(v).cuda().repeat((T + len(v) - 1) // len(v), 1)[:T].contiguous() for v in (xc, xs))
+    xs = (xs.int() + torch.arange(T, device="cuda", dtype=torch.int32)[:, None] % 5).to(torch.uint8)   # no two parts alike
+    Y = torch.full((T, O), float("nan"), dtype=out_dtype, device="cuda")
+    sq.sq_fwd_act4("mx", xc, xs, codes, scales, Y=Y)
+    x, w = _dequant(xc, xs), _dequant(codes, scales)
+    _check_device(Y, x @ w.t().contiguous(), x.abs() @ w.abs().t().contiguous(), I + 8)
+
+
+@pytest.mark.parametrize("E,T,K,O,I", [(8, 4096, 2, 776, 160), (16, 2000, 3, 520, 288), (40, 700, 4, 264, 96), (8, 512, 2, 1536, 256),
+                                       (128, 16, 8, 768, 128), (4, 333, 1, 4104, 544)])
+def test_larger_experts(sq, E, T, K, O, I):
+    """Uneven ranges under every kind of tile, their offsets from the sort, some pairs dropped."""
+    g = inputs.rng(E + T)
+    ids = np.minimum((E * g.random((T, K)) ** 1.7).astype(np.int64), E - 1)
+    ids[g.random((T, K)) < 0.03] = -1
+    offsets, rows, _ = sq.sq_moe_sort(torch.from_numpy(ids).cuda(), E)
+    codes, scales = (v.view(E, O, -1) for v in _dev(*_layer("mx", E, E * O, I)))
+    xc, xs, _ = _rows("mx", T, T, I)
+    xc, xs = _dev(xc, xs)
+    Y = torch.full((T * K, O), float("nan"), dtype=BF16, device="cuda")
+    sq.sq_fwd_act4_batched("mx", xc, xs, rows, offsets, codes, scales, Y=Y)
+    x, o = _dequant(xc, xs)[rows.long()], offsets.tolist()
+    for e in range(E):
+        w, r = _dequant(codes[e], scales[e]), x[o[e]:o[e + 1]]
+        _check_device(Y[o[e]:o[e + 1]], r @ w.t().contiguous(), r.abs() @ w.abs().t().contiguous(), I)
+    assert not Y[o[E]:].any()
+
+
 @pytest.mark.parametrize("T", [5, 300])
 def test_every_scale_byte(sq, T):
     """All pairs of E8M0 bytes whose product stays in fp32, and NaN scales of either operand."""
