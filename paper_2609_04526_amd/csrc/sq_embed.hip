@@ -6,8 +6,8 @@
 //   dS[v,g] = factor sum_{j in g} code[v,j] sum_{t : ids[t] = v} dOut[t,j]
 //
 // All of it is bound by memory.  The gradients sort the tokens by id (stable), sum
-// the runs of one id in token order, and write zeros where an id has no token.
-// Nothing is added atomically, so the same bits come out of every run.
+// the runs of one id in token order, and write zeros where an id has no token.  The
+// only atomics count, so the same bits come out of every run.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -50,53 +50,85 @@ __global__ __launch_bounds__(256) void embed_kernel(const void* __restrict__ ids
 }
 
 // ------------------------------------------------------------------ sort
-// Place of each token in the stable order by id: the smaller keys, and the equal ones
-// of earlier tokens.  A workgroup takes 64 tokens, one per lane; its waves share the
-// other tokens, whose keys lie in LDS.  Every token meets every other: T^2 steps of
-// two instructions, but one launch and no pass over the vocabulary.
-// The other workgroups clear the gradient meanwhile.
-__global__ __launch_bounds__(1024) void embed_rank_kernel(const void* __restrict__ ids, int id_bytes, int T, int V,
-                                                          int* __restrict__ keys, int* __restrict__ tokens,
-                                                          float* __restrict__ grad, int64_t grad_words) {
-  const int sorters = (T + 63) / 64;
-  if ((int)blockIdx.x >= sorters) {
-    const int64_t n = (int64_t)(gridDim.x - sorters) * 1024, at = (int64_t)(blockIdx.x - sorters) * 1024 + threadIdx.x;
-    for (int64_t i = at; i < grad_words / 4; i += n) reinterpret_cast<f32x4*>(grad)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (at < grad_words % 4) grad[grad_words / 4 * 4 + at] = 0.0f;
+// One pass of a stable sort by 9 bits of the keys, from `shift` on: of the ids (FIRST)
+// or of the pass before.  A workgroup places 1024 tokens.  It counts the digits of all
+// tokens and of those before its own by itself, from keys that stay in L2, so that a
+// pass is one launch and nothing is exchanged between workgroups.  The other
+// workgroups of the first pass clear `marks`; the last pass sets those of the ids that
+// occur.  A pass leaves most CUs idle, so further workgroups clear part of the gradient
+// meanwhile, which the sums would have to otherwise (50001 x 2048 fp32 of 1999 tokens
+// 96 -> 86 us with the lookup).
+template <bool FIRST>
+__global__ __launch_bounds__(1024) void embed_pass_kernel(const void* __restrict__ ids, int id_bytes, int T, int V,
+                                                          const int* __restrict__ keys_in, const int* __restrict__ tokens_in,
+                                                          int shift, int* __restrict__ keys, int* __restrict__ tokens,
+                                                          uint8_t* __restrict__ marks, int64_t mark_words,
+                                                          u32x4* __restrict__ part, int64_t part_words) {
+  const int blocks = (T + 1023) / 1024;
+  if ((int)blockIdx.x >= blocks) {
+    const int64_t n = (int64_t)(gridDim.x - blocks) * 1024, i0 = (int64_t)(blockIdx.x - blocks) * 1024 + threadIdx.x;
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    if (FIRST)
+      for (int64_t i = i0; i < mark_words; i += n) reinterpret_cast<u32x4*>(marks)[i] = zero;
+    for (int64_t i = i0; i < part_words; i += n) part[i] = zero;
     return;
   }
-  __shared__ int s_key[kEmbedRankTokens];
-  __shared__ int s_n[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int padded = sorters * 64;
-  for (int i = threadIdx.x; i < padded; i += 1024) s_key[i] = i < T ? key_at(ids, id_bytes, i, V) : 0x7FFFFFFF;
+  __shared__ int s_all[kEmbedDigits], s_before[kEmbedDigits], s_next[16][kEmbedDigits], s_sum[8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int d = tid; d < kEmbedDigits; d += 1024) s_all[d] = s_before[d] = 0;
+  for (int i = tid; i < 16 * kEmbedDigits; i += 1024) (&s_next[0][0])[i] = 0;
   __syncthreads();
-  const int own = (int)blockIdx.x * 64, k = s_key[own + lane];
-  // blocks of 64 tokens, wave w takes every 16th
-  int n = 0;
-  for (int b = wave; b < sorters; b += 16) {
-    const int* s = s_key + b * 64;
-    if (b == (int)blockIdx.x) {
-      for (int j = 0; j < 64; ++j) n += s[j] < k || (s[j] == k && j < lane);
-    } else if (b < (int)blockIdx.x) {
-#pragma unroll 16
-      for (int j = 0; j < 64; ++j) n += s[j] <= k;
-    } else {
-#pragma unroll 16
-      for (int j = 0; j < 64; ++j) n += s[j] < k;
+  auto key_of = [&](int i) { return FIRST ? key_at(ids, id_bytes, i, V) : keys_in[i]; };
+  auto digit = [&](int k) { return (k >> shift) & (kEmbedDigits - 1); };
+  const int own = (int)blockIdx.x * 1024, mine = own + tid;
+#pragma unroll 4
+  for (int i = tid; i < own; i += 1024) atomicAdd(&s_before[digit(key_of(i))], 1);
+#pragma unroll 4
+  for (int i = mine + 1024; i < T; i += 1024) atomicAdd(&s_all[digit(key_of(i))], 1);
+  const bool in = mine < T;
+  const int key = in ? key_of(mine) : 0, d = digit(key);
+  if (in) atomicAdd(&s_next[wave][d], 1);
+  __syncthreads();
+  // where the digit starts among all tokens, then behind those before this workgroup
+  // and those of its earlier waves
+  int total = 0, before = 0, upto = 0;
+  if (tid < kEmbedDigits) {
+    before = s_before[tid];
+    total = s_all[tid] + before;
+    for (int w = 0; w < 16; ++w) total += s_next[w][tid];
+    upto = total;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o);
+      upto += lane >= o ? v : 0;
+    }
+    if (lane == 63) s_sum[wave] = upto;
+  }
+  __syncthreads();
+  if (tid < kEmbedDigits) {
+    int at = upto - total + before;
+    for (int w = 0; w < wave; ++w) at += s_sum[w];
+    for (int w = 0; w < 16; ++w) {
+      const int n = s_next[w][tid];
+      s_next[w][tid] = at;
+      at += n;
     }
   }
-  s_n[wave][lane] = n;
   __syncthreads();
-  if (wave == 0 && own + lane < T) {
+  uint64_t same = __ballot(in);
 #pragma unroll
-    for (int w = 1; w < 16; ++w) n += s_n[w][lane];
-    keys[n] = k;
-    tokens[n] = own + lane;
+  for (int b = 0; b < kEmbedDigitBits; ++b) {
+    const uint64_t m = __ballot((d >> b) & 1);
+    same &= (d >> b) & 1 ? m : ~m;
   }
+  if (!in) return;
+  const int at = s_next[wave][d] + __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+  keys[at] = key;
+  tokens[at] = FIRST ? mine : tokens_in[mine];
+  if (!FIRST && marks && key < V) marks[key] = 1;
 }
 
-// More tokens: two stable sorts, by the low and by the high bits of the key.
+// More tokens than every workgroup should read: the same passes by the sort of routed pairs.
 // `bits` of the key from `shift` on, of tokens in the order `from` (null: as they come).
 __global__ __launch_bounds__(256) void embed_digit_kernel(const void* __restrict__ ids, int id_bytes, int T, int V,
                                                           const int* __restrict__ from, int shift, int mask,
@@ -107,12 +139,16 @@ __global__ __launch_bounds__(256) void embed_digit_kernel(const void* __restrict
 // The order `place` of the tokens that stand in the order `from` (null: as they come).
 __global__ __launch_bounds__(256) void embed_order_kernel(const void* __restrict__ ids, int id_bytes, int T, int V,
                                                           const int* __restrict__ from, const int* __restrict__ place,
-                                                          int* __restrict__ keys, int* __restrict__ tokens) {
+                                                          int* __restrict__ keys, int* __restrict__ tokens,
+                                                          uint8_t* __restrict__ marks) {
   const int s = (int)blockIdx.x * 256 + threadIdx.x;
   if (s >= T) return;
   const int t = from ? from[place[s]] : place[s];
   tokens[s] = t;
-  if (keys) keys[s] = key_at(ids, id_bytes, t, V);
+  if (!keys) return;
+  const int key = key_at(ids, id_bytes, t, V);
+  keys[s] = key;
+  if (key < V) marks[key] = 1;
 }
 
 // ------------------------------------------------------------------ sums
@@ -123,7 +159,12 @@ struct EmbedArgs {
   const uint8_t* codes;     // 4-bit tables
   void* grad;               // dW [V, H] or dS [V, G]
   float* part;              // sums of whole chunks of one id, [chunks, H]
+  const uint8_t* marks;     // [V]: the ids that occur
   int T, V, H, chunk;
+  int units, lanes;         // 16-byte (or 4-byte) units of a row of the gradient, and lanes that clear one, a power of 2
+  int narrow;               // rows are not whole 16 bytes
+  int heads;                // workgroups of the sums, before those that clear
+  int64_t clear_from;       // the first row that is not clear yet
   float factor;
 };
 
@@ -161,58 +202,112 @@ __global__ __launch_bounds__(256) void embed_chunk_kernel(EmbedArgs g) {
 
 enum EmbedGrad { kDwF32 = 0, kDwBf16 = 1, kDsMx = 2, kDsNv = 3 };
 
-// The first place of each id sums its run: its tokens in order, whole chunks by
-// their sums.
+// Zeros in the rows of ids that do not occur: workgroup i of n.
+__device__ __forceinline__ void clear_rows(const EmbedArgs& g, int i, int n) {
+  const int per = (int)blockDim.x / g.lanes, sub = (int)threadIdx.x / g.lanes, l = (int)threadIdx.x % g.lanes;
+  for (int64_t r = g.clear_from + (int64_t)i * per + sub; r < g.V; r += (int64_t)n * per) {
+    if (g.marks[r]) continue;
+    for (int u = l; u < g.units; u += g.lanes) {
+      if (g.narrow) reinterpret_cast<float*>(g.grad)[r * g.units + u] = 0.0f;
+      else reinterpret_cast<f32x4*>(g.grad)[r * g.units + u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  }
+}
+
+// A workgroup has 8 places, and sums the runs that start there: their tokens in order,
+// one row after another whichever run they belong to, 8 on their way together.  A run
+// that goes on past the 64 places whose keys a wave holds takes whole chunks by their
+// sums.  The workgroups past the places clear the rows of ids that do not occur.
 template <int GRAD, bool BF16>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs g) {
-  const int64_t at = (int64_t)blockIdx.z * kGroupsX + blockIdx.x;
-  if (at >= g.T) return;
-  const int s = (int)at, key = g.keys[s], lane = threadIdx.x & 63;
-  if (key >= g.V || (s > 0 && g.keys[s - 1] == key)) return;
-  int end = s;
-  for (;;) {
-    const uint64_t other = __ballot(end + lane >= g.T || g.keys[min(end + lane, g.T - 1)] != key);
-    if (other) {
-      end += __builtin_ctzll(other);
-      break;
-    }
-    end += 64;
+  if ((int)blockIdx.x >= g.heads) {
+    if (blockIdx.y == 0) clear_rows(g, (int)blockIdx.x - g.heads, (int)gridDim.x - g.heads);
+    return;
   }
+  const int lane = threadIdx.x & 63;
   const int h = ((int)blockIdx.y * (int)blockDim.x + (int)threadIdx.x) * 8;
   const bool in = h < g.H;                                    // the lanes of a block are all in or all out
-  float v[8] = {};
-  if (in) {
-    const int c0 = (s + g.chunk - 1) / g.chunk, c1 = end / g.chunk;
-    if (c0 < c1) {
-      add_rows<BF16>(g, s, c0 * g.chunk, h, v);
-#pragma unroll 8
-      for (int c = c0; c < c1; ++c) {
-        float w[8];
-        load8<false>(g.part, (int64_t)c * g.H + h, w);
+  float v[8];
+  auto zero = [&]() {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] += w[k];
-      }
-      add_rows<BF16>(g, c1 * g.chunk, end, h, v);
+    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+  };
+  auto codes_of = [&](int key) { return in ? *reinterpret_cast<const uint32_t*>(g.codes + ((int64_t)key * g.H + h) / 2) : 0u; };
+  // the sums in v to the row of `key`, whose codes are q
+  auto put = [&](int key, uint32_t q) {
+    if constexpr (GRAD == kDwF32 || GRAD == kDwBf16) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= g.factor;
+      if (in) store8<GRAD == kDwBf16>(g.grad, (int64_t)key * g.H + h, v);
     } else {
-      add_rows<BF16>(g, s, end, h, v);
+      constexpr int kLanes = GRAD == kDsMx ? 4 : 2, kBlock = 8 * kLanes;
+      const f32x2 c[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
+                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3)};
+      float sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += v[2 * j] * c[j].x + v[2 * j + 1] * c[j].y;
+      sum += __shfl_xor(sum, 1);
+      if (kLanes == 4) sum += __shfl_xor(sum, 2);
+      if (in && lane % kLanes == 0) static_cast<float*>(g.grad)[(int64_t)key * (g.H / kBlock) + h / kBlock] = sum * g.factor;
     }
-  }
-  if constexpr (GRAD == kDwF32 || GRAD == kDwBf16) {
+  };
+  for (int64_t at = (int64_t)blockIdx.x * 8; at < g.T; at += (int64_t)g.heads * 8) {
+    const int a = (int)at, i = min(a + lane, g.T - 1);
+    const int k = g.keys[i], t = g.tokens[i], before = a + lane > 0 ? g.keys[min(a + lane, g.T) - 1] : -1;
+    // the places where a run starts, the dropped ids' and the end of all among them
+    const uint64_t starts = __ballot(a + lane == g.T || (a + lane < g.T && k != before));
+    const uint64_t mine = starts & 0xFFull & __ballot(a + lane < g.T && k < g.V);
+    if (!mine) continue;
+    const int first = __builtin_ctzll(mine), last = 63 - __builtin_clzll(mine);
+    const uint64_t after = starts & ~((2ull << last) - 1);
+    const int end = after ? __builtin_ctzll(after) : last;    // of the runs that end inside the 64 places
+    for (int p0 = first; p0 < end; p0 += 8) {
+      Raw8<BF16> w[8];
+      uint32_t q[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] *= g.factor;
-    if (in) store8<GRAD == kDwBf16>(g.grad, (int64_t)key * g.H + h, v);
-  } else {
-    constexpr int kLanes = GRAD == kDsMx ? 4 : 2;
-    const uint32_t q = in ? *reinterpret_cast<const uint32_t*>(g.codes + ((int64_t)key * g.H + h) / 2) : 0u;
-    const f32x2 c[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
-                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3)};
-    float sum = 0.0f;
+      for (int u = 0; u < 8; ++u) {
+        const int p = min(p0 + u, end - 1);
+        w[u].load(g.d, in ? (int64_t)__builtin_amdgcn_readlane(t, p) * g.H + h : 0);
+        if constexpr (GRAD == kDsMx || GRAD == kDsNv) q[u] = codes_of(__builtin_amdgcn_readlane(k, p));
+        else q[u] = 0;
+      }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sum += v[2 * k] * c[k].x + v[2 * k + 1] * c[k].y;
-    sum += __shfl_xor(sum, 1);
-    if (kLanes == 4) sum += __shfl_xor(sum, 2);
-    constexpr int kBlock = 8 * kLanes;
-    if (in && lane % kLanes == 0) static_cast<float*>(g.grad)[(int64_t)key * (g.H / kBlock) + h / kBlock] = sum * g.factor;
+      for (int u = 0; u < 8; ++u) {
+        const int p = p0 + u;
+        if (p >= end) break;
+        if ((starts >> p) & 1) zero();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += w[u].at(j);
+        if (p + 1 == end || ((starts >> (p + 1)) & 1)) put(__builtin_amdgcn_readlane(k, p), q[u]);
+      }
+    }
+    if (after) continue;
+    const int s = a + last, key = __builtin_amdgcn_readlane(k, last);
+    const uint32_t q = GRAD == kDsMx || GRAD == kDsNv ? codes_of(key) : 0u;
+    int n = 64 - last;
+    for (;;) {
+      const uint64_t past = __ballot(s + n + lane >= g.T || g.keys[min(s + n + lane, g.T - 1)] != key);
+      n += past ? __builtin_ctzll(past) : 64;
+      if (past) break;
+    }
+    zero();
+    if (in) {
+      const int stop = s + n, c0 = (s + g.chunk - 1) / g.chunk, c1 = stop / g.chunk;
+      if (c0 >= c1) {                                         // the chunks are longer than the run
+        add_rows<BF16>(g, s, stop, h, v);
+      } else {
+        add_rows<BF16>(g, s, c0 * g.chunk, h, v);
+#pragma unroll 8
+        for (int c = c0; c < c1; ++c) {
+          float w[8];
+          load8<false>(g.part, (int64_t)c * g.H + h, w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += w[j];
+        }
+        add_rows<BF16>(g, c1 * g.chunk, stop, h, v);
+      }
+    }
+    put(key, q);
   }
 }
 
@@ -227,7 +322,7 @@ inline int chunk_of(int64_t T) {
 }
 
 struct EmbedPlan {
-  size_t keys, tokens, part, digit, orders[2], place, slot, offsets, sort, total;
+  size_t keys, tokens, part, marks, orders[2], others, place, slot, offsets, sort, total;
 };
 EmbedPlan embed_plan(int64_t T, int64_t V, int64_t H) {
   EmbedPlan p{};
@@ -240,9 +335,10 @@ EmbedPlan embed_plan(int64_t T, int64_t V, int64_t H) {
   p.keys = take((size_t)T * 4);
   p.tokens = take((size_t)T * 4);
   p.part = take((size_t)(T / chunk_of(T)) * H * 4);
-  if (T > kEmbedRankTokens) {
-    p.digit = take((size_t)T * 4);
-    for (size_t& o : p.orders) o = take((size_t)T * 4);
+  p.marks = take((size_t)V);
+  for (size_t& o : p.orders) o = take((size_t)T * 4);
+  if (T > kEmbedPassTokens) {
+    p.others = take((size_t)T * 4);
     p.place = take((size_t)T * 4);
     p.slot = take((size_t)T * 4);
     p.offsets = take((size_t)(kEmbedDigits + 1) * 4);
@@ -252,56 +348,92 @@ EmbedPlan embed_plan(int64_t T, int64_t V, int64_t H) {
   return p;
 }
 
-__global__ __launch_bounds__(256) void embed_clear_kernel(float* __restrict__ grad, int64_t words) {
+__global__ __launch_bounds__(256) void embed_clear_kernel(u32x4* __restrict__ to, int64_t units, int words) {
   const int64_t n = (int64_t)gridDim.x * 256, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  for (int64_t i = at; i < words / 4; i += n) reinterpret_cast<f32x4*>(grad)[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  if (at < words % 4) grad[words / 4 * 4 + at] = 0.0f;
+  for (int64_t i = at; i < units; i += n) to[i] = u32x4{0u, 0u, 0u, 0u};
+  if (at < words) reinterpret_cast<uint32_t*>(to + units)[at] = 0u;
+}
+int clear(void* to, int64_t bytes, hipStream_t s) {             // bytes a multiple of 4
+  const int64_t want = (bytes / 16 + 1023) / 1024;
+  hipLaunchKernelGGL(embed_clear_kernel, dim3((unsigned)(want < 1 ? 1 : want < 8192 ? want : 8192)), dim3(256), 0, s,
+                     static_cast<u32x4*>(to), bytes / 16, (int)(bytes % 16 / 4));
+  return ok();
 }
 
-// Tokens sorted by id into the workspace, and `words` words of the gradient cleared.
-int embed_sort(const EmbedPlan& p, const void* ids, int id_bytes, int T, int V, uint8_t* ws, void* grad, int64_t words, hipStream_t s) {
-  int* keys = reinterpret_cast<int*>(ws + p.keys);
-  int* tokens = reinterpret_cast<int*>(ws + p.tokens);
-  const int64_t want = (words / 4 + 4095) / 4096;             // workgroups of the clearing, 4 steps each
-  const int clear = (int)(want < 1 ? 1 : want < 2048 ? want : 2048);
-  if (T <= kEmbedRankTokens) {
-    hipLaunchKernelGGL(embed_rank_kernel, dim3((unsigned)((T + 63) / 64 + clear)), dim3(1024), 0, s, ids, id_bytes, T, V, keys,
-                       tokens, static_cast<float*>(grad), words);
-    return ok();
+// Tokens sorted by id into the workspace, and the ids that occur marked; *cleared: the
+// bytes of the gradient that are zero by then.
+constexpr int64_t kEmbedPassClears = int64_t(28) << 20;      // bytes in the time of a pass
+int embed_sort(const EmbedPlan& p, const void* ids, int id_bytes, int T, int V, uint8_t* ws, void* grad, int64_t bytes,
+               int64_t* cleared, hipStream_t s) {
+  auto at = [&](size_t o) { return reinterpret_cast<int*>(ws + o); };
+  int passes = 1;
+  while ((int64_t)V >> (passes * kEmbedDigitBits) > 0) ++passes;         // the keys are 0 .. V
+  if (T <= kEmbedPassTokens) {
+    passes = passes < 2 ? 2 : passes;
+    const unsigned blocks = (unsigned)((T + 1023) / 1024);
+    const int64_t words = (V + 15) / 16;                      // marks are padded to whole 256 bytes
+    const int* keys_in = nullptr;
+    const int* tokens_in = nullptr;
+    *cleared = 0;
+    for (int k = 0; k < passes; ++k) {
+      u32x4* part = reinterpret_cast<u32x4*>(static_cast<uint8_t*>(grad) + *cleared);
+      const int64_t left = bytes - *cleared, part_words = (left < kEmbedPassClears ? left : kEmbedPassClears) / 16;
+      const int64_t most = k == 0 && words > part_words ? words : part_words, more = (most + 4095) / 4096;
+      const unsigned others = (unsigned)(more < 1024 ? more : 1024);
+      *cleared += part_words * 16;
+      const bool last = k + 1 == passes, even = (passes - k) % 2 == 0;
+      int* keys = even ? at(p.orders[0]) : at(p.keys);
+      int* tokens = even ? at(p.orders[1]) : at(p.tokens);
+      uint8_t* marks = k == 0 || last ? ws + p.marks : nullptr;
+      if (k == 0)
+        hipLaunchKernelGGL((embed_pass_kernel<true>), dim3(blocks + others), dim3(1024), 0, s, ids, id_bytes, T, V, keys_in,
+                           tokens_in, 0, keys, tokens, marks, words, part, part_words);
+      else
+        hipLaunchKernelGGL((embed_pass_kernel<false>), dim3(blocks + others), dim3(1024), 0, s, ids, id_bytes, T, V, keys_in,
+                           tokens_in, k * kEmbedDigitBits, keys, tokens, marks, words, part, part_words);
+      if (ok() != 0) return -1;
+      keys_in = keys;
+      tokens_in = tokens;
+    }
+    return 0;
   }
-  hipLaunchKernelGGL(embed_clear_kernel, dim3((unsigned)(4 * clear)), dim3(256), 0, s, static_cast<float*>(grad), words);
-  if (ok() != 0) return -1;
-  int* digit = reinterpret_cast<int*>(ws + p.digit);
-  int* place = reinterpret_cast<int*>(ws + p.place);
+  *cleared = 0;
+  if (clear(ws + p.marks, (int64_t)up(V, 16), s) != 0) return -1;
   const dim3 grid((unsigned)((T + 255) / 256)), block(256);
   const int* from = nullptr;
-  for (int pass = 0;; ++pass) {
-    const int shift = pass * kEmbedDigitBits;
-    hipLaunchKernelGGL(embed_digit_kernel, grid, block, 0, s, ids, id_bytes, T, V, from, shift, kEmbedDigits - 1, digit);
+  for (int k = 0; k < passes; ++k) {
+    hipLaunchKernelGGL(embed_digit_kernel, grid, block, 0, s, ids, id_bytes, T, V, from, k * kEmbedDigitBits, kEmbedDigits - 1, at(p.others));
     if (ok() != 0) return -1;
-    if (moe_sort_launch(T, 1, kEmbedDigits, digit, 4, reinterpret_cast<int*>(ws + p.offsets), place,
-                        reinterpret_cast<int*>(ws + p.slot), ws + p.sort, s) != 0)
-      return -1;
-    const bool last = (int64_t)V >> (shift + kEmbedDigitBits) == 0;      // the keys are 0 .. V
-    int* out = last ? tokens : reinterpret_cast<int*>(ws + p.orders[pass & 1]);
-    hipLaunchKernelGGL(embed_order_kernel, grid, block, 0, s, ids, id_bytes, T, V, from, place, last ? keys : nullptr, out);
+    if (moe_sort_launch(T, 1, kEmbedDigits, at(p.others), 4, at(p.offsets), at(p.place), at(p.slot), ws + p.sort, s) != 0) return -1;
+    const bool last = k + 1 == passes;
+    int* out = last ? at(p.tokens) : at(p.orders[k & 1]);
+    hipLaunchKernelGGL(embed_order_kernel, grid, block, 0, s, ids, id_bytes, T, V, from, at(p.place), last ? at(p.keys) : nullptr, out,
+                       ws + p.marks);
     if (ok() != 0) return -1;
-    if (last) return 0;
     from = out;
   }
+  return 0;
 }
 
 template <int GRAD, bool BF16>
-int embed_sums(const EmbedArgs& g, hipStream_t s) {
+int embed_sums(EmbedArgs g, hipStream_t s) {
   const int block = (int)(up(g.H / 8, 64) < 256 ? up(g.H / 8, 64) : 256);
-  const unsigned slabs = (unsigned)((g.H / 8 + block - 1) / block);
   const int chunks = g.T / g.chunk;
-  if (chunks > 0) {
-    hipLaunchKernelGGL((embed_chunk_kernel<BF16>), dim3((unsigned)chunks, slabs), dim3(block), 0, s, g);
+  if (g.T > 56 && chunks > 0) {                               // shorter runs are summed token by token
+    hipLaunchKernelGGL((embed_chunk_kernel<BF16>), dim3((unsigned)chunks, (unsigned)((g.H / 8 + block - 1) / block)), dim3(block), 0, s, g);
     if (ok() != 0) return -1;
   }
-  const dim3 grid((unsigned)(g.T < kGroupsX ? g.T : kGroupsX), slabs, (unsigned)((g.T + kGroupsX - 1) / kGroupsX));
-  hipLaunchKernelGGL((embed_sum_kernel<GRAD, BF16>), grid, dim3(block), 0, s, g);
+  const int64_t cols = GRAD == kDsMx ? g.H / 32 : GRAD == kDsNv ? g.H / 16 : GRAD == kDwBf16 ? g.H / 2 : g.H;   // words of a row
+  g.narrow = cols % 4 != 0;
+  g.units = (int)(g.narrow ? cols : cols / 4);
+  g.lanes = 1;
+  while (g.lanes < g.units && g.lanes < block) g.lanes *= 2;
+  if (block % g.lanes != 0) g.lanes = 64;                     // blocks of 192
+  const int groups = (g.T + 7) / 8;
+  g.heads = groups < (1 << 20) ? groups : 1 << 20;
+  const int64_t rows = (g.V - g.clear_from + block / g.lanes - 1) / (block / g.lanes), clears = rows < 4096 ? rows : 4096;
+  hipLaunchKernelGGL((embed_sum_kernel<GRAD, BF16>), dim3((unsigned)(g.heads + clears), (unsigned)((g.H / 8 + block - 1) / block)),
+                     dim3(block), 0, s, g);
   return ok();
 }
 
@@ -328,18 +460,16 @@ int embed_bwd_launch(int head, int T, int V, int H, const void* ids, int id_byte
   const EmbedPlan p = embed_plan(T, V, H);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const int64_t cols = head == kCeBf16 ? H : H / (head == kMX ? 32 : 16);
-  const int64_t words = (int64_t)V * cols / (head == kCeBf16 && grad_bf16 ? 2 : 1);
-  if (T == 0) {
-    const int64_t want = (words / 4 + 1023) / 1024;
-    hipLaunchKernelGGL(embed_clear_kernel, dim3((unsigned)(want < 1 ? 1 : want < 8192 ? want : 8192)), dim3(256), 0, s,
-                       static_cast<float*>(grad), words);
-    return ok();
-  }
-  if (embed_sort(p, ids, id_bytes, T, V, ws, grad, words, s) != 0) return -1;
+  if (T == 0) return clear(grad, V * cols * (head == kCeBf16 && grad_bf16 ? 2 : 4), s);
+  const int64_t row = cols * (head == kCeBf16 && grad_bf16 ? 2 : 4);
+  int64_t cleared;
+  if (embed_sort(p, ids, id_bytes, T, V, ws, grad, V * row, &cleared, s) != 0) return -1;
   EmbedArgs g{};
+  g.clear_from = cleared / row;
   g.keys = reinterpret_cast<int*>(ws + p.keys);
   g.tokens = reinterpret_cast<int*>(ws + p.tokens);
   g.part = reinterpret_cast<float*>(ws + p.part);
+  g.marks = ws + p.marks;
   g.d = dOut; g.codes = codes; g.grad = grad;
   g.T = T; g.V = V; g.H = H; g.chunk = chunk_of(T); g.factor = factor;
   if (head == kMX) return d_bf16 ? embed_sums<kDsMx, true>(g, s) : embed_sums<kDsMx, false>(g, s);

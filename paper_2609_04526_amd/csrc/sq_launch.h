@@ -236,7 +236,7 @@ int distill_bwd_launch(int head, int T, int64_t V, int H, const void* X, const v
                        hipStream_t s);
 
 // Embedding lookup and its gradients (sq_embed.hip).  head as the loss's.
-constexpr int kEmbedRankTokens = 16384;   // up to these one launch sorts the tokens
+constexpr int kEmbedPassTokens = 131072;  // up to these every workgroup of a pass counts all tokens' digits
 constexpr int kEmbedDigitBits = 9, kEmbedDigits = 1 << kEmbedDigitBits;
 int embed_launch(int head, int64_t T, int V, int H, const void* ids, int id_bytes, const void* W, const uint8_t* scales,
                  float ws2, float factor, void* out, int out_bf16, hipStream_t s);

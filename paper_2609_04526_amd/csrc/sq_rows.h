@@ -70,4 +70,19 @@ __device__ __forceinline__ void store8(void* p, int64_t i, const float (&v)[8]) 
   }
 }
 
+// 8 values of a row as loaded.
+template <bool BF16>
+struct Raw8 {
+  u32x4 w[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const void* p, int64_t i) {
+    const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p) + i * (BF16 ? 2 : 4));
+#pragma unroll
+    for (int k = 0; k < (BF16 ? 1 : 2); ++k) w[k] = q[k];
+  }
+  __device__ __forceinline__ float at(int k) const {
+    if constexpr (BF16) return __uint_as_float(k & 1 ? w[0][k >> 1] & 0xFFFF0000u : w[0][k >> 1] << 16);
+    else return __uint_as_float(w[k >> 2][k & 3]);
+  }
+};
+
 }  // namespace sq

@@ -105,9 +105,10 @@ def test_gradients(sq, head, T, V, I, kind):
 
 
 @pytest.mark.parametrize("kind", ["ragged", "one"])
-@pytest.mark.parametrize("T,V", [(16384, 50001), (16385, 700), (20000, 300001), (70000, 1000)])
+@pytest.mark.parametrize("T,V", [(1023, 511), (1024, 512), (1025, 5000), (16384, 50001), (20000, 300001), (70000, 1000), (131073, 600),
+                                 (140000, 270001)])
 def test_many_tokens(sq, T, V, kind):
-    """Up to 16384 tokens one launch sorts them; more take two sorts by digits, of 9 bits each, from 2^18 ids on three."""
+    """The sort by 9 bits a pass: two passes, three from 2^18 ids on; more than 131072 tokens take the other sort."""
     _check_grad(sq, "mx", T, V, 32, kind, torch.int64, BF16, F32)
 
 
