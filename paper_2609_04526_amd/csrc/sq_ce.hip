@@ -797,6 +797,7 @@ struct CeRest {
   const float* d;           // [T, 8] logit gradients of the rows from `first` on
   int64_t first;
   int rows;
+  const DistillLost* more;  // [T, kDistillLost] by compact row: what rounding took from a teacher's entries, or null
 };
 
 // 8 values of a head from element i (a multiple of 8) of its rows on.
@@ -876,6 +877,14 @@ __global__ __launch_bounds__(128) void ce_dx_kernel(const float* __restrict__ su
     };
     if (own < rest.first) add(rest.lost[b] * ws2, own);
     for (int r = 0; r < rest.rows; ++r) add(rest.d[b * 8 + r] * ws2, rest.first + r);
+    if (rest.more) {
+      DistillLost e[kDistillLost];
+#pragma unroll
+      for (int r = 0; r < kDistillLost; ++r) e[r] = rest.more[(size_t)b * kDistillLost + r];
+#pragma unroll
+      for (int r = 0; r < kDistillLost; ++r)
+        if (e[r].id >= 0) add(e[r].lost * ws2, e[r].id);
+    }
     put(t, v);
   }
   if (ignored) {
@@ -1392,6 +1401,7 @@ struct CeCall {
   const void* y;
   int y_bytes;
   float f;                  // of the logits, 1 / temperature
+  DistillLost* lost;        // with k, of the gradient
 };
 
 int ce_join(const CeCall& call, const float2* part, const float* tlogit, const CePiece& c, int tiles, float* loss, float* lse,
@@ -1446,7 +1456,7 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
   tail.d = dtail;
   if (ce_grad_go(head, c, lse, dloss, p.groups * p.width, p.width, p.shift, d, lost, tail, s) != 0) return -1;
   if (call.k) {
-    const DistillPiece piece{d, 0, (int)p.main, p.width, p.groups, p.shift, dtail, p.main, nullptr, nullptr, T, (int)V};
+    const DistillPiece piece{d, 0, (int)p.main, p.width, p.groups, p.shift, dtail, p.main, nullptr, nullptr, T, (int)V, call.lost};
     if (distill_put_launch(*call.k, piece, lse, dloss, s) != 0) return -1;
   }
   // dX of every group of rows, as the layer's grouped product
@@ -1456,7 +1466,7 @@ int ce_few_bwd(int head, int T, int64_t V, int H, const void* X, const uint8_t* 
     e[k] = ExpertProblem{d + (size_t)k * p.width * T, nullptr, codes + v0 * H / 2, scales + v0 * G, sums + (size_t)k * T * H, T, ws2};
   }
   if (gemm_dx_grouped(head, p.width, H, p.groups, e, 0, s) != 0) return -1;
-  const CeRest rest{codes, scales, lost, dtail, p.main, p.tail};
+  const CeRest rest{codes, scales, lost, dtail, p.main, p.tail, call.lost};
   const float f = call.k ? call.k->tau : 1.0f;
   auto finish = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, ce_dx_grid(T, H), dim3(128), 0, s, sums, p.groups, (int64_t)T, nullptr, nullptr, call.y,
@@ -1554,7 +1564,7 @@ static int ce_bwd(int head, int T, int64_t V, int H, const void* X, const void* 
   const int64_t tt = (T + p.bt - 1) / p.bt, tn = (H + 255) / 256;
   auto put = [&]() {                     // a teacher's entries among the piece's gradients
     if (!call.k) return 0;
-    const DistillPiece piece{g.d, g.v0, g.Vn, g.ld, 1, 0, nullptr, V, g.rows, g.count, T, (int)V};
+    const DistillPiece piece{g.d, g.v0, g.Vn, g.ld, 1, 0, nullptr, V, g.rows, g.count, T, (int)V, g.v0 == 0 ? call.lost : nullptr};
     return distill_put_launch(*call.k, piece, lse, dloss, s);
   };
   for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
@@ -1578,7 +1588,7 @@ static int ce_bwd(int head, int T, int64_t V, int H, const void* X, const void* 
     }
     if (put() != 0 || ce_go<kCeDx>(g, p.bx, p.groups, s) != 0) return -1;
   }
-  const CeRest rest{W, scales, g.tlogit, nullptr, V, 0};
+  const CeRest rest{W, scales, g.tlogit, nullptr, V, 0, call.lost};
   const float f = call.k ? ws2 * call.k->tau : ws2;
   auto finish = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, ce_dx_grid(T, H), dim3(128), 0, s, g.sums, 0, (int64_t)0, g.rows, g.count, call.y, call.y_bytes,
@@ -1590,36 +1600,39 @@ static int ce_bwd(int head, int T, int64_t V, int H, const void* X, const void* 
 
 int ce_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
                   const void* y, int y_bytes, float* loss, float* lse, void* workspace, hipStream_t s) {
-  return ce_fwd(head, T, V, H, X, W, scales, ws2, CeCall{nullptr, V, y, y_bytes, 1.0f}, loss, lse, static_cast<uint8_t*>(workspace), s);
+  return ce_fwd(head, T, V, H, X, W, scales, ws2, CeCall{nullptr, V, y, y_bytes, 1.0f, nullptr}, loss, lse, static_cast<uint8_t*>(workspace), s);
 }
 
 int ce_bwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
                   const void* y, int y_bytes, const float* lse, const float* dloss, void* dX, int dx_bf16,
                   void* workspace, hipStream_t s) {
-  return ce_bwd(head, T, V, H, X, W, scales, ws2, CeCall{nullptr, V, y, y_bytes, 1.0f}, lse, dloss, dX, dx_bf16,
+  return ce_bwd(head, T, V, H, X, W, scales, ws2, CeCall{nullptr, V, y, y_bytes, 1.0f, nullptr}, lse, dloss, dX, dx_bf16,
                 static_cast<uint8_t*>(workspace), s);
 }
 
 // ------------------------------------------------------------------ distillation
 // The same products with a teacher's entries in the place of the targets.  Behind
 // their workspace, a target for each token: V where it has an entry that counts (no
-// row of the head), else -1.
-size_t distill_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H) {
-  return ((ce_workspace(bwd, head, T, V, H) + 255) & ~(size_t)255) + (size_t)T * 4;
+// row of the head), else -1; and, of the gradient, what its rounding lost.
+struct DistillPlan {
+  size_t y, lost, total;
+};
+static DistillPlan distill_plan(int bwd, int head, int64_t T, int64_t V, int64_t H) {
+  DistillPlan p;
+  p.y = (ce_workspace(bwd, head, T, V, H) + 255) & ~(size_t)255;
+  p.lost = (p.y + (size_t)T * 4 + 255) & ~(size_t)255;
+  p.total = bwd ? p.lost + (size_t)T * kDistillLost * sizeof(DistillLost) : p.lost;
+  return p;
 }
 
-static int distill_begin(int bwd, int head, int T, int64_t V, int H, const Distill& k, uint8_t* ws, CeCall* call, hipStream_t s) {
-  int* y = reinterpret_cast<int*>(ws + distill_workspace(bwd, head, T, V, H) - (size_t)T * 4);
-  *call = CeCall{&k, V + 1, y, 4, 1.0f / k.tau};
-  return distill_live_launch(k, T, (int)V, y, s);
-}
+size_t distill_workspace(int bwd, int head, int64_t T, int64_t V, int64_t H) { return distill_plan(bwd, head, T, V, H).total; }
 
 int distill_fwd_launch(int head, int T, int64_t V, int H, const void* X, const void* W, const uint8_t* scales, float ws2,
                        const Distill& k, float* loss, float* lse, void* workspace, hipStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  CeCall call;
-  if (distill_begin(0, head, T, V, H, k, ws, &call, s) != 0) return -1;
-  if (distill_pick_launch(k, head, T, (int)V, H, X, W, scales, ws2 * call.f, s) != 0) return -1;
+  int* y = reinterpret_cast<int*>(ws + distill_plan(0, head, T, V, H).y);
+  const CeCall call{&k, V + 1, y, 4, 1.0f / k.tau, nullptr};
+  if (distill_pick_launch(k, head, T, (int)V, H, X, W, scales, ws2 * call.f, y, s) != 0) return -1;
   return ce_fwd(head, T, V, H, X, W, scales, ws2, call, loss, lse, ws, s);
 }
 
@@ -1627,8 +1640,10 @@ int distill_bwd_launch(int head, int T, int64_t V, int H, const void* X, const v
                        const Distill& k, const float* lse, const float* dloss, void* dX, int dx_bf16, void* workspace,
                        hipStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  CeCall call;
-  if (distill_begin(1, head, T, V, H, k, ws, &call, s) != 0) return -1;
+  const DistillPlan p = distill_plan(1, head, T, V, H);
+  int* y = reinterpret_cast<int*>(ws + p.y);
+  const CeCall call{&k, V + 1, y, 4, 1.0f / k.tau, reinterpret_cast<DistillLost*>(ws + p.lost)};
+  if (distill_live_launch(k, T, (int)V, y, s) != 0) return -1;
   return ce_bwd(head, T, V, H, X, W, scales, ws2, call, lse, dloss, dX, dx_bf16, ws, s);
 }
 
