@@ -26,8 +26,6 @@ namespace {
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
 
-constexpr int kPer = kDistillMax / 64;  // entries per lane
-
 // Workgroups by token (or by 4), on in y where x is full.
 __device__ __forceinline__ int64_t group_at() { return (int64_t)blockIdx.y * kGroupsX + blockIdx.x; }
 inline dim3 groups_of(int64_t n) {
@@ -53,18 +51,20 @@ __device__ __forceinline__ int entry_at(const Distill& g, int64_t t, int k, int 
   return v >= 0 && v < V && *z != -INFINITY ? (int)v : -1;
 }
 
-// A token's entries, one wave's: lane l has entries l, l + 64, ..; the teacher's
-// probabilities and their logarithms (0 where an entry does not count).
+// A token's entries, one wave's: lane l has entries l, l + 64, .., P in all; the
+// teacher's probabilities and their logarithms (0 where an entry does not count).
+template <int P>
 struct Entries {
-  int id[kPer];
-  float q[kPer], log_q[kPer];
+  int id[P];
+  float q[P], log_q[P];
 };
-__device__ __forceinline__ Entries entries_of(const Distill& g, int64_t t, int V) {
+template <int P>
+__device__ __forceinline__ Entries<P> entries_of(const Distill& g, int64_t t, int V) {
   const int lane = threadIdx.x & 63;
-  Entries e;
-  float z[kPer], top = -INFINITY, sum = 0.0f;
+  Entries<P> e;
+  float z[P], top = -INFINITY, sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < P; ++i) {
     z[i] = -INFINITY;
     e.id[i] = entry_at(g, t, i * 64 + lane, V, &z[i]);
     // a NaN stays: fmax would drop it
@@ -77,7 +77,7 @@ __device__ __forceinline__ Entries entries_of(const Distill& g, int64_t t, int V
   }
   const float f = 1.0f / g.tau;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < P; ++i) {
     e.log_q[i] = e.id[i] >= 0 ? (z[i] - top) * f : 0.0f;
     e.q[i] = e.id[i] >= 0 ? __expf(e.log_q[i]) : 0.0f;
     sum += e.q[i];
@@ -85,7 +85,7 @@ __device__ __forceinline__ Entries entries_of(const Distill& g, int64_t t, int V
   sum = sum_of(sum);
   const float log_sum = __logf(sum);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < P; ++i) {
     if (e.id[i] < 0) continue;
     e.q[i] /= sum;
     e.log_q[i] -= log_sum;
@@ -94,9 +94,8 @@ __device__ __forceinline__ Entries entries_of(const Distill& g, int64_t t, int V
 }
 
 // ------------------------------------------------------------------ live tokens
-__global__ __launch_bounds__(256) void distill_live_kernel(Distill g, int T, int V, int* __restrict__ y) {
-  const int64_t t = group_at() * 4 + (threadIdx.x >> 6);
-  if (t >= T) return;
+// One wave's answer for token t.
+__device__ __forceinline__ void put_live(const Distill& g, int64_t t, int V, int* y) {
   const int lane = threadIdx.x & 63;
   bool any = false;
   for (int k = lane; k < g.K; k += 64) {
@@ -106,30 +105,34 @@ __global__ __launch_bounds__(256) void distill_live_kernel(Distill g, int T, int
   const bool live = __ballot(any) != 0;
   if (lane == 0) y[t] = live ? V : -1;
 }
+__global__ __launch_bounds__(256) void distill_live_kernel(Distill g, int T, int V, int* __restrict__ y) {
+  const int64_t t = group_at() * 4 + (threadIdx.x >> 6);
+  if (t < T) put_live(g, t, V, y);
+}
 
 // ------------------------------------------------------------------ their logits
-// One token per workgroup; a wave takes 4 entries at a time, 8 columns per lane.
+// 16 entries of one token per workgroup, 4 per wave (all of a token's in one: 200 tokens of
+// 50000 x 2048 bf16 with 256 entries each 124 us, so 29).  The first workgroup of a token
+// also finds whether it counts.
 template <int HEAD>
 __global__ __launch_bounds__(256) void distill_pick_kernel(Distill g, int T, int V, int H, const uint16_t* __restrict__ X,
                                                            const void* __restrict__ W, const uint8_t* __restrict__ scales,
                                                            float f, int* __restrict__ y) {
-  __shared__ int s_any;
-  const int64_t t = group_at();
+  const int64_t t = (int64_t)blockIdx.z * kGroupsX + blockIdx.x;
   if (t >= T) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (threadIdx.x == 0) s_any = 0;
-  __syncthreads();
-  for (int k0 = wave * 4; k0 < g.K; k0 += 16) {
-    int id[4];
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f}, z;
-    bool any = false;
+  const int lane = threadIdx.x & 63, k0 = (int)blockIdx.y * 16 + (int)(threadIdx.x >> 6) * 4;
+  if (blockIdx.y == 0 && threadIdx.x < 64) put_live(g, t, V, y);
+  if (k0 >= g.K) return;
+  int id[4];
+  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f}, z;
+  bool any = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      id[i] = __builtin_amdgcn_readfirstlane(entry_at(g, t, k0 + i, V, &z));
-      any |= id[i] >= 0;
-    }
-    if (any) {
-      s_any = 1;
+  for (int i = 0; i < 4; ++i) {
+    id[i] = __builtin_amdgcn_readfirstlane(entry_at(g, t, k0 + i, V, &z));
+    any |= id[i] >= 0;
+  }
+  if (any) {
+    if constexpr (HEAD == kCeBf16) {
       for (int h = lane * 8; h < H; h += 512) {
         float x[8];
         load8<true>(X, t * H + h, x);
@@ -141,115 +144,146 @@ __global__ __launch_bounds__(256) void distill_pick_kernel(Distill g, int T, int
           for (int j = 0; j < 8; ++j) sum[i] = __builtin_fmaf(x[j], w[j], sum[i]);
         }
       }
-    }
+    } else {
+      // a block per lane: its codes in words (codes are 4-byte aligned), its scale once
+      // (1999 tokens of 50001 x 4096 MXFP4, 64 entries each, 40% ignored: 76 -> 44 us)
+      constexpr int B = ScaleOperand<HEAD>::kBlock;
+      for (int h = lane * B; h < H; h += 64 * B) {
+        uint32_t q[4][B / 8], b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float v = sum_of(sum[i]) * f;
-      if (lane == 0 && k0 + i < g.K) g.picked[t * g.K + k0 + i] = id[i] >= 0 ? v : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+          const int64_t at = (int64_t)max(id[i], 0) * H + h;
+          const uint32_t* c = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(W) + at / 2);
+#pragma unroll
+          for (int j = 0; j < B / 8; ++j) q[i][j] = c[j];
+          b[i] = scales[at / B];
+        }
+        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < B / 8; ++j) {
+          float x[8];
+          load8<true>(X, t * H + h + 8 * j, x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float w[8];
+            codes8(q[i][j], w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) part[i] = __builtin_fmaf(x[k], w[k], part[i]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          sum[i] = __builtin_fmaf(part[i], HEAD == kMX ? e8m0_to_f32(b[i]) : e4m3_to_f32(b[i]), sum[i]);
+      }
     }
   }
-  __syncthreads();
-  if (threadIdx.x == 0) y[t] = s_any ? V : -1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float v = sum_of(sum[i]) * f;
+    if (lane == 0 && k0 + i < g.K) g.picked[t * g.K + k0 + i] = id[i] >= 0 ? v : 0.0f;
+  }
 }
 
 // ------------------------------------------------------------------ loss
-// 64 tokens per workgroup: 16 waves share the tiles' pairs, then take 4 tokens each.
+// 16 tokens per workgroup: its threads share the tiles' pairs, 64 to a token, then a
+// wave takes a token.
+template <int P>
 __global__ __launch_bounds__(1024) void distill_loss_kernel(Distill g, const float2* __restrict__ part, const int* __restrict__ rows,
                                                             const int* __restrict__ count, const int* __restrict__ y, int T, int V,
                                                             int tiles, float* __restrict__ loss, float* __restrict__ lse) {
-  __shared__ float s_top[16][64], s_sum[16][64];
+  __shared__ float2 s_part[16][64 + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int live = count ? min(*count, T) : T;
-  const int row = (int)blockIdx.x * 64 + lane;
-  float top = -INFINITY, sum = 0.0f;
-  if (row < live) {
+  auto join = [](float2 a, float2 b) {
+    const float m = fmaxf(a.x, b.x), ref = m == -INFINITY ? 0.0f : m;
+    return make_float2(m, a.y * __expf(a.x - ref) + b.y * __expf(b.x - ref));
+  };
+  {
+    const int n = threadIdx.x & 15, first = threadIdx.x >> 4, row = (int)blockIdx.x * 16 + n;
+    float2 p = make_float2(-INFINITY, 0.0f);
+    if (row < live) {
 #pragma unroll 4
-    for (int i = wave; i < tiles; i += 16) {
-      const float2 p = part[(size_t)i * T + row];
-      const float m = fmaxf(top, p.x), ref = m == -INFINITY ? 0.0f : m;
-      sum = sum * __expf(top - ref) + p.y * __expf(p.x - ref);
-      top = m;
+      for (int i = first; i < tiles; i += 64) p = join(p, part[(size_t)i * T + row]);
     }
-  }
-  s_top[wave][lane] = top;
-  s_sum[wave][lane] = sum;
-  __syncthreads();
-  if (wave == 0) {
-    for (int w = 1; w < 16; ++w) {
-      const float b = s_top[w][lane], m = fmaxf(top, b), ref = m == -INFINITY ? 0.0f : m;
-      sum = sum * __expf(top - ref) + s_sum[w][lane] * __expf(b - ref);
-      top = m;
-    }
-    s_top[0][lane] = top;
-    s_sum[0][lane] = __logf(sum);
+    s_part[n][first] = p;
   }
   __syncthreads();
-  for (int i = wave; i < 64; i += 16) {
-    const int r = (int)blockIdx.x * 64 + i;
-    if (r >= live) continue;
-    const int t = rows ? rows[r] : r;
-    if (y[t] < 0) continue;
-    const Entries e = entries_of(g, t, V);
-    const float most = s_top[0][i], rest = s_sum[0][i];
-    float v = 0.0f;
+  const int t0 = (int)blockIdx.x * 16 + wave;                 // tokens that are ignored
+  if (lane == 0 && t0 < T && y[t0] < 0) loss[t0] = lse[t0] = 0.0f;
+  if (t0 >= live) return;
+  const int t = rows ? rows[t0] : t0;
+  if (y[t] < 0) return;
+  float2 p = s_part[wave][lane];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      // the distance to the largest logit first, as the cross entropy takes it
-      const int at = k * 64 + lane;
-      if (e.id[k] >= 0) v += e.q[k] != 0.0f ? e.q[k] * (e.log_q[k] + ((most - g.picked[(int64_t)t * g.K + at]) + rest)) : 0.0f;
-    }
-    v = sum_of(v);
-    if (lane == 0) {
-      loss[t] = g.tau * g.tau * v;
-      lse[t] = most + rest;
-    }
+  for (int d = 1; d < 64; d <<= 1) p = join(p, make_float2(__shfl_xor(p.x, d), __shfl_xor(p.y, d)));
+  const float most = p.x, rest = __logf(p.y);
+  const Entries<P> e = entries_of<P>(g, t, V);
+  float v = 0.0f;
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    // the distance to the largest logit first, as the cross entropy takes it
+    const int at = k * 64 + lane;
+    if (e.id[k] >= 0) v += e.q[k] != 0.0f ? e.q[k] * (e.log_q[k] + ((most - g.picked[(int64_t)t * g.K + at]) + rest)) : 0.0f;
   }
-  const int t = (int)blockIdx.x * 64 + lane;                  // tokens that are ignored
-  if (wave == 0 && t < T && y[t] < 0) loss[t] = lse[t] = 0.0f;
+  v = sum_of(v);
+  if (lane == 0) {
+    loss[t] = g.tau * g.tau * v;
+    lse[t] = most + rest;
+  }
 }
 
 // ------------------------------------------------------------------ gradient
 // A wave per live token.  Entries of one id are one column: each writes the same
 // value, with all their probabilities taken off.
+template <int P>
 __global__ __launch_bounds__(256) void distill_put_kernel(Distill g, DistillPiece p, const float* __restrict__ lse,
                                                           const float* __restrict__ dloss) {
-  __shared__ int s_id[4][kDistillMax];
-  __shared__ float s_q[4][kDistillMax];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row = group_at() * 4 + wave;
-  if (row >= (p.count ? min(*p.count, p.T) : p.T)) return;                                    // no barrier below: a wave's LDS is its own
+  if (row >= (p.count ? min(*p.count, p.T) : p.T)) return;
   const int64_t t = p.rows ? p.rows[row] : row;
-  const Entries e = entries_of(g, t, p.V);
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    s_id[wave][i * 64 + lane] = e.id[i];
-    s_q[wave][i * 64 + lane] = e.q[i];
-  }
-  __builtin_amdgcn_wave_barrier();
+  const Entries<P> e = entries_of<P>(g, t, p.V);
   const float z = lse[t], c = dloss[t];
-  float lost[kPer];
+  // each entry against all, one broadcast at a time: its column's probabilities, and
+  // whether it is the first of them
+  float q[P], lost[P];
+  bool first[P];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < P; ++i) {
+    q[i] = 0.0f;
+    first[i] = true;
+  }
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    const int n = min(g.K - j * 64, 64);
+    for (int l0 = 0; l0 < n; l0 += 8)                         // (past the last entry: of no id, probability 0)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int l = l0 + u, id = __builtin_amdgcn_readlane(e.id[j], l);
+        const float of = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(e.q[j]), l));
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const bool same = e.id[i] == id;
+          q[i] += same ? of : 0.0f;
+          if (j <= i) first[i] = first[i] && !(same && (j < i || l < lane));
+        }
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
     const int k = i * 64 + lane;
     lost[i] = 0.0f;
     if (e.id[i] < 0) continue;
     const int64_t at = e.id[i] - p.v0;
     const bool tail = p.dtail && e.id[i] >= p.main, here = at >= 0 && at < p.n;
     if (!tail && !here && !p.lost) continue;
-    float q = 0.0f;
-    bool first = true;
-    for (int j = 0; j < g.K; ++j) {
-      const bool same = s_id[wave][j] == e.id[i];
-      q += same ? s_q[wave][j] : 0.0f;
-      first &= !same || j >= k;
-    }
-    const float d = c * (__expf(g.picked[t * g.K + k] - z) - q);
+    const float d = c * (__expf(g.picked[t * g.K + k] - z) - q[i]);
     if (tail) {
       p.dtail[t * 8 + (e.id[i] - p.main)] = d;
       continue;
     }
     const uint32_t b = bits_of(__builtin_convertvector((f32x2{d, d}), bf16x2));
-    if (first) lost[i] = d - __uint_as_float(b << 16);
+    if (first[i]) lost[i] = d - __uint_as_float(b << 16);
     if (!here) continue;
     const int group = min((int)(at / p.width), p.groups - 1);
     const int64_t last = (int64_t)(p.groups - 1) * p.width - p.shift;     // the last group's first column
@@ -265,7 +299,7 @@ __global__ __launch_bounds__(256) void distill_put_kernel(Distill g, DistillPiec
     float most = 0.0f;
     int which = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
+    for (int i = 0; i < P; ++i)
       if (fabsf(lost[i]) > most) {
         most = fabsf(lost[i]);
         which = i;
@@ -278,7 +312,7 @@ __global__ __launch_bounds__(256) void distill_put_kernel(Distill g, DistillPiec
     }
     if (lane == __builtin_ctzll(who)) {
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
+      for (int i = 0; i < P; ++i)
         if (i == which) {
           p.lost[row * kDistillLost + r] = DistillLost{e.id[i], lost[i]};
           lost[i] = 0.0f;
@@ -296,8 +330,9 @@ int distill_live_launch(const Distill& k, int T, int V, int* y, hipStream_t s) {
 
 int distill_pick_launch(const Distill& k, int head, int T, int V, int H, const void* X, const void* W, const uint8_t* scales,
                         float f, int* y, hipStream_t s) {
+  const dim3 grid((unsigned)(T < kGroupsX ? T : kGroupsX), (unsigned)((k.K + 15) / 16), (unsigned)((T + kGroupsX - 1) / kGroupsX));
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, groups_of(T), dim3(256), 0, s, k, T, V, H, static_cast<const uint16_t*>(X), W, scales, f, y);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, k, T, V, H, static_cast<const uint16_t*>(X), W, scales, f, y);
     return ok();
   };
   return head == kMX ? go(distill_pick_kernel<kMX>) : head == kNV ? go(distill_pick_kernel<kNV>) : go(distill_pick_kernel<kCeBf16>);
@@ -305,14 +340,19 @@ int distill_pick_launch(const Distill& k, int head, int T, int V, int H, const v
 
 int distill_loss_launch(const Distill& k, const float2* part, const int* rows, const int* count, const int* y, int T, int V,
                         int tiles, float* loss, float* lse, hipStream_t s) {
-  hipLaunchKernelGGL(distill_loss_kernel, dim3((unsigned)((T + 63) / 64)), dim3(1024), 0, s, k, part, rows, count, y, T, V,
-                     tiles, loss, lse);
-  return ok();
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((T + 15) / 16)), dim3(1024), 0, s, k, part, rows, count, y, T, V, tiles, loss, lse);
+    return ok();
+  };
+  return k.K <= 64 ? go(distill_loss_kernel<1>) : k.K <= 128 ? go(distill_loss_kernel<2>) : go(distill_loss_kernel<4>);
 }
 
 int distill_put_launch(const Distill& k, const DistillPiece& piece, const float* lse, const float* dloss, hipStream_t s) {
-  hipLaunchKernelGGL(distill_put_kernel, groups_of((piece.T + 3) / 4), dim3(256), 0, s, k, piece, lse, dloss);
-  return ok();
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, groups_of((piece.T + 3) / 4), dim3(256), 0, s, k, piece, lse, dloss);
+    return ok();
+  };
+  return k.K <= 64 ? go(distill_put_kernel<1>) : k.K <= 128 ? go(distill_put_kernel<2>) : go(distill_put_kernel<4>);
 }
 
 }  // namespace sq

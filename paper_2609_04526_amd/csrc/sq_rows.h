@@ -46,6 +46,17 @@ __device__ __forceinline__ void table8(const void* w, const uint8_t* scales, flo
   }
 }
 
+// 8 codes of one dword as fp32.
+__device__ __forceinline__ void codes8(uint32_t q, float (&v)[8]) {
+  const f32x2 c[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3)};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] = c[k].x;
+    v[2 * k + 1] = c[k].y;
+  }
+}
+
 template <bool BF16>
 __device__ __forceinline__ void load8(const void* p, int64_t i, float (&v)[8]) {
   if constexpr (BF16) {
