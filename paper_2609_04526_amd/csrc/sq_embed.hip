@@ -50,6 +50,85 @@ __global__ __launch_bounds__(256) void embed_kernel(const void* __restrict__ ids
 }
 
 // ------------------------------------------------------------------ sort
+// What a workgroup of 1024 does with counts [wave][digit] of its tokens: they become the
+// places where each wave's tokens of a digit start, behind the smaller digits of all
+// tokens, the digit's own before this workgroup (`before`, of digit threadIdx.x) and
+// those of its earlier waves; `after`: the digit's tokens past this workgroup.  Gives
+// this lane's place among its wave's tokens of digit d.
+__device__ __forceinline__ int place_digits(int (&s_next)[16][kEmbedDigits], int (&s_sum)[8], int before, int after, int d, bool in) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int total = 0, upto = 0;
+  if (tid < kEmbedDigits) {
+    total = before + after;
+    for (int w = 0; w < 16; ++w) total += s_next[w][tid];
+    upto = total;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o);
+      upto += lane >= o ? v : 0;
+    }
+    if (lane == 63) s_sum[wave] = upto;
+  }
+  __syncthreads();
+  if (tid < kEmbedDigits) {
+    int at = upto - total + before;
+    for (int w = 0; w < wave; ++w) at += s_sum[w];
+    for (int w = 0; w < 16; ++w) {
+      const int n = s_next[w][tid];
+      s_next[w][tid] = at;
+      at += n;
+    }
+  }
+  __syncthreads();
+  uint64_t same = __ballot(in);
+#pragma unroll
+  for (int b = 0; b < kEmbedDigitBits; ++b) {
+    const uint64_t m = __ballot((d >> b) & 1);
+    same &= (d >> b) & 1 ? m : ~m;
+  }
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+}
+
+// Up to 1024 tokens: all passes in one workgroup, through LDS, while the others clear
+// the gradient, so that the sums have nothing to clear (a launch and the marks less: 5
+// tokens of 1000 x 256 bf16 with the lookup 26 -> 23 us, the host's calls).
+__global__ __launch_bounds__(1024) void embed_few_kernel(const void* __restrict__ ids, int id_bytes, int T, int V, int passes,
+                                                         int* __restrict__ keys, int* __restrict__ tokens, u32x4* __restrict__ grad,
+                                                         int64_t units, int words) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (blockIdx.x > 0) {
+    const int64_t n = (int64_t)(gridDim.x - 1) * 1024, at = (int64_t)(blockIdx.x - 1) * 1024 + tid;
+    for (int64_t i = at; i < units; i += n) grad[i] = u32x4{0u, 0u, 0u, 0u};
+    if (at < words) reinterpret_cast<uint32_t*>(grad + units)[at] = 0u;
+    return;
+  }
+  __shared__ int s_next[16][kEmbedDigits], s_sum[8], s_key[1024], s_token[1024];
+  const bool in = tid < T;
+  int key = in ? key_at(ids, id_bytes, tid, V) : 0, token = tid;
+  for (int p = 0; p < passes; ++p) {
+    for (int i = tid; i < 16 * kEmbedDigits; i += 1024) (&s_next[0][0])[i] = 0;
+    __syncthreads();
+    const int d = (key >> (p * kEmbedDigitBits)) & (kEmbedDigits - 1);
+    if (in) atomicAdd(&s_next[wave][d], 1);
+    __syncthreads();
+    const int rank = place_digits(s_next, s_sum, 0, 0, d, in);
+    if (in) {
+      const int at = s_next[wave][d] + rank;
+      s_key[at] = key;
+      s_token[at] = token;
+    }
+    __syncthreads();
+    if (in) {
+      key = s_key[tid];
+      token = s_token[tid];
+    }
+  }
+  if (in) {
+    keys[tid] = key;
+    tokens[tid] = token;
+  }
+}
+
 // One pass of a stable sort by 9 bits of the keys, from `shift` on: of the ids (FIRST)
 // or of the pass before.  A workgroup places 1024 tokens.  It counts the digits of all
 // tokens and of those before its own by itself, from keys that stay in L2, so that a
@@ -89,40 +168,9 @@ __global__ __launch_bounds__(1024) void embed_pass_kernel(const void* __restrict
   const int key = in ? key_of(mine) : 0, d = digit(key);
   if (in) atomicAdd(&s_next[wave][d], 1);
   __syncthreads();
-  // where the digit starts among all tokens, then behind those before this workgroup
-  // and those of its earlier waves
-  int total = 0, before = 0, upto = 0;
-  if (tid < kEmbedDigits) {
-    before = s_before[tid];
-    total = s_all[tid] + before;
-    for (int w = 0; w < 16; ++w) total += s_next[w][tid];
-    upto = total;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o);
-      upto += lane >= o ? v : 0;
-    }
-    if (lane == 63) s_sum[wave] = upto;
-  }
-  __syncthreads();
-  if (tid < kEmbedDigits) {
-    int at = upto - total + before;
-    for (int w = 0; w < wave; ++w) at += s_sum[w];
-    for (int w = 0; w < 16; ++w) {
-      const int n = s_next[w][tid];
-      s_next[w][tid] = at;
-      at += n;
-    }
-  }
-  __syncthreads();
-  uint64_t same = __ballot(in);
-#pragma unroll
-  for (int b = 0; b < kEmbedDigitBits; ++b) {
-    const uint64_t m = __ballot((d >> b) & 1);
-    same &= (d >> b) & 1 ? m : ~m;
-  }
+  const int rank = place_digits(s_next, s_sum, tid < kEmbedDigits ? s_before[tid] : 0, tid < kEmbedDigits ? s_all[tid] : 0, d, in);
   if (!in) return;
-  const int at = s_next[wave][d] + __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+  const int at = s_next[wave][d] + rank;
   keys[at] = key;
   tokens[at] = FIRST ? mine : tokens_in[mine];
   if (!FIRST && marks && key < V) marks[key] = 1;
@@ -161,6 +209,7 @@ struct EmbedArgs {
   float* part;              // sums of whole chunks of one id, [chunks, H]
   const uint8_t* marks;     // [V]: the ids that occur
   int T, V, H, chunk;
+  int chunks;               // whether the chunks' sums are there
   int units, lanes;         // 16-byte (or 4-byte) units of a row of the gradient, and lanes that clear one, a power of 2
   int narrow;               // rows are not whole 16 bytes
   int heads;                // workgroups of the sums, before those that clear
@@ -293,7 +342,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs g) {
     zero();
     if (in) {
       const int stop = s + n, c0 = (s + g.chunk - 1) / g.chunk, c1 = stop / g.chunk;
-      if (c0 >= c1) {                                         // the chunks are longer than the run
+      if (c0 >= c1 || !g.chunks) {                            // no chunk inside the run, or none summed
         add_rows<BF16>(g, s, stop, h, v);
       } else {
         add_rows<BF16>(g, s, c0 * g.chunk, h, v);
@@ -368,6 +417,13 @@ int embed_sort(const EmbedPlan& p, const void* ids, int id_bytes, int T, int V, 
   auto at = [&](size_t o) { return reinterpret_cast<int*>(ws + o); };
   int passes = 1;
   while ((int64_t)V >> (passes * kEmbedDigitBits) > 0) ++passes;         // the keys are 0 .. V
+  if (T <= 1024) {
+    *cleared = bytes;
+    const int64_t want = (bytes / 16 + 4095) / 4096;
+    hipLaunchKernelGGL(embed_few_kernel, dim3(1 + (unsigned)(want < 1 ? 1 : want < 2048 ? want : 2048)), dim3(1024), 0, s, ids, id_bytes, T, V,
+                       passes, at(p.keys), at(p.tokens), static_cast<u32x4*>(grad), bytes / 16, (int)(bytes % 16 / 4));
+    return ok();
+  }
   if (T <= kEmbedPassTokens) {
     passes = passes < 2 ? 2 : passes;
     const unsigned blocks = (unsigned)((T + 1023) / 1024);
@@ -415,11 +471,17 @@ int embed_sort(const EmbedPlan& p, const void* ids, int id_bytes, int T, int V, 
   return 0;
 }
 
+// Up to these tokens a run is summed by one workgroup per 2048 columns, whatever its length:
+// a launch less (us in a graph, without against with the chunks' sums: 128 tokens of
+// 1000 x 4096 9.9, 11.4, all of one id 16.2, 13.4; 256 of one id 26.4, 13.5).
+constexpr int kEmbedRunTokens = 128;
+
 template <int GRAD, bool BF16>
 int embed_sums(EmbedArgs g, hipStream_t s) {
   const int block = (int)(up(g.H / 8, 64) < 256 ? up(g.H / 8, 64) : 256);
   const int chunks = g.T / g.chunk;
-  if (g.T > 56 && chunks > 0) {                               // shorter runs are summed token by token
+  g.chunks = g.T > kEmbedRunTokens && chunks > 0;
+  if (g.chunks) {
     hipLaunchKernelGGL((embed_chunk_kernel<BF16>), dim3((unsigned)chunks, (unsigned)((g.H / 8 + block - 1) / block)), dim3(block), 0, s, g);
     if (ok() != 0) return -1;
   }
