@@ -145,13 +145,21 @@ __device__ __forceinline__ Chunk chunk_at(const int* offsets, int E, int N, int 
     const int r0 = c * per;
     return r0 < N ? Chunk{0, r0, min(r0 + per, N), 0} : Chunk{-1, N, N, c - (N + per - 1) / per};
   }
+  // 4 experts per lane: 256 for one round of loads (512 experts of 256 x 512 with one row
+  // each 14.1 -> 9.8 us)
   const int lane = threadIdx.x & 63;
   int before = 0;
-  for (int e0 = 0; e0 < E; e0 += 64) {
-    const int e = e0 + lane;
-    const int a = e < E ? min(max(offsets[e], 0), N) : 0, b = e < E ? min(max(offsets[e + 1], 0), N) : 0;
-    const int n = max(b - a, 0), t = (n + per - 1) / per;
-    int upto = t;
+  for (int e0 = 0; e0 < E; e0 += 256) {
+    const int e = e0 + 4 * lane;
+    int o[5], t[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 5; ++i) o[i] = min(max(offsets[min(e + i, E)], 0), N);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      t[i] = (max(o[i + 1] - o[i], 0) + per - 1) / per;       // 0 past the last expert
+      sum += t[i];
+    }
+    int upto = sum;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int v = __shfl_up(upto, d);
@@ -159,10 +167,17 @@ __device__ __forceinline__ Chunk chunk_at(const int* offsets, int E, int N, int 
     }
     const uint64_t in = __ballot(before + upto > c);
     if (in) {
+      int at = c - (before + upto - sum), i = 0;
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (i == k && at >= t[k]) {
+          at -= t[k];
+          ++i;
+        }
+      const int first = i == 0 ? o[0] : i == 1 ? o[1] : i == 2 ? o[2] : o[3], end = i == 0 ? o[1] : i == 1 ? o[2] : i == 2 ? o[3] : o[4];
       const int l = __builtin_ctzll(in);
-      const int at = __builtin_amdgcn_readfirstlane(c - before - __shfl(upto - t, l));
-      const int first = __builtin_amdgcn_readfirstlane(__shfl(a, l)), end = __builtin_amdgcn_readfirstlane(__shfl(b, l));
-      return Chunk{e0 + l, first + at * per, min(first + (at + 1) * per, end), 0};
+      const int r0 = __builtin_amdgcn_readlane(first, l) + __builtin_amdgcn_readlane(at, l) * per;
+      return Chunk{e0 + 4 * l + __builtin_amdgcn_readlane(i, l), r0, min(r0 + per, __builtin_amdgcn_readlane(end, l)), 0};
     }
     before += __builtin_amdgcn_readlane(upto, 63);
   }

@@ -223,7 +223,7 @@ def _split(g, E, N, kind):
 
 
 @pytest.mark.parametrize("kind", ["even", "one", "dropped", "empty"])
-@pytest.mark.parametrize("E,T,N,O,I", [(1, 4, 7, 24, 32), (3, 9, 40, 264, 160), (7, 30, 130, 136, 256), (130, 16, 128, 40, 96),
+@pytest.mark.parametrize("E,T,N,O,I", [(1, 4, 7, 24, 32), (3, 9, 40, 264, 160), (7, 30, 130, 136, 256), (130, 16, 128, 40, 96), (700, 16, 300, 24, 64), (8192, 50, 400, 16, 32),
                                        (5, 200, 1200, 520, 288), (2, 300, 900, 256, 512), (70, 64, 700, 72, 128)])
 def test_experts(sq, E, T, N, O, I, kind):
     g = inputs.rng(E * N)
