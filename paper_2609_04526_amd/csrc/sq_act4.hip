@@ -130,6 +130,7 @@ struct Act4Args {
   int T, N, E, O, I, G;
   int Gs;                   // bytes from one row's scales to the next
   int chunks;               // workgroups along the rows
+  const int* table;         // act4_table_kernel's, or null
   int splits, per;          // of the sum over the inputs: planes [N, O] of `per` stages each (an even number), one layer only
 };
 
@@ -177,11 +178,45 @@ __device__ __forceinline__ Chunk chunk_at(const int* offsets, int E, int N, int 
       const int first = i == 0 ? o[0] : i == 1 ? o[1] : i == 2 ? o[2] : o[3], end = i == 0 ? o[1] : i == 1 ? o[2] : i == 2 ? o[3] : o[4];
       const int l = __builtin_ctzll(in);
       const int r0 = __builtin_amdgcn_readlane(first, l) + __builtin_amdgcn_readlane(at, l) * per;
-      return Chunk{e0 + 4 * l + __builtin_amdgcn_readlane(i, l), r0, min(r0 + per, __builtin_amdgcn_readlane(end, l)), 0};
+      return Chunk{e0 + 4 * l + __builtin_amdgcn_readlane(i, l), max(r0, 0), min(r0 + per, __builtin_amdgcn_readlane(end, l)), 0};
     }
     before += __builtin_amdgcn_readlane(upto, 63);
   }
   return Chunk{-1, min(max(offsets[E], 0), N), N, c - before};
+}
+
+// The chunks of all experts in a table, for products of several rounds of the CUs, whose
+// workgroups would each look for theirs: word 0 their number, from word 4 on (expert,
+// first row, end, 0) of each.  One workgroup.  Sums are held to `most`, which ranges in
+// order never pass.
+__global__ __launch_bounds__(1024) void act4_table_kernel(const int* __restrict__ offsets, int E, int N, int per, int most, int* __restrict__ table) {
+  __shared__ int s_sum[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int before = 0;
+  for (int e0 = 0; e0 < E; e0 += 1024) {
+    const int e = e0 + tid;
+    const int a = e < E ? min(max(offsets[e], 0), N) : 0, b = e < E ? min(max(offsets[e + 1], 0), N) : 0;
+    const int t = min((max(b - a, 0) + per - 1) / per, most);
+    int upto = t;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int v = __shfl_up(upto, d);
+      upto = min(upto + (lane >= d ? v : 0), most);
+    }
+    if (lane == 63) s_sum[wave] = upto;
+    __syncthreads();
+    int front = before;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) front = min(front + s_sum[w], most);
+      before = min(before + s_sum[w], most);
+    }
+    const int at = front + upto - t;
+    for (int k = 0; k < t && at + k < most; ++k)
+      reinterpret_cast<int4*>(table)[1 + at + k] = make_int4(e, a + k * per, min(a + (k + 1) * per, b), 0);
+    __syncthreads();
+  }
+  if (tid == 0) table[0] = before;
 }
 
 // 4 consecutive outputs of one row.
@@ -202,7 +237,7 @@ __device__ __forceinline__ void put4(void* out, size_t at, f32x4 v) {
 template <bool BF16>
 __device__ __forceinline__ void zero_rows(const Act4Args& g, const Chunk& c, int chunk, int o0, int cols) {
   if (!g.offsets) return;
-  const int step = g.chunks - (chunk - c.n);                  // chunks past the last
+  const int step = max(g.chunks - (chunk - c.n), 1);          // chunks past the last
   const int front = min(min(max(g.offsets[0], 0), g.N), c.r0), all = front + c.r1 - c.r0;
   const int quads = (min(o0 + cols, g.O) - o0) / 4;           // O is a multiple of 8
   for (int r = c.n; r < all; r += step) {
@@ -379,23 +414,39 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
 
-  // the tile: chunks of the experts' rows dealt to the XCDs in turn (those past the
-  // last are spread as well), with their tiles of outputs beside each other, or groups
-  // of 4 x n tiles
+  // The tile: of the experts' chunks from a table, the tiles of a chunk and the chunks of
+  // an expert beside each other, in stretches that the XCDs take, so that one L2 reads an
+  // expert's weight; without one dealt to the XCDs in turn (those past the last are spread
+  // as well); of one layer in groups of 4 x n tiles.
   const int tiles_m = (g.O + BM - 1) / BM;
   int chunk, tm, split = 0;
-  if (g.offsets) {
+  Chunk c;
+  if (g.table) {
+    const int total = g.table[0], n = total * tiles_m;
+    if ((int)blockIdx.x < n) {
+      const int pos = xcd_stretch((int)blockIdx.x, n);
+      chunk = pos / tiles_m;
+      tm = pos - chunk * tiles_m;
+      const int4 t = reinterpret_cast<const int4*>(g.table)[1 + chunk];
+      c = Chunk{t.x, t.y, t.z, 0};
+    } else {
+      chunk = (int)blockIdx.x / tiles_m;
+      tm = (int)blockIdx.x % tiles_m;
+      c = Chunk{-1, min(max(g.offsets[g.E], 0), g.N), g.N, chunk - total};
+    }
+  } else if (g.offsets) {
     const int at = (int)blockIdx.x / kXcds;
     chunk = at / tiles_m * kXcds + (int)blockIdx.x % kXcds;
     tm = at % tiles_m;
     if (chunk >= g.chunks) return;
+    c = chunk_at(g.offsets, g.E, g.N, BT, chunk);
   } else {
     const int tiles = tiles_m * g.chunks, pos = xcd_stretch((int)blockIdx.x, tiles * g.splits);
     split = pos / tiles;
     tile_at<4>(pos - split * tiles, tiles_m, g.chunks, tm, chunk);
+    c = chunk_at(nullptr, 1, g.N, BT, chunk);
   }
   const int m0 = tm * BM;
-  const Chunk c = chunk_at(g.offsets, g.E, g.N, BT, chunk);
   if (c.e < 0) {
     zero_rows<BF16>(g, c, chunk, m0, BM);
     return;
@@ -666,10 +717,18 @@ __global__ __launch_bounds__(256) void act4_join_kernel(const f32x4* __restrict_
   put4<BF16>(out, 8 * i + 4, b);
 }
 
+// Chunks of `per` rows of the experts' ranges at most, since every range's last may be
+// short, and one for the rows of no expert.
+inline int64_t most_chunks(int64_t E, int64_t N, int64_t per) { return N / per + (E < N ? E : N) + 1; }
+
 template <int BM, int BT, int WGM, int WGN, int STAGES>
 int tile_go(Act4Args g, int bf16, hipStream_t s) {
-  g.chunks = g.offsets ? g.N / BT + (g.E < g.N ? g.E : g.N) + 1 : (g.N + BT - 1) / BT;
-  const int along = g.offsets ? (g.chunks + kXcds - 1) / kXcds * kXcds : g.chunks;
+  g.chunks = g.offsets ? (int)most_chunks(g.E, g.N, BT) : (g.N + BT - 1) / BT;
+  if (g.table) {
+    hipLaunchKernelGGL(act4_table_kernel, dim3(1), dim3(1024), 0, s, g.offsets, g.E, g.N, BT, g.chunks - 1, const_cast<int*>(g.table));
+    if (ok() != 0) return -1;
+  }
+  const int along = g.offsets && !g.table ? (g.chunks + kXcds - 1) / kXcds * kXcds : g.chunks;
   const dim3 grid((unsigned)((g.O + BM - 1) / BM * along * g.splits)), block(512);
   if (bf16) hipLaunchKernelGGL((act4_tile_kernel<BM, BT, WGM, WGN, STAGES, true>), grid, block, 0, s, g);
   else hipLaunchKernelGGL((act4_tile_kernel<BM, BT, WGM, WGN, STAGES, false>), grid, block, 0, s, g);
@@ -680,8 +739,13 @@ int tile_go(Act4Args g, int bf16, hipStream_t s) {
 // the splits of one layer's sums.
 struct Act4Plan {
   int bm, bt, splits, per;
+  bool table;
 };
 
+// Experts of 3 rounds of the CUs and more take their chunks from a table (512 experts of
+// 768 x 2048 with one row each 41.7 -> 37.4 us, 128 of 1536 x 2048 with 256 122 -> 116);
+// its launch costs 2.3 (128 of 768 x 2048 with one 12.4 -> 14.7, 2 rounds of 16 rows each
+// 30.1 -> 29.8).
 // The smallest tiles that one round of the CUs holds, or else the largest that the rows
 // fill.  us in a graph, of 128 x 64, 128 x 128, 256 x 64, 256 x 128 and 256 x 256 tiles:
 // 512 rows of 4096 x 4096 10.7, 11.9, 12.8, 15.5, 23.1; 512 of 14336 x 4096 40.9, 28.5,
@@ -695,7 +759,7 @@ struct Act4Plan {
 // join cost 5 us (64 rows of 4096 x 14336 26.7, in two 19.8).
 Act4Plan act4_plan(bool batched, int64_t E, int64_t N, int64_t O, int64_t I) {
   const int64_t live = E < N ? E : N, avg = (N + live - 1) / live, stages = (I + 255) / 256;
-  Act4Plan p{256, 256, 1, (int)stages};
+  Act4Plan p{256, 256, 1, (int)stages, false};
   if (avg <= 16 && (!batched || live * O <= 64 * 256)) p.bt = 0;
   if (!batched && avg <= 64 && O <= 16 * kCUs) p.bt = 0;
   if (p.bt == 0) return p;
@@ -712,7 +776,10 @@ Act4Plan act4_plan(bool batched, int64_t E, int64_t N, int64_t O, int64_t I) {
       p.bt = t[1];
     }
   }
-  if (batched && !found) p.bt = avg <= 48 ? 64 : avg <= 160 ? 128 : 256;
+  if (batched && !found) {
+    p.bt = avg <= 48 ? 64 : avg <= 160 ? 128 : 256;
+    p.table = live * ((avg + p.bt - 1) / p.bt) * ((O + 255) / 256) >= 3 * kCUs;
+  }
   const int64_t t = (O + p.bm - 1) / p.bm * ((N + p.bt - 1) / p.bt);
   if (!batched && 2 * t <= kCUs && stages >= 24) {
     int64_t n = kCUs / t < stages / 8 ? kCUs / t : stages / 8;
@@ -724,13 +791,14 @@ Act4Plan act4_plan(bool batched, int64_t E, int64_t N, int64_t O, int64_t I) {
 }
 
 // Bytes of the workspace: scales whose rows are not whole words, laid out anew for the
-// tiles, and the planes of split sums behind them.
+// tiles, and behind them the planes of split sums or the table of chunks.
 size_t words_bytes(const Act4Plan& p, int64_t E, int64_t T, int64_t O, int64_t I) {
   const int64_t G = I / 32;
   return G % 4 == 0 || p.bt == 0 ? 0 : ((size_t)((T + E * O) * ((G + 3) / 4 * 4)) + 255) & ~(size_t)255;
 }
 size_t plan_bytes(const Act4Plan& p, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I) {
-  return words_bytes(p, E, T, O, I) + (p.splits > 1 ? (size_t)p.splits * N * O * 4 : 0);
+  return words_bytes(p, E, T, O, I) + (p.splits > 1 ? (size_t)p.splits * N * O * 4 : 0) +
+         (p.table ? (size_t)most_chunks(E, N, p.bt) * 16 : 0);
 }
 
 int product(Act4Args g, int bf16, void* workspace, hipStream_t s) {
@@ -756,7 +824,9 @@ int product(Act4Args g, int bf16, void* workspace, hipStream_t s) {
     g.Gs = 4 * words;
   }
   void* const out = g.out;
-  if (p.splits > 1) g.out = static_cast<uint8_t*>(workspace) + words_bytes(p, g.E, g.T, g.O, g.I);
+  uint8_t* const behind = static_cast<uint8_t*>(workspace) + words_bytes(p, g.E, g.T, g.O, g.I);
+  if (p.splits > 1) g.out = behind;
+  if (p.table) g.table = reinterpret_cast<int*>(behind);
   const int as_bf16 = bf16 && p.splits == 1;
   int rc;
   if (p.bm == 128) rc = p.bt == 64 ? tile_go<128, 64, 4, 2, 6>(g, as_bf16, s) : tile_go<128, 128, 4, 2, 4>(g, as_bf16, s);

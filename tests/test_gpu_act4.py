@@ -239,6 +239,29 @@ def test_experts(sq, E, T, N, O, I, kind):
         _check(Y, student.experts(x, rows, offsets, w), student.experts(np.abs(x), rows, offsets, np.abs(w)), I)
 
 
+@pytest.mark.parametrize("kind", ["even", "one", "dropped", "empty"])
+@pytest.mark.parametrize("E,T,N,O,I", [(200, 64, 512, 1288, 64), (1500, 40, 1600, 264, 96)])
+def test_experts_of_several_rounds(sq, E, T, N, O, I, kind):
+    """So many experts that their chunks come from a table; rows before the first range as well."""
+    g = inputs.rng(E + N)
+    codes, scales = (v.view(E, O, -1) for v in _dev(*_layer("mx", N, E * O, I)))
+    xc, xs, _ = _rows("mx", T, T, I)
+    xc, xs = _dev(xc, xs)
+    offsets, rows = _split(g, E, N, kind), g.integers(0, T, N).astype(np.int32)
+    if kind == "dropped":
+        offsets = np.maximum(offsets, 3)
+    Y = torch.full((N, O), float("nan"), dtype=BF16, device="cuda")
+    sq.sq_fwd_act4_batched("mx", xc, xs, *_dev(rows, offsets), codes, scales, Y=Y)
+    x = _dequant(xc, xs)[torch.from_numpy(rows).long().cuda()]
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        if lo == hi:
+            continue
+        w, r = _dequant(codes[e], scales[e]), x[lo:hi]
+        _check_device(Y[lo:hi], r @ w.t().contiguous(), r.abs() @ w.abs().t().contiguous(), I)
+    assert not Y[:offsets[0]].any() and not Y[offsets[E]:].any()
+
+
 def test_experts_rows_in_place(sq):
     """Without row numbers, row s is row s; rows before the first range are zeros too; offsets past the rows are held."""
     E, N, O, I = 4, 90, 72, 128
