@@ -693,14 +693,14 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
 // Scale rows of G bytes laid out in whole words.
 __global__ __launch_bounds__(256) void act4_words_kernel(const uint8_t* __restrict__ from, int64_t rows, int G, int words,
                                                          uint32_t* __restrict__ to) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows * words) return;
-  const int64_t r = i / words;
-  const int k = (int)(i - r * words) * 4;
-  uint32_t v = 0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / words;
+    const int k = (int)(i - r * words) * 4;
+    uint32_t v = 0;
 #pragma unroll
-  for (int b = 0; b < 4; ++b) v |= k + b < G ? (uint32_t)from[r * G + k + b] << (8 * b) : 0u;
-  to[i] = v;
+    for (int b = 0; b < 4; ++b) v |= k + b < G ? (uint32_t)from[r * G + k + b] << (8 * b) : 0u;
+    to[i] = v;
+  }
 }
 
 // 8 outputs per lane: the planes added in order.
@@ -814,7 +814,9 @@ int product(Act4Args g, int bf16, void* workspace, hipStream_t s) {
     const int words = (g.G + 3) / 4;
     uint32_t* to = static_cast<uint32_t*>(workspace);
     auto lay = [&](const uint8_t* from, int64_t rows, uint32_t* at) {
-      hipLaunchKernelGGL(act4_words_kernel, dim3((unsigned)((rows * words + 255) / 256)), dim3(256), 0, s, from, rows, g.G, words, at);
+      if (rows == 0) return 0;
+      const int64_t groups = (rows * words + 255) / 256;
+      hipLaunchKernelGGL(act4_words_kernel, dim3((unsigned)(groups < kGroupsX ? groups : kGroupsX)), dim3(256), 0, s, from, rows, g.G, words, at);
       return ok();
     };
     uint32_t* ws = to + (size_t)g.T * words;

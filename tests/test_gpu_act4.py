@@ -277,6 +277,34 @@ def test_experts_rows_in_place(sq):
         _check(Y, student.experts(x, np.arange(N), held, w), student.experts(np.abs(x), np.arange(N), held, np.abs(w)), I)
 
 
+@pytest.mark.parametrize("T", [3, 700])
+def test_nan_blocks_of_either_nvfp4_operand(sq, T):
+    """A kept block that held a NaN or Inf makes its row NaN, and a NaN scale of the layer its output; no other."""
+    O, I = 72, 160
+    codes, scales = _layer("nv", 5, O, I)
+    X = torch.randn(T, I, generator=torch.Generator().manual_seed(T)).to(BF16)
+    X[1, 37], X[2, 159] = float("nan"), float("-inf")
+    xc, xs = sq.sq_act4_pack("nv", X.cuda(), XWS2)
+    c, s = _dev(codes, scales)
+    s[5, 3] = 0x7F
+    Y = sq.sq_fwd_act4("nv", xc, xs, c, s, x_ws2=XWS2, ws2=WS2)
+    bad = torch.zeros((T, O), dtype=torch.bool)
+    bad[1:3], bad[:, 5] = True, True
+    assert torch.equal(Y.cpu().isnan(), bad)
+
+
+@pytest.mark.parametrize("G", [1, 4])
+def test_experts_of_no_kept_row(sq, G):
+    """Without a kept row every row number lies outside, and all of Y is zeros."""
+    E, N, O, I = 3, 90, 264, 32 * G
+    codes, scales = (v.view(E, O, -1) for v in _dev(*_layer("mx", 8, E * O, I)))
+    offsets, rows = _dev(np.array([0, 10, 60, 90], np.int32), np.arange(N, dtype=np.int32))
+    x, xs = torch.empty((0, I // 2), dtype=torch.uint8, device="cuda"), torch.empty((0, G), dtype=torch.uint8, device="cuda")
+    Y = torch.full((N, O), float("nan"), device="cuda")
+    sq.sq_fwd_act4_batched("mx", x, xs, rows, offsets, codes, scales, Y=Y)
+    assert not Y.any()
+
+
 def test_empty_calls(sq):
     c, s = _dev(*_layer("mx", 1, 64, 128))
     e = torch.empty((0, 64), dtype=torch.uint8, device="cuda")
