@@ -662,7 +662,8 @@ int sq_ce_bwd(int head, int64_t T, int64_t V, int64_t I, const void* X, const vo
  *   (sq_moe_sort's token) times the expert's weight, or row s with rows NULL
  *   (then N == T).  Rows that no expert has, before offsets[0] and from
  *   offsets[E] on, are zeros; a row number outside 0 .. T-1 reads as a row of
- *   zeros, and offsets are held to 0 .. N.  E <= 8192; (N/64 + min(E, N) + 8)
+ *   zeros, and offsets are held to 0 .. N; they must not decrease (where they do,
+ *   rows are undefined, but nothing outside Y is touched).  E <= 8192; (N/64 + min(E, N) + 8)
  *   ceil(O/128) <= 2^22.
  * x_codes and codes 16-byte, x_scales and scales 4-byte aligned; workspace: at
  * least the bytes of the _workspace call, 256-byte aligned (NULL where that is
@@ -702,7 +703,8 @@ int sq_fwd_act4_batched(int fmt, int64_t E, int64_t T, int64_t N, int64_t O, int
  *   them and dloss fp32 [T] -> dX [T, I] in dx_dtype.  Logit gradients are
  *   rounded to bf16 for the product with W; those of the entries are formed in
  *   fp32 from picked first.
- * 1 <= K <= 256; 2^-20 <= temperature <= 2^20.  Head formats, shapes, alignment
+ * 1 <= K <= 256; 2^-20 <= temperature <= 2^20, and with an NVFP4 head ws2 times
+ * and divided by it finite and > 0.  Head formats, shapes, alignment
  * and workspace otherwise as sq_ce_fwd / sq_ce_bwd.  Deterministic.
  */
 size_t sq_distill_fwd_workspace(int head, int64_t T, int64_t V, int64_t I);
@@ -729,6 +731,7 @@ int sq_distill_bwd(int head, int64_t T, int64_t V, int64_t I, int64_t K, const v
  *   fp32 [V, G], every row written.
  * dOut [T, I] fp32 or bf16 by d_dtype; fp32 sums in token order (an id with many
  * tokens: in runs of 32 and more), the same bits on every run.  factor finite;
+ * T <= 2^30; I <= 2^26;
  * I % 8 == 0 (bf16) or I % B == 0; W (bf16), out, dOut, dW, dS 16-byte, codes
  * 4-byte aligned.  workspace: at least sq_embed_bwd_workspace bytes (0 when T =
  * 0), 256-byte aligned, contents irrelevant.

@@ -18,7 +18,7 @@ bool fmt_ok(int fmt) { return fmt == SQ_MXFP4 || fmt == SQ_NVFP4; }
 constexpr int64_t kExpertsMax = 8192;
 constexpr int64_t kXcds = 8;                // the experts' chunks are dealt to them in turn
 
-// X bf16 [T, I] and its 4-bit form; code_align: 4 bytes as a layer's codes.
+// X bf16 [T, I] and its 4-bit form.
 int check_act4(int fmt, int64_t T, int64_t I, const void* X, float ws2, const uint8_t* codes, const uint8_t* scales) {
   if (!fmt_ok(fmt)) return SQ_ERR_FORMAT;
   // 8 values a work-item, 32 a launch's: one of 2^32 work-items would be cut short
@@ -126,9 +126,9 @@ int check_distill(int head, int64_t T, int64_t V, int64_t I, int64_t K, const vo
   if (st != SQ_OK) return st;
   if ((id_bytes != 4 && id_bytes != 8) || !dtype_ok(logit_dtype)) return SQ_ERR_ARG;
   if (!W || (head != SQ_HEAD_BF16 && !scales) || (T > 0 && (!X || !ids || !logits || !picked))) return SQ_ERR_ARG;
-  if (head == SQ_HEAD_NVFP4 && !ws2_ok(ws2)) return SQ_ERR_ARG;
-  // the logits' factor and its square have to stay numbers
+  // the logits' factor, the gradient's and the temperature's square have to stay numbers
   if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return SQ_ERR_ARG;
+  if (head == SQ_HEAD_NVFP4 && !(ws2_ok(ws2) && ws2_ok(ws2 / temperature) && ws2_ok(ws2 * temperature))) return SQ_ERR_ARG;
   return aligned(X, 16) && aligned(W, head == SQ_HEAD_BF16 ? 16 : 4) && aligned(ids, (uintptr_t)id_bytes) &&
                  aligned(logits, logit_dtype == SQ_OUT_BF16 ? 2 : 4) && aligned(picked, 4) ? SQ_OK : SQ_ERR_ALIGN;
 }
@@ -178,16 +178,20 @@ SQ_EXPORT int sq_distill_bwd(int head, int64_t T, int64_t V, int64_t I, int64_t 
 // ---------------------------------------------------------------- embedding
 namespace {
 
+// Places go by 32 bits, 64 past the last token among them, and columns in launches of
+// 2048 each.
+constexpr int64_t kEmbedTokensMax = int64_t(1) << 30, kEmbedColumnsMax = int64_t(1) << 26;
+
 int check_table(int head, int64_t T, int64_t V, int64_t I, const void* ids, int id_bytes, float factor) {
   if (head != SQ_HEAD_MXFP4 && head != SQ_HEAD_NVFP4 && head != SQ_HEAD_BF16) return SQ_ERR_FORMAT;
-  if (T < 0 || V < 1 || I < 1 || T > kDimMax || V > kDimMax - 256 || I > kDimMax) return SQ_ERR_SHAPE;
+  if (T < 0 || V < 1 || I < 1 || T > kEmbedTokensMax || V > kDimMax - 256 || I > kEmbedColumnsMax) return SQ_ERR_SHAPE;
   if (I % (head == SQ_HEAD_BF16 ? 8 : block_of(head)) != 0) return SQ_ERR_SHAPE;
   if ((id_bytes != 4 && id_bytes != 8) || !isfinite(factor) || (T > 0 && !ids)) return SQ_ERR_ARG;
   return aligned(ids, (uintptr_t)id_bytes) ? SQ_OK : SQ_ERR_ALIGN;
 }
 
 size_t embed_bwd_workspace(int64_t T, int64_t V, int64_t I) {
-  if (T < 1 || V < 1 || I < 1 || T > kDimMax || V > kDimMax - 256 || I > kDimMax || I % 8 != 0) return 0;
+  if (T < 1 || V < 1 || I < 1 || T > kEmbedTokensMax || V > kDimMax - 256 || I > kEmbedColumnsMax || I % 8 != 0) return 0;
   return embed_workspace(T, V, I);
 }
 

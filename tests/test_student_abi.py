@@ -128,6 +128,26 @@ def test_embed_bwd_dscale_refusals(lib, kw, status):
     assert _call(lib.sq_embed_bwd_dscale, args, kw) == status
 
 
+# ---------------------------------------------------------------- the largest sizes
+@pytest.mark.parametrize("kw,status", [(dict(T=1 << 30), WORKSPACE), (dict(T=(1 << 30) + 1), SHAPE), (dict(I=1 << 26), WORKSPACE),
+                                       (dict(I=(1 << 26) + 8), SHAPE)])
+def test_embed_largest(lib, kw, status):
+    args = dict(T=16, V=100, I=64, ids=FAKE, ib=8, d=FAKE, dd=1, f=1.0, grad=FAKE, gd=0, ws=None, size=0, stream=None)
+    assert _call(lib.sq_embed_bwd, args, kw) == status
+    assert (_call(lib.sq_embed_bwd_workspace, dict(T=16, V=100, I=64), kw) > 0) == (status == WORKSPACE)
+    if status == SHAPE:
+        args = dict(head=BF, T=16, V=100, I=64, ids=FAKE, ib=8, W=FAKE, sc=FAKE, ws2=1.0, f=1.0, out=FAKE, od=1, stream=None)
+        assert _call(lib.sq_embed_fwd, args, kw) == SHAPE
+
+
+@pytest.mark.parametrize("ws2,tau,status", [(1.0, 2.0 ** 20, WORKSPACE), (1.0, 2.0 ** -20, WORKSPACE), (2.0 ** 120, 2.0 ** -20, ARG),
+                                            (2.0 ** 120, 2.0 ** 20, ARG), (2.0 ** -140, 2.0 ** 20, ARG), (2.0 ** -140, 2.0 ** -20, ARG)])
+def test_distill_factors_stay_numbers(lib, ws2, tau, status):
+    args = dict(head=NV, T=16, V=100, I=64, K=4, X=FAKE, W=FAKE, sc=FAKE, ws2=ws2, ids=FAKE, ib=8, z=FAKE, zd=0, tau=tau, loss=FAKE,
+                lse=FAKE, picked=FAKE, ws=None, size=0, stream=None)
+    assert _call(lib.sq_distill_fwd, args, {}) == status
+
+
 # ---------------------------------------------------------------- binding
 def test_binding_refuses_what_the_library_cannot_see():
     ensure_library()
