@@ -386,15 +386,25 @@ __device__ __forceinline__ void times(F f) {
   for_each(std::make_integer_sequence<int, N>{}, f);
 }
 
-// Many rows: tiles of 256 outputs by BT rows of Y, so that a lane holds one row's
+// Many rows: tiles of BM outputs by BT rows of Y, so that a lane holds one row's
 // outputs.  A stage is 256 inputs: the 128 bytes of codes of each row, a cache line,
 // copied to LDS with the 16-byte chunks placed as a bf16 tile's (a chunk is one lane's
 // 32 codes of a product); the scales come for two stages at a time, 16 bytes of each
 // row.  Between a slice's products go the reads of the next slice and the copies of a
 // later stage, and the barrier that publishes the next stage stands amid the last
 // slice.
+// 8192 tokens of 14336 x 4096 take 243 us: matrix cores busy 0.61 at 1.69 GHz, the chip's
+// power limit.  128 experts of 1536 x 2048 over 32768 rows (105) are bound by memory and by
+// the tiles' ends: without copies 82, without stores 95, without both 74, of which the
+// products and their reads of LDS, at 1.3 us a stage, are 50.  Tiles that follow each other in
+// resident workgroups, the next one's first copies under the last products, took the
+// same (116, 122), since the stores then hold up the next tile's stages.
+template <int BM, int BT, int STAGES>
+constexpr int tile_lds() {
+  return STAGES * (BM + BT) * 128 + (STAGES <= 3 ? 2 : 4) * (BM + BT) * 16;
+}
 template <int BM, int BT, int WGM, int WGN, int STAGES, bool BF16>
-__global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
+__device__ __forceinline__ void act4_tile(const Act4Args& g, const Chunk& c, int m0, int split, uint8_t* lds) {
   constexpr int kStageI = 256, kRow = kStageI / 2, kSlices = 4;
   constexpr int WM = BM / WGM, WN = BT / WGN, TM = WM / 32, TN = WN / 32;
   static_assert(WGM * WGN == 8 && TM >= 1 && TN >= 1, "8 waves");
@@ -408,49 +418,11 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   // each operand's buffers lie beside each other, so that their places are one
   // register's and a constant
   constexpr int kAtB = STAGES * kA, kAtSa = kAtB + STAGES * kB, kAtSb = kAtSa + kSets * kSa, kAll = kAtSb + kSets * kSb;
-  static_assert(kAll <= 160 * 1024 && BM * BT * 2 <= kAll, "LDS, of the loop and of the outputs in bf16");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kAll];
+  static_assert(kAll == tile_lds<BM, BT, STAGES>() && kAll <= 160 * 1024 && BM * BT * 2 <= kAll, "LDS, of the loop and of the outputs in bf16");
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
 
-  // The tile: of the experts' chunks from a table, the tiles of a chunk and the chunks of
-  // an expert beside each other, in stretches that the XCDs take, so that one L2 reads an
-  // expert's weight; without one dealt to the XCDs in turn (those past the last are spread
-  // as well); of one layer in groups of 4 x n tiles.
-  const int tiles_m = (g.O + BM - 1) / BM;
-  int chunk, tm, split = 0;
-  Chunk c;
-  if (g.table) {
-    const int total = g.table[0], n = total * tiles_m;
-    if ((int)blockIdx.x < n) {
-      const int pos = xcd_stretch((int)blockIdx.x, n);
-      chunk = pos / tiles_m;
-      tm = pos - chunk * tiles_m;
-      const int4 t = reinterpret_cast<const int4*>(g.table)[1 + chunk];
-      c = Chunk{t.x, t.y, t.z, 0};
-    } else {
-      chunk = (int)blockIdx.x / tiles_m;
-      tm = (int)blockIdx.x % tiles_m;
-      c = Chunk{-1, min(max(g.offsets[g.E], 0), g.N), g.N, chunk - total};
-    }
-  } else if (g.offsets) {
-    const int at = (int)blockIdx.x / kXcds;
-    chunk = at / tiles_m * kXcds + (int)blockIdx.x % kXcds;
-    tm = at % tiles_m;
-    if (chunk >= g.chunks) return;
-    c = chunk_at(g.offsets, g.E, g.N, BT, chunk);
-  } else {
-    const int tiles = tiles_m * g.chunks, pos = xcd_stretch((int)blockIdx.x, tiles * g.splits);
-    split = pos / tiles;
-    tile_at<4>(pos - split * tiles, tiles_m, g.chunks, tm, chunk);
-    c = chunk_at(nullptr, 1, g.N, BT, chunk);
-  }
-  const int m0 = tm * BM;
-  if (c.e < 0) {
-    zero_rows<BF16>(g, c, chunk, m0, BM);
-    return;
-  }
   const int half = g.I / 2, kt_first = split * g.per;
   const int nk = min((g.I + kStageI - 1) / kStageI - kt_first, g.per);
   const int live_m = min(BM, g.O - m0);
@@ -690,6 +662,60 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   }
 }
 
+// A tile per workgroup: of the experts' chunks dealt to the XCDs in turn (those past the
+// last are spread as well), of one layer in groups of 4 x n tiles.
+template <int BM, int BT, int WGM, int WGN, int STAGES, bool BF16>
+__global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[tile_lds<BM, BT, STAGES>()];
+  const int tiles_m = (g.O + BM - 1) / BM;
+  int chunk, tm, split = 0;
+  if (g.offsets) {
+    const int at = (int)blockIdx.x / kXcds;
+    chunk = at / tiles_m * kXcds + (int)blockIdx.x % kXcds;
+    tm = at % tiles_m;
+    if (chunk >= g.chunks) return;
+  } else {
+    const int tiles = tiles_m * g.chunks, pos = xcd_stretch((int)blockIdx.x, tiles * g.splits);
+    split = pos / tiles;
+    tile_at<4>(pos - split * tiles, tiles_m, g.chunks, tm, chunk);
+  }
+  const Chunk c = chunk_at(g.offsets, g.E, g.N, BT, chunk);
+  if (c.e < 0) zero_rows<BF16>(g, c, chunk, tm * BM, BM);
+  else act4_tile<BM, BT, WGM, WGN, STAGES, BF16>(g, c, tm * BM, split, lds);
+}
+
+// Experts' chunks of BT rows from a table, the tiles of a chunk and the chunks of an
+// expert beside each other, in stretches that the XCDs take, so that one L2 reads an
+// expert's weight.  An expert's last chunk takes the smallest tile that holds its rows.
+template <int BT, bool BF16>
+__global__ __launch_bounds__(512) void act4_experts_kernel(Act4Args g) {
+  constexpr int kLds = BT == 64 ? tile_lds<256, 64, 3>() : tile_lds<256, 128, 3>();
+  static_assert(tile_lds<256, 256, 2>() <= tile_lds<256, 128, 3>(), "the largest");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kLds];
+  const int tiles_m = (g.O + 255) / 256, total = g.table[0], n = total * tiles_m;
+  if ((int)blockIdx.x >= n) {                                 // past the last chunk: rows that no expert has
+    const int chunk = (int)blockIdx.x / tiles_m;
+    const Chunk c{-1, min(max(g.offsets[g.E], 0), g.N), g.N, chunk - total};
+    zero_rows<BF16>(g, c, chunk, (int)blockIdx.x % tiles_m * 256, 256);
+    return;
+  }
+  const int pos = xcd_stretch((int)blockIdx.x, n), chunk = pos / tiles_m, m0 = (pos - chunk * tiles_m) * 256;
+  const int4 t = reinterpret_cast<const int4*>(g.table)[1 + chunk];
+  const Chunk c{__builtin_amdgcn_readfirstlane(t.x), __builtin_amdgcn_readfirstlane(t.y), __builtin_amdgcn_readfirstlane(t.z), 0};
+  const int rows = c.r1 - c.r0;
+  if constexpr (BT == 256)
+    if (rows > 128) {
+      act4_tile<256, 256, 2, 4, 2, BF16>(g, c, m0, 0, lds);
+      return;
+    }
+  if constexpr (BT >= 128)
+    if (rows > 64) {
+      act4_tile<256, 128, 4, 2, 3, BF16>(g, c, m0, 0, lds);
+      return;
+    }
+  act4_tile<256, 64, 8, 1, 3, BF16>(g, c, m0, 0, lds);
+}
+
 // Scale rows of G bytes laid out in whole words.
 __global__ __launch_bounds__(256) void act4_words_kernel(const uint8_t* __restrict__ from, int64_t rows, int G, int words,
                                                          uint32_t* __restrict__ to) {
@@ -724,14 +750,21 @@ inline int64_t most_chunks(int64_t E, int64_t N, int64_t per) { return N / per +
 template <int BM, int BT, int WGM, int WGN, int STAGES>
 int tile_go(Act4Args g, int bf16, hipStream_t s) {
   g.chunks = g.offsets ? (int)most_chunks(g.E, g.N, BT) : (g.N + BT - 1) / BT;
-  if (g.table) {
-    hipLaunchKernelGGL(act4_table_kernel, dim3(1), dim3(1024), 0, s, g.offsets, g.E, g.N, BT, g.chunks - 1, const_cast<int*>(g.table));
-    if (ok() != 0) return -1;
-  }
-  const int along = g.offsets && !g.table ? (g.chunks + kXcds - 1) / kXcds * kXcds : g.chunks;
+  const int along = g.offsets ? (g.chunks + kXcds - 1) / kXcds * kXcds : g.chunks;
   const dim3 grid((unsigned)((g.O + BM - 1) / BM * along * g.splits)), block(512);
   if (bf16) hipLaunchKernelGGL((act4_tile_kernel<BM, BT, WGM, WGN, STAGES, true>), grid, block, 0, s, g);
   else hipLaunchKernelGGL((act4_tile_kernel<BM, BT, WGM, WGN, STAGES, false>), grid, block, 0, s, g);
+  return ok();
+}
+
+template <int BT>
+int experts_go(Act4Args g, int bf16, hipStream_t s) {
+  g.chunks = (int)most_chunks(g.E, g.N, BT);
+  hipLaunchKernelGGL(act4_table_kernel, dim3(1), dim3(1024), 0, s, g.offsets, g.E, g.N, BT, g.chunks - 1, const_cast<int*>(g.table));
+  if (ok() != 0) return -1;
+  const dim3 grid((unsigned)((g.O + 255) / 256 * g.chunks)), block(512);
+  if (bf16) hipLaunchKernelGGL((act4_experts_kernel<BT, true>), grid, block, 0, s, g);
+  else hipLaunchKernelGGL((act4_experts_kernel<BT, false>), grid, block, 0, s, g);
   return ok();
 }
 
@@ -742,10 +775,11 @@ struct Act4Plan {
   bool table;
 };
 
-// Experts of 3 rounds of the CUs and more take their chunks from a table (512 experts of
-// 768 x 2048 with one row each 41.7 -> 37.4 us, 128 of 1536 x 2048 with 256 122 -> 116);
-// its launch costs 2.3 (128 of 768 x 2048 with one 12.4 -> 14.7, 2 rounds of 16 rows each
-// 30.1 -> 29.8).
+// Experts of more than one round of the CUs take their chunks from a table, and their last
+// rows a smaller tile (128 of 1536 x 2048 with 256 rows each 122 us, with the table 114,
+// with both 105; 128 of 2048 x 768 with 256 83, 76, 69; 128 of 768 x 2048 with 128 42.4,
+// -, 38.9).  With the smallest tiles only from 3 rounds on, since the table's launch costs
+// 2 (512 of 768 x 2048 with one row each 41.7 -> 34.9, 128 with 16 22.4 -> 24.0).
 // The smallest tiles that one round of the CUs holds, or else the largest that the rows
 // fill.  us in a graph, of 128 x 64, 128 x 128, 256 x 64, 256 x 128 and 256 x 256 tiles:
 // 512 rows of 4096 x 4096 10.7, 11.9, 12.8, 15.5, 23.1; 512 of 14336 x 4096 40.9, 28.5,
@@ -778,7 +812,7 @@ Act4Plan act4_plan(bool batched, int64_t E, int64_t N, int64_t O, int64_t I) {
   }
   if (batched && !found) {
     p.bt = avg <= 48 ? 64 : avg <= 160 ? 128 : 256;
-    p.table = live * ((avg + p.bt - 1) / p.bt) * ((O + 255) / 256) >= 3 * kCUs;
+    p.table = p.bt > 64 || live * ((O + 255) / 256) >= 3 * kCUs;
   }
   const int64_t t = (O + p.bm - 1) / p.bm * ((N + p.bt - 1) / p.bt);
   if (!batched && 2 * t <= kCUs && stages >= 24) {
@@ -831,7 +865,8 @@ int product(Act4Args g, int bf16, void* workspace, hipStream_t s) {
   if (p.table) g.table = reinterpret_cast<int*>(behind);
   const int as_bf16 = bf16 && p.splits == 1;
   int rc;
-  if (p.bm == 128) rc = p.bt == 64 ? tile_go<128, 64, 4, 2, 6>(g, as_bf16, s) : tile_go<128, 128, 4, 2, 4>(g, as_bf16, s);
+  if (p.table) rc = p.bt == 64 ? experts_go<64>(g, as_bf16, s) : p.bt == 128 ? experts_go<128>(g, as_bf16, s) : experts_go<256>(g, as_bf16, s);
+  else if (p.bm == 128) rc = p.bt == 64 ? tile_go<128, 64, 4, 2, 6>(g, as_bf16, s) : tile_go<128, 128, 4, 2, 4>(g, as_bf16, s);
   else if (p.bt == 64) rc = tile_go<256, 64, 8, 1, 3>(g, as_bf16, s);
   else rc = p.bt == 128 ? tile_go<256, 128, 4, 2, 3>(g, as_bf16, s) : tile_go<256, 256, 2, 4, 2>(g, as_bf16, s);
   if (rc != 0 || p.splits == 1) return rc;

@@ -240,9 +240,10 @@ def test_experts(sq, E, T, N, O, I, kind):
 
 
 @pytest.mark.parametrize("kind", ["even", "one", "dropped", "empty"])
-@pytest.mark.parametrize("E,T,N,O,I", [(200, 64, 512, 1288, 64), (1500, 40, 1600, 264, 96)])
+@pytest.mark.parametrize("E,T,N,O,I", [(200, 64, 512, 1288, 64), (1500, 40, 1600, 264, 96), (30, 200, 3300, 2056, 288),
+                                       (12, 300, 3000, 4104, 544)])
 def test_experts_of_several_rounds(sq, E, T, N, O, I, kind):
-    """So many experts that their chunks come from a table; rows before the first range as well."""
+    """So many tiles that the chunks come from a table, and last ones take smaller tiles; rows before the first range as well."""
     g = inputs.rng(E + N)
     codes, scales = (v.view(E, O, -1) for v in _dev(*_layer("mx", N, E * O, I)))
     xc, xs, _ = _rows("mx", T, T, I)

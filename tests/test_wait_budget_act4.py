@@ -86,7 +86,7 @@ def test_one_copy_more_in_flight_would_show(tile):
 def test_model_follows_the_kernel_source():
     """The copies, waits and barriers that the replay assumes, in their order."""
     src = text()
-    body = src[src.index("void act4_tile_kernel("):src.index("// 32 x 32 result")]
+    body = src[src.index("void act4_tile("):src.index("// 32 x 32 result")]
     for line in ("kAhead = (STAGES - 2) * kDma;", "kLead = STAGES == 3 ? 1 : STAGES / 2, kSets = STAGES <= 3 ? 2 : 4;",
                  "kFirst = kDma / 2, kSecond = kDma - kFirst;", "kInstA = BM / 64, kInstB = BT / 64, kDma = kInstA + kInstB;"):
         assert line in body
