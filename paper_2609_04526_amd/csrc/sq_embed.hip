@@ -23,6 +23,11 @@ namespace {
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
 
+// 16 bytes of a gradient that no token reaches.  They pass the caches by, which such a
+// table would fill (gradient of 1999 tokens, 50001 x 2048 fp32: 89 -> 76 us; where nothing
+// else runs, in embed_few_kernel, they go through: 80 MB 20 us, so 18).
+__device__ __forceinline__ void zero16(u32x4* p) { __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, p); }
+
 // The id, or V where it is outside the table.
 __device__ __forceinline__ int key_at(const void* ids, int bytes, int64_t t, int V) {
   const int64_t v = id_at(ids, bytes, t);
@@ -97,8 +102,8 @@ __global__ __launch_bounds__(1024) void embed_few_kernel(const void* __restrict_
                                                          int64_t units, int words) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (blockIdx.x > 0) {
-    const int64_t n = (int64_t)(gridDim.x - 1) * 1024, at = (int64_t)(blockIdx.x - 1) * 1024 + tid;
-    for (int64_t i = at; i < units; i += n) grad[i] = u32x4{0u, 0u, 0u, 0u};
+    const int64_t at = (int64_t)(blockIdx.x - 1) * 1024 + tid;
+    if (at < units) grad[at] = u32x4{0u, 0u, 0u, 0u};
     if (at < words) reinterpret_cast<uint32_t*>(grad + units)[at] = 0u;
     return;
   }
@@ -135,8 +140,9 @@ __global__ __launch_bounds__(1024) void embed_few_kernel(const void* __restrict_
 // pass is one launch and nothing is exchanged between workgroups.  The other
 // workgroups of the first pass clear `marks`; the last pass sets those of the ids that
 // occur.  A pass leaves most CUs idle, so further workgroups clear part of the gradient
-// meanwhile, which the sums would have to otherwise (lookup and gradient of 1999 tokens,
-// 50001 x 2048 fp32, 96 -> 93 us; 131072 x 128 fp32 of 16384 tokens 123 -> 121).
+// meanwhile, which the sums would have to otherwise, and so they do in the launch of the
+// chunks' sums (gradient of 1999 tokens, 50001 x 2048 fp32, 28 MiB a pass 80 us, 40 and 24
+// with the chunks 75; 4000 tokens, bf16, 46.8, 42.7).
 template <bool FIRST>
 __global__ __launch_bounds__(1024) void embed_pass_kernel(const void* __restrict__ ids, int id_bytes, int T, int V,
                                                           const int* __restrict__ keys_in, const int* __restrict__ tokens_in,
@@ -149,7 +155,7 @@ __global__ __launch_bounds__(1024) void embed_pass_kernel(const void* __restrict
     const u32x4 zero = {0u, 0u, 0u, 0u};
     if (FIRST)
       for (int64_t i = i0; i < mark_words; i += n) reinterpret_cast<u32x4*>(marks)[i] = zero;
-    for (int64_t i = i0; i < part_words; i += n) part[i] = zero;
+    for (int64_t i = i0; i < part_words; i += n) zero16(&part[i]);
     return;
   }
   __shared__ int s_all[kEmbedDigits], s_before[kEmbedDigits], s_next[16][kEmbedDigits], s_sum[8];
@@ -209,11 +215,14 @@ struct EmbedArgs {
   float* part;              // sums of whole chunks of one id, [chunks, H]
   const uint8_t* marks;     // [V]: the ids that occur
   int T, V, H, chunk;
-  int chunks;               // whether the chunks' sums are there
+  int chunks;               // of which the sums are there
   int units, lanes;         // 16-byte (or 4-byte) units of a row of the gradient, and lanes that clear one, a power of 2
   int narrow;               // rows are not whole 16 bytes
   int heads;                // workgroups of the sums, before those that clear
   int64_t clear_from;       // the first row that is not clear yet
+  int clear_rows;           // of a workgroup
+  u32x4* clear;             // and what the chunks' launch clears, before that row
+  int64_t clear_words;
   float factor;
 };
 
@@ -242,6 +251,12 @@ __device__ __forceinline__ void add_rows(const EmbedArgs& g, int a, int b, int h
 // is summed by many workgroups.
 template <bool BF16>
 __global__ __launch_bounds__(256) void embed_chunk_kernel(EmbedArgs g) {
+  if ((int)blockIdx.x >= g.chunks) {                          // (as in a pass)
+    if (blockIdx.y > 0) return;
+    const int64_t n = (int64_t)((int)gridDim.x - g.chunks) * blockDim.x;
+    for (int64_t i = (int64_t)((int)blockIdx.x - g.chunks) * blockDim.x + threadIdx.x; i < g.clear_words; i += n) zero16(&g.clear[i]);
+    return;
+  }
   const int a = (int)blockIdx.x * g.chunk, b = a + g.chunk, h = ((int)blockIdx.y * (int)blockDim.x + (int)threadIdx.x) * 8;
   if (b > g.T || g.keys[a] != g.keys[b - 1] || g.keys[a] >= g.V || h >= g.H) return;
   float v[8] = {};
@@ -251,14 +266,18 @@ __global__ __launch_bounds__(256) void embed_chunk_kernel(EmbedArgs g) {
 
 enum EmbedGrad { kDwF32 = 0, kDwBf16 = 1, kDsMx = 2, kDsNv = 3 };
 
-// Zeros in the rows of ids that do not occur: workgroup i of n.
-__device__ __forceinline__ void clear_rows(const EmbedArgs& g, int i, int n) {
+// Zeros in the rows of ids that do not occur: the i-th `clear_rows` of them, so that the
+// workgroups, in their order, write through the memory from its start to its end (1999
+// tokens, 50001 x 2048 fp32 in steps of all workgroups 76 us, so 66; 16384 tokens, 100000 x
+// 2048 183, 150).
+__device__ __forceinline__ void clear_rows(const EmbedArgs& g, int i) {
   const int per = (int)blockDim.x / g.lanes, sub = (int)threadIdx.x / g.lanes, l = (int)threadIdx.x % g.lanes;
-  for (int64_t r = g.clear_from + (int64_t)i * per + sub; r < g.V; r += (int64_t)n * per) {
+  const int64_t r0 = g.clear_from + (int64_t)i * g.clear_rows, end = min(r0 + g.clear_rows, (int64_t)g.V);
+  for (int64_t r = r0 + sub; r < end; r += per) {
     if (g.marks[r]) continue;
     for (int u = l; u < g.units; u += g.lanes) {
       if (g.narrow) reinterpret_cast<float*>(g.grad)[r * g.units + u] = 0.0f;
-      else reinterpret_cast<f32x4*>(g.grad)[r * g.units + u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      else zero16(&reinterpret_cast<u32x4*>(g.grad)[r * g.units + u]);
     }
   }
 }
@@ -270,7 +289,7 @@ __device__ __forceinline__ void clear_rows(const EmbedArgs& g, int i, int n) {
 template <int GRAD, bool BF16>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs g) {
   if ((int)blockIdx.x >= g.heads) {
-    if (blockIdx.y == 0) clear_rows(g, (int)blockIdx.x - g.heads, (int)gridDim.x - g.heads);
+    if (blockIdx.y == 0) clear_rows(g, (int)blockIdx.x - g.heads);
     return;
   }
   const int lane = threadIdx.x & 63;
@@ -399,7 +418,7 @@ EmbedPlan embed_plan(int64_t T, int64_t V, int64_t H) {
 
 __global__ __launch_bounds__(256) void embed_clear_kernel(u32x4* __restrict__ to, int64_t units, int words) {
   const int64_t n = (int64_t)gridDim.x * 256, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  for (int64_t i = at; i < units; i += n) to[i] = u32x4{0u, 0u, 0u, 0u};
+  for (int64_t i = at; i < units; i += n) zero16(&to[i]);
   if (at < words) reinterpret_cast<uint32_t*>(to + units)[at] = 0u;
 }
 int clear(void* to, int64_t bytes, hipStream_t s) {             // bytes a multiple of 4
@@ -411,7 +430,7 @@ int clear(void* to, int64_t bytes, hipStream_t s) {             // bytes a multi
 
 // Tokens sorted by id into the workspace, and the ids that occur marked; *cleared: the
 // bytes of the gradient that are zero by then.
-constexpr int64_t kEmbedPassClears = int64_t(28) << 20, kEmbedClearsFrom = int64_t(48) << 20;   // bytes a pass, of so many or more
+constexpr int64_t kEmbedPassClears = int64_t(40) << 20, kEmbedChunkClears = int64_t(24) << 20, kEmbedClearsFrom = int64_t(48) << 20;   // bytes a pass, of so many or more
 int embed_sort(const EmbedPlan& p, const void* ids, int id_bytes, int T, int V, uint8_t* ws, void* grad, int64_t bytes,
                int64_t* cleared, hipStream_t s) {
   auto at = [&](size_t o) { return reinterpret_cast<int*>(ws + o); };
@@ -419,8 +438,7 @@ int embed_sort(const EmbedPlan& p, const void* ids, int id_bytes, int T, int V, 
   while ((int64_t)V >> (passes * kEmbedDigitBits) > 0) ++passes;         // the keys are 0 .. V
   if (T <= 1024) {
     *cleared = bytes;
-    const int64_t want = (bytes / 16 + 4095) / 4096;
-    hipLaunchKernelGGL(embed_few_kernel, dim3(1 + (unsigned)(want < 1 ? 1 : want < 2048 ? want : 2048)), dim3(1024), 0, s, ids, id_bytes, T, V,
+    hipLaunchKernelGGL(embed_few_kernel, dim3(1 + (unsigned)(bytes / 16 / 1024 + 1)), dim3(1024), 0, s, ids, id_bytes, T, V,
                        passes, at(p.keys), at(p.tokens), static_cast<u32x4*>(grad), bytes / 16, (int)(bytes % 16 / 4));
     return ok();
   }
@@ -471,6 +489,10 @@ int embed_sort(const EmbedPlan& p, const void* ids, int id_bytes, int T, int V, 
   return 0;
 }
 
+// What a workgroup clears of a gradient (gradient of 4000 tokens, 50001 x 2048 bf16, with 4, 8
+// and 16 KiB 48.4, 42.8, 42.3 us; of 1999, fp32, 65.4, 65.6, 75.7).
+constexpr int64_t kEmbedClearBytes = 8192;
+
 // Up to these tokens a run is summed by one workgroup per 2048 columns, whatever its length:
 // a launch less (us in a graph, without against with the chunks' sums: 128 tokens of
 // 1000 x 4096 9.9, 11.4, all of one id 16.2, 13.4; 256 of one id 26.4, 13.5).
@@ -480,9 +502,10 @@ template <int GRAD, bool BF16>
 int embed_sums(EmbedArgs g, hipStream_t s) {
   const int block = (int)(up(g.H / 8, 64) < 256 ? up(g.H / 8, 64) : 256);
   const int chunks = g.T / g.chunk;
-  g.chunks = g.T > kEmbedRunTokens && chunks > 0;
+  g.chunks = g.T > kEmbedRunTokens ? chunks : 0;
   if (g.chunks) {
-    hipLaunchKernelGGL((embed_chunk_kernel<BF16>), dim3((unsigned)chunks, (unsigned)((g.H / 8 + block - 1) / block)), dim3(block), 0, s, g);
+    const int64_t more = (g.clear_words + 4095) / 4096;
+    hipLaunchKernelGGL((embed_chunk_kernel<BF16>), dim3((unsigned)(chunks + (more < 1024 ? more : 1024)), (unsigned)((g.H / 8 + block - 1) / block)), dim3(block), 0, s, g);
     if (ok() != 0) return -1;
   }
   const int64_t cols = GRAD == kDsMx ? g.H / 32 : GRAD == kDsNv ? g.H / 16 : GRAD == kDwBf16 ? g.H / 2 : g.H;   // words of a row
@@ -493,7 +516,10 @@ int embed_sums(EmbedArgs g, hipStream_t s) {
   if (block % g.lanes != 0) g.lanes = 64;                     // blocks of 192
   const int groups = (g.T + 7) / 8;
   g.heads = groups < (1 << 20) ? groups : 1 << 20;
-  const int64_t rows = (g.V - g.clear_from + block / g.lanes - 1) / (block / g.lanes), clears = rows < 4096 ? rows : 4096;
+  const int64_t row = cols * 4, per = block / g.lanes, some = up(kEmbedClearBytes / row < 1 ? 1 : kEmbedClearBytes / row, per);
+  const int64_t most = up((g.V - g.clear_from + (1 << 20) - 1) >> 20, per);
+  g.clear_rows = (int)(some > most ? some : most);
+  const int64_t clears = (g.V - g.clear_from + g.clear_rows - 1) / g.clear_rows;
   hipLaunchKernelGGL((embed_sum_kernel<GRAD, BF16>), dim3((unsigned)(g.heads + clears), (unsigned)((g.H / 8 + block - 1) / block)),
                      dim3(block), 0, s, g);
   return ok();
@@ -527,6 +553,12 @@ int embed_bwd_launch(int head, int T, int V, int H, const void* ids, int id_byte
   int64_t cleared;
   if (embed_sort(p, ids, id_bytes, T, V, ws, grad, V * row, &cleared, s) != 0) return -1;
   EmbedArgs g{};
+  if (T > 1024 && T <= kEmbedPassTokens && V * row >= kEmbedClearsFrom) {      // more of it beside the chunks' sums
+    const int64_t left = V * row - cleared;
+    g.clear = reinterpret_cast<u32x4*>(static_cast<uint8_t*>(grad) + cleared);
+    g.clear_words = (left < kEmbedChunkClears ? left : kEmbedChunkClears) / 16;
+    cleared += g.clear_words * 16;
+  }
   g.clear_from = cleared / row;
   g.keys = reinterpret_cast<int*>(ws + p.keys);
   g.tokens = reinterpret_cast<int*>(ws + p.tokens);
