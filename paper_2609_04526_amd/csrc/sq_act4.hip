@@ -73,6 +73,8 @@ __device__ __forceinline__ void pack8(u32x4 h, float ws2, const RcpDivisor& wd, 
   if (p % kLanes == 0) scales[p / kLanes] = (uint8_t)(bad ? (FMT == kMX ? 0xFFu : 0x7Fu) : byte);
 }
 
+// Bound by memory: 8192 x 14336 in 72 us with NVFP4's exact quotients (4.2 TB/s), 8192 x 4096
+// MXFP4 in 20 to 28; back again 52 us (5.8 TB/s).
 template <int FMT>
 __global__ __launch_bounds__(256) void act4_pack_kernel(const u32x4* __restrict__ X, int64_t pieces, float ws2,
                                                         uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
@@ -252,7 +254,8 @@ __device__ __forceinline__ i32x8 codes_operand(u32x4 c) {
 
 // Few rows: the weight's codes go from memory into the operand registers, each once
 // per chunk of 16 NT rows.  A workgroup takes 16 RM outputs; its waves take a stretch of
-// the inputs each, in steps of 128, and their sums meet in LDS in wave order.  WORDS:
+// the inputs each, in steps of 128, and their sums meet in LDS in wave order.  Bound by the
+// round trips of the loads: one row of 4096 x 4096 4.2 us (2.1 TB/s), 64 rows 8.6.  WORDS:
 // scale rows are whole words, and 4 steps' scales of a row come in one load.
 template <int RM, int NT, bool WORDS, bool BF16>
 __global__ __launch_bounds__(512) void act4_thin_kernel(Act4Args g) {

@@ -112,8 +112,9 @@ __global__ __launch_bounds__(256) void distill_live_kernel(Distill g, int T, int
 
 // ------------------------------------------------------------------ their logits
 // 16 entries of one token per workgroup, 4 per wave (all of a token's in one: 200 tokens of
-// 50000 x 2048 bf16 with 256 entries each 124 us, so 29).  The first workgroup of a token
-// also finds whether it counts.
+// 50000 x 2048 bf16 with 256 entries each 124 us, so 29).  Bound by the gathered rows: 4096
+// tokens of 131072 x 4096 bf16 with 64 entries 286 us, 2.1 GB at 7.5 TB/s.  The first
+// workgroup of a token also finds whether it counts.
 template <int HEAD>
 __global__ __launch_bounds__(256) void distill_pick_kernel(Distill g, int T, int V, int H, const uint16_t* __restrict__ X,
                                                            const void* __restrict__ W, const uint8_t* __restrict__ scales,
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(256) void distill_pick_kernel(Distill g, int T, int
 
 // ------------------------------------------------------------------ loss
 // 16 tokens per workgroup: its threads share the tiles' pairs, 64 to a token, then a
-// wave takes a token.
+// wave takes a token.  Latency: 5 tokens of 4 tiles 3.7 us, 4096 of 512 tiles 9.
 template <int P>
 __global__ __launch_bounds__(1024) void distill_loss_kernel(Distill g, const float2* __restrict__ part, const int* __restrict__ rows,
                                                             const int* __restrict__ count, const int* __restrict__ y, int T, int V,
@@ -234,7 +235,8 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(Distill g, const flo
 
 // ------------------------------------------------------------------ gradient
 // A wave per live token.  Entries of one id are one column: each writes the same
-// value, with all their probabilities taken off.
+// value, with all their probabilities taken off.  Latency: 5 tokens with 16 entries 5.6 us,
+// 4096 with 64 11.
 template <int P>
 __global__ __launch_bounds__(256) void distill_put_kernel(Distill g, DistillPiece p, const float* __restrict__ lse,
                                                           const float* __restrict__ dloss) {

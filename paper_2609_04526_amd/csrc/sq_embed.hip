@@ -35,7 +35,8 @@ __device__ __forceinline__ int key_at(const void* ids, int bytes, int64_t t, int
 }
 
 // ------------------------------------------------------------------ lookup
-// One token per workgroup, 8 columns per lane and step.
+// One token per workgroup, 8 columns per lane and step.  Bound by memory: 16384 tokens of
+// 4096 MXFP4 to bf16 31 us (170 MB, 5.5 TB/s).
 template <int HEAD, bool BF16>
 __global__ __launch_bounds__(256) void embed_kernel(const void* __restrict__ ids, int id_bytes, int64_t T, int V, int H,
                                                     const void* __restrict__ W, const uint8_t* __restrict__ scales, float ws2,
@@ -102,8 +103,8 @@ __global__ __launch_bounds__(1024) void embed_few_kernel(const void* __restrict_
                                                          int64_t units, int words) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (blockIdx.x > 0) {
-    const int64_t at = (int64_t)(blockIdx.x - 1) * 1024 + tid;
-    if (at < units) grad[at] = u32x4{0u, 0u, 0u, 0u};
+    const int64_t n = (int64_t)(gridDim.x - 1) * 1024, at = (int64_t)(blockIdx.x - 1) * 1024 + tid;
+    for (int64_t i = at; i < units; i += n) grad[i] = u32x4{0u, 0u, 0u, 0u};
     if (at < words) reinterpret_cast<uint32_t*>(grad + units)[at] = 0u;
     return;
   }
@@ -285,7 +286,9 @@ __device__ __forceinline__ void clear_rows(const EmbedArgs& g, int i) {
 // A workgroup has 8 places, and sums the runs that start there: their tokens in order,
 // one row after another whichever run they belong to, 8 on their way together.  A run
 // that goes on past the 64 places whose keys a wave holds takes whole chunks by their
-// sums.  The workgroups past the places clear the rows of ids that do not occur.
+// sums.  The workgroups past the places clear the rows of ids that do not occur.  16384
+// tokens of 131072 x 4096 MXFP4 take 40 us, the rows' 134 MB at 3.4 TB/s: the round trips of
+// places, rows and codes; 1999 of 50001 x 2048 bf16 43, of which zeros, 308 MB at 7.1.
 template <int GRAD, bool BF16>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs g) {
   if ((int)blockIdx.x >= g.heads) {
@@ -442,7 +445,9 @@ int embed_sort(const EmbedPlan& p, const void* ids, int id_bytes, int T, int V, 
   while ((int64_t)V >> (passes * kEmbedDigitBits) > 0) ++passes;         // the keys are 0 .. V
   if (T <= 1024) {
     *cleared = bytes;
-    hipLaunchKernelGGL(embed_few_kernel, dim3(1 + (unsigned)(bytes / 16 / 1024 + 1)), dim3(1024), 0, s, ids, id_bytes, T, V,
+    // a store per lane, up to 16 GiB: 2^32 lanes would be cut short
+    const int64_t want = bytes / 16 / 1024 + 1;
+    hipLaunchKernelGGL(embed_few_kernel, dim3(1 + (unsigned)(want < (1 << 20) ? want : 1 << 20)), dim3(1024), 0, s, ids, id_bytes, T, V,
                        passes, at(p.keys), at(p.tokens), static_cast<u32x4*>(grad), bytes / 16, (int)(bytes % 16 / 4));
     return ok();
   }

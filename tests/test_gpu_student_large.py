@@ -41,6 +41,20 @@ def test_embedding_of_a_large_table(sq):
     assert not any(part.any() for part in dW.split(50000))
 
 
+@pytest.mark.parametrize("T", [3, 1500])
+def test_gradient_of_more_units_than_a_launch_has(sq, T):
+    V, H = (1 << 21) + 3, 8200                                 # 6.9e10 bytes: more than 2^32 of 16
+    if torch.cuda.mem_get_info()[0] < V * H * 4 + (4 << 30):
+        pytest.skip("needs 73 GB")
+    ids = torch.full((T,), V - 2, device="cuda", dtype=torch.int32)
+    ids[0] = 11
+    dW = torch.ones((V, H), device="cuda")
+    sq.sq_embed_bwd(ids, torch.ones((T, H), dtype=BF16, device="cuda"), V, dW=dW)
+    assert (dW[11] == 1).all() and (dW[V - 2] == T - 1).all()
+    dW[11] = dW[V - 2] = 0
+    assert not any(part.any() for part in dW.split(50000))
+
+
 def test_scales_of_a_large_table(sq):
     V, H = 1100003, 4096                                       # codes of 2.25e9 bytes
     codes = torch.full((V, H // 2), 0x22, dtype=torch.uint8, device="cuda")          # ones
