@@ -263,6 +263,32 @@ def test_experts_of_several_rounds(sq, E, T, N, O, I, kind):
     assert not Y[:offsets[0]].any() and not Y[offsets[E]:].any()
 
 
+@pytest.mark.parametrize("E,T,N,O,I", [(200, 64, 512, 1288, 64), (12, 300, 3000, 4104, 96), (8, 60, 200, 264, 160), (4, 5, 10, 40, 64)])
+def test_experts_captured_with_other_offsets(sq, E, T, N, O, I):
+    """A graph of the product follows the offsets and rows that lie in its buffers at each replay."""
+    g = inputs.rng(E + T)
+    codes, scales = (v.view(E, O, -1) for v in _dev(*_layer("mx", N, E * O, I)))
+    xc, xs, _ = _rows("mx", T, T, I)
+    xc, xs = _dev(xc, xs)
+    offsets, rows = _dev(_split(g, E, N, "even"), g.integers(0, T, N).astype(np.int32))
+    ws = torch.empty(max(sq.sq_fwd_act4_batched_workspace("mx", E, T, N, O, I), 1), dtype=torch.uint8, device="cuda")
+    Y = torch.empty((N, O), dtype=BF16, device="cuda")
+    run = lambda out: sq.sq_fwd_act4_batched("mx", xc, xs, rows, offsets, codes, scales, Y=out, workspace=ws)
+    run(Y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(Y)
+    for kind in ("one", "dropped", "empty", "even", "even"):
+        offsets.copy_(torch.from_numpy(_split(g, E, N, kind)))
+        rows.copy_(torch.from_numpy(g.integers(0, T, N).astype(np.int32)))
+        want = run(torch.full((N, O), float("nan"), dtype=BF16, device="cuda"))
+        Y.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, want)
+
+
 def test_experts_rows_in_place(sq):
     """Without row numbers, row s is row s; rows before the first range are zeros too; offsets past the rows are held."""
     E, N, O, I = 4, 90, 72, 128
