@@ -649,18 +649,29 @@ __device__ __forceinline__ void act4_tile(const Act4Args& g, const Chunk& c, int
       if (row < c.r1 && o < g.O) *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(g.out) + (size_t)row * g.O + o) = v;
     }
   } else {
+    // the same for 32 rows at a time, whose 16-byte units of fp32 a wave's share of LDS holds
+    __syncthreads();
+    static_assert(8 * 32 * WM * 4 <= kAll, "LDS, of 32 rows of a wave's outputs");
+    constexpr int kUnits = WM / 4, kRows = 64 / kUnits;
+    SQ_LDS f32x4* s = (SQ_LDS f32x4*)lds + wave * 32 * kUnits;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const int row = c.r0 + wn0 + j * 32 + (lane & 31);
-      if (row >= c.r1) continue;
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int o = m0 + wm0 + i * 32 + 8 * q + 4 * (lane >> 5);
-          if (o < g.O)
-            put4<false>(g.out, ((size_t)split * g.N + row) * g.O + o, f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+          const int n = lane & 31, u = i * 8 + 2 * q + (lane >> 5);
+          s[n * kUnits + (u ^ (n & (kUnits - 1)))] = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int it = 0; it < 32 / kRows; ++it) {
+        const int n = it * kRows + lane / kUnits, u = lane % kUnits;
+        const f32x4 v = s[n * kUnits + (u ^ (n & (kUnits - 1)))];
+        const int row = c.r0 + wn0 + j * 32 + n, o = m0 + wm0 + 4 * u;
+        if (row < c.r1 && o < g.O) put4<false>(g.out, ((size_t)split * g.N + row) * g.O + o, v);
+      }
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
