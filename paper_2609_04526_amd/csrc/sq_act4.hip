@@ -406,7 +406,10 @@ template <int BM, int BT, int STAGES>
 constexpr int tile_lds() {
   return STAGES * (BM + BT) * 128 + (STAGES <= 3 ? 2 : 4) * (BM + BT) * 16;
 }
-template <int BM, int BT, int WGM, int WGN, int STAGES, bool BF16>
+// PAST: outputs pass the caches by, which the experts' weights and rows need (128 experts of
+// 1536 x 2048 over 32768 rows 108 -> 88 us, of 2048 x 768 to fp32 98 -> 77; of one layer it
+// is a loss as often as a gain: 8192 tokens of 8192 x 1024 55 -> 64, 4096 x 4096 41.2 -> 40.5).
+template <int BM, int BT, int WGM, int WGN, int STAGES, bool PAST, bool BF16>
 __device__ __forceinline__ void act4_tile(const Act4Args& g, const Chunk& c, int m0, int split, uint8_t* lds) {
   constexpr int kStageI = 256, kRow = kStageI / 2, kSlices = 4;
   constexpr int WM = BM / WGM, WN = BT / WGN, TM = WM / 32, TN = WN / 32;
@@ -620,6 +623,10 @@ __device__ __forceinline__ void act4_tile(const Act4Args& g, const Chunk& c, int
     });
   wait_vm_lgkm0<0>();
 
+  auto put = [](auto* to, auto v) {
+    if constexpr (PAST) __builtin_nontemporal_store(v, to);
+    else *to = v;
+  };
   // 32 x 32 result: lane l, register r holds output 8 (r / 4) + 4 (l / 32) + r % 4 of
   // row l % 32.
   if constexpr (BF16) {
@@ -646,7 +653,7 @@ __device__ __forceinline__ void act4_tile(const Act4Args& g, const Chunk& c, int
       const int n = it * kTok + lane / kLanes, u = lane % kLanes;
       const u32x4 v = *(const SQ_LDS u32x4*)(s + n * WM + ((u ^ n) & (kLanes - 1)) * 8);
       const int row = c.r0 + wn0 + n, o = m0 + wm0 + 8 * u;
-      if (row < c.r1 && o < g.O) *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(g.out) + (size_t)row * g.O + o) = v;
+      if (row < c.r1 && o < g.O) put(reinterpret_cast<u32x4*>(static_cast<uint16_t*>(g.out) + (size_t)row * g.O + o), v);
     }
   } else {
     // the same for 32 rows at a time, whose 16-byte units of fp32 a wave's share of LDS holds
@@ -669,7 +676,7 @@ __device__ __forceinline__ void act4_tile(const Act4Args& g, const Chunk& c, int
         const int n = it * kRows + lane / kUnits, u = lane % kUnits;
         const f32x4 v = s[n * kUnits + (u ^ (n & (kUnits - 1)))];
         const int row = c.r0 + wn0 + j * 32 + n, o = m0 + wm0 + 4 * u;
-        if (row < c.r1 && o < g.O) put4<false>(g.out, ((size_t)split * g.N + row) * g.O + o, v);
+        if (row < c.r1 && o < g.O) put(reinterpret_cast<f32x4*>(static_cast<float*>(g.out) + ((size_t)split * g.N + row) * g.O + o), v);
       }
       __builtin_amdgcn_wave_barrier();
     }
@@ -695,7 +702,7 @@ __global__ __launch_bounds__(512) void act4_tile_kernel(Act4Args g) {
   }
   const Chunk c = chunk_at(g.offsets, g.E, g.N, BT, chunk);
   if (c.e < 0) zero_rows<BF16>(g, c, chunk, tm * BM, BM);
-  else act4_tile<BM, BT, WGM, WGN, STAGES, BF16>(g, c, tm * BM, split, lds);
+  else act4_tile<BM, BT, WGM, WGN, STAGES, false, BF16>(g, c, tm * BM, split, lds);
 }
 
 // Experts' chunks of BT rows from a table, the tiles of a chunk and the chunks of an
@@ -719,15 +726,15 @@ __global__ __launch_bounds__(512) void act4_experts_kernel(Act4Args g) {
   const int rows = c.r1 - c.r0;
   if constexpr (BT == 256)
     if (rows > 128) {
-      act4_tile<256, 256, 2, 4, 2, BF16>(g, c, m0, 0, lds);
+      act4_tile<256, 256, 2, 4, 2, true, BF16>(g, c, m0, 0, lds);
       return;
     }
   if constexpr (BT >= 128)
     if (rows > 64) {
-      act4_tile<256, 128, 4, 2, 3, BF16>(g, c, m0, 0, lds);
+      act4_tile<256, 128, 4, 2, 3, true, BF16>(g, c, m0, 0, lds);
       return;
     }
-  act4_tile<256, 64, 8, 1, 3, BF16>(g, c, m0, 0, lds);
+  act4_tile<256, 64, 8, 1, 3, true, BF16>(g, c, m0, 0, lds);
 }
 
 // Scale rows of G bytes laid out in whole words.
