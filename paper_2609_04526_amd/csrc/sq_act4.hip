@@ -397,9 +397,9 @@ __device__ __forceinline__ void times(F f) {
 // later stage, and the barrier that publishes the next stage stands amid the last
 // slice.
 // 8192 tokens of 14336 x 4096 take 243 us: matrix cores busy 0.61 at 1.69 GHz, the chip's
-// power limit.  128 experts of 1536 x 2048 over 32768 rows (105) are bound by memory and by
-// the tiles' ends: without copies 82, without stores 95, without both 74, of which the
-// products and their reads of LDS, at 1.3 us a stage, are 50.  Tiles that follow each other in
+// power limit.  128 experts of 1536 x 2048 over 32768 rows (87) are bound by memory and by
+// the tiles' ends: when they took 116, 82 without copies, 95 without stores, 74 without both,
+// of which the products and their reads of LDS, at 1.3 us a stage, were 50.  Tiles that follow each other in
 // resident workgroups, the next one's first copies under the last products, took the
 // same (116, 122), since the stores then hold up the next tile's stages.
 template <int BM, int BT, int STAGES>
