@@ -36,7 +36,7 @@ __device__ __forceinline__ int key_at(const void* ids, int bytes, int64_t t, int
 
 // ------------------------------------------------------------------ lookup
 // One token per workgroup, 8 columns per lane and step.  Bound by memory: 16384 tokens of
-// 4096 MXFP4 to bf16 31 us (170 MB, 5.5 TB/s).
+// 4096 MXFP4 to bf16 23 us (170 MB, 7.3 TB/s; 26 through the caches).
 template <int HEAD, bool BF16>
 __global__ __launch_bounds__(256) void embed_kernel(const void* __restrict__ ids, int id_bytes, int64_t T, int V, int H,
                                                     const void* __restrict__ W, const uint8_t* __restrict__ scales, float ws2,
@@ -51,7 +51,9 @@ __global__ __launch_bounds__(256) void embed_kernel(const void* __restrict__ ids
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] *= factor;
     }
-    store8<BF16>(out, t * H + h, v);
+    // bf16 rows, whole lines at once, pass the caches by, which the table's rows need
+    if constexpr (BF16) __builtin_nontemporal_store(bf16_of(v), reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + t * H + h));
+    else store8<BF16>(out, t * H + h, v);
   }
 }
 
