@@ -26,10 +26,11 @@ namespace {
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -1; }
 
-// Workgroups by token (or by 4), on in y where x is full.
-__device__ __forceinline__ int64_t group_at() { return (int64_t)blockIdx.y * kGroupsX + blockIdx.x; }
-inline dim3 groups_of(int64_t n) {
-  return dim3((unsigned)(n < kGroupsX ? n : kGroupsX), (unsigned)((n + kGroupsX - 1) / kGroupsX));
+// Workgroups by token (or by 4 or 16), on in y where x is full: `most` of them, whose
+// work-items stay below the 2^32 from which a launch is cut short without an error.
+__device__ __forceinline__ int64_t group_at() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+inline dim3 groups_of(int64_t n, int64_t most = kGroupsX) {
+  return dim3((unsigned)(n < most ? n : most), (unsigned)((n + most - 1) / most));
 }
 
 __device__ __forceinline__ float max_of(float v) {
@@ -200,7 +201,8 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(Distill g, const flo
     return make_float2(m, a.y * __expf(a.x - ref) + b.y * __expf(b.x - ref));
   };
   {
-    const int n = threadIdx.x & 15, first = threadIdx.x >> 4, row = (int)blockIdx.x * 16 + n;
+    const int n = threadIdx.x & 15, first = threadIdx.x >> 4;
+    const int64_t row = group_at() * 16 + n;
     float2 p = make_float2(-INFINITY, 0.0f);
     if (row < live) {
 #pragma unroll 4
@@ -209,10 +211,10 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(Distill g, const flo
     s_part[n][first] = p;
   }
   __syncthreads();
-  const int t0 = (int)blockIdx.x * 16 + wave;                 // tokens that are ignored
+  const int64_t t0 = group_at() * 16 + wave;                  // tokens that are ignored
   if (lane == 0 && t0 < T && y[t0] < 0) loss[t0] = lse[t0] = 0.0f;
   if (t0 >= live) return;
-  const int t = rows ? rows[t0] : t0;
+  const int64_t t = rows ? rows[t0] : t0;
   if (y[t] < 0) return;
   float2 p = s_part[wave][lane];
 #pragma unroll
@@ -224,7 +226,7 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(Distill g, const flo
   for (int k = 0; k < P; ++k) {
     // the distance to the largest logit first, as the cross entropy takes it
     const int at = k * 64 + lane;
-    if (e.id[k] >= 0) v += e.q[k] != 0.0f ? e.q[k] * (e.log_q[k] + ((most - g.picked[(int64_t)t * g.K + at]) + rest)) : 0.0f;
+    if (e.id[k] >= 0) v += e.q[k] != 0.0f ? e.q[k] * (e.log_q[k] + ((most - g.picked[t * g.K + at]) + rest)) : 0.0f;
   }
   v = sum_of(v);
   if (lane == 0) {
@@ -326,7 +328,7 @@ __global__ __launch_bounds__(256) void distill_put_kernel(Distill g, DistillPiec
 }  // namespace
 
 int distill_live_launch(const Distill& k, int T, int V, int* y, hipStream_t s) {
-  hipLaunchKernelGGL(distill_live_kernel, groups_of((T + 3) / 4), dim3(256), 0, s, k, T, V, y);
+  hipLaunchKernelGGL(distill_live_kernel, groups_of(((int64_t)T + 3) / 4), dim3(256), 0, s, k, T, V, y);
   return ok();
 }
 
@@ -343,7 +345,7 @@ int distill_pick_launch(const Distill& k, int head, int T, int V, int H, const v
 int distill_loss_launch(const Distill& k, const float2* part, const int* rows, const int* count, const int* y, int T, int V,
                         int tiles, float* loss, float* lse, hipStream_t s) {
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((T + 15) / 16)), dim3(1024), 0, s, k, part, rows, count, y, T, V, tiles, loss, lse);
+    hipLaunchKernelGGL(kernel, groups_of(((int64_t)T + 15) / 16, kGroupsX / 2), dim3(1024), 0, s, k, part, rows, count, y, T, V, tiles, loss, lse);
     return ok();
   };
   return k.K <= 64 ? go(distill_loss_kernel<1>) : k.K <= 128 ? go(distill_loss_kernel<2>) : go(distill_loss_kernel<4>);
@@ -351,7 +353,7 @@ int distill_loss_launch(const Distill& k, const float2* part, const int* rows, c
 
 int distill_put_launch(const Distill& k, const DistillPiece& piece, const float* lse, const float* dloss, hipStream_t s) {
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, groups_of((piece.T + 3) / 4), dim3(256), 0, s, k, piece, lse, dloss);
+    hipLaunchKernelGGL(kernel, groups_of(((int64_t)piece.T + 3) / 4), dim3(256), 0, s, k, piece, lse, dloss);
     return ok();
   };
   return k.K <= 64 ? go(distill_put_kernel<1>) : k.K <= 128 ? go(distill_put_kernel<2>) : go(distill_put_kernel<4>);
