@@ -265,7 +265,7 @@ __device__ __forceinline__ i32x8 codes_operand(u32x4 c) {
 // scale rows are whole words, and 4 steps' scales of a row come in one load.
 template <int RM, int NT, bool WORDS, bool BF16>
 __global__ __launch_bounds__(512) void act4_thin_kernel(Act4Args g) {
-  constexpr int kWaves = 8, kUnroll = WORDS && RM * NT <= 8 ? 4 : 2;
+  constexpr int kWaves = 8, kUnroll = WORDS ? 4 : 2;
   __shared__ f32x4 part[kWaves][RM * NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int groups = (g.O + 16 * RM - 1) / (16 * RM);
@@ -311,13 +311,7 @@ __global__ __launch_bounds__(512) void act4_thin_kernel(Act4Args g) {
       u32x4 words = {0u, 0u, 0u, 0u};
       if constexpr (WORDS) {
         const int at = (int)(row == kOOB ? kOOB : row * (uint32_t)g.G + 4u * (uint32_t)s0);
-        if constexpr (kUnroll == 4) {
-          words = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0));
-        } else {
-          const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0));
-          words[0] = v[0];
-          words[1] = v[1];
-        }
+        words = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0));
       }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
@@ -376,13 +370,14 @@ int thin_go(Act4Args g, int bf16, hipStream_t s) {
 }
 
 // Outputs per workgroup: the more, the less often the rows are read, but a workgroup
-// for every CU.
-template <int NT>
+// for every CU.  One layer of more than 16 rows comes here with up to 4096 outputs
+// (act4_plan), of which 16 to a workgroup leave one for each CU.
 int thin_by(const Act4Args& g, int bf16, hipStream_t s) {
+  if (!g.offsets && g.N > 16) return g.N <= 32 ? thin_go<1, 2>(g, bf16, s) : thin_go<1, 4>(g, bf16, s);
   const int64_t chunks = g.offsets ? (g.E < g.N ? g.E : g.N) : 1;
   const int64_t groups = (g.O + 63) / 64 * chunks;
-  if (groups >= kCUs * 3 / 4) return thin_go<4, NT>(g, bf16, s);
-  return 2 * groups >= kCUs * 3 / 4 ? thin_go<2, NT>(g, bf16, s) : thin_go<1, NT>(g, bf16, s);
+  if (groups >= kCUs * 3 / 4) return thin_go<4, 1>(g, bf16, s);
+  return 2 * groups >= kCUs * 3 / 4 ? thin_go<2, 1>(g, bf16, s) : thin_go<1, 1>(g, bf16, s);
 }
 
 // f(0), f(1), .. with constants, in this order.
@@ -867,10 +862,7 @@ int product(Act4Args g, int bf16, void* workspace, hipStream_t s) {
   g.Gs = g.G;
   g.splits = p.splits;
   g.per = p.per;
-  if (p.bt == 0) {
-    if (g.offsets || g.N <= 16) return thin_by<1>(g, bf16, s);
-    return g.N <= 32 ? thin_by<2>(g, bf16, s) : thin_by<4>(g, bf16, s);
-  }
+  if (p.bt == 0) return thin_by(g, bf16, s);
   if (g.G % 4 != 0) {
     const int words = (g.G + 3) / 4;
     uint32_t* to = static_cast<uint32_t*>(workspace);
