@@ -664,7 +664,7 @@ int sq_ce_bwd(int head, int64_t T, int64_t V, int64_t I, const void* X, const vo
  *   offsets[E] on, are zeros; a row number outside 0 .. T-1 reads as a row of
  *   zeros, and offsets are held to 0 .. N; they must not decrease (where they do,
  *   rows are undefined, but nothing outside Y is touched).  E <= 8192; (N/64 + min(E, N) + 8)
- *   ceil(O/128) <= 2^22.
+ *   ceil(O/128) <= 2^22; T*I*2 and O*I/2 below 2 GiB, Y of any size.
  * x_codes and codes 16-byte, x_scales and scales 4-byte aligned; workspace: at
  * least the bytes of the _workspace call, 256-byte aligned (NULL where that is
  * 0), contents irrelevant.  Deterministic.

@@ -35,9 +35,13 @@ int check_fwd_act4(int64_t T, int64_t N, const uint8_t* x, const uint8_t* xs, co
   return aligned(x, 16) && aligned(codes, 16) && aligned(xs, 4) && aligned(scales, 4) && aligned(Y, 16) ? SQ_OK : SQ_ERR_ALIGN;
 }
 
+// (the kept rows as sq_fwd_act4 takes them and an expert's codes go through 32-bit offsets;
+// Y, whose rows are N and not T, does not)
 int check_batched(int fmt, int64_t E, int64_t T, int64_t N, int64_t O, int64_t I) {
-  const int st = check_layer(fmt, T, O, I);
-  if (st != SQ_OK) return st;
+  if (!fmt_ok(fmt)) return SQ_ERR_FORMAT;
+  if (T < 0 || O < 1 || I < 1 || T > kDimMax || O > kDimMax || I > kDimMax) return SQ_ERR_SHAPE;
+  if (O % 8 != 0 || I % block_of(fmt) != 0) return SQ_ERR_SHAPE;
+  if (T * I * 2 > kOperandBytesMax || O * I / 2 > kOperandBytesMax) return SQ_ERR_SHAPE;
   if (fmt != SQ_MXFP4) return SQ_ERR_UNIMPLEMENTED;
   if (E < 1 || E > kExpertsMax || N < 0 || N > kDimMax) return SQ_ERR_SHAPE;
   // the workgroups of a launch: 64 rows by 128 outputs each at least (and 16 by 16 for the

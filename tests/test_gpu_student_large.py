@@ -100,3 +100,25 @@ def test_experts_of_many_bytes(sq, N):
     assert not Y[:N // 2].any()
     # sums of multiples of 2^-9 below 2^15: exact in fp32
     assert np.array_equal(Y[N // 2:].double().cpu().numpy(), ref)
+
+
+@pytest.mark.parametrize("out_dtype", [BF16, torch.float32])
+def test_experts_of_many_rows_times_outputs(sq, out_dtype):
+    """Rows and outputs of which a bf16 matrix takes more than 2 GiB, and an fp32 one more than 4."""
+    E, N, O, I = 4, 131072 + 37, 8448, 32
+    codes = torch.from_numpy(inputs.codes_uniform(3, E * O, I)).cuda().view(E, O, I // 2)
+    scales = torch.full((E, O, 1), 127, dtype=torch.uint8, device="cuda")
+    xc, xs = torch.from_numpy(inputs.codes_uniform(4, N, I)).cuda(), torch.full((N, 1), 120, dtype=torch.uint8, device="cuda")
+    ends = [0, 30000, 30000, 100001, N - 20]
+    offsets = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    Y = torch.full((N, O), float("nan"), dtype=out_dtype, device="cuda")
+    sq.sq_fwd_act4_batched("mx", xc, xs, None, offsets, codes, scales, Y=Y)
+    table = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, 0, -.5, -1, -1.5, -2, -3, -4, -6], device="cuda")
+    values = lambda c: table[torch.stack((c & 15, c >> 4), -1).long()].flatten(-2)
+    for e in range(E):
+        w = values(codes[e]).t().contiguous()
+        for a in range(ends[e], ends[e + 1], 8192):
+            b = min(a + 8192, ends[e + 1])
+            # sums of multiples of 2^-9 below 2^11 at most: exact in fp32, and rounded once to bf16
+            assert torch.equal(Y[a:b], (values(xc[a:b]) @ w * 2.0 ** -7).to(out_dtype))
+    assert not Y[ends[-1]:].any()

@@ -70,6 +70,18 @@ def test_experts_refusals(lib, kw, status):
     assert _call(lib.sq_fwd_act4_batched, args, dict(T=0, N=0, xc=None, xs=None, rows=None, Y=None)) == 0
 
 
+@pytest.mark.parametrize("kw,status", [
+    (dict(), 0), (dict(N=1 << 18), 0), (dict(N=1 << 20, T=1 << 20), 0),                    # T*O*2 and N*O*2 of 2.2 GB and more
+    (dict(T=(1 << 25) - 1), 0), (dict(T=1 << 25), SHAPE), (dict(I=1 << 12, T=8, N=8, O=1 << 20), SHAPE),
+    (dict(I=1 << 12, T=8, N=8, O=(1 << 20) - 8), 0), (dict(O=8444), SHAPE), (dict(I=48), SHAPE), (dict(T=-1), SHAPE), (dict(O=0), SHAPE)])
+def test_experts_refuse_what_lies_beyond_32_bits_only(lib, kw, status):
+    """The kept rows and one expert's codes are limited, not the rows times the outputs, which nothing holds."""
+    args = dict(E=4, T=131072, N=131072, O=8448, I=32)
+    a = {**args, **kw}
+    st = lib.sq_fwd_act4_batched(MX, *a.values(), FAKE, FAKE, FAKE, None, FAKE, FAKE, FAKE, 1, None, 0, None)
+    assert st == (status or ARG)                               # without offsets, where the shape is taken
+
+
 # ---------------------------------------------------------------- distillation
 HEAD = [(dict(head=3), FORMAT), (dict(T=-1), SHAPE), (dict(V=0), SHAPE), (dict(I=0), SHAPE), (dict(I=12), SHAPE),
         (dict(head=MX, I=48), SHAPE), (dict(K=0), SHAPE), (dict(K=257), SHAPE), (dict(T=1 << 25), SHAPE), (dict(I=1 << 22), SHAPE),
