@@ -216,8 +216,9 @@ def _check(fn, status):
 # device query per tensor.  A forward that allocates its output takes the host
 # 8.8 us instead of 12.4, of which the launch itself is 3.4.  By the time that
 # they ask for the current device its tensors exist, so they need not initialise
-# the runtime (0.26 -> 0.13 us).
-_device = torch._C._cuda_getDevice
+# the runtime (0.26 -> 0.13 us); a torch without a GPU build has only the other,
+# which says so.
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream():

@@ -2,11 +2,13 @@
 on the host before a launch (no GPU needed; the addresses are never used)."""
 
 import math
+import subprocess
+import sys
 
 import pytest
 import torch
 
-from conftest import ensure_library
+from conftest import ROOT, ensure_library
 
 FAKE, OFF = 0x10000, 0x10008
 ARG, SHAPE, ALIGN, FORMAT, WORKSPACE, UNIMPLEMENTED = -1, -2, -3, -4, -5, -7
@@ -215,3 +217,21 @@ def test_binding_refuses_what_the_library_cannot_see():
         sq.sq_embed_bwd(ids[:, 0].contiguous(), X, 10, dW=torch.zeros((9, 64)))
     with pytest.raises(ValueError, match="codes"):
         sq.sq_embed_bwd_dscale("mx", ids[:, 0].contiguous(), X, c[:, :8].contiguous())
+
+
+def test_binding_imports_under_a_torch_without_a_gpu_build():
+    """Such a torch lacks the runtime's own calls; the host's checks work there all the same."""
+    code = """
+import torch
+for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
+from paper_2609_04526_amd import sq
+try:
+    sq.sq_act4_pack("mx", torch.zeros((4, 64), dtype=torch.bfloat16))
+except ValueError as e:
+    print("refused:", e)
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr
+    assert "refused: libscaleqlora takes device tensors" in done.stdout
