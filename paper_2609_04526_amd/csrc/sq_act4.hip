@@ -104,8 +104,13 @@ __device__ __forceinline__ u32x4 unpack8(uint32_t c, uint32_t byte, float ws2) {
   return r;
 }
 
-// PAST: the values pass the caches by (8192 x 14336 NVFP4 55 -> 43 us, 7 TB/s; 2000 x 4096 MXFP4
-// 5.2 -> 4.1), but not those that a product reads next.
+// PAST: the values pass the caches by, where they and their codes are more than these hold:
+// a product reads them next.  us of this kernel and with sq_bwd_dscale behind it, through and
+// past them: 8000 x 4096 MXFP4 to 1024 outputs (83 MB) 14.2, 12.0 and 74.6, 81.0; 20000 (207)
+// 31.7, 31.1 and 160, 174; 28000 (290) 49.5, 42.7 and 246, 243; 36000 (373) 66, 54 and 317, 309;
+// 7000 x 14336 NVFP4 to 4096 (257) 38.7, 38.1 and 655, 668; 8192 (301) 55, 44 and 795, 796;
+// 12000 (441) 77, 64 and 1206, 1190.  sq_fwd_act4's own, which the product reads at once, stay
+// in them at any size (8192 tokens of 4096 x 14336 836, 850).
 template <int FMT, bool PAST>
 __global__ __launch_bounds__(256) void act4_unpack_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                           int64_t pieces, float ws2, u32x4* __restrict__ X) {
@@ -908,17 +913,20 @@ int act4_pack_launch(int fmt, int64_t T, int64_t I, const void* X, float ws2, ui
   return ok();
 }
 
-template <int FMT, bool PAST>
-static int unpack_go(int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, float ws2, void* X, hipStream_t s) {
+static int unpack_go(int fmt, bool past, int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, float ws2, void* X, hipStream_t s) {
   const int64_t pieces = T * I / 8;
   const dim3 grid((unsigned)((pieces + 256 * kSteps - 1) / (256 * kSteps))), block(256);
-  hipLaunchKernelGGL((act4_unpack_kernel<FMT, PAST>), grid, block, 0, s, reinterpret_cast<const uint32_t*>(codes), scales, pieces, ws2,
-                     static_cast<u32x4*>(X));
-  return ok();
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, reinterpret_cast<const uint32_t*>(codes), scales, pieces, ws2, static_cast<u32x4*>(X));
+    return ok();
+  };
+  if (past) return fmt == kMX ? go(act4_unpack_kernel<kMX, true>) : go(act4_unpack_kernel<kNV, true>);
+  return fmt == kMX ? go(act4_unpack_kernel<kMX, false>) : go(act4_unpack_kernel<kNV, false>);
 }
 
 int act4_unpack_launch(int fmt, int64_t T, int64_t I, const uint8_t* codes, const uint8_t* scales, float ws2, void* X, hipStream_t s) {
-  return fmt == kMX ? unpack_go<kMX, true>(T, I, codes, scales, 1.0f, X, s) : unpack_go<kNV, true>(T, I, codes, scales, ws2, X, s);
+  const int64_t bytes = 2 * T * I + T * I / 2 + T * I / (fmt == kMX ? 32 : 16);
+  return unpack_go(fmt, bytes > kCacheBytes, T, I, codes, scales, fmt == kMX ? 1.0f : ws2, X, s);
 }
 
 size_t act4_workspace(int fmt, int64_t T, int64_t O, int64_t I) {
@@ -928,7 +936,7 @@ size_t act4_workspace(int fmt, int64_t T, int64_t O, int64_t I) {
 int act4_fwd(int fmt, int T, int O, int I, const uint8_t* x, const uint8_t* xs, float x_ws2, const uint8_t* codes,
              const uint8_t* scales, float ws2, void* Y, int y_bf16, void* workspace, hipStream_t s) {
   if (fmt == kNV) {
-    if (unpack_go<kNV, false>(T, I, x, xs, 1.0f, workspace, s) != 0) return -1;
+    if (unpack_go(fmt, false, T, I, x, xs, 1.0f, workspace, s) != 0) return -1;
     return gemm_fwd(fmt, T, O, I, workspace, codes, scales, x_ws2 * ws2, Y, y_bf16, s);
   }
   Act4Args g{};

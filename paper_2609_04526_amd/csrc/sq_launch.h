@@ -163,6 +163,9 @@ int byte_diff_launch(int64_t n, const uint8_t* a, const uint8_t* b, uint64_t* co
 // Workgroups in x of a launch whose count goes with the tokens.  One that asks for
 // 2^32 work-items in a dimension, or for more, is cut short without an error.
 constexpr int64_t kGroupsX = int64_t(1) << 22;   // of up to 512 threads: 2^31 work-items
+// The last cache before the memory, which all XCDs share: what is written is still there for
+// a reader if it and what it was made from fit.
+constexpr int64_t kCacheBytes = int64_t(256) << 20;
 
 // Tokens to experts and back (sq_moe.hip).  routed: device pointer to the
 // number of routed pairs (the sort's offsets[E]).

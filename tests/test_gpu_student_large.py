@@ -122,3 +122,17 @@ def test_experts_of_many_rows_times_outputs(sq, out_dtype):
             # sums of multiples of 2^-9 below 2^11 at most: exact in fp32, and rounded once to bf16
             assert torch.equal(Y[a:b], (values(xc[a:b]) @ w * 2.0 ** -7).to(out_dtype))
     assert not Y[ends[-1]:].any()
+
+
+@pytest.mark.parametrize("fmt,T", [("mx", 25600), ("mx", 26000), ("nv", 25500), ("nv", 25700)])
+def test_values_of_about_the_caches_size(sq, fmt, T):
+    """Values and codes of a little less and a little more than 256 MiB, which are stored in different ways."""
+    I, n, ws2 = 4096, 100, 2.0 ** -9
+    block = 32 if fmt == "mx" else 16
+    assert (T * I * 2 + T * I // 2 + T * I // block > 256 << 20) == (T in (26000, 25700))
+    xc, xs = student.act4_pack(fmt, inputs.bf16_normal(2, (n, I)).float().numpy(), ws2)
+    codes, scales = (torch.from_numpy(v).cuda().repeat(T // n, 1) for v in (xc, xs))
+    X = torch.full((T, I), float("nan"), dtype=BF16, device="cuda")
+    sq.sq_act4_unpack(fmt, codes, scales, ws2=ws2, X=X)
+    want = torch.from_numpy(student.act4_values(fmt, xc, xs).astype(np.float32) * np.float32(ws2 if fmt == "nv" else 1)).to(BF16)
+    assert (X.view(T // n, n, I) == want.cuda()).all()
