@@ -36,11 +36,17 @@ __device__ __forceinline__ int key_at(const void* ids, int bytes, int64_t t, int
 
 // ------------------------------------------------------------------ lookup
 // One token per workgroup, 8 columns per lane and step.  Bound by memory: 16384 tokens of
-// 4096 MXFP4 to bf16 23 us (170 MB, 7.3 TB/s; 26 through the caches).
-template <int HEAD, bool BF16>
+// 4096 MXFP4 to bf16 27 us (170 MB, 6.3 TB/s).
+// PAST: bf16 rows, whole lines at once, pass the caches by, where they and the table's are more
+// than these hold: a product reads them next.  us of this kernel and with sq_fwd of 1024
+// outputs behind it, through and past them: 2000 tokens of 4096 MXFP4 (21 MB) 6.0, 5.7 and
+// 38, 42; 16384 (170) 27, 25.5 and 129, 150; 32768 (340) 74, 50 and 318, 303; bf16 2000 (33) 6.0, 5.2 and
+// 38, 42; 16384 (268) 43, 40 and 148, 167; 24000 (393) 68, 57 and 267, 261.
+template <int HEAD, bool BF16, bool PAST>
 __global__ __launch_bounds__(256) void embed_kernel(const void* __restrict__ ids, int id_bytes, int64_t T, int V, int H,
                                                     const void* __restrict__ W, const uint8_t* __restrict__ scales, float ws2,
                                                     float factor, void* __restrict__ out) {
+  static_assert(BF16 || !PAST, "bf16 rows");
   const int64_t t = (int64_t)blockIdx.y * kGroupsX + blockIdx.x;
   if (t >= T) return;
   const int key = key_at(ids, id_bytes, t, V);
@@ -51,8 +57,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const void* __restrict__ ids
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] *= factor;
     }
-    // bf16 rows, whole lines at once, pass the caches by, which the table's rows need
-    if constexpr (BF16) __builtin_nontemporal_store(bf16_of(v), reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + t * H + h));
+    if constexpr (PAST) __builtin_nontemporal_store(bf16_of(v), reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + t * H + h));
     else store8<BF16>(out, t * H + h, v);
   }
 }
@@ -546,9 +551,15 @@ int embed_launch(int head, int64_t T, int V, int H, const void* ids, int id_byte
     hipLaunchKernelGGL(kernel, grid, dim3(block), 0, s, ids, id_bytes, T, V, H, W, scales, ws2, factor, out);
     return ok();
   };
-  if (head == kMX) return out_bf16 ? go(embed_kernel<kMX, true>) : go(embed_kernel<kMX, false>);
-  if (head == kNV) return out_bf16 ? go(embed_kernel<kNV, true>) : go(embed_kernel<kNV, false>);
-  return out_bf16 ? go(embed_kernel<kCeBf16, true>) : go(embed_kernel<kCeBf16, false>);
+  // the rows written, and those read, each once at most
+  const int64_t row = head == kCeBf16 ? 2 * (int64_t)H : H / 2 + H / (head == kMX ? 32 : 16), bytes = 2 * T * H + (T < V ? T : V) * row;
+  const bool past = out_bf16 && bytes > kCacheBytes;
+  auto by = [&](auto HEAD) {
+    constexpr int h = decltype(HEAD)::value;
+    return past ? go(embed_kernel<h, true, true>) : out_bf16 ? go(embed_kernel<h, true, false>) : go(embed_kernel<h, false, false>);
+  };
+  if (head == kMX) return by(std::integral_constant<int, kMX>{});
+  return head == kNV ? by(std::integral_constant<int, kNV>{}) : by(std::integral_constant<int, kCeBf16>{});
 }
 
 size_t embed_workspace(int64_t T, int64_t V, int64_t H) { return embed_plan(T, V, H).total; }

@@ -136,3 +136,27 @@ def test_values_of_about_the_caches_size(sq, fmt, T):
     sq.sq_act4_unpack(fmt, codes, scales, ws2=ws2, X=X)
     want = torch.from_numpy(student.act4_values(fmt, xc, xs).astype(np.float32) * np.float32(ws2 if fmt == "nv" else 1)).to(BF16)
     assert (X.view(T // n, n, I) == want.cuda()).all()
+
+
+@pytest.mark.parametrize("head,T", [("bf16", 16384), ("bf16", 16385), ("mx", 25801), ("mx", 25950), ("nv", 25500), ("nv", 25700)])
+def test_lookup_of_about_the_caches_size(sq, head, T):
+    """Rows read and written of 256 MiB, or a little less, and of a little more, which are stored in different ways; each
+    a row of a small call on the same table."""
+    V, H = 40000, 4096
+    gen = inputs.device_generator(T)
+    scales = None
+    if head == "bf16":
+        W = torch.randn((V, H), generator=gen, device="cuda").to(BF16)
+    else:
+        W = torch.randint(0, 256, (V, H // 2), generator=gen, device="cuda", dtype=torch.uint8)
+        scales = torch.randint(100, 126, (V, H // (32 if head == "mx" else 16)), generator=gen, device="cuda", dtype=torch.uint8)
+    row = 2 * H if head == "bf16" else H // 2 + scales.shape[1]
+    assert (T * (2 * H + row) > 256 << 20) == (T in (16385, 25950, 25700))
+    ids = torch.randint(-2, V, (T,), generator=gen, device="cuda")
+    more = dict(scales=scales, ws2=0.01, factor=1.5)
+    out = torch.full((T, H), float("nan"), dtype=BF16, device="cuda")
+    sq.sq_embed_fwd(head, ids, W, out=out, **more)
+    for a in range(0, T, 4000):
+        part = sq.sq_embed_fwd(head, ids[a:a + 4000].contiguous(), W, **more)
+        assert torch.equal(out[a:a + 4000], part)
+    assert torch.isfinite(out).all() and not out[ids < 0].any() and out[ids >= 0].any(1).all()
