@@ -348,3 +348,74 @@ def test_same_bits_on_every_run(sq):
         xc, xs, _ = _rows("mx", T, T, 1024)
         d = _dev(xc, xs, *_layer("mx", 5, 520, 1024))
         assert torch.equal(sq.sq_fwd_act4("mx", *d), sq.sq_fwd_act4("mx", *d))
+
+
+# inputs that end within a stage of 256, with scale rows of whole words (whose next row's bytes lie in the same copy) and
+# of others, through tiles of every extent and split sums
+@pytest.mark.parametrize("T,O,I", [(300, 264, 128), (300, 264, 384), (65, 264, 640), (129, 520, 160), (700, 2056, 384), (2000, 4096, 128),
+                                   (4100, 4104, 384), (100, 264, 6272), (100, 264, 6304), (5, 264, 384), (5, 264, 96), (40, 520, 640)])
+def test_nan_scales_beside_the_inputs_end(sq, T, O, I):
+    """A NaN scale in a row's first block reaches that row of Y, or column, and not the row before it, whose stage ends there."""
+    g = inputs.rng(T + I)
+    xc, codes = inputs.codes_uniform(1, T, I), inputs.codes_uniform(2, O, I)
+    xs, ws = g.integers(118, 128, (T, I // 32)).astype(np.uint8), g.integers(118, 128, (O, I // 32)).astype(np.uint8)
+    d = _dev(xc, xs, codes, ws)
+    for out_dtype in (F32, BF16):
+        want = sq.sq_fwd_act4("mx", *d, out_dtype=out_dtype)
+        assert torch.isfinite(want).all()
+        r, c = [v for v in (1, 3, 32, 64, T - 1) if v < T], [0, 7, 63, 64, 128, O - 1]
+        nx, nw = d[1].clone(), d[3].clone()
+        nx[r, 0], nw[c, 0] = 0xFF, 0xFF
+        Y = sq.sq_fwd_act4("mx", d[0], nx, d[2], nw, out_dtype=out_dtype)
+        bad = torch.zeros((T, O), dtype=torch.bool, device="cuda")
+        bad[r], bad[:, c] = True, True
+        assert torch.equal(Y.isnan(), bad)
+        assert torch.equal(torch.where(bad, torch.zeros_like(Y), Y), torch.where(bad, torch.zeros_like(Y), want))
+
+
+@pytest.mark.parametrize("E,T,N,O,I", [(200, 64, 512, 1288, 128), (30, 200, 3300, 2056, 384), (12, 300, 3000, 4104, 640), (8, 60, 200, 264, 384)])
+def test_nan_scales_beside_the_inputs_end_of_experts(sq, E, T, N, O, I):
+    """The same over experts, the last row of one and the first of the next among them."""
+    g = inputs.rng(E + I)
+    xc, codes = inputs.codes_uniform(1, T, I), inputs.codes_uniform(2, E * O, I).reshape(E, O, -1)
+    xs, ws = g.integers(118, 128, (T, I // 32)).astype(np.uint8), g.integers(118, 128, (E, O, I // 32)).astype(np.uint8)
+    offsets, rows = _split(g, E, N, "even"), g.integers(0, T, N).astype(np.int32)
+    xc, xs, rows, offsets, codes, ws = _dev(xc, xs, rows, offsets, codes, ws)
+    want = sq.sq_fwd_act4_batched("mx", xc, xs, rows, offsets, codes, ws)
+    assert torch.isfinite(want).all()
+    nx, nw = xs.clone(), ws.clone()
+    r, e, c = [1, 7, T - 1], [0, E // 2, E - 1], [0, 64, O - 1]
+    nx[r, 0] = 0xFF
+    for k in e:
+        nw[k, c, 0] = 0xFF
+    Y = sq.sq_fwd_act4_batched("mx", xc, nx, rows, offsets, codes, nw)
+    bad = torch.isin(rows, torch.tensor(r, dtype=torch.int32, device="cuda"))[:, None].repeat(1, O)
+    o = offsets.tolist()
+    for k in e:
+        bad[o[k]:o[k + 1], c] = True
+    bad[:o[0]], bad[o[E]:] = False, False
+    assert torch.equal(Y.isnan(), bad)
+    assert torch.equal(torch.where(bad, torch.zeros_like(Y), Y), torch.where(bad, torch.zeros_like(Y), want))
+
+
+@pytest.mark.parametrize("kind", ["even", "one", "dropped", "empty"])
+@pytest.mark.parametrize("E,T,N,O,I", [(200, 64, 512, 1288, 64), (30, 200, 3300, 2056, 288), (12, 300, 3000, 4104, 544)])
+def test_experts_of_several_rounds_to_fp32(sq, E, T, N, O, I, kind):
+    """Chunks from a table with tiles of 64, 128 and 256 rows, whose fp32 outputs leave 32 rows at a time."""
+    g = inputs.rng(E + N)
+    codes, scales = (v.view(E, O, -1) for v in _dev(*_layer("mx", N, E * O, I)))
+    xc, xs, _ = _rows("mx", T, T, I)
+    xc, xs = _dev(xc, xs)
+    offsets, rows = _split(g, E, N, kind), g.integers(0, T, N).astype(np.int32)
+    if kind == "dropped":
+        offsets = np.maximum(offsets, 3)
+    Y = torch.full((N, O), float("nan"), device="cuda")
+    sq.sq_fwd_act4_batched("mx", xc, xs, *_dev(rows, offsets), codes, scales, Y=Y)
+    x = _dequant(xc, xs)[torch.from_numpy(rows).long().cuda()]
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        if lo == hi:
+            continue
+        w, r = _dequant(codes[e], scales[e]), x[lo:hi]
+        _check_device(Y[lo:hi], r @ w.t().contiguous(), r.abs() @ w.abs().t().contiguous(), I)
+    assert not Y[:offsets[0]].any() and not Y[offsets[E]:].any()

@@ -160,3 +160,33 @@ def test_lookup_of_about_the_caches_size(sq, head, T):
         part = sq.sq_embed_fwd(head, ids[a:a + 4000].contiguous(), W, **more)
         assert torch.equal(out[a:a + 4000], part)
     assert torch.isfinite(out).all() and not out[ids < 0].any() and out[ids >= 0].any(1).all()
+
+
+@pytest.mark.parametrize("T", [(1 << 30) - 5, 1 << 30])
+def test_embedding_of_the_most_tokens(sq, T):
+    """As many tokens as the entry points take: two ids in turn, one of them outside the table, and then one id's run
+    of a third of them.
+
+    A run's ones are summed in fp32: those before its first whole chunk of 8192 one by one (exact), then the chunks' sums,
+    then those past its last one by one.  Up to 2^24 all of it is exact.  From there on a chunk's 8192 is a multiple of the
+    sum's step u (at most 32 below 2^29), so the sum is rounded only where the step doubles, by u / 2 at most, 31 in all
+    for u = 2 .. 32; and a one added to a multiple of u is off by 1 at most, 8191 of them by 8191."""
+    V, I = 700, 8
+    if torch.cuda.mem_get_info()[0] < T * 80:
+        pytest.skip("needs 80 GB")
+    ids = torch.full((T,), 699, dtype=torch.int32, device="cuda")
+    n = T // 3 * 2
+    ids[:n:2], ids[1:n:2] = 5, -1
+    ids[T - 1] = 0
+    W = inputs.bf16_normal(1, (V, I)).cuda()
+    out = sq.sq_embed_fwd("bf16", ids, W)
+    for a in (0, 1 << 22, 1 << 29, T - (1 << 20)):
+        part = ids[a:a + (1 << 20)]
+        live = part >= 0
+        assert torch.equal(out[a:a + (1 << 20)], torch.where(live[:, None], W[torch.where(live, part, 0)], torch.zeros((), dtype=BF16, device="cuda")))
+    out.fill_(1.0)
+    dW = sq.sq_embed_bwd(ids, out, V)
+    want = torch.zeros(V, dtype=torch.float64, device="cuda")
+    want[5], want[699], want[0] = (n + 1) // 2, T - n - 1, 1
+    off = (dW.double() - want[:, None]).abs()
+    assert (off <= torch.where(want > 1 << 24, 8191.0 + 31.0, 0.0)[:, None]).all()
