@@ -967,9 +967,11 @@ __device__ __forceinline__ void tail_logits(const CeTail& g, int t, float* s_l) 
 }
 
 // (max, sum) of 256 logits of one token per wave, and the target's logit; past the
-// n logits, a workgroup per token for the tail (HEAD a 4-bit format).
+// n logits, a workgroup per token for the tail (HEAD a 4-bit format).  8 waves per SIMD,
+// since most workgroups have no tail: its loads unrolled without regard to them take 106
+// registers (200 tokens of 50003 x 2048 NVFP4, loss 98.0 us, so 95.4).
 template <int HEAD>
-__global__ __launch_bounds__(256) void ce_part_kernel(CePiece p, float2* __restrict__ part, float* __restrict__ tlogit,
+__global__ __launch_bounds__(256, 8) void ce_part_kernel(CePiece p, float2* __restrict__ part, float* __restrict__ tlogit,
                                                       CeTail tail) {
   const int extra = (int)blockIdx.x - (p.n + 255) / 256;
   if (HEAD != kCeBf16 && extra >= 0) {
