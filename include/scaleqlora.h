@@ -645,7 +645,8 @@ int sq_ce_bwd(int head, int64_t T, int64_t V, int64_t I, const void* X, const vo
  *   codes, and reads as NaN.
  * sq_act4_unpack: the values x^ = code * eff as bf16 [T, I], rounded to nearest
  *   even (exact for MXFP4 but below bf16's range and from 2^128 on, where they
- *   read as infinities).  The backward products of a layer whose forward took
+ *   read as infinities; for NVFP4 code * e4m3(byte), which is exact, times ws2 is
+ *   rounded to fp32 first, then to bf16).  The backward products of a layer whose forward took
  *   x^ are the layer's own: sq_bwd_dx, and sq_bwd_dscale with x^ for X.
  *   X 16-byte, codes 4-byte aligned; T*I <= 2^36.
  *

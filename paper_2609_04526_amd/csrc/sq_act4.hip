@@ -89,7 +89,8 @@ __global__ __launch_bounds__(256) void act4_pack_kernel(const u32x4* __restrict_
 }
 
 // 8 codes times their scale as bf16: exact but below bf16's range, at 2^128 and
-// more (infinite) and, with NVFP4, by the tensor's ws2 (rounded once).
+// more (infinite) and, with NVFP4, by the tensor's ws2 (rounded to fp32, then to bf16: off
+// by 2^-8 (1 + 2^-15) of itself at most).
 template <int FMT>
 __device__ __forceinline__ u32x4 unpack8(uint32_t c, uint32_t byte, float ws2) {
   const float s = FMT == kMX ? e8m0_to_f32(byte) : e4m3_to_f32(byte);
@@ -402,12 +403,11 @@ __device__ __forceinline__ void times(F f) {
 // row.  Between a slice's products go the reads of the next slice and the copies of a
 // later stage, and the barrier that publishes the next stage stands amid the last
 // slice.
-// 8192 tokens of 14336 x 4096 take 243 us: matrix cores busy 0.61 at 1.69 GHz, the chip's
-// power limit.  128 experts of 1536 x 2048 over 32768 rows (87) are bound by memory and by
-// the tiles' ends: when they took 116, 82 without copies, 95 without stores, 74 without both,
-// of which the products and their reads of LDS, at 1.3 us a stage, were 50.  Tiles that follow each other in
-// resident workgroups, the next one's first copies under the last products, took the
-// same (116, 122), since the stores then hold up the next tile's stages.
+// 8192 tokens of 14336 x 4096 take 243 to 250 us: matrix cores busy 0.52 at 1.78 GHz, the
+// chip's power limit.  128 experts of 1536 x 2048 over 32768 rows (81 to 87) are bound by memory
+// and by the tiles' ends, 8 stages apart: busy 0.29 at 2.23 GHz.  Tiles that follow each other
+// in resident workgroups, the next one's first copies under the last products, gained
+// nothing, since the stores then hold up the next tile's stages.
 template <int BM, int BT, int STAGES>
 constexpr int tile_lds() {
   return STAGES * (BM + BT) * 128 + (STAGES <= 3 ? 2 : 4) * (BM + BT) * 16;
