@@ -1,5 +1,6 @@
 """Distillation of more tokens than one dimension of a launch holds by 16 in 1024
-work-items (2^26 of them are 2^32), with rows as narrow as they may be.  Tokens
+work-items (2^26 of them are 2^32), up to the most that are taken (2^27 - 1, whose
+rows end 32-bit offsets), with rows as narrow as they may be.  Tokens
 repeat after 1024, some of them ignored, so every run of 1024 has to come out as
 the first; that one is compared with the oracle.
 
@@ -29,7 +30,7 @@ def sq():
 
 
 def _case(T):
-    n = T // 1024
+    n = (T + 1023) // 1024
     X, W = inputs.bf16_normal(1, (1024, I)), inputs.bf16_normal(2, (V, I))
     g = inputs.rng(3)
     ids = g.integers(0, V, (1024, K)).astype(np.int32)
@@ -37,10 +38,10 @@ def _case(T):
     ids[::7] = -1
     z = g.standard_normal((1024, K)).astype(np.float32)
     one = [X.cuda(), torch.from_numpy(ids).cuda(), torch.from_numpy(z).cuda()]
-    return X, W, ids, z, one, [v.repeat(n, 1) for v in one]
+    return X, W, ids, z, one, [v.repeat(n, 1)[:T] for v in one]
 
 
-@pytest.mark.parametrize("T", [1 << 26, (1 << 26) + 1024])
+@pytest.mark.parametrize("T", [1 << 26, (1 << 26) + 1024, (1 << 27) - 1])
 def test_loss(sq, T):
     X, W, ids, z, one, many = _case(T)
     loss, lse = (torch.full((T,), float("nan"), device="cuda") for _ in range(2))
@@ -52,9 +53,11 @@ def test_loss(sq, T):
         first = got[:1024]
         assert (np.abs(first.double().cpu().numpy() - want) <= 8 * own).all()
         # in parts, whose differences take no memory to speak of
-        for part in got.view(-1, 1024).split(4096):
+        whole = T // 1024 * 1024
+        for part in got[:whole].view(-1, 1024).split(4096):
             assert ((part - first).abs() <= 4 * own).all()
-    assert all((part == picked[:1024]).all() for part in picked.view(-1, 1024, K).split(4096))
+        assert ((got[whole:] - first[:T - whole]).abs() <= 4 * own).all()
+    assert all((part == picked[:1024]).all() for part in picked[:whole].view(-1, 1024, K).split(4096))
 
 
 def test_gradient(sq):
